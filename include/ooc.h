@@ -17,7 +17,8 @@
  *  - No exception or signal crosses this interface.  Every failure returns a
  *    negative ooc_status and sets a message readable with ooc_last_error():
  *    on the context for calls that take one (const queries included), else
- *    (a NULL context, ooc_create, ooc_link_probe, ooc_wgrad_slices) on
+ *    (a NULL context, ooc_create, ooc_link_probe, ooc_wgrad_slices,
+ *    ooc_qknorm_slices, ooc_attention_slices, ooc_run_fn) on
  *    ooc_last_error(NULL).  A NULL out-pointer, or a NULL buffer with a
  *    nonzero capacity, is OOC_E_INVALID; a query made before the stage it
  *    needs is OOC_E_STATE.
@@ -162,6 +163,42 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *  UPSAMPLE_BWD  dX[n][h][w] = sum over i, j in {0, 1} of dY[n][2h+i][2w+j],
  *                added in the order (0,0) (0,1) (1,0) (1,1)
  *                                     dY[R] dX[W]                      N H W C (of dX)
+ *  ROPE_FWD      rotary positions: of each row [cols], the first `heads` heads of dh
+ *                columns (head h in columns h dh .. (h+1) dh) have their first rot
+ *                columns rotated in pairs, (2 i, 2 i + 1) for layout 0 or (i, i + rot/2)
+ *                for layout 1; all other columns are copied.  pos is one int32 per row,
+ *                table rot/2 doubles (radians per position of pair i) then one double, a
+ *                magnitude m: with a = pos table[i], a double,
+ *                (y0, y1) = m (x0 cos a - x1 sin a, x0 sin a + x1 cos a)
+ *                                     X[R] pos[R] table[R] Y[W]    rows cols heads dh rot layout
+ *  ROPE_BWD      the transposed rotation: (dx0, dx1) = m (dy0 cos a + dy1 sin a,
+ *                dy1 cos a - dy0 sin a)
+ *                                     dY[R] pos[R] table[R] dX[W]  rows cols heads dh rot layout
+ *  QKNORM_FWD    per row, the first h1 heads of dh columns are divided by their root mean
+ *                square sqrt(mean x^2 + 1e-5) and scaled by gain row 0, the next h2 heads by
+ *                gain row 1 (gain [1 + (h2 > 0)][dh]), then rotated as by ROPE_FWD; all other
+ *                columns are copied.  rot = 0: no rotation, and no pos and table
+ *                                     X[R] gain[R] [pos[R] table[R]] Y[W]
+ *                                                                  rows cols h1 h2 dh rot layout
+ *  QKNORM_BWD    dX and dgain of the above; part = one partial dgain per row slice
+ *                (ooc_qknorm_slices gives a count)
+ *                                     X[R] gain[R] [pos[R] table[R]] dY[R] dX[W] dgain[W] part[W]
+ *                                                           rows cols h1 h2 dh rot layout slices
+ *  CROSS_ATTENTION_FWD
+ *                q [B Tq][H dh] attends to the first klen[b] (int32) of the Tk states of its
+ *                sequence, kv [B Tk][2 Hkv dh], keys in the first half of the columns, values
+ *                in the second; query head h reads key head h Hkv / H (Hkv divides H), dh <= 256:
+ *                S = q k^T / sqrt(dh), Y [B Tq][H dh] = softmax(S) v, lse [B][H][Tq] = ln sum
+ *                exp S.  klen 0: Y = 0 and lse = -inf; klen outside 0..Tk: NaN.  States at and
+ *                past klen may hold anything.  part = partial results, present iff slices > 1
+ *                (ooc_attention_slices gives counts and its bytes)
+ *                                     q[R] kv[R] klen[R] Y[W] lse[W] [part[W]]
+ *                                                                  B Tq Tk H Hkv dh slices
+ *  CROSS_ATTENTION_BWD
+ *                dq and dkv (zero at and past klen) of the above; delta [B][H][Tq] receives the
+ *                row sums of dY Y.  part = partial sums, present iff a slice count > 1
+ *                                     q[R] kv[R] klen[R] Y[R] lse[R] dY[R] dq[W] dkv[W] delta[W]
+ *                                     [part[W]]          B Tq Tk H Hkv dh q_slices kv_slices
  *  MIX           swap-integrity test op on uint32 words (sizes multiple of
  *                4): the last variable y is the only one written (W or RW),
  *                the others are read; y[j] = seed ^ (j * 2654435761) ^ sum
@@ -202,7 +239,13 @@ enum {
   OOC_OP_UPSAMPLE_FWD = 29,
   OOC_OP_UPSAMPLE_BWD = 30,
   OOC_OP_ACC = 31,
-  OOC_OP_COUNT = 32
+  OOC_OP_ROPE_FWD = 32,
+  OOC_OP_ROPE_BWD = 33,
+  OOC_OP_QKNORM_FWD = 34,
+  OOC_OP_QKNORM_BWD = 35,
+  OOC_OP_CROSS_ATTENTION_FWD = 36,
+  OOC_OP_CROSS_ATTENTION_BWD = 37,
+  OOC_OP_COUNT = 38
 };
 
 /* One schedule op.  fn = N for END ops; held = budget bytes held after it
@@ -466,6 +509,41 @@ ooc_status ooc_link_probe(int32_t hip_device, uint64_t bytes, int32_t reps, doub
  * for another op, too few or negative attributes, or an empty shape
  * (message on ooc_last_error(NULL)). */
 ooc_status ooc_wgrad_slices(int32_t op, const int64_t *attrs, int32_t n_attrs, int64_t *slices);
+
+/* Row slices for OOC_OP_QKNORM_BWD's partial sums: min(ceil(rows / 8), 2048).
+ * Host only; no context.  OOC_E_INVALID for rows < 1. */
+ooc_status ooc_qknorm_slices(int64_t rows, int64_t *slices);
+
+/* Slice counts the cross attention runs best with, and the bytes of its part
+ * variable (0: none), for the attributes B Tq Tk H Hkv dh (further ones are
+ * ignored).  OOC_OP_CROSS_ATTENTION_FWD: slices[0] parts of the keys
+ * (slices[1] = 1).  OOC_OP_CROSS_ATTENTION_BWD: slices[0] parts of the keys
+ * for dq, slices[1] parts of the queries for dkv.  Any counts that ooc_add_fn
+ * accepts give the same results up to the order of sums; part then has
+ * slices (B Tq H dh + B H Tq) floats forward and max(q_slices B Tq H dh,
+ * kv_slices 2 B Tk Hkv dh) backward, a count of 1 taking none.  Host only; no
+ * context.  OOC_E_INVALID for another op or a bad shape. */
+ooc_status ooc_attention_slices(int32_t op, const int64_t *attrs, int32_t n_attrs,
+                                int64_t slices[2], uint64_t *part_bytes);
+
+/* Runs one operation of the table above alone, outside any context, on device
+ * memory of the caller's: ptrs[j] and bytes[j] are its variables in the
+ * operation's order with the access flags ooc_add_fn takes, and the same
+ * attributes.  For programs that hold their tensors themselves.  The kernels
+ * are those a step runs, enqueued on `stream` (a hipStream_t of hip_device;
+ * NULL: its null stream); the call returns without waiting and may be
+ * recorded into a graph.  It keeps no state: calls on different streams or
+ * from different threads run independently as long as no variable that one
+ * writes is used by the other.
+ *   OOC_E_INVALID: what ooc_add_fn refuses; a NULL pointer or one that is not
+ * aligned to 16 bytes; memory that is not device memory of hip_device or is
+ * shorter than bytes[j]; a variable that is written and overlaps another;
+ * a stream of another device.  OOC_E_UNSUPPORTED: SGD, whose rates belong to
+ * ooc_step.  OOC_E_DEVICE: a launch failed, or there is no such device.
+ * Message on ooc_last_error(NULL).  The caller's current device is kept. */
+ooc_status ooc_run_fn(int32_t hip_device, void *stream, int32_t op, void *const *ptrs,
+                      const uint64_t *bytes, const uint8_t *access, int32_t n,
+                      const int64_t *attrs, int32_t n_attrs);
 
 /* Duration in milliseconds of each function's kernels in the last step,
  * measured with events on the compute stream right before and after its

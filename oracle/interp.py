@@ -21,8 +21,10 @@ import numpy as np
 from . import ops
 
 
-def run(reg, x, labels, params, state=None, dtype=np.float64, decisions=None):
+def run(reg, x, labels, params, state=None, dtype=np.float64, decisions=None, inputs=None):
     """One step.  ``params`` / ``state``: {name: array}.  Returns {var name: array}.
+
+    ``inputs``: {name: array} of the network's further inputs.
 
     ``state`` holds momentum buffers by name (``m:<param>``); missing ones start at 0.
     ``decisions``: {variable name: array}, read by the backward of the ReLU with that output
@@ -38,6 +40,8 @@ def run(reg, x, labels, params, state=None, dtype=np.float64, decisions=None):
             env[nm] = np.asarray(x, dtype=np.int64 if v["dtype"] == "i32" else dtype)
         elif nm == "labels":
             env[nm] = np.asarray(labels, dtype=np.int64)
+        elif v["kind"] == 0:
+            env[nm] = np.asarray(inputs[nm], dtype=np.int64 if v["dtype"] == "i32" else np.float64)
         elif v["kind"] == 1:
             env[nm] = np.asarray(params[nm], dtype=dtype).copy()
         elif v["kind"] == 2:
@@ -163,6 +167,22 @@ def run(reg, x, labels, params, state=None, dtype=np.float64, decisions=None):
             env[Pb] = ops.attention_fwd(g(X), a["B"], a["T"], a["H"], bool(a["causal"]))[0]
             env[dX] = ops.attention_bwd(g(X), env[Pb], g(dY), a["B"], a["T"], a["H"])
             env[dS] = np.zeros_like(env[Pb])
+        elif op in ("rope_fwd", "rope_bwd"):
+            X, pos, table, Y = vs
+            env[Y] = ops.rope(g(X), g(pos), g(table), a, back=op == "rope_bwd")
+        elif op == "qknorm_fwd":
+            X, gn, *where, Y = vs
+            env[Y] = ops.qknorm_fwd(g(X), g(gn), *[g(w) for w in where], a=a)
+        elif op == "qknorm_bwd":
+            X, gn, *where, dY, dX, dgn, part = vs
+            env[dX], env[dgn] = ops.qknorm_bwd(g(X), g(gn), g(dY), *[g(w) for w in where], a=a)
+            env[part] = np.zeros(1)
+        elif op == "cross_attention_fwd":
+            q, kv, n, Y, lse = vs[:5]
+            env[Y], env[lse] = ops.cross_attention_fwd(g(q), g(kv), g(n), a)
+        elif op == "cross_attention_bwd":
+            q, kv, n, Y, lse, dY, dq, dkv, delta = vs[:9]
+            env[dq], env[dkv], env[delta] = ops.cross_attention_bwd(g(q), g(kv), g(n), g(dY), a)
         else:
             raise ValueError(f"unknown function {op}")
     return env

@@ -50,6 +50,12 @@ concat_fwd     X_1 R, ..., X_k R, Y W          (channel concatenation)
 concat_bwd     dY R, dX_1 W, ..., dX_k W
 upsample_fwd   X R, Y W                        (nearest, factor 2)
 upsample_bwd   dY R, dX W
+rope_fwd       X R, pos R, table R, Y W
+rope_bwd       dY R, pos R, table R, dX W
+qknorm_fwd     X R, gain R [, pos R, table R], Y W          (pos, table when it rotates)
+qknorm_bwd     X R, gain R [, pos R, table R], dY R, dX W, dgain W, part W
+cross_attention_fwd  q R, kv R, klen R, Y W, lse W [, part W]
+cross_attention_bwd  q R, kv R, klen R, Y R, lse R, dY R, dq W, dkv W, delta W [, part W]
 =============  ======================================================================
 
 The backward of an addition is the identity, so both inputs receive the
@@ -64,7 +70,10 @@ partial sums per feature for each of S row slices, S = min(ceil(rows / 32),
 2048); a convolution's
 ``part`` holds S_w slices of dW and a dense layer's S_w slices of dW then
 S_w slices of db, S_w being given per layer by the caller (``lower``'s
-``slices``).
+``slices``); a per-head norm's ``part`` holds S partial gains, S = min(ceil(rows
+/ 8), 2048); a cross attention's, S partial outputs and row logarithms forward
+and the larger of S_q partial dq and S_kv partial dkv backward, counts of 1
+taking nothing, ``slices`` giving (S, S_q, S_kv).
 
 Kinds: x and labels INPUT, parameters PARAM, momentum buffers STATE, loss
 OUTPUT (parameter gradients too when ``keep_grads``), everything else TEMP.
@@ -78,7 +87,7 @@ import math
 
 INPUT, PARAM, STATE, OUTPUT, TEMP = 0, 1, 2, 3, 4
 R, W, RW = 1, 2, 3
-ITEMSIZE = {"f32": 4, "i32": 4, "u8": 1}
+ITEMSIZE = {"f32": 4, "i32": 4, "u8": 1, "f64": 8}
 
 
 def bn_slices(rows):
@@ -112,6 +121,20 @@ def lower(spec, keep_grads=False, slices=None):
         return name
 
     var("x", spec["input"], dtype="i32" if spec.get("tokens") else "f32", kind=INPUT)
+    inputs = {"x"}
+    for v in spec.get("inputs", ()):
+        shapes[v["name"]] = tuple(v["shape"])
+        inputs.add(var(v["name"], v["shape"], dtype=v["dtype"], kind=INPUT))
+
+    def turned(L):
+        return [(L["pos"], R), (L["table"], R)] if L["rot"] else []
+
+    def cross(L):
+        q, kv = (shapes[t] for t in L["in"])
+        Bt = spec["input"][0]
+        return {"B": Bt, "Tq": q[0] // Bt, "Tk": kv[0] // Bt, "H": L["heads"],
+                "Hkv": L["kv_heads"], "dh": q[1] // L["heads"]}
+
     params_of = {}
 
     # ---------------- forward
@@ -217,12 +240,36 @@ def lower(spec, keep_grads=False, slices=None):
         elif op == "attention":
             rows, d3 = xs
             d, H = d3 // 3, L["heads"]
-            Bt, T = spec["input"]
+            Bt = spec["input"][0]
+            T = rows // Bt
             Pv = var(name + ".P", (Bt, H, T, T))
             shapes[name] = (rows, d)
             var(name, shapes[name])
             fns.append(("attention_fwd", [(X, R), (Pv, W), (name, W)],
                         {"B": Bt, "T": T, "H": H, "dh": d // H, "causal": int(L["causal"])}))
+        elif op == "rope":
+            shapes[name] = xs
+            var(name, xs)
+            fns.append(("rope_fwd", [(X, R)] + turned(L) + [(name, W)],
+                        {k: L[k] for k in ("heads", "dh", "rot", "layout")}))
+        elif op == "qknorm":
+            g = var(name + ".gain", (2 if L["h2"] else 1, L["dh"]), kind=PARAM)
+            shapes[name] = xs
+            var(name, xs)
+            params_of[name] = [g]
+            fns.append(("qknorm_fwd", [(X, R), (g, R)] + turned(L) + [(name, W)],
+                        {k: L[k] for k in ("h1", "h2", "dh", "rot", "layout")}))
+        elif op == "cross_attention":
+            a = cross(L)
+            rows_h = a["B"] * a["H"] * a["Tq"]
+            shapes[name] = xs
+            var(name, xs)
+            lse = var(name + ".lse", (a["B"], a["H"], a["Tq"]))
+            S = (slices or {}).get(name, (1, 1, 1))[0]
+            vs = [(X, R), (ins[1], R), (L["klen"], R), (name, W), (lse, W)]
+            if S > 1:
+                vs.append((var(name + ".part", (S * (math.prod(xs) + rows_h),)), W))
+            fns.append(("cross_attention_fwd", vs, a))
         else:
             raise ValueError(f"unknown layer kind {op}")
 
@@ -240,7 +287,7 @@ def lower(spec, keep_grads=False, slices=None):
     count = {}
 
     def contribute(tensor, g, pending):
-        if tensor == "x":
+        if tensor in inputs:
             return
         pending.append((tensor, g))
 
@@ -295,7 +342,7 @@ def lower(spec, keep_grads=False, slices=None):
             if Sw > 1:
                 vs.append((var(name + ".part", (Sw * (attrs["N"] * attrs["K"] + attrs["N"]),)), W))
             fns.append(("linear_bwd_w", vs, dict(attrs, slices=Sw)))
-            if X != "x":
+            if X not in inputs:
                 dX = var(f"d:{X}@{name}", xs)
                 fns.append(("linear_bwd_x", [(Wn, R), (dY, R), (dX, W)], attrs))
                 contribute(X, dX, pending)
@@ -313,7 +360,7 @@ def lower(spec, keep_grads=False, slices=None):
             if Sw > 1:
                 vs.append((var(name + ".part", (Sw * K * k * k * c,)), W))
             fns.append(("conv_bwd_w", vs, dict(attrs, slices=Sw)))
-            if X != "x":
+            if X not in inputs:
                 dX = var(f"d:{X}@{name}", xs)
                 fns.append(("conv_bwd_x", [(Wn, R), (dY, R), (dX, W)], attrs))
                 contribute(X, dX, pending)
@@ -385,7 +432,8 @@ def lower(spec, keep_grads=False, slices=None):
             contribute(X, dX, pending)
         elif op == "attention":
             rows, d3 = xs
-            Bt, T = spec["input"]
+            Bt = spec["input"][0]
+            T = rows // Bt
             H = L["heads"]
             dX = var(f"d:{X}@{name}", xs)
             Pb = var(name + ".Pb", (Bt, H, T, T))
@@ -394,6 +442,37 @@ def lower(spec, keep_grads=False, slices=None):
                         {"B": Bt, "T": T, "H": H, "dh": d3 // 3 // H,
                          "causal": int(L["causal"])}))
             contribute(X, dX, pending)
+        elif op == "rope":
+            dX = var(f"d:{X}@{name}", xs)
+            fns.append(("rope_bwd", [(dY, R)] + turned(L) + [(dX, W)],
+                        {k: L[k] for k in ("heads", "dh", "rot", "layout")}))
+            contribute(X, dX, pending)
+        elif op == "qknorm":
+            (gn,) = params_of[name]
+            dX = var(f"d:{X}@{name}", xs)
+            dgn = var("d:" + gn, decl[gn][0], kind=grad_kind)
+            S = min(math.ceil(xs[0] / 8), 2048)
+            part = var(name + ".part", (S,) + decl[gn][0])
+            fns.append(("qknorm_bwd", [(X, R), (gn, R)] + turned(L) +
+                        [(dY, R), (dX, W), (dgn, W), (part, W)],
+                        {k: L[k] for k in ("h1", "h2", "dh", "rot", "layout")}))
+            contribute(X, dX, pending)
+            update(name)
+        elif op == "cross_attention":
+            a, kv = cross(L), L["in"][1]
+            dq = var(f"d:{X}@{name}", xs)
+            dkv = var(f"d:{kv}@{name}", shapes[kv])
+            delta = var(name + ".delta", (a["B"], a["H"], a["Tq"]))
+            _, Sq, Skv = (slices or {}).get(name, (1, 1, 1))
+            n = max(Sq * math.prod(xs) if Sq > 1 else 0,
+                    Skv * math.prod(shapes[kv]) if Skv > 1 else 0)
+            vs = [(X, R), (kv, R), (L["klen"], R), (name, R), (name + ".lse", R), (dY, R),
+                  (dq, W), (dkv, W), (delta, W)]
+            if n:
+                vs.append((var(name + ".bpart", (n,)), W))
+            fns.append(("cross_attention_bwd", vs, a))
+            contribute(X, dq, pending)
+            contribute(kv, dkv, pending)
         done.add(name)
         settle(pending)
 

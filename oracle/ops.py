@@ -22,6 +22,10 @@ boundary: images NHWC, conv weights [K, R, S, C], dense weights [out, in].
                 positions masked (causal), context = P v; q, k, v are the
                 column thirds of one [rows, 3 d] projection, head h owning
                 columns h dh .. (h + 1) dh of each third
+* rotation:     the pair (x0, x1) of a head's columns, as x0 + i x1, times m e^(i pos f)
+* head norm:    per row and head, gain x / sqrt(mean x^2 + eps), eps = 1e-5, then the rotation
+* cross attention: per sequence and head, softmax(q k^T / sqrt(dh)) v over the first klen
+                states; no states: zero; query head h reads key head h Hkv / H
 * embedding:    x[b, t] = E[id[b, t]] + pos[t]
 * concat:       channel (last axis) concatenation; its backward hands each input
                 its own channel range of the output gradient
@@ -298,3 +302,113 @@ def embed_bwd(ids, dX, vocab):
     dE = np.zeros((vocab, d), dtype=dX.dtype)
     np.add.at(dE, ids.reshape(-1), dX)
     return dE, dX.reshape(B, T, d).sum(axis=0)
+
+
+# ---------------------------------------------------------------- rotary positions, head norms
+def _pairs(rot, layout):
+    i = np.arange(rot // 2)
+    return (2 * i, 2 * i + 1) if layout == 0 else (i, i + rot // 2)
+
+
+def _rotate(heads, pos, table, rot, layout, back):
+    """heads [rows, n, dh] with their pairs turned by pos * table."""
+    a = np.asarray(pos, np.float64)[:, None] * table[:-1]
+    w = table[-1] * np.exp(1j * (-a if back else a))[:, None, :]
+    i0, i1 = _pairs(rot, layout)
+    z = (heads[..., i0] + 1j * heads[..., i1]) * w
+    out = heads.copy()
+    out[..., i0], out[..., i1] = z.real, z.imag
+    return out
+
+
+def rope(X, pos, table, a, back=False):
+    n = a["heads"] * a["dh"]
+    out = X.copy()
+    h = X[:, :n].reshape(len(X), a["heads"], a["dh"])
+    out[:, :n] = _rotate(h, pos, table, a["rot"], a["layout"], back).reshape(len(X), n)
+    return out
+
+
+def _head_gain(gain, a):
+    return gain[(np.arange(a["h1"] + a["h2"]) >= a["h1"]).astype(int)]
+
+
+def qknorm_fwd(X, gain, pos=None, table=None, *, a):
+    heads = a["h1"] + a["h2"]
+    n = heads * a["dh"]
+    h = X[:, :n].reshape(len(X), heads, a["dh"])
+    y = _head_gain(gain, a) * h / np.sqrt((h * h).mean(-1, keepdims=True) + LN_EPS)
+    if a["rot"]:
+        y = _rotate(y, pos, table, a["rot"], a["layout"], False)
+    out = X.copy()
+    out[:, :n] = y.reshape(len(X), n)
+    return out
+
+
+def qknorm_bwd(X, gain, dY, pos=None, table=None, *, a):
+    """Returns (dX, dgain)."""
+    heads = a["h1"] + a["h2"]
+    n = heads * a["dh"]
+    h = X[:, :n].reshape(len(X), heads, a["dh"])
+    z = dY[:, :n].reshape(len(X), heads, a["dh"])
+    if a["rot"]:
+        z = _rotate(z, pos, table, a["rot"], a["layout"], True)
+    r = 1.0 / np.sqrt((h * h).mean(-1, keepdims=True) + LN_EPS)
+    u = h * r
+    per_head = (z * u).sum(0)
+    dgain = np.stack([per_head[s].sum(0) for s in ([slice(0, a["h1"])] +
+                     ([slice(a["h1"], None)] if a["h2"] else []))])
+    w = _head_gain(gain, a) * z
+    out = dY.copy()
+    out[:, :n] = (r * (w - u * (w * u).mean(-1, keepdims=True))).reshape(len(X), n)
+    return out, dgain
+
+
+# ---------------------------------------------------------------- cross attention
+def _cross_parts(q, kv, a):
+    B, Tq, Tk, H, Hkv, dh = (a[k] for k in ("B", "Tq", "Tk", "H", "Hkv", "dh"))
+    k, v = kv.reshape(B, Tk, 2, Hkv, dh).transpose(2, 0, 3, 1, 4)
+    return q.reshape(B, Tq, H, dh).transpose(0, 2, 1, 3), k, v, H // Hkv
+
+
+def _cross_probs(q, k, n):
+    """(P, lse) of one head over its first n keys (n >= 1)."""
+    S = q @ k[:n].T / np.sqrt(q.shape[-1])
+    top = S.max(-1, keepdims=True)
+    e = np.exp(S - top)
+    total = e.sum(-1, keepdims=True)
+    return e / total, (top + np.log(total))[:, 0]
+
+
+def cross_attention_fwd(q, kv, klen, a):
+    """Returns (Y [B Tq, H dh], lse [B, H, Tq])."""
+    Q, K, V, G = _cross_parts(q, kv, a)
+    Y, lse = np.zeros_like(Q), np.full(Q.shape[:3], -np.inf)
+    for b in range(a["B"]):
+        n = int(klen[b])
+        for h in range(a["H"] if n else 0):
+            P, lse[b, h] = _cross_probs(Q[b, h], K[b, h // G], n)
+            Y[b, h] = P @ V[b, h // G, :n]
+    return Y.transpose(0, 2, 1, 3).reshape(q.shape), lse
+
+
+def cross_attention_bwd(q, kv, klen, dY, a):
+    """Returns (dq, dkv, delta [B, H, Tq])."""
+    Q, K, V, G = _cross_parts(q, kv, a)
+    g = dY.reshape(a["B"], a["Tq"], a["H"], a["dh"]).transpose(0, 2, 1, 3)
+    dQ, dK, dV = np.zeros_like(Q), np.zeros_like(K), np.zeros_like(V)
+    delta = np.zeros(Q.shape[:3])
+    scale = 1.0 / np.sqrt(a["dh"])
+    for b in range(a["B"]):
+        n = int(klen[b])
+        for h in range(a["H"] if n else 0):
+            j = h // G
+            P, _ = _cross_probs(Q[b, h], K[b, j], n)
+            dP = g[b, h] @ V[b, j, :n].T
+            delta[b, h] = (P * dP).sum(-1)
+            dS = P * (dP - delta[b, h][:, None]) * scale
+            dQ[b, h] = dS @ K[b, j, :n]
+            dK[b, j, :n] += dS.T @ Q[b, h]
+            dV[b, j, :n] += P.T @ g[b, h]
+    dkv = np.stack([dK, dV]).transpose(1, 3, 0, 2, 4).reshape(kv.shape)
+    return dQ.transpose(0, 2, 1, 3).reshape(q.shape), dkv, delta

@@ -15,6 +15,9 @@ ooc_status transfer_resident(ooc_ctx* ctx, bool to_device);
 void release_device(ooc_ctx* ctx);
 ooc_status link_probe(int32_t device, uint64_t bytes, int32_t reps, double* h2d, double* d2h,
                       double* both, std::string* err);
+ooc_status run_fn(int32_t device, hipStream_t stream, int32_t op, void* const* ptrs,
+                  const uint64_t* bytes, const uint8_t* access, int32_t n, const int64_t* attrs,
+                  int32_t n_attrs, std::string* err);
 }  // namespace ooc
 
 using namespace ooc;
@@ -436,6 +439,51 @@ ooc_status ooc_wgrad_slices(int32_t op, const int64_t* attrs, int32_t n_attrs, i
   }
   g_create_error = "ooc_wgrad_slices: op must be CONV_BWD_W (11 attributes) or LINEAR_BWD_W (3)";
   return OOC_E_INVALID;
+}
+
+ooc_status ooc_qknorm_slices(int64_t rows, int64_t* slices) {
+  if (!slices || rows < 1) {
+    g_create_error = "ooc_qknorm_slices: bad argument";
+    return OOC_E_INVALID;
+  }
+  *slices = rows > 8 * 2048 ? 2048 : (rows + 7) / 8;
+  return OOC_OK;
+}
+
+ooc_status ooc_attention_slices(int32_t op, const int64_t* attrs, int32_t n_attrs,
+                                int64_t slices[2], uint64_t* part_bytes) {
+  if (!slices || !attrs || !part_bytes || n_attrs < 6) {
+    g_create_error = "ooc_attention_slices: NULL argument or fewer than 6 attributes";
+    return OOC_E_INVALID;
+  }
+  const bool fwd = op == OOC_OP_CROSS_ATTENTION_FWD;
+  if (!fwd && op != OOC_OP_CROSS_ATTENTION_BWD) {
+    g_create_error = "ooc_attention_slices: op must be CROSS_ATTENTION_FWD or _BWD";
+    return OOC_E_INVALID;
+  }
+  const std::string e = check_attention_shape(attrs);
+  if (!e.empty()) {
+    g_create_error = "ooc_attention_slices: " + e;
+    return OOC_E_INVALID;
+  }
+  const AttendShape a{attrs[0], attrs[1], attrs[2], attrs[3], attrs[4], attrs[5]};
+  int64_t full[8];
+  for (int j = 0; j < 6; ++j) full[j] = attrs[j];
+  slices[0] = full[6] = attention_key_slices(a, fwd);
+  slices[1] = full[7] = fwd ? 1 : attention_query_slices(a);
+  *part_bytes = (uint64_t)attention_part_bytes(fwd, full);
+  return OOC_OK;
+}
+
+ooc_status ooc_run_fn(int32_t hip_device, void* stream, int32_t op, void* const* ptrs,
+                      const uint64_t* bytes, const uint8_t* access, int32_t n,
+                      const int64_t* attrs, int32_t n_attrs) {
+  try {
+    return run_fn(hip_device, static_cast<hipStream_t>(stream), op, ptrs, bytes, access, n, attrs,
+                  n_attrs, &g_create_error);
+  } catch (const std::bad_alloc&) {
+    return OOC_E_HOST_OOM;   // no message: that would take memory
+  }
 }
 
 ooc_status ooc_fn_times(const ooc_ctx* ctx, double* buf, uint64_t cap, uint64_t* n) {

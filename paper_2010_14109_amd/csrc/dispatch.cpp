@@ -118,6 +118,30 @@ hipError_t launch_fn(const Fn& fn, void* const* p, const uint64_t* bytes, const 
       return upsample(true, F(0), F(1), a[0], a[1], a[2], a[3], s);
     case OOC_OP_UPSAMPLE_BWD:
       return upsample(false, F(0), F(1), a[0], a[1], a[2], a[3], s);
+    case OOC_OP_ROPE_FWD:
+    case OOC_OP_ROPE_BWD:
+      return rope(fn.op == OOC_OP_ROPE_BWD, F(0), static_cast<const int32_t*>(p[1]),
+                  static_cast<const double*>(p[2]), F(3), {a[0], a[1], a[2], a[3], a[4], a[5]}, s);
+    case OOC_OP_QKNORM_FWD:
+    case OOC_OP_QKNORM_BWD: {
+      const bool turn = a[5] > 0;
+      const int w = turn ? 4 : 2;   // the first variable behind pos and table
+      const int32_t* pos = turn ? static_cast<const int32_t*>(p[2]) : nullptr;
+      const double* table = turn ? static_cast<const double*>(p[3]) : nullptr;
+      const RopeShape r{a[0], a[1], a[2] + a[3], a[4], a[5], a[6]};
+      if (fn.op == OOC_OP_QKNORM_FWD)
+        return qknorm_fwd(F(0), F(1), pos, table, F(w), r, a[2], s);
+      return qknorm_bwd(F(0), F(1), pos, table, F(w), F(w + 1), F(w + 2), F(w + 3), r, a[2], a[7],
+                        s);
+    }
+    case OOC_OP_CROSS_ATTENTION_FWD:
+      return cross_attention_fwd(F(0), F(1), static_cast<const int32_t*>(p[2]), F(3), F(4),
+                                 a[6] > 1 ? F(5) : nullptr, {a[0], a[1], a[2], a[3], a[4], a[5]},
+                                 a[6], s);
+    case OOC_OP_CROSS_ATTENTION_BWD:
+      return cross_attention_bwd(F(0), F(1), static_cast<const int32_t*>(p[2]), F(3), F(4), F(5),
+                                 F(6), F(7), F(8), a[6] > 1 || a[7] > 1 ? F(9) : nullptr,
+                                 {a[0], a[1], a[2], a[3], a[4], a[5]}, a[6], a[7], s);
     default:
       return hipErrorInvalidValue;
   }

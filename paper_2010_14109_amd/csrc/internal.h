@@ -105,6 +105,12 @@ void build_plan(const std::vector<Var>& vars, const Schedule& s, bool incore, ui
 // Function-sequence rules and operation signatures; returns "" when valid.
 std::string check_fn(const std::vector<Var>& vars, const Fn& fn);
 
+// Cross attention: the shape B Tq Tk H Hkv dh ("" when valid), and the bytes of the partial results
+// for these attributes with their slice counts (0: none).
+constexpr int64_t kMaxAttentionSlices = 64;
+std::string check_attention_shape(const int64_t* attrs);
+int64_t attention_part_bytes(bool fwd, const int64_t* attrs);
+
 inline uint64_t round_up(uint64_t b, uint64_t c) { return (b + c - 1) / c * c; }
 
 }  // namespace ooc

@@ -117,6 +117,36 @@ hipError_t attention_bwd(const float* qkv, float* P, const float* dy, float* dqk
                          int64_t B, int64_t T, int64_t H, int64_t dh, bool causal, bool whole_P,
                          bool whole_dS, hipStream_t s);
 
+// Rotary positions and per-head norms (rope.hip).  Rows of cols floats; see ROPE_FWD / QKNORM_FWD.
+struct RopeShape {
+  int64_t rows, cols, heads, dh, rot, layout;
+};
+// back: the transposed rotation
+hipError_t rope(bool back, const float* x, const int32_t* pos, const double* table, float* y,
+                const RopeShape& r, hipStream_t s);
+// the first h1 of r.heads heads take gain row 0, the others row 1; pos and table null iff r.rot = 0
+hipError_t qknorm_fwd(const float* x, const float* gain, const int32_t* pos, const double* table,
+                      float* y, const RopeShape& r, int64_t h1, hipStream_t s);
+hipError_t qknorm_bwd(const float* x, const float* gain, const int32_t* pos, const double* table,
+                      const float* dy, float* dx, float* dgain, float* part, const RopeShape& r,
+                      int64_t h1, int64_t slices, hipStream_t s);
+
+// Cross attention (attend.hip); part null iff every slice count is 1.
+struct AttendShape {
+  int64_t B, Tq, Tk, H, Hkv, dh;
+};
+hipError_t cross_attention_fwd(const float* q, const float* kv, const int32_t* klen, float* y,
+                               float* lse, float* part, const AttendShape& a, int64_t slices,
+                               hipStream_t s);
+hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* klen,
+                               const float* y, const float* lse, const float* dy, float* dq,
+                               float* dkv, float* delta, float* part, const AttendShape& a,
+                               int64_t q_slices, int64_t kv_slices, hipStream_t s);
+// Slice counts the launchers run best with: of the keys for a pass over query rows (forward, dq),
+// of the query rows for the pass over keys (dkv).
+int64_t attention_key_slices(const AttendShape& a, bool fwd);
+int64_t attention_query_slices(const AttendShape& a);
+
 hipError_t mix(void* const* ptrs, const uint64_t* words, int nvars, uint32_t seed, hipStream_t s,
                bool y_read);
 

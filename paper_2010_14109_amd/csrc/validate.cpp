@@ -2,6 +2,8 @@
 // attribute count and each variable's byte size against the attributes.
 // A kernel indexes its buffers from the attributes alone, so nothing reaches
 // the device unless these checks passed.
+#include <algorithm>
+#include <initializer_list>
 #include <string>
 
 #include "internal.h"
@@ -50,11 +52,45 @@ const Sig kSig[OOC_OP_COUNT] = {
     {"UPSAMPLE_FWD", 2, 4, {OOC_R, OOC_W}},
     {"UPSAMPLE_BWD", 2, 4, {OOC_R, OOC_W}},
     {"ACC", 2, 1, {OOC_RW, OOC_R}},
+    {"ROPE_FWD", 4, 6, {OOC_R, OOC_R, OOC_R, OOC_W}},
+    {"ROPE_BWD", 4, 6, {OOC_R, OOC_R, OOC_R, OOC_W}},
+    {"QKNORM_FWD", -1, 7, {}},
+    {"QKNORM_BWD", -1, 8, {}},
+    {"CROSS_ATTENTION_FWD", -1, 7, {}},
+    {"CROSS_ATTENTION_BWD", -1, 8, {}},
 };
 
 const int64_t kMaxElems = int64_t(1) << 40;
 
+// The product of non-negative factors, or -1 where it passes 2^52 (no variable is that large).
+int64_t product(std::initializer_list<int64_t> factors) {
+  int64_t p = 1;
+  for (int64_t f : factors)
+    if (__builtin_mul_overflow(p, f, &p) || p > (int64_t(1) << 52)) return -1;
+  return p;
+}
+
 }  // namespace
+
+std::string check_attention_shape(const int64_t* a) {
+  const int64_t B = a[0], Tq = a[1], Tk = a[2], H = a[3], Hkv = a[4], dh = a[5];
+  if (B <= 0 || Tq <= 0 || Tk <= 0 || H <= 0 || Hkv <= 0 || dh <= 0 || H % Hkv)
+    return "bad attributes";
+  if (dh > 256) return "head width above 256";
+  // the kernels count rows of a sequence in 32 bits, heads and sequences in 16
+  if (Tk > (1 << 28) || product({Tq, H / Hkv}) < 0 || Tq * (H / Hkv) > (1 << 28) || H > 65535 ||
+      product({B, H}) < 0 || B * H > (1 << 24))
+    return "sequence, head or batch count too large";
+  if (product({B, Tq, H, dh, 4}) < 0 || product({B, Tk, Hkv, dh, 8}) < 0) return "tensor too large";
+  return "";
+}
+
+int64_t attention_part_bytes(bool fwd, const int64_t* a) {
+  const int64_t B = a[0], Tq = a[1], Tk = a[2], H = a[3], Hkv = a[4], dh = a[5];
+  const int64_t q = B * Tq * H * dh * 4, kv = B * Tk * Hkv * dh * 8, rows = B * H * Tq * 4;
+  if (fwd) return a[6] > 1 ? a[6] * (q + rows) : 0;
+  return std::max(a[6] > 1 ? a[6] * q : 0, a[7] > 1 ? a[7] * kv : 0);
+}
 
 std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
   if (fn.op < 0 || fn.op >= OOC_OP_COUNT) return "unknown operation " + std::to_string(fn.op);
@@ -325,6 +361,81 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
       const int64_t small = N * H * W * C * 4, big = 4 * small;
       NEED(0, fn.op == OOC_OP_UPSAMPLE_FWD ? small : big, "input");
       NEED(1, fn.op == OOC_OP_UPSAMPLE_FWD ? big : small, "output");
+      return "";
+    }
+    case OOC_OP_ROPE_FWD:
+    case OOC_OP_ROPE_BWD: {
+      const int64_t rows = a[0], cols = a[1], heads = a[2], dh = a[3], rot = a[4], layout = a[5];
+      const int64_t used = product({heads, dh});
+      if (rows <= 0 || rows > INT32_MAX || heads <= 0 || dh <= 0 || used < 0 || cols < used ||
+          cols > INT32_MAX / 4 || rot < 2 || rot % 2 || rot > dh || rot > 1024 || (layout != 0 && layout != 1))
+        return nm + ": bad attributes";
+      const int64_t xb = product({rows, cols, 4});
+      NEED(0, xb, "rows");
+      NEED(1, rows * 4, "pos");
+      NEED(2, (rot / 2 + 1) * 8, "table");
+      NEED(3, xb, "output");
+      return "";
+    }
+    case OOC_OP_QKNORM_FWD:
+    case OOC_OP_QKNORM_BWD: {
+      const int64_t rows = a[0], cols = a[1], h1 = a[2], h2 = a[3], dh = a[4], rot = a[5],
+                    layout = a[6];
+      const int64_t used = product({h1 + h2, dh});
+      const bool fwd = fn.op == OOC_OP_QKNORM_FWD;
+      if (rows <= 0 || rows > INT32_MAX || h1 <= 0 || dh <= 0 || dh > 1024 || used < 0 || cols < used ||
+          cols > INT32_MAX / 4 || rot % 2 || rot > dh || (layout != 0 && layout != 1))
+        return nm + ": bad attributes";
+      const int w = rot > 0 ? 2 : 0;   // pos and table
+      if (nv != (fwd ? 3 : 6) + w) return nm + ": takes pos and table iff rot > 0";
+      for (int j = 0; j < nv; ++j)
+        if (v[j].access != (j < (fwd ? 2 : 3) + w ? OOC_R : OOC_W)) return nm + ": wrong access";
+      const int64_t xb = product({rows, cols, 4}), gb = (h2 > 0 ? 2 : 1) * dh * 4;
+      NEED(0, xb, "X");
+      NEED(1, gb, "gain");
+      if (w) {
+        NEED(2, rows * 4, "pos");
+        NEED(3, (rot / 2 + 1) * 8, "table");
+      }
+      if (fwd) {
+        NEED(2 + w, xb, "Y");
+        return "";
+      }
+      const int64_t slices = a[7];
+      if (slices < 1 || slices > rows || slices > 65535) return nm + ": bad slice count";
+      NEED(2 + w, xb, "dY");
+      NEED(3 + w, xb, "dX");
+      NEED(4 + w, gb, "dgain");
+      NEED(5 + w, slices * gb, "partial sums");
+      return "";
+    }
+    case OOC_OP_CROSS_ATTENTION_FWD:
+    case OOC_OP_CROSS_ATTENTION_BWD: {
+      const bool fwd = fn.op == OOC_OP_CROSS_ATTENTION_FWD;
+      e = check_attention_shape(a.data());
+      if (!e.empty()) return nm + ": " + e;
+      const int64_t B = a[0], Tq = a[1], Tk = a[2], H = a[3], Hkv = a[4], dh = a[5];
+      const int64_t qb = product({B, Tq, H, dh, 4}), kb = product({B, Tk, Hkv, dh, 8}),
+                    lb = product({B, H, Tq, 4});
+      if (a[6] < 1 || a[6] > kMaxAttentionSlices || a[6] > Tk || (!fwd && (a[7] < 1 ||
+          a[7] > kMaxAttentionSlices || a[7] > product({Tq, H / Hkv}))))
+        return nm + ": bad slice count";
+      const int64_t part = attention_part_bytes(fwd, a.data());
+      if (nv != (fwd ? 5 : 9) + (part > 0)) return nm + ": partial variable iff a slice count > 1";
+      for (int j = 0; j < nv; ++j)
+        if (v[j].access != (j < (fwd ? 3 : 6) ? OOC_R : OOC_W)) return nm + ": wrong access";
+      NEED(0, qb, "q");
+      NEED(1, kb, "kv");
+      NEED(2, B * 4, "klen");
+      NEED(3, qb, "Y");
+      NEED(4, lb, "lse");
+      if (!fwd) {
+        NEED(5, qb, "dY");
+        NEED(6, qb, "dq");
+        NEED(7, kb, "dkv");
+        NEED(8, lb, "delta");
+      }
+      if (part) NEED(nv - 1, part, "partial results");
       return "";
     }
     case OOC_OP_MIX: {

@@ -26,12 +26,16 @@ S_w > 1; a LayerNorm keeps mean and 1/std per row and 2 S floats per feature
 with S = min(ceil(rows / 32), 2048) (its rows are d floats wide); attention
 writes its probabilities [B, H, T, T] in the forward, where they die, and its
 backward recomputes them into a variable of its own beside a scratch of the
-same size.
+same size; cross attention keeps one logarithm per row and head instead.
+
+``spec["input"]`` is the shape of the input ``x``; ``spec["inputs"]`` lists
+further INPUT variables, ``{"name", "shape", "dtype"}``: the tokens and lengths
+of a second sequence, positions, tables of angles.
 """
 
 from __future__ import annotations
 
-from math import ceil, prod
+from math import ceil, log, pi, prod
 
 from . import ooc
 
@@ -46,6 +50,24 @@ def ln_row_slices(rows):
     return min(ceil(rows / 32), 2048)
 
 
+def rotary_table(rot, base=10000.0, scale=1.0, trained=None, turns=(1.0, 32.0)):
+    """The table of a rotation over ``rot`` columns: radians per position of each pair, base^(-2 i
+    / rot), then the magnitude.  ``scale`` > 1 stretches the context: without ``trained`` every
+    angle is divided by it; with ``trained`` (positions of the trained context) pairs that turn
+    fewer than ``turns[0]`` times in it are divided, those that turn more than ``turns[1]`` times
+    are kept, those in between mixed in proportion, and the magnitude is 1 + ln(scale) / 10."""
+    if rot < 2 or rot % 2:
+        raise ValueError("the rotated width must be even and positive")
+    if base <= 0 or scale < 1 or not 0 <= turns[0] < turns[1] or (trained is not None and trained <= 0):
+        raise ValueError("rotary_table: base and trained positive, scale at least 1, turns increasing")
+    f = [base ** (-2.0 * i / rot) for i in range(rot // 2)]
+    if trained is None:
+        return [a / scale for a in f] + [1.0]
+    keep = [min(1.0, max(0.0, (trained * a / (2 * pi) - turns[0]) / (turns[1] - turns[0])))
+            for a in f]
+    return [a * k + a / scale * (1 - k) for a, k in zip(f, keep)] + [1.0 + 0.1 * log(scale)]
+
+
 class Net:
     """Function sequence of one training step of ``spec``."""
 
@@ -56,7 +78,8 @@ class Net:
         self.calls = []       # (op, [(name, access)], attrs)
         self.shape = {}
         self.params = {}      # layer name -> [param names]
-        self.slices = {}      # layer name -> split-K slices of its weight gradient
+        self.slices = {}      # layer name -> split-K slices of its weight gradient, or a cross
+                              # attention's slice counts (forward, dq, dkv)
         self._lower()
         self._number()
 
@@ -191,7 +214,8 @@ class Net:
 
     def _attn_attrs(self, L, X):
         rows, d3 = self.shape[X]
-        B, T = self.spec["input"]
+        B = self.spec["input"][0]
+        T = rows // B
         H = L["heads"]
         return [B, T, H, d3 // 3 // H, 1 if L["causal"] else 0]
 
@@ -202,6 +226,58 @@ class Net:
         Y = self._decl(L["name"], (B * T, H * dh))
         self._call("attention_fwd", [(X, ooc.R), (Pr, ooc.W), (Y, ooc.W)], a)
         return (B * T, H * dh)
+
+    def _turned_by(self, L, rows):
+        """The pos and table variables of a rotating layer, checked against its rows."""
+        pos, table = L["pos"], L["table"]
+        for name, shape, dtype in ((pos, (rows,), "i32"), (table, (L["rot"] // 2 + 1,), "f64")):
+            if name not in self.inputs or self.meta[name][:2] != (shape, dtype):
+                raise ValueError(f"{L['name']}: {name} must be an input of {shape} {dtype}")
+        return [(pos, ooc.R), (table, ooc.R)]
+
+    def _fwd_rope(self, L, X):
+        rows, cols = self.shape[X]
+        Y = self._decl(L["name"], (rows, cols))
+        self._call("rope_fwd", [(X, ooc.R)] + self._turned_by(L, rows) + [(Y, ooc.W)],
+                   [rows, cols, L["heads"], L["dh"], L["rot"], L["layout"]])
+        return (rows, cols)
+
+    def _qknorm_attrs(self, L, X):
+        return list(self.shape[X]) + [L["h1"], L["h2"], L["dh"], L["rot"], L["layout"]]
+
+    def _fwd_qknorm(self, L, X):
+        rows, cols = self.shape[X]
+        g = self._decl(L["name"] + ".gain", (2 if L["h2"] else 1, L["dh"]), kind=ooc.PARAM)
+        self.params[L["name"]] = [g]
+        Y = self._decl(L["name"], (rows, cols))
+        where = self._turned_by(L, rows) if L["rot"] else []
+        self._call("qknorm_fwd", [(X, ooc.R), (g, ooc.R)] + where + [(Y, ooc.W)],
+                   self._qknorm_attrs(L, X))
+        return (rows, cols)
+
+    def _cross_attrs(self, L):
+        q, kv = L["in"]
+        B = self.spec["input"][0]
+        H, Hkv = L["heads"], L["kv_heads"]
+        dh = self.shape[q][1] // H
+        if self.shape[q][1] != H * dh or self.shape[kv][1] != 2 * Hkv * dh:
+            raise ValueError(f"{L['name']}: query and key widths do not fit the heads")
+        if self.meta.get(L["klen"], (None,))[0] != (B,) or L["klen"] not in self.inputs:
+            raise ValueError(f"{L['name']}: {L['klen']} must be an input of one length per sequence")
+        return [B, self.shape[q][0] // B, self.shape[kv][0] // B, H, Hkv, dh]
+
+    def _fwd_cross_attention(self, L, X):
+        a = self._cross_attrs(L)
+        B, Tq, _, H, _, _ = a
+        slices, part = ooc.attention_slices("cross_attention_fwd", a)
+        Y = self._decl(L["name"], self.shape[X])
+        lse = self._decl(L["name"] + ".lse", (B, H, Tq))
+        pairs = [(X, ooc.R), (L["in"][1], ooc.R), (L["klen"], ooc.R), (Y, ooc.W), (lse, ooc.W)]
+        if part:
+            pairs.append((self._decl(L["name"] + ".part", (part // FLOAT,)), ooc.W))
+        self._call("cross_attention_fwd", pairs, a + slices)
+        self.slices[L["name"]] = slices + ooc.attention_slices("cross_attention_bwd", a)[0]
+        return self.shape[X]
 
     # ------------------------------------------------------------ backward
     def _grad_of_param(self, p):
@@ -234,7 +310,7 @@ class Net:
             if sw > 1:
                 pairs.append((self._decl(name + ".part", (sw * (fout * fin + fout),)), ooc.W))
             self._call("linear_bwd_w", pairs, attrs + [sw])
-            if X != "x":
+            if X not in self.inputs:
                 dX = self._decl(f"d:{X}@{name}", xs)
                 self._call("linear_bwd_x", [(W, ooc.R), (dY, ooc.R), (dX, ooc.W)], attrs)
                 out.append((X, dX))
@@ -249,7 +325,7 @@ class Net:
             if sw > 1:
                 pairs.append((self._decl(name + ".part", (sw * K * R * S * c,)), ooc.W))
             self._call("conv_bwd_w", pairs, a + [sw])
-            if X != "x":
+            if X not in self.inputs:
                 dX = self._decl(f"d:{X}@{name}", xs)
                 self._call("conv_bwd_x", [(W, ooc.R), (dY, ooc.R), (dX, ooc.W)], a)
                 out.append((X, dX))
@@ -324,18 +400,57 @@ class Net:
                                          (dX, ooc.W), (dS, ooc.W)], a)
             out.append((X, dX))
 
+        elif op == "rope":
+            dX = self._decl(f"d:{X}@{name}", xs)
+            self._call("rope_bwd", [(dY, ooc.R)] + self._turned_by(L, xs[0]) + [(dX, ooc.W)],
+                       list(xs) + [L["heads"], L["dh"], L["rot"], L["layout"]])
+            out.append((X, dX))
+        elif op == "qknorm":
+            (g,) = self.params[name]
+            S = ooc.qknorm_slices(xs[0])
+            dX = self._decl(f"d:{X}@{name}", xs)
+            dg = self._grad_of_param(g)
+            part = self._decl(name + ".part", (S,) + self.meta[g][0])
+            where = self._turned_by(L, xs[0]) if L["rot"] else []
+            self._call("qknorm_bwd", [(X, ooc.R), (g, ooc.R)] + where +
+                       [(dY, ooc.R), (dX, ooc.W), (dg, ooc.W), (part, ooc.W)],
+                       self._qknorm_attrs(L, X) + [S])
+            out.append((X, dX))
+            self._sgd(name)
+        elif op == "cross_attention":
+            a = self._cross_attrs(L)
+            B, Tq, _, H, _, _ = a
+            kv = L["in"][1]
+            slices, part = ooc.attention_slices("cross_attention_bwd", a)
+            dq = self._decl(f"d:{X}@{name}", xs)
+            dkv = self._decl(f"d:{kv}@{name}", self.shape[kv])
+            delta = self._decl(name + ".delta", (B, H, Tq))
+            pairs = [(X, ooc.R), (kv, ooc.R), (L["klen"], ooc.R), (name, ooc.R),
+                     (name + ".lse", ooc.R), (dY, ooc.R), (dq, ooc.W), (dkv, ooc.W),
+                     (delta, ooc.W)]
+            if part:
+                pairs.append((self._decl(name + ".bpart", (part // FLOAT,)), ooc.W))
+            self._call("cross_attention_bwd", pairs, a + slices)
+            out += [(X, dq), (kv, dkv)]
+
     # ------------------------------------------------------------ whole step
     def _lower(self):
         spec = self.spec
         self.shape["x"] = tuple(spec["input"])
         self._decl("x", spec["input"], dtype="i32" if spec.get("tokens") else "f32",
                    kind=ooc.INPUT)
+        self.inputs = {"x"}
+        for v in spec.get("inputs", ()):
+            self.shape[v["name"]] = tuple(v["shape"])
+            self._decl(v["name"], v["shape"], dtype=v["dtype"], kind=ooc.INPUT)
+            self.inputs.add(v["name"])
         fwd = {"linear": self._fwd_linear, "conv": self._fwd_conv, "bn": self._fwd_bn,
                "relu": self._fwd_relu, "maxpool": self._fwd_maxpool,
                "avgpool": self._fwd_avgpool, "add": self._fwd_add, "embed": self._fwd_embed,
                "layernorm": self._fwd_layernorm, "gelu": self._fwd_gelu,
                "attention": self._fwd_attention, "concat": self._fwd_concat,
-               "upsample": self._fwd_upsample}
+               "upsample": self._fwd_upsample, "rope": self._fwd_rope,
+               "qknorm": self._fwd_qknorm, "cross_attention": self._fwd_cross_attention}
         for L in spec["layers"]:
             self.shape[L["name"]] = fwd[L["op"]](L, L["in"][0])
         logits = spec["logits"]
@@ -356,7 +471,7 @@ class Net:
             self._bwd(L, grads[L["name"]], contributions)
             visited.add(L["name"])
             for tensor, g in contributions:
-                if tensor == "x":
+                if tensor in self.inputs:
                     continue
                 if tensor not in grads:
                     grads[tensor] = g
@@ -382,7 +497,7 @@ class Net:
             for nm, _ in pairs:
                 self.ids.setdefault(nm, len(self.ids))
         self.names = sorted(self.ids, key=self.ids.get)
-        itemsize = {"f32": 4, "i32": 4, "u8": 1}
+        itemsize = {"f32": 4, "i32": 4, "u8": 1, "f64": 8}
         self.var_bytes = [prod(self.meta[n][0]) * itemsize[self.meta[n][1]] for n in self.names]
         self.var_kinds = [self.meta[n][2] for n in self.names]
         self.fn_vars = [[(self.ids[nm], a) for nm, a in pairs] for _, pairs, _ in self.calls]

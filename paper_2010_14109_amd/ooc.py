@@ -34,6 +34,8 @@ OPS = {
     "layernorm_fwd": 21, "layernorm_bwd": 22, "gelu_fwd": 23, "gelu_bwd": 24,
     "attention_fwd": 25, "attention_bwd": 26, "concat_fwd": 27, "concat_bwd": 28,
     "upsample_fwd": 29, "upsample_bwd": 30, "acc": 31,
+    "rope_fwd": 32, "rope_bwd": 33, "qknorm_fwd": 34, "qknorm_bwd": 35,
+    "cross_attention_fwd": 36, "cross_attention_bwd": 37,
 }
 
 #: every symbol ``include/ooc.h`` declares
@@ -45,6 +47,7 @@ EXPORTS = [
     "ooc_download", "ooc_step", "ooc_get_stats", "ooc_fn_times", "ooc_link_probe",
     "ooc_timeline", "ooc_set_swapout_depth", "ooc_set_fixed_distance", "ooc_bestfit_extent",
     "ooc_set_wait_order", "ooc_set_host_limit", "ooc_wgrad_slices", "ooc_set_layout",
+    "ooc_qknorm_slices", "ooc_attention_slices", "ooc_run_fn",
 ]
 
 
@@ -138,6 +141,12 @@ def load(path=LIB_PATH):
         "ooc_timeline": ([P, c.POINTER(ooc_span), c.c_uint64, c.POINTER(c.c_uint64)], c.c_int32),
         "ooc_wgrad_slices": ([c.c_int32, c.POINTER(c.c_int64), c.c_int32, c.POINTER(c.c_int64)],
                              c.c_int32),
+        "ooc_qknorm_slices": ([c.c_int64, c.POINTER(c.c_int64)], c.c_int32),
+        "ooc_attention_slices": ([c.c_int32, c.POINTER(c.c_int64), c.c_int32,
+                                  c.POINTER(c.c_int64), c.POINTER(c.c_uint64)], c.c_int32),
+        "ooc_run_fn": ([c.c_int32, P, c.c_int32, c.POINTER(P), c.POINTER(c.c_uint64),
+                        c.POINTER(c.c_uint8), c.c_int32, c.POINTER(c.c_int64), c.c_int32],
+                       c.c_int32),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -174,7 +183,41 @@ def wgrad_slices(op, attrs):
     return out.value
 
 
-_NP = {"f32": np.float32, "i32": np.int32, "u8": np.uint8, "u32": np.uint32}
+def qknorm_slices(rows):
+    """Row slices of a per-head norm's backward (``qknorm_bwd``)."""
+    out = ctypes.c_int64()
+    _check(load().ooc_qknorm_slices(rows, ctypes.byref(out)), None)
+    return out.value
+
+
+def attention_slices(op, attrs):
+    """``(slice counts, bytes of the part variable)`` of a cross attention with the shape B, Tq,
+    Tk, H, Hkv, dh, as the library's kernels want them: one count for ``cross_attention_fwd``,
+    two for ``cross_attention_bwd``.  They follow the shape in the operation's attributes."""
+    a = (ctypes.c_int64 * len(attrs))(*attrs)
+    out, part = (ctypes.c_int64 * 2)(), ctypes.c_uint64()
+    op = OPS[op] if isinstance(op, str) else op
+    _check(load().ooc_attention_slices(op, a, len(attrs), out, ctypes.byref(part)), None)
+    return list(out)[:1 if op == OPS["cross_attention_fwd"] else 2], part.value
+
+
+def run_fn(op, vars_, access, attrs=(), device=0, stream=0):
+    """Runs one operation alone on the caller's device memory (see ooc_run_fn): ``vars_`` are its
+    variables as ``(device address, bytes)``, ``access`` and ``attrs`` as ``add_fn`` takes them,
+    ``stream`` a HIP stream handle of ``device`` (a PyTorch stream's ``cuda_stream``).  Returns
+    once the kernels are enqueued.  A program that passes PyTorch's memory imports torch before
+    the first call here, so that both use one HIP runtime."""
+    n = len(vars_)
+    p = (ctypes.c_void_p * n)(*[v for v, _ in vars_])
+    b = (ctypes.c_uint64 * n)(*[s for _, s in vars_])
+    a = (ctypes.c_uint8 * n)(*access)
+    at = (ctypes.c_int64 * max(1, len(attrs)))(*attrs)
+    op = OPS[op] if isinstance(op, str) else op
+    _check(load().ooc_run_fn(device, stream, op, p, b, a, n, at, len(attrs)), None)
+
+
+_NP = {"f32": np.float32, "i32": np.int32, "u8": np.uint8, "u32": np.uint32,
+       "f64": np.float64}
 
 
 class Context:

@@ -147,6 +147,77 @@ def transformer(batch=64, seq=512, d=1024, heads=16, ffn=4096, layers=48, vocab=
             "optimizer": {"lr": lr, "momentum": momentum}}
 
 
+def seq2seq(batch=24, src_seq=512, seq=512, d=1024, heads=16, kv_heads=4, ffn=4096, layers=6,
+            vocab=32000, lr=0.01, momentum=0.9):
+    """Encoder-decoder transformer: every self-attention reads rotated queries and keys (in the
+    encoder adjacent pairs of half of each head, in the decoder, after per-head norms, pairs half
+    a head apart), and each decoder layer attends to the encoder's states, padded to ``src_seq``
+    and of ``src_len`` tokens each, with ``kv_heads`` shared key heads and normalised queries and
+    keys.  Trained on next-token cross-entropy of the decoder."""
+    dh = d // heads
+    L = []
+
+    def lin(name, src, fin, fout):
+        L.append({"name": name, "op": "linear", "in": [src], "in_features": fin,
+                  "out_features": fout})
+        return name
+
+    def norm(name, src):
+        L.append({"name": name, "op": "layernorm", "in": [src]})
+        return name
+
+    def join(name, a, b):
+        L.append({"name": name, "op": "add", "in": [a, b]})
+        return name
+
+    def qknorm(name, src, h1, h2, turn):
+        L.append({"name": name, "op": "qknorm", "in": [src], "h1": h1, "h2": h2, "dh": dh,
+                  "rot": dh // 2 * 2 if turn else 0, "layout": 1, "pos": "pos", "table": "table"})
+        return name
+
+    def attend(b, qkv, src, causal):
+        L.append({"name": f"{b}.attn", "op": "attention", "in": [qkv], "heads": heads,
+                  "causal": causal})
+        return join(f"{b}.res1", lin(f"{b}.proj", f"{b}.attn", d, d), src)
+
+    def feed(b, src):
+        lin(f"{b}.fc1", norm(f"{b}.lnf", src), d, ffn)
+        L.append({"name": f"{b}.gelu", "op": "gelu", "in": [f"{b}.fc1"]})
+        return join(f"{b}.res3", lin(f"{b}.fc2", f"{b}.gelu", ffn, d), src)
+
+    L.append({"name": "src_embed", "op": "embed", "in": ["src"], "vocab": vocab, "d": d})
+    prev = "src_embed"
+    rot = max(2, dh // 4 * 2)
+    for i in range(layers):
+        b = f"e{i + 1}"
+        lin(f"{b}.qkv", norm(f"{b}.ln1", prev), d, 3 * d)
+        L.append({"name": f"{b}.rope", "op": "rope", "in": [f"{b}.qkv"], "heads": 2 * heads,
+                  "dh": dh, "rot": rot, "layout": 0, "pos": "src_pos", "table": "src_table"})
+        prev = feed(b, attend(b, f"{b}.rope", prev, False))
+    memory = norm("memory", prev)
+    L.append({"name": "embed", "op": "embed", "in": ["x"], "vocab": vocab, "d": d})
+    prev = "embed"
+    for i in range(layers):
+        b = f"d{i + 1}"
+        lin(f"{b}.qkv", norm(f"{b}.ln1", prev), d, 3 * d)
+        prev = attend(b, qknorm(f"{b}.qk", f"{b}.qkv", heads, heads, True), prev, True)
+        q = qknorm(f"{b}.qn", lin(f"{b}.q", norm(f"{b}.ln2", prev), d, d), heads, 0, False)
+        kv = qknorm(f"{b}.kn", lin(f"{b}.kv", memory, d, 2 * kv_heads * dh), kv_heads, 0, False)
+        L.append({"name": f"{b}.cross", "op": "cross_attention", "in": [q, kv], "heads": heads,
+                  "kv_heads": kv_heads, "klen": "src_len"})
+        prev = feed(b, join(f"{b}.res2", lin(f"{b}.cproj", f"{b}.cross", d, d), prev))
+    lin("head", norm("lnf", prev), d, vocab)
+    inputs = [{"name": "src", "shape": [batch, src_seq], "dtype": "i32"},
+              {"name": "src_len", "shape": [batch], "dtype": "i32"},
+              {"name": "src_pos", "shape": [batch * src_seq], "dtype": "i32"},
+              {"name": "src_table", "shape": [rot // 2 + 1], "dtype": "f64"},
+              {"name": "pos", "shape": [batch * seq], "dtype": "i32"},
+              {"name": "table", "shape": [dh // 2 + 1], "dtype": "f64"}]
+    return {"name": f"seq2seq{layers}_d{d}_b{batch}_t{src_seq}_{seq}", "input": [batch, seq],
+            "inputs": inputs, "tokens": True, "classes": vocab, "layers": L, "logits": "head",
+            "init": "normal", "optimizer": {"lr": lr, "momentum": momentum}}
+
+
 def densenet(batch=64, hw=64, growth=32, blocks=(6, 12, 24, 16), stem=64, classes=10,
              lr=0.01, momentum=0.9):
     """DenseNet-shaped network (no bottleneck): inside a block every layer reads the channel
@@ -243,14 +314,16 @@ def unet(batch=8, hw=256, base=64, depth=4, classes=8, lr=0.01, momentum=0.9):
 
 
 #: The workloads: name -> (network description, budget as a fraction of the
-#: in-core peak).  The first five are the benchmark configurations; densenet
-#: and unet are long-skip networks whose feature maps are read many times.
+#: in-core peak).  seq2seq is an encoder-decoder transformer; densenet and unet
+#: are long-skip networks whose feature maps are read many times; the others are
+#: the benchmark configurations.
 WORKLOADS = {
     "mlp": (lambda: mlp(), 0.40),
     "cnn": (lambda: plain_cnn(), 0.50),
     "resnet50_b256": (lambda: resnet(batch=256), 0.25),
     "resnet50_b1440": (lambda: resnet(batch=1440), 1.0 / 7.5),
     "transformer": (lambda: transformer(), 0.20),
+    "seq2seq": (lambda: seq2seq(), 0.20),
     "densenet": (lambda: densenet(), 0.25),
     "unet": (lambda: unet(), 0.25),
 }
@@ -260,7 +333,7 @@ def workload(name, **overrides):
     """Network description of a named workload, with keyword overrides (e.g. ``batch=8``)."""
     builders = {"mlp": mlp, "cnn": plain_cnn, "resnet50_b256": resnet,
                 "resnet50_b1440": resnet, "transformer": transformer, "densenet": densenet,
-                "unet": unet}
+                "unet": unet, "seq2seq": seq2seq}
     defaults = {"resnet50_b256": {"batch": 256}, "resnet50_b1440": {"batch": 1440}}
     kw = dict(defaults.get(name, {}))
     kw.update(overrides)
@@ -282,10 +355,14 @@ def param_shapes(spec):
     The shapes are read off the layer hyper-parameters only.
     """
     out = []
+    length = {"x": spec["input"][1]} if spec.get("tokens") else {}
+    length.update((v["name"], v["shape"][1]) for v in spec.get("inputs", ()) if len(v["shape"]) == 2)
     for L in spec["layers"]:
         if L["op"] == "embed":
             out.append((L["name"] + ".E", (L["vocab"], L["d"])))
-            out.append((L["name"] + ".pos", (spec["input"][1], L["d"])))
+            out.append((L["name"] + ".pos", (length[L["in"][0]], L["d"])))
+        elif L["op"] == "qknorm":
+            out.append((L["name"] + ".gain", (2 if L["h2"] else 1, L["dh"])))
         elif L["op"] == "layernorm":
             out.append((L["name"] + ".gamma", (_width(spec, L),)))
             out.append((L["name"] + ".beta", (_width(spec, L),)))
@@ -320,6 +397,27 @@ def make_inputs(spec, seed=0):
     return x, labels
 
 
+def make_extra_inputs(spec, tables, seed=2):
+    """``{name: array}`` of ``spec["inputs"]``: tokens uniform over the vocabulary, lengths uniform
+    over 1 .. the sequence, positions counting up in each sequence, and ``tables`` (name -> table
+    of angles)."""
+    g = np.random.Generator(np.random.PCG64(seed))
+    shapes = {v["name"]: tuple(v["shape"]) for v in spec.get("inputs", ())}
+    batch = spec["input"][0]
+    out = {}
+    for v in spec.get("inputs", ()):
+        name, shape = v["name"], tuple(v["shape"])
+        if name in tables:
+            out[name] = np.asarray(tables[name], np.float64).reshape(shape)
+        elif name.endswith("_len"):
+            out[name] = g.integers(1, shapes[name[:-4]][1] + 1, size=shape).astype(np.int32)
+        elif name.endswith("pos"):
+            out[name] = (np.arange(shape[0]) % (shape[0] // batch)).astype(np.int32)
+        else:
+            out[name] = g.integers(0, spec["classes"], size=shape).astype(np.int32)
+    return out
+
+
 def make_params(spec, seed=1):
     """Initial parameters ``{name: float32 array}`` (He-normal fan-in, zero bias, BN 1/0)."""
     g = np.random.Generator(np.random.PCG64(seed))
@@ -334,7 +432,7 @@ def make_params(spec, seed=1):
             fan_in = int(np.prod(shape[1:]))
             std = np.float32(np.sqrt(2.0 / fan_in))
             params[name] = (g.standard_normal(size=shape, dtype=np.float32) * std).astype(np.float32)
-        elif kind == "gamma":
+        elif kind in ("gamma", "gain"):
             params[name] = np.ones(shape, np.float32)
         else:  # bias or beta
             params[name] = np.zeros(shape, np.float32)
