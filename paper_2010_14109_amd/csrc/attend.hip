@@ -1,10 +1,32 @@
 // Cross attention: queries against the first klen states of their sequence (gfx950).
 //
 // One pass over the states with the running maximum and sum of the softmax; no matrix of scores is
-// kept.  The backward recomputes the probabilities from the forward's row logarithms lse.
+// kept.  The backward recomputes the probabilities from the forward's row logarithms lse, in two
+// passes, one over the states for dq and one over the queries for dk and dv, so that every sum has
+// a fixed order and no two workgroups add to the same memory.
+//
+// Products.  All of it is fp32, and the fp32 matrix instructions run at a sixteenth of the fp16
+// ones' rate.  A row x of a matrix is scaled by a power of two that brings its largest value to
+// 2^14 .. 2^15 and split into fp16 pieces, h = fp16(x), l = fp16(x - h), which keep 23 bits of every
+// value and at least the 40 bits below the row's largest; x y is the sum of h h, h l and l h,
+// accumulated in fp32 (l l is below 2^-22 of x y).  Three instructions where splitting into
+// bfloat16 pieces takes six, two pieces to keep and move instead of three.  The scales are exact;
+// where the scaled rows are the terms of a sum (the states in P v and dS k, the queries in P^T dy
+// and dS^T q), the row's scale is multiplied into the other factor, which is computed anyway.  That
+// factor is itself scaled by a running power of two for each output row: its values lie within
+// 2^15, and sums are rescaled, as for the running maximum, in the rare tiles where one passes it.
+//
+// Tiles.  A wave owns 32 columns: of queries (forward, dq) or of states (dk, dv).  Their pieces stay
+// in registers as the B operands of 32 x 32 x 16 products.  The other side passes through LDS in
+// tiles of rows, split once for the four waves of a workgroup.  Products are formed transposed
+// (rows of the tile x own columns), so a lane holds 16 rows of one column: the softmax's maximum
+// and sum take one exchange between the two halves of a wave, and the probabilities are already
+// the B operand of the next product, up to the order of its terms, in which the A operand (the same
+// tile, read through the transposing LDS loads) follows.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdint>
 
 #include "kernels.h"
 
@@ -12,160 +34,849 @@ namespace ooc {
 
 namespace {
 
-constexpr int TPB = 256;
-constexpr int kJ = 4;   // columns a lane owns at dh = 256
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-__device__ inline float wave_sum(float v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+constexpr int kWaves = 4;
+constexpr int TPB = 64 * kWaves;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kUnit = 0x1p-14f;    // a scaled row's largest value is 2^14 .. 2^15 of its exponent
+constexpr uint32_t kNone = 0x80000000u;   // past the length of every descriptor
+constexpr uint32_t kXcds = 8;
+
+// A width of head columns, padded to DH: a piece's row is DH / 8 chunks of 16 bytes in kRow bytes.
+// The odd number of chunks a row is long spreads the 16 rows of 256 bytes' worth of row reads over
+// all banks, and the four rows of a transposing read too.
+template <int DH>
+struct Width {
+  static constexpr int kSteps = DH / 16;                  // 16-wide products over the head columns
+  static constexpr int kBlocks = DH / 32;                 // 32-row blocks of head columns
+  static constexpr int kChunks = DH / 8;
+  static constexpr int kLanes = DH == 32 ? 4 : DH == 64 ? 8 : DH <= 128 ? 16 : 32;   // that load a row
+  static constexpr int kRow = (DH == 32 ? 7 : DH == 64 ? 9 : DH == 96 ? 13 : DH == 128 ? 19 : 35) * 16;
+  static constexpr int kTile = DH <= 64 ? 64 : 32;        // rows of a tile
+  // waves that share 32 columns, each with its part of the sums (registers hold no more)
+  static constexpr int kParts = DH <= 128 ? 1 : 2;
+  static constexpr int kCols = 32 * kWaves / kParts;      // columns of a workgroup
+  static constexpr int kSums = kBlocks / kParts;          // blocks of head columns a wave sums
+};
+
+// ---------------------------------------------------------------- exchange between lanes
+// the values of the two lanes 32 apart, the lower one's first
+__device__ inline floatx2 halves(float x) {
+  const uint32_t v = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  const uint32_t lo = r[0], hi = r[1];   // a bit_cast of a vector's element takes its first
+  return {__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi)};
+}
+__device__ inline float max_of_halves(float x) {
+  const floatx2 r = halves(x);
+  return fmaxf(r[0], r[1]);
+}
+__device__ inline float sum_of_halves(float x) {
+  const floatx2 r = halves(x);
+  return r[0] + r[1];
+}
+template <int CTRL>
+__device__ inline float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL,
+                                                               0xf, 0xf, true));
+}
+// largest of N = 4, 8, 16 or 32 neighbouring lanes (values >= 0)
+template <int N>
+__device__ inline float max_of_lanes(float x) {
+  x = fmaxf(x, dpp<0xb1>(x));                        // quad_perm 1 0 3 2
+  x = fmaxf(x, dpp<0x4e>(x));                        // quad_perm 2 3 0 1
+  if constexpr (N >= 8) x = fmaxf(x, dpp<0x141>(x)); // mirrored within 8
+  if constexpr (N >= 16) x = fmaxf(x, dpp<0x140>(x));// mirrored within 16
+  if constexpr (N >= 32) x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return x;
+}
+__device__ inline float wave_max(float v) {
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
 }
 
-struct Row {
-  float v[kJ];
+// ---------------------------------------------------------------- scaled pieces
+__device__ inline float exp2_of(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
+// floor(log2 x) of x >= 0, at least -112 and at most 128: with it 2^(14 - e) and 2^(e - 14) are
+// normal numbers
+__device__ inline int exponent(float x) {
+  return max((int)(__builtin_bit_cast(uint32_t, x) >> 23) - 127, -112);
+}
+
+struct Pieces {
+  half8v h, l;
 };
-__device__ inline Row load_row(const float* p, int dh) {
-  Row r;
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int j = 0; j < kJ; ++j) r.v[j] = lane + 64 * j < dh ? p[lane + 64 * j] : 0.f;
-  return r;
+__device__ inline void split2(float x, float y, uint32_t& h, uint32_t& l) {
+  const half2v hh = __builtin_convertvector((floatx2){x, y}, half2v);
+  const half2v ll = __builtin_convertvector((floatx2){x - (float)hh[0], y - (float)hh[1]}, half2v);
+  h = __builtin_bit_cast(uint32_t, hh);
+  l = __builtin_bit_cast(uint32_t, ll);
 }
-__device__ inline void store_row(float* p, const Row& r, int dh) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int j = 0; j < kJ; ++j)
-    if (lane + 64 * j < dh) p[lane + 64 * j] = r.v[j];
+__device__ inline Pieces split8(const float* v, float scale) {
+  uint4 h, l;
+  split2(v[0] * scale, v[1] * scale, h.x, l.x);
+  split2(v[2] * scale, v[3] * scale, h.y, l.y);
+  split2(v[4] * scale, v[5] * scale, h.z, l.z);
+  split2(v[6] * scale, v[7] * scale, h.w, l.w);
+  return {__builtin_bit_cast(half8v, h), __builtin_bit_cast(half8v, l)};
 }
-__device__ inline float dot(const Row& a, const Row& b) {
-  float s = 0.f;
+__device__ inline float max_abs(const float* v, int n) {
+  float m = 0.f;
 #pragma unroll
-  for (int j = 0; j < kJ; ++j) s += a.v[j] * b.v[j];
-  return wave_sum(s);
-}
-__device__ inline void fma_row(Row& a, float s, const Row& b) {
-#pragma unroll
-  for (int j = 0; j < kJ; ++j) a.v[j] += s * b.v[j];
+  for (int e = 0; e < n; ++e) m = fmaxf(m, fabsf(v[e]));
+  return m;
 }
 
-__device__ inline bool bad_length(int n, int Tk) { return n < 0 || n > Tk; }
+__device__ inline floatx16 mma(half8v a, half8v b, floatx16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ inline floatx16 mma(const Pieces& a, const Pieces& b, floatx16 c) {
+  c = mma(a.l, b.h, c);
+  c = mma(a.h, b.l, c);
+  return mma(a.h, b.h, c);
+}
 
-// One wave per query row: (b, i, h) in the order of q's rows and heads.
-__global__ __launch_bounds__(TPB) void fwd_kernel(const float* __restrict__ q,
-                                                  const float* __restrict__ kv,
-                                                  const int32_t* __restrict__ klen,
-                                                  float* __restrict__ y, float* __restrict__ lse,
-                                                  AttendShape a, float scale) {
-  const int64_t u = (int64_t)blockIdx.x * (TPB / 64) + (threadIdx.x >> 6);
-  if (u >= a.B * a.Tq * a.H) return;
-  const int64_t h = u % a.H, i = u / a.H % a.Tq, b = u / a.H / a.Tq;
-  const int n = klen[b], dh = (int)a.dh;
-  const int64_t d2 = 2 * a.Hkv * a.dh;
-  const float* k = kv + b * a.Tk * d2 + h / (a.H / a.Hkv) * a.dh;
-  const Row qr = load_row(q + u * a.dh, dh);
-  Row acc = {};
-  float m = -INFINITY, sum = 0.f;
-  for (int j = 0; j < n && !bad_length(n, (int)a.Tk); ++j) {
-    const float s = dot(qr, load_row(k + j * d2, dh)) * scale;
-    const float top = fmaxf(m, s), f = expf(m - top), p = expf(s - top);
+// ---------------------------------------------------------------- rows of memory
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const float* p, int64_t values) {
+  const int64_t n = values < 0 ? 0 : values > (int64_t(1) << 29) ? (int64_t(1) << 29) : values;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), 0, (int)((uint32_t)n * 4u),
+                                           0x00020000);
+}
+// eight values at a byte offset (of any 4-byte alignment); what lies past the length is zero
+__device__ inline void load8(__amdgpu_buffer_rsrc_t r, uint32_t off, float* v) {
+  const float4 a = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+  const float4 b = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 16, 0));
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+// columns at and past dh of the eight from d on are zero
+template <bool EXACT>
+__device__ inline void trim(float* v, int d, int dh) {
+  if constexpr (!EXACT) {
 #pragma unroll
-    for (int e = 0; e < kJ; ++e) acc.v[e] *= f;
-    sum = sum * f + p;
-    fma_row(acc, p, load_row(k + j * d2 + a.Hkv * a.dh, dh));
-    m = top;
+    for (int e = 0; e < 8; ++e) v[e] = d + e < dh ? v[e] : 0.f;
   }
-  const float inv = bad_length(n, (int)a.Tk) ? NAN : n ? 1.f / sum : 0.f;
+}
+
+// The query rows of a key head are numbered g Tq + i over its G heads and their positions.
+struct Shape {
+  int B, Tq, Tk, H, Hkv, G, dh;
+  int R;                // G Tq
+  int64_t ldq, ldk;     // H dh, 2 Hkv dh
+  float scale;          // 1 / sqrt(dh)
+};
+__device__ inline int64_t query_row(const Shape& s, int b, int hk, int r) {
+  const int g = r / s.Tq, i = r - g * s.Tq;
+  return ((int64_t)b * s.Tq + i) * s.ldq + (int64_t)(hk * s.G + g) * s.dh;
+}
+__device__ inline int64_t key_row(const Shape& s, int b, int hk, int j) {
+  return ((int64_t)b * s.Tk + j) * s.ldk + (int64_t)hk * s.dh;
+}
+__device__ inline int64_t stat_row(const Shape& s, int b, int hk) {
+  return ((int64_t)b * s.H + (int64_t)hk * s.G) * s.Tq;
+}
+
+// A wave's own columns: lane l holds column l mod 32, head columns 16 s + 8 (l / 32) .. + 8 of every
+// step s.  p: the column's row; nothing is read unless `valid`.
+template <int DH, bool EXACT>
+__device__ inline void load_column(const float* p, bool valid, int dh, float (&v)[DH / 2]) {
+  const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-  for (int e = 0; e < kJ; ++e) acc.v[e] *= inv;
-  store_row(y + u * a.dh, acc, dh);
-  if ((threadIdx.x & 63) == 0)
-    lse[(b * a.H + h) * a.Tq + i] = bad_length(n, (int)a.Tk) ? NAN : m + logf(sum);
+  for (int s = 0; s < DH / 16; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int d = 16 * s + 8 * half + e;
+      v[8 * s + e] = valid && (EXACT || d < dh) ? p[d] : 0.f;
+    }
+}
+// Returns the inverse scale.
+template <int DH>
+__device__ inline float split_column(const float (&v)[DH / 2], Pieces (&o)[DH / 16]) {
+  float m = max_abs(v, DH / 2);
+  m = max_of_halves(m);
+  const int e = exponent(m);
+  const float scale = exp2_of(14 - e);
+#pragma unroll
+  for (int s = 0; s < DH / 16; ++s) o[s] = split8(v + 8 * s, scale);
+  return exp2_of(e - 14);
 }
 
-__global__ __launch_bounds__(TPB) void dq_kernel(const float* __restrict__ q,
-                                                 const float* __restrict__ kv,
-                                                 const int32_t* __restrict__ klen,
-                                                 const float* __restrict__ y,
-                                                 const float* __restrict__ lse,
-                                                 const float* __restrict__ dy,
-                                                 float* __restrict__ dq, float* __restrict__ delta,
-                                                 AttendShape a, float scale) {
-  const int64_t u = (int64_t)blockIdx.x * (TPB / 64) + (threadIdx.x >> 6);
-  if (u >= a.B * a.Tq * a.H) return;
-  const int64_t h = u % a.H, i = u / a.H % a.Tq, b = u / a.H / a.Tq;
-  const int n = klen[b], dh = (int)a.dh;
-  const int64_t d2 = 2 * a.Hkv * a.dh, at = (b * a.H + h) * a.Tq + i;
-  const float* k = kv + b * a.Tk * d2 + h / (a.H / a.Hkv) * a.dh;
-  const Row qr = load_row(q + u * a.dh, dh), g = load_row(dy + u * a.dh, dh);
-  const float l = lse[at], dl = n ? dot(g, load_row(y + u * a.dh, dh)) : 0.f;
-  Row acc = {};
-  for (int j = 0; j < n && !bad_length(n, (int)a.Tk); ++j) {
-    const Row kr = load_row(k + j * d2, dh);
-    const float p = expf(dot(qr, kr) * scale - l);
-    fma_row(acc, p * (dot(g, load_row(k + j * d2 + a.Hkv * a.dh, dh)) - dl) * scale, kr);
+// One matrix of a tile: T rows of pieces in LDS.
+template <int DH, int T>
+struct Rows {
+  using Wd = Width<DH>;
+  static constexpr int kPiece = T * Wd::kRow;
+  static constexpr int kBytes = 2 * kPiece;
+  static __device__ void store(char* lds, int row, int c, const Pieces& p) {
+    *reinterpret_cast<half8v*>(lds + row * Wd::kRow + c * 16) = p.h;
+    *reinterpret_cast<half8v*>(lds + kPiece + row * Wd::kRow + c * 16) = p.l;
   }
-  if (bad_length(n, (int)a.Tk))
-    for (int e = 0; e < kJ; ++e) acc.v[e] = NAN;
-  store_row(dq + u * a.dh, acc, dh);
-  if ((threadIdx.x & 63) == 0) delta[at] = dl;
+  // A operand, rows r0 .. r0 + 31 of the tile x step s of the head columns
+  static __device__ Pieces by_row(const char* lds, int r0, int s) {
+    const int l = threadIdx.x & 63;
+    const char* p = lds + (r0 + (l & 31)) * Wd::kRow + (2 * s + (l >> 5)) * 16;
+    return {*reinterpret_cast<const half8v*>(p), *reinterpret_cast<const half8v*>(p + kPiece)};
+  }
+  // A operand, head columns 32 block .. + 31 x the 16 rows r0 .. of the tile, in the order in which
+  // a lane of a 32 x 32 result holds rows: half h of the wave has rows 4 h .. + 3 and 8 + 4 h .. + 3
+  static __device__ half8v transposed(const char* lds, int r0, int block) {
+    const int l = threadIdx.x & 63, t = l & 15;
+    const char* p = lds + (r0 + 4 * (l >> 5) + (t >> 2)) * Wd::kRow +
+                    (32 * block + 16 * ((l >> 4) & 1) + 4 * (t & 3)) * 2;
+    typedef __attribute__((address_space(3))) short4v* Lds;
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
+    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 8 * Wd::kRow));
+    const half4v x = __builtin_bit_cast(half4v, a), y = __builtin_bit_cast(half4v, b);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  static __device__ Pieces by_column(const char* lds, int r0, int block) {
+    return {transposed(lds, r0, block), transposed(lds + kPiece, r0, block)};
+  }
+};
+
+// The values of two matrices' next tile on their way from memory: unit u of a thread is 8 head
+// columns of row u / lanes of the two tiles on top of each other.
+template <int DH, int T>
+struct Flight {
+  using Wd = Width<DH>;
+  static constexpr int kUnits = 2 * T * Wd::kLanes / TPB;
+  static_assert(kUnits >= 1 && 2 * T * Wd::kLanes % TPB == 0, "units per thread");
+  float v[kUnits][8];
+  static __device__ int row(int u) { return ((int)threadIdx.x + u * TPB) / Wd::kLanes; }
+  static __device__ int chunk() { return (int)threadIdx.x % Wd::kLanes; }
+  // a, b: the two matrices from the tile's first row on, n values a row's distance, `rows` of them
+  // there.  The matrix of a unit is uniform over the thread block's unit index.
+  template <bool EXACT>
+  __device__ void load(const float* a, const float* b, int64_t lda, int64_t ldb, int rows, int dh) {
+    const auto ra = buffer(a, rows > 0 ? (int64_t)(rows - 1) * lda + dh : 0);
+    const auto rb = buffer(b, rows > 0 ? (int64_t)(rows - 1) * ldb + dh : 0);
+    const int c = chunk();
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const bool second = u >= kUnits / 2;
+      const int r = row(u) - (second ? T : 0);
+      uint32_t off = (uint32_t)(r * (second ? ldb : lda) + 8 * c) * 4u;
+      if (r >= rows || 8 * c >= dh) off = kNone;
+      load8(second ? rb : ra, off, v[u]);
+      trim<EXACT>(v[u], 8 * c, dh);
+    }
+  }
+};
+
+// The workgroup's place: pairs (b, key head), tiles of columns, slices of the other side.  The
+// tiles of a pair run on one die, whose L2 then holds the pair's states (or queries).
+struct Place {
+  int b, hk, tile, slice;
+  bool none;
+};
+__device__ inline Place place(const Shape& s, int tiles) {
+  const uint32_t pairs = (uint32_t)s.B * s.Hkv, id = blockIdx.x;
+  const uint32_t idx = id / kXcds, pair = idx / tiles * kXcds + id % kXcds;
+  return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), (int)(idx % tiles), (int)blockIdx.y, pair >= pairs};
 }
 
-// One wave per state and key head, over the query rows of its heads.
-__global__ __launch_bounds__(TPB) void dkv_kernel(const float* __restrict__ q,
-                                                  const float* __restrict__ kv,
-                                                  const int32_t* __restrict__ klen,
-                                                  const float* __restrict__ lse,
-                                                  const float* __restrict__ dy,
-                                                  const float* __restrict__ delta,
-                                                  float* __restrict__ dkv, AttendShape a,
-                                                  float scale) {
-  const int64_t u = (int64_t)blockIdx.x * (TPB / 64) + (threadIdx.x >> 6);
-  if (u >= a.B * a.Tk * a.Hkv) return;
-  const int64_t hk = u % a.Hkv, j = u / a.Hkv % a.Tk, b = u / a.Hkv / a.Tk, G = a.H / a.Hkv;
-  const int n = klen[b], dh = (int)a.dh;
-  const int64_t at = (b * a.Tk + j) * 2 * a.Hkv * a.dh + hk * a.dh, v = a.Hkv * a.dh;
-  Row dk = {}, dv = {};
-  if (bad_length(n, (int)a.Tk)) {
-    for (int e = 0; e < kJ; ++e) dk.v[e] = dv.v[e] = NAN;
-  } else if (j < n) {
-    const Row kr = load_row(kv + at, dh), vr = load_row(kv + at + v, dh);
-    for (int64_t h = hk * G; h < (hk + 1) * G; ++h)
-      for (int64_t i = 0; i < a.Tq; ++i) {
-        const int64_t row = ((b * a.Tq + i) * a.H + h) * a.dh, st = (b * a.H + h) * a.Tq + i;
-        const Row qr = load_row(q + row, dh), g = load_row(dy + row, dh);
-        const float p = expf(dot(qr, kr) * scale - lse[st]);
-        fma_row(dv, p, g);
-        fma_row(dk, p * (dot(g, vr) - delta[st]) * scale, qr);
+// Sum t of a lane holds, in r, head column 32 (first + t) + 8 (r / 4) + 4 half + r % 4 of its column.
+template <int DH, bool EXACT, class F>
+__device__ inline void store_column(float* p, int first, int dh, F value) {
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int t = 0; t < Width<DH>::kSums; ++t)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int d = 32 * (first + t) + 8 * q + 4 * half;
+      if constexpr (EXACT) {
+        *reinterpret_cast<float4*>(p + d) =
+            make_float4(value(t, 4 * q), value(t, 4 * q + 1), value(t, 4 * q + 2), value(t, 4 * q + 3));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (d + e < dh) p[d + e] = value(t, 4 * q + e);
       }
-  }
-  store_row(dkv + at, dk, dh);
-  store_row(dkv + at + v, dv, dh);
+    }
 }
 
-unsigned waves(int64_t n) { return (unsigned)((n + TPB / 64 - 1) / (TPB / 64)); }
+__device__ inline float4 at4(const float* lds, int row) {
+  return *reinterpret_cast<const float4*>(lds + row);
+}
+__device__ inline float pick(const float4& v, int e) {
+  return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
+}
+
+// 16 values of a column, scaled, as the B operands of two 16-row steps
+__device__ inline void split_values(const float (&p)[16], float scale, Pieces (&o)[2]) {
+  o[0] = split8(p, scale);
+  o[1] = split8(p + 8, scale);
+}
+
+// ---------------------------------------------------------------- forward
+template <int DH, bool EXACT>
+__global__ __launch_bounds__(TPB, 2) void fwd_kernel(const float* __restrict__ q,
+                                                     const float* __restrict__ kv,
+                                                     const int32_t* __restrict__ klen,
+                                                     float* __restrict__ y, float* __restrict__ lse,
+                                                     Shape s, int tiles, int slice_len,
+                                                     int64_t y_slice, int64_t lse_slice) {
+  using Wd = Width<DH>;
+  constexpr int T = Wd::kTile;
+  using Rw = Rows<DH, T>;
+  __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
+  __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
+  __shared__ __attribute__((aligned(16))) float kf[T], ve[T], vi[T];
+  const Place at = place(s, tiles);
+  if (at.none) return;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int col = at.tile * Wd::kCols + w / Wd::kParts * 32 + (lane & 31);
+  const int first = w % Wd::kParts * Wd::kSums;
+  const bool mine = col < s.R;
+  const int n = klen[at.b];
+  const bool bad = n < 0 || n > s.Tk;
+  const int k0 = bad ? 0 : min(n, at.slice * slice_len), k1 = bad ? 0 : min(n, k0 + slice_len);
+
+  Pieces qp[Wd::kSteps];
+  float qc;
+  const int64_t qrow = mine ? query_row(s, at.b, at.hk, col) : 0;
+  {
+    float v[DH / 2];
+    load_column<DH, EXACT>(q + qrow, mine, s.dh, v);
+    qc = split_column<DH>(v, qp) * s.scale * kLog2e;
+  }
+  floatx16 o[Wd::kSums];
+#pragma unroll
+  for (int t = 0; t < Wd::kSums; ++t) o[t] = floatx16{};
+  // Powers of two: m above the largest score plus value exponent so far (less base), and the sums
+  // of 2^(score - m + 8) and of that times the values.  m stays while no term passes 2^15.
+  float m = -INFINITY, sum = 0.f;
+  int base = 0;
+  Flight<DH, T> next;
+  const auto fetch = [&](int j) {
+    const int64_t r = key_row(s, at.b, at.hk, j);
+    next.template load<EXACT>(kv + r, kv + r + (int64_t)s.Hkv * s.dh, s.ldk, s.ldk, min(T, k1 - j), s.dh);
+  };
+  if (k0 < k1) fetch(k0);
+  for (int j0 = k0; j0 < k1; j0 += T) {
+    constexpr int U = Flight<DH, T>::kUnits;
+    int e[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      e[u] = exponent(max_of_lanes<Wd::kLanes>(max_abs(next.v[u], 8)));
+    const int c = next.chunk();
+    __syncthreads();
+    if (j0 == k0) {   // base: the largest exponent of the first tile's values
+      if (c == 0)
+#pragma unroll
+        for (int u = U / 2; u < U; ++u) ve[next.row(u) - T] = (float)e[u];
+      __syncthreads();
+      const float top = wave_max(lane < T ? ve[lane] : -112.f);
+      base = top <= -112.f || top >= 128.f ? 0 : __builtin_amdgcn_readfirstlane((int)top);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool value = u >= U / 2;
+      const int r = next.row(u) - (value ? T : 0);
+      // values far below base keep a common exponent; rows of zeros count as base
+      if (value) e[u] = e[u] <= -112 ? base : max(e[u], base - 40);
+      const Pieces p = split8(next.v[u], exp2_of(14 - e[u]));
+      if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks) Rw::store(value ? vs : ks, r, c, p);
+      if (c == 0) {
+        if (value) {
+          const bool there = j0 + r < k1;
+          ve[r] = there ? (float)(e[u] - base) : -INFINITY;
+          vi[r] = there ? exp2_of(max(base - e[u], -126)) : 0.f;
+        } else {
+          kf[r] = exp2_of(e[u] - 14);
+        }
+      }
+    }
+    __syncthreads();
+    if (j0 + T < k1) fetch(j0 + T);
+#pragma unroll
+    for (int r0 = 0; r0 < T; r0 += 32) {
+      floatx16 a = {};
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(ks, r0, t), qp[t], a);
+      float p[16], top = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 f = at4(kf, r0 + 8 * g + 4 * half), x = at4(ve, r0 + 8 * g + 4 * half);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[4 * g + i] = fmaf(a[4 * g + i] * pick(f, i), qc, pick(x, i));
+          top = fmaxf(top, p[4 * g + i]);
+        }
+      }
+      top = max_of_halves(top);
+      if (__any(top > m + 7.f)) {
+        const float up = fmaxf(m, top), f = m == up ? 1.f : exp2f(m - up);
+        m = up;
+        sum *= f;
+#pragma unroll
+        for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[t][i] *= f;
+      }
+      float part = 0.f;
+      const float off = 8.f - m;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 x = at4(vi, r0 + 8 * g + 4 * half);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[4 * g + i] = __builtin_amdgcn_exp2f(p[4 * g + i] + off);
+          part = fmaf(p[4 * g + i], pick(x, i), part);
+        }
+      }
+      sum += part;
+      Pieces pp[2];
+      split_values(p, 1.f, pp);
+#pragma unroll
+      for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) o[t] = mma(Rw::by_column(vs, r0 + 16 * h, first + t), pp[h], o[t]);
+    }
+  }
+  sum = sum_of_halves(sum);
+  if (!mine) return;
+  float f = 0.f, l = -INFINITY;
+  if (bad) f = l = NAN;
+  else if (k0 < k1) {
+    f = kUnit * exp2_of(base) / sum;
+    l = (m - 8.f + log2f(sum)) * kLn2;
+  }
+  store_column<DH, EXACT>(y + at.slice * y_slice + qrow, first, s.dh, [&](int t, int i) {
+    return k0 < k1 ? o[t][i] * f : f;
+  });
+  if (half == 0 && first == 0) lse[at.slice * lse_slice + stat_row(s, at.b, at.hk) + col] = l;
+}
+
+// y and lse of a row from its slices': the slices' outputs weighted by exp(lse_s - lse)
+__global__ void join_kernel(const float* __restrict__ part, float* __restrict__ y,
+                            float* __restrict__ lse, Shape s, int slices, int64_t y_size,
+                            int64_t rows) {
+  const float* pl = part + slices * y_size;
+  const int64_t stride = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t u = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u < y_size; u += stride) {
+    const int64_t row = u / s.dh, d = u - row * s.dh;   // row (b, i, h)
+    const int64_t h = row % s.H, bi = row / s.H, i = bi % s.Tq, b = bi / s.Tq;
+    const int64_t st = (b * s.H + h) * s.Tq + i;
+    float top = -INFINITY;
+    bool nan = false;
+    for (int k = 0; k < slices; ++k) {
+      const float l = pl[k * rows + st];
+      top = fmaxf(top, l);
+      nan |= l != l;
+    }
+    float sum = 0.f, acc = 0.f;
+    if (top > -INFINITY)
+      for (int k = 0; k < slices; ++k) {
+        const float l = pl[k * rows + st];
+        if (l == -INFINITY) continue;
+        const float f = expf(l - top);
+        sum += f;
+        acc = fmaf(f, part[k * y_size + u], acc);
+      }
+    y[u] = nan ? NAN : sum > 0.f ? acc / sum : 0.f;
+    if (d == 0) lse[st] = nan ? NAN : sum > 0.f ? top + logf(sum) : -INFINITY;
+  }
+}
+
+// ---------------------------------------------------------------- backward over the states: dq
+template <int DH, bool EXACT>
+__global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dq_kernel(
+    const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
+    const float* __restrict__ y, const float* __restrict__ lse, const float* __restrict__ dy,
+    float* __restrict__ dq, float* __restrict__ delta, Shape s, int tiles, int slice_len,
+    int64_t dq_slice) {
+  using Wd = Width<DH>;
+  constexpr int T = Wd::kTile;
+  using Rw = Rows<DH, T>;
+  __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
+  __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
+  __shared__ __attribute__((aligned(16))) float kf[T], vf[T], off[T];
+  const Place at = place(s, tiles);
+  if (at.none) return;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int col = at.tile * Wd::kCols + w / Wd::kParts * 32 + (lane & 31);
+  const int first = w % Wd::kParts * Wd::kSums;
+  const bool mine = col < s.R;
+  const int n = klen[at.b];
+  const bool bad = n < 0 || n > s.Tk;
+  const int k0 = bad ? 0 : min(n, at.slice * slice_len), k1 = bad ? 0 : min(n, k0 + slice_len);
+
+  Pieces qp[Wd::kSteps], gp[Wd::kSteps];
+  float qc, gf, dl = 0.f;
+  const int64_t qrow = mine ? query_row(s, at.b, at.hk, col) : 0;
+  const int64_t st = stat_row(s, at.b, at.hk) + col;
+  {
+    float v[DH / 2], u[DH / 2];
+    load_column<DH, EXACT>(q + qrow, mine, s.dh, v);
+    qc = split_column<DH>(v, qp) * s.scale * kLog2e;
+    load_column<DH, EXACT>(dy + qrow, mine, s.dh, v);
+    gf = split_column<DH>(v, gp);
+    load_column<DH, EXACT>(y + qrow, mine, s.dh, u);
+#pragma unroll
+    for (int i = 0; i < DH / 2; ++i) dl = fmaf(v[i], u[i], dl);
+    dl = sum_of_halves(dl);
+  }
+  if (mine && half == 0 && first == 0 && at.slice == 0) delta[st] = dl;
+  const float nl = mine ? -lse[st] * kLog2e : -INFINITY;
+  floatx16 o[Wd::kSums];
+#pragma unroll
+  for (int t = 0; t < Wd::kSums; ++t) o[t] = floatx16{};
+  float f = 0x1p126f;   // scale of the score gradients: they stay within 2^15
+  Flight<DH, T> next;
+  const auto fetch = [&](int j) {
+    const int64_t r = key_row(s, at.b, at.hk, j);
+    next.template load<EXACT>(kv + r, kv + r + (int64_t)s.Hkv * s.dh, s.ldk, s.ldk, min(T, k1 - j), s.dh);
+  };
+  if (k0 < k1) fetch(k0);
+  for (int j0 = k0; j0 < k1; j0 += T) {
+    constexpr int U = Flight<DH, T>::kUnits;
+    const int c = next.chunk();
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool value = u >= U / 2;
+      const int r = next.row(u) - (value ? T : 0);
+      const int e = exponent(max_of_lanes<Wd::kLanes>(max_abs(next.v[u], 8)));
+      const Pieces p = split8(next.v[u], exp2_of(14 - e));
+      if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks) Rw::store(value ? vs : ks, r, c, p);
+      if (c == 0) {
+        (value ? vf : kf)[r] = exp2_of(e - 14);
+        if (value) off[r] = j0 + r < k1 ? 0.f : -INFINITY;
+      }
+    }
+    __syncthreads();
+    if (j0 + T < k1) fetch(j0 + T);
+#pragma unroll
+    for (int r0 = 0; r0 < T; r0 += 32) {
+      floatx16 a = {}, b = {};
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(ks, r0, t), qp[t], a);
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) b = mma(Rw::by_row(vs, r0, t), gp[t], b);
+      float x[16], top = 0.f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int row = r0 + 8 * g + 4 * half;
+        const float4 fk = at4(kf, row), fv = at4(vf, row), z = at4(off, row);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(a[4 * g + i] * pick(fk, i), qc, nl + pick(z, i)));
+          const float d = fmaf(b[4 * g + i] * pick(fv, i), gf, -dl);
+          x[4 * g + i] = p * d * pick(fk, i);
+          top = fmaxf(top, fabsf(x[4 * g + i]));
+        }
+      }
+      top = max_of_halves(top);
+      if (__any(top * f > 0x1p15f)) {
+        const float g = top * f > 0x1p15f ? exp2_of(max(8 - exponent(top), -126)) : f;
+        const float up = g / f;
+        f = g;
+#pragma unroll
+        for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[t][i] *= up;
+      }
+      Pieces xp[2];
+      split_values(x, f, xp);
+#pragma unroll
+      for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) o[t] = mma(Rw::by_column(ks, r0 + 16 * h, first + t), xp[h], o[t]);
+    }
+  }
+  if (!mine) return;
+  const float out = s.scale / f;
+  store_column<DH, EXACT>(dq + at.slice * dq_slice + qrow, first, s.dh, [&](int t, int i) {
+    return bad ? NAN : o[t][i] * out;
+  });
+}
+
+// ---------------------------------------------------------------- backward over the queries: dk, dv
+template <int DH, bool EXACT>
+__global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dkv_kernel(
+    const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
+    const float* __restrict__ lse, const float* __restrict__ dy, const float* __restrict__ delta,
+    float* __restrict__ dkv, Shape s, int tiles, int slice_len, int64_t dkv_slice) {
+  using Wd = Width<DH>;
+  constexpr int T = Wd::kTile;
+  using Rw = Rows<DH, T>;
+  __shared__ __attribute__((aligned(16))) char qs[Rw::kBytes];
+  __shared__ __attribute__((aligned(16))) char gs[Rw::kBytes];
+  __shared__ __attribute__((aligned(16))) float qf[T], gf[T], nl[T], dl[T];
+  const Place at = place(s, tiles);
+  if (at.none) return;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int j = at.tile * Wd::kCols + w / Wd::kParts * 32 + (lane & 31);
+  const int first = w % Wd::kParts * Wd::kSums;
+  const int n = klen[at.b];
+  const bool bad = n < 0 || n > s.Tk, mine = j < s.Tk, live = mine && j < n && !bad;
+  // rows of this slice; a workgroup without states has nothing to add
+  const bool any = !bad && at.tile * Wd::kCols < n;
+  const int i0 = any ? min(s.R, at.slice * slice_len) : 0, i1 = any ? min(s.R, i0 + slice_len) : 0;
+
+  const int64_t krow = mine ? key_row(s, at.b, at.hk, j) : 0, to_v = (int64_t)s.Hkv * s.dh;
+  Pieces kp[Wd::kSteps], vp[Wd::kSteps];
+  float kc, vf;
+  {
+    float v[DH / 2];
+    load_column<DH, EXACT>(kv + krow, live, s.dh, v);
+    kc = split_column<DH>(v, kp) * s.scale * kLog2e;
+    load_column<DH, EXACT>(kv + krow + to_v, live, s.dh, v);
+    vf = split_column<DH>(v, vp);
+  }
+  floatx16 dk[Wd::kSums], dv[Wd::kSums];
+#pragma unroll
+  for (int t = 0; t < Wd::kSums; ++t) dk[t] = dv[t] = floatx16{};
+  float fk = 0x1p126f, fv = 0x1p126f;
+  const int64_t st = stat_row(s, at.b, at.hk);
+  Flight<DH, T> next;
+  float ll = 0.f, dd = 0.f;
+  // tiles of rows stay within a head where a head fills one, else they pack the group's heads
+  const bool packed = s.Tq < T;
+  const auto fetch = [&](int i) {
+    if (!packed) {
+      const int64_t r = query_row(s, at.b, at.hk, i);
+      const int rows = min(min(T, i1 - i), s.Tq - i % s.Tq);
+      next.template load<EXACT>(q + r, dy + r, s.ldq, s.ldq, rows, s.dh);
+      if ((int)threadIdx.x < T) {
+        const bool there = (int)threadIdx.x < rows;
+        ll = there ? -lse[st + i + threadIdx.x] * kLog2e : -INFINITY;
+        dd = there ? delta[st + i + threadIdx.x] : 0.f;
+      }
+    } else {
+      const int rows = min(T, i1 - i), c = next.chunk();
+      const int64_t first = (int64_t)at.b * s.Tq * s.ldq + (int64_t)at.hk * s.G * s.dh;
+      const int64_t values = (int64_t)(s.Tq - 1) * s.ldq + (int64_t)s.G * s.dh;
+      const auto rq = buffer(q + first, values), rg = buffer(dy + first, values);
+#pragma unroll
+      for (int u = 0; u < Flight<DH, T>::kUnits; ++u) {
+        const bool second = u >= Flight<DH, T>::kUnits / 2;
+        const int r = next.row(u) - (second ? T : 0), g = (i + r) / s.Tq, k = i + r - g * s.Tq;
+        uint32_t o = (uint32_t)(k * s.ldq + (int64_t)g * s.dh + 8 * c) * 4u;
+        if (r >= rows || 8 * c >= s.dh) o = kNone;
+        load8(second ? rg : rq, o, next.v[u]);
+        trim<EXACT>(next.v[u], 8 * c, s.dh);
+      }
+      if ((int)threadIdx.x < T) {
+        const bool there = (int)threadIdx.x < rows;
+        ll = there ? -lse[st + i + threadIdx.x] * kLog2e : -INFINITY;
+        dd = there ? delta[st + i + threadIdx.x] : 0.f;
+      }
+    }
+  };
+  const auto step = [&](int i) { return packed ? i + T : min(i + T, i - i % s.Tq + s.Tq); };
+  if (i0 < i1) fetch(i0);
+  for (int i = i0; i < i1;) {
+    constexpr int U = Flight<DH, T>::kUnits;
+    const int c = next.chunk();
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool second = u >= U / 2;
+      const int r = next.row(u) - (second ? T : 0);
+      const int e = exponent(max_of_lanes<Wd::kLanes>(max_abs(next.v[u], 8)));
+      const Pieces p = split8(next.v[u], exp2_of(14 - e));
+      if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks) Rw::store(second ? gs : qs, r, c, p);
+      if (c == 0) (second ? gf : qf)[r] = exp2_of(e - 14);
+    }
+    if ((int)threadIdx.x < T) {
+      nl[threadIdx.x] = ll;
+      dl[threadIdx.x] = dd;
+    }
+    __syncthreads();
+    i = step(i);
+    if (i < i1) fetch(i);
+#pragma unroll
+    for (int r0 = 0; r0 < T; r0 += 32) {
+      floatx16 a = {}, b = {};
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(qs, r0, t), kp[t], a);
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) b = mma(Rw::by_row(gs, r0, t), vp[t], b);
+      float p[16], x[16], ptop = 0.f, xtop = 0.f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int row = r0 + 8 * g + 4 * half;
+        const float4 fq = at4(qf, row), fg = at4(gf, row), l4 = at4(nl, row), d4 = at4(dl, row);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float pr = __builtin_amdgcn_exp2f(fmaf(a[4 * g + e] * pick(fq, e), kc, pick(l4, e)));
+          const float d = fmaf(b[4 * g + e] * pick(fg, e), vf, -pick(d4, e));
+          p[4 * g + e] = pr * pick(fg, e);
+          x[4 * g + e] = pr * d * pick(fq, e);
+          ptop = fmaxf(ptop, p[4 * g + e]);
+          xtop = fmaxf(xtop, fabsf(x[4 * g + e]));
+        }
+      }
+      ptop = max_of_halves(ptop);
+      xtop = max_of_halves(xtop);
+      if (__any(ptop * fv > 0x1p15f || xtop * fk > 0x1p15f)) {
+        const float gv = ptop * fv > 0x1p15f ? exp2_of(max(8 - exponent(ptop), -126)) : fv;
+        const float gk = xtop * fk > 0x1p15f ? exp2_of(max(8 - exponent(xtop), -126)) : fk;
+        const float uv = gv / fv, uk = gk / fk;
+        fv = gv;
+        fk = gk;
+#pragma unroll
+        for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            dv[t][e] *= uv;
+            dk[t][e] *= uk;
+          }
+      }
+      Pieces pp[2], xp[2];
+      split_values(p, fv, pp);
+      split_values(x, fk, xp);
+#pragma unroll
+      for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          dv[t] = mma(Rw::by_column(gs, r0 + 16 * h, first + t), pp[h], dv[t]);
+          dk[t] = mma(Rw::by_column(qs, r0 + 16 * h, first + t), xp[h], dk[t]);
+        }
+    }
+  }
+  if (!mine) return;
+  const float ok = s.scale / fk, ov = 1.f / fv;
+  float* out = dkv + at.slice * dkv_slice + krow;
+  store_column<DH, EXACT>(out, first, s.dh, [&](int t, int e) {
+    return bad ? NAN : live ? dk[t][e] * ok : 0.f;
+  });
+  store_column<DH, EXACT>(out + to_v, first, s.dh, [&](int t, int e) {
+    return bad ? NAN : live ? dv[t][e] * ov : 0.f;
+  });
+}
+
+// out = the slices' partial sums added in order
+__global__ void sum_kernel(const float* __restrict__ part, float* __restrict__ out, int slices,
+                           int64_t size) {
+  const int64_t stride = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t u = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u < size; u += stride) {
+    float acc = part[u];
+    for (int k = 1; k < slices; ++k) acc += part[k * size + u];
+    out[u] = acc;
+  }
+}
+
+// ---------------------------------------------------------------- launches
+Shape shape_of(const AttendShape& a) {
+  Shape s;
+  s.B = (int)a.B; s.Tq = (int)a.Tq; s.Tk = (int)a.Tk; s.H = (int)a.H; s.Hkv = (int)a.Hkv;
+  s.G = (int)(a.H / a.Hkv);
+  s.dh = (int)a.dh;
+  s.R = s.G * s.Tq;
+  s.ldq = a.H * a.dh;
+  s.ldk = 2 * a.Hkv * a.dh;
+  s.scale = 1.f / sqrtf((float)a.dh);
+  return s;
+}
+
+int tile_rows(int64_t dh) { return dh <= 64 ? 64 : 32; }
+int columns(int64_t dh) { return dh <= 128 ? 32 * kWaves : 16 * kWaves; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+dim3 grid_of(const Shape& s, int tiles, int64_t slices) {
+  return dim3((unsigned)(ceil_div((int64_t)s.B * s.Hkv, kXcds) * kXcds * tiles), (unsigned)slices);
+}
+unsigned flat_grid(int64_t n) { return (unsigned)std::min<int64_t>(ceil_div(n, 256), 4096); }
+int64_t slice_of(int64_t n, int64_t slices, int64_t tile) {
+  return ceil_div(ceil_div(n, slices), tile) * tile;
+}
+
+// Workgroups to aim for, and the fewest tiles a slice is worth cutting off for.
+constexpr int64_t kWant = 512, kMinTiles = 2;
+int64_t slices_for(int64_t groups, int64_t tiles) {
+  if (groups >= kWant) return 1;
+  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(kWant, groups), tiles / kMinTiles,
+                                                  kMaxAttentionSlices}));
+}
+
+#define WIDTHS(CALL)                                            \
+  if (s.dh == 32) CALL(32, true);                               \
+  else if (s.dh < 32) CALL(32, false);                          \
+  else if (s.dh == 64) CALL(64, true);                          \
+  else if (s.dh < 64) CALL(64, false);                          \
+  else if (s.dh == 96) CALL(96, true);                          \
+  else if (s.dh < 96) CALL(96, false);                          \
+  else if (s.dh == 128) CALL(128, true);                        \
+  else if (s.dh < 128) CALL(128, false);                        \
+  else if (s.dh == 256) CALL(256, true);                        \
+  else CALL(256, false)
 
 }  // namespace
 
-int64_t attention_key_slices(const AttendShape&, bool) { return 1; }
-int64_t attention_query_slices(const AttendShape&) { return 1; }
+int64_t attention_key_slices(const AttendShape& a, bool) {
+  return slices_for(a.B * a.Hkv * ceil_div(a.Tq * (a.H / a.Hkv), columns(a.dh)),
+                    ceil_div(a.Tk, tile_rows(a.dh)));
+}
+int64_t attention_query_slices(const AttendShape& a) {
+  return slices_for(a.B * a.Hkv * ceil_div(a.Tk, columns(a.dh)),
+                    ceil_div(a.Tq * (a.H / a.Hkv), tile_rows(a.dh)));
+}
 
 hipError_t cross_attention_fwd(const float* q, const float* kv, const int32_t* klen, float* y,
-                               float* lse, float*, const AttendShape& a, int64_t, hipStream_t s) {
-  hipLaunchKernelGGL(fwd_kernel, dim3(waves(a.B * a.Tq * a.H)), dim3(TPB), 0, s, q, kv, klen, y,
-                     lse, a, 1.f / sqrtf((float)a.dh));
+                               float* lse, float* part, const AttendShape& a, int64_t slices,
+                               hipStream_t st) {
+  const Shape s = shape_of(a);
+  const int tiles = (int)ceil_div(s.R, columns(s.dh));
+  const int len = (int)slice_of(s.Tk, slices, tile_rows(s.dh));
+  const int64_t size = a.B * a.Tq * s.ldq, rows = a.B * a.H * a.Tq;
+  float* yo = slices > 1 ? part : y;
+  float* lo = slices > 1 ? part + slices * size : lse;
+#define FWD(D, X)                                                                                 \
+  hipLaunchKernelGGL((fwd_kernel<D, X>), grid_of(s, tiles, slices), dim3(TPB), 0, st, q, kv, klen, \
+                     yo, lo, s, tiles, len, size, rows)
+  WIDTHS(FWD);
+#undef FWD
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || slices == 1) return e;
+  hipLaunchKernelGGL(join_kernel, dim3(flat_grid(size)), dim3(256), 0, st, part, y, lse, s,
+                     (int)slices, size, rows);
   return hipGetLastError();
 }
 
 hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* klen,
                                const float* y, const float* lse, const float* dy, float* dq,
-                               float* dkv, float* delta, float*, const AttendShape& a, int64_t,
-                               int64_t, hipStream_t s) {
-  const float scale = 1.f / sqrtf((float)a.dh);
-  hipLaunchKernelGGL(dq_kernel, dim3(waves(a.B * a.Tq * a.H)), dim3(TPB), 0, s, q, kv, klen, y, lse,
-                     dy, dq, delta, a, scale);
+                               float* dkv, float* delta, float* part, const AttendShape& a,
+                               int64_t q_slices, int64_t kv_slices, hipStream_t st) {
+  const Shape s = shape_of(a);
+  const int64_t q_size = a.B * a.Tq * s.ldq, kv_size = a.B * a.Tk * s.ldk;
+  {
+    const int tiles = (int)ceil_div(s.R, columns(s.dh));
+    const int len = (int)slice_of(s.Tk, q_slices, tile_rows(s.dh));
+    float* out = q_slices > 1 ? part : dq;
+#define DQ(D, X)                                                                                   \
+  hipLaunchKernelGGL((dq_kernel<D, X>), grid_of(s, tiles, q_slices), dim3(TPB), 0, st, q, kv, klen, \
+                     y, lse, dy, out, delta, s, tiles, len, q_size)
+    WIDTHS(DQ);
+#undef DQ
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (q_slices > 1) {
+      hipLaunchKernelGGL(sum_kernel, dim3(flat_grid(q_size)), dim3(256), 0, st, part, dq,
+                         (int)q_slices, q_size);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  const int tiles = (int)ceil_div(s.Tk, columns(s.dh));
+  const int len = (int)slice_of(s.R, kv_slices, tile_rows(s.dh));
+  float* out = kv_slices > 1 ? part : dkv;
+#define DKV(D, X)                                                                                    \
+  hipLaunchKernelGGL((dkv_kernel<D, X>), grid_of(s, tiles, kv_slices), dim3(TPB), 0, st, q, kv, klen, \
+                     lse, dy, delta, out, s, tiles, len, kv_size)
+  WIDTHS(DKV);
+#undef DKV
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(dkv_kernel, dim3(waves(a.B * a.Tk * a.Hkv)), dim3(TPB), 0, s, q, kv, klen, lse,
-                     dy, delta, dkv, a, scale);
+  if (e != hipSuccess || kv_slices == 1) return e;
+  hipLaunchKernelGGL(sum_kernel, dim3(flat_grid(kv_size)), dim3(256), 0, st, part, dkv,
+                     (int)kv_slices, kv_size);
   return hipGetLastError();
 }
 

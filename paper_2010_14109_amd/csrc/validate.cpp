@@ -81,6 +81,9 @@ std::string check_attention_shape(const int64_t* a) {
   if (Tk > (1 << 28) || product({Tq, H / Hkv}) < 0 || Tq * (H / Hkv) > (1 << 28) || H > 65535 ||
       product({B, H}) < 0 || B * H > (1 << 24))
     return "sequence, head or batch count too large";
+  // and the bytes from a row to the 64th behind it
+  if (product({H, dh}) > (1 << 20) || product({Hkv, dh}) > (1 << 20)) return "rows too wide";
+  if (B * Hkv * (std::max(Tq * (H / Hkv), Tk) / 64 + 1) > (1 << 28)) return "too many tiles";
   if (product({B, Tq, H, dh, 4}) < 0 || product({B, Tk, Hkv, dh, 8}) < 0) return "tensor too large";
   return "";
 }

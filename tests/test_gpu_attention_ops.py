@@ -527,6 +527,35 @@ def seq2seq_data(spec):
     return x, labels, synth.make_params(spec, 1), synth.make_extra_inputs(spec, tables)
 
 
+def rounding_floors(spec, ref, extra):
+    """What rounding alone leaves in gradients that are zero in exact arithmetic.  With one state
+    to attend to, P = 1 and dP - delta is the difference of two sums of equal value, so dq and dk
+    are zero up to the bounds of ``cross_bounds`` (a few u sum |dy| |v| each), and so is everything
+    they alone feed: the gains of both norms and the query projection.  Returns {gradient: bound},
+    the bounds carried through |.| of the exact factors."""
+    out = {}
+    for L in spec["layers"]:
+        if L["op"] != "cross_attention":
+            continue
+        b = L["name"].rsplit(".", 1)[0]
+        q, kv = (ref[f"{b}.{n}"] for n in ("qn", "kn"))
+        B, H, Hkv = spec["input"][0], L["heads"], L["kv_heads"]
+        a = {"B": B, "Tq": len(q) // B, "Tk": len(kv) // B, "H": H, "Hkv": Hkv, "dh": q.shape[1] // H}
+        _, _, bq, bk = au.cross_bounds(q, kv, extra["src_len"], ref[f"d:{b}.cross@{b}.cproj"], a)
+        for name, bound, src, heads in (("qn", bq, "q", H), ("kn", bk[:, :bk.shape[1] // 2], "kv", Hkv)):
+            x = ref[f"{b}.{src}"][:, :heads * a["dh"]].reshape(-1, heads, a["dh"])
+            r = 1 / np.sqrt((x * x).mean(-1, keepdims=True) + 1e-5)
+            w = bound.reshape(x.shape)
+            out[f"d:{b}.{name}.gain"] = (w * np.abs(x) * r).sum((0, 1))
+            if name == "qn":
+                w = w * np.abs(ref[f"{b}.qn.gain"][0])
+                u = np.abs(x) * r
+                dx = (r * (w + u * (w * u).mean(-1, keepdims=True))).reshape(len(x), -1)
+                out[f"d:{b}.q.W"] = dx.T @ np.abs(ref[f"{b}.ln2"])
+                out[f"d:{b}.q.b"] = dx.sum(0)
+    return out
+
+
 @pytest.mark.parametrize("kw", [{}, dict(d=64, heads=2, kv_heads=1, seq=33, src_seq=70, vocab=50),
                                 dict(batch=1, seq=1, src_seq=1)], ids=str)
 def test_seq2seq_step(kw):
@@ -537,12 +566,14 @@ def test_seq2seq_step(kw):
     reg = lower(spec, keep_grads=True, slices=netdef.Net(spec, True).slices)
     ref = oracle_run(reg, x, labels, {k: v.astype(np.float64) for k, v in params.items()}, inputs=extra)
     assert abs(loss - ref["loss"][-1]) <= 1e-5 * abs(ref["loss"][-1])
+    floors = rounding_floors(spec, ref, extra)
+    lr = spec["optimizer"]["lr"]
     for name, v in outs.items():
         want = ref[name].reshape(v.shape)
-        # a handful of layers, each off by a few ten-thousandths of a percent (test_oracle_numerics'
-        # whole-step tolerance)
+        # the whole-step tolerance of the other networks; a momentum buffer holds its gradient
+        floor = floors.get(name.replace("m:", "d:"), np.multiply(floors.get("d:" + name, 0.0), lr))
         norm = np.linalg.norm(want)
-        assert np.linalg.norm(v - want) <= 1e-4 * norm + 1e-9, name
+        assert np.linalg.norm(v - want) <= 1e-4 * norm + np.linalg.norm(floor) + 1e-9, name
     net = netdef.Net(spec, keep_grads=True)
     b, k, f = net.var_bytes, net.var_kinds, net.fn_vars
     for frac, policy in ((0.5, "C"), (0.0, "C"), (0.4, "L")):
