@@ -6,15 +6,15 @@
 // a fixed order and no two workgroups add to the same memory.
 //
 // Products.  All of it is fp32, and the fp32 matrix instructions run at a sixteenth of the fp16
-// ones' rate.  A row x of a matrix is scaled by a power of two that brings its largest value to
-// 2^14 .. 2^15 and split into fp16 pieces, h = fp16(x), l = fp16(x - h), which keep 23 bits of every
-// value and at least the 40 bits below the row's largest; x y is the sum of h h, h l and l h,
-// accumulated in fp32 (l l is below 2^-22 of x y).  Three instructions where splitting into
-// bfloat16 pieces takes six, two pieces to keep and move instead of three.  The scales are exact;
-// where the scaled rows are the terms of a sum (the states in P v and dS k, the queries in P^T dy
-// and dS^T q), the row's scale is multiplied into the other factor, which is computed anyway.  That
-// factor is itself scaled by a running power of two for each output row: its values lie within
-// 2^15, and sums are rescaled, as for the running maximum, in the rare tiles where one passes it.
+// ones' rate.  A matrix (a column of the wave's own side, a tile of rows of the other) is scaled by
+// a power of two that brings its largest value to 2^14 .. 2^15 and split into fp16 pieces, h =
+// fp16(x), l = fp16(x - h), which keep 23 bits of every value, and of small ones the 40 bits below
+// the largest; x y is the sum of h h, h l and l h, accumulated in fp32 (l l is below 2^-22 of x y).
+// Three instructions where splitting into bfloat16 pieces takes six, two pieces to keep and move
+// instead of three.  The scales are exact and multiply into factors that are applied anyway.  What
+// is computed and multiplied again (probabilities, score gradients) is itself scaled by a running
+// power of two per column: its values lie within 2^15, and sums are rescaled, as for the running
+// maximum, in the rare tiles where one passes it.
 //
 // Tiles.  A wave owns 32 columns: of queries (forward, dq) or of states (dk, dv).  Their pieces stay
 // in registers as the B operands of 32 x 32 x 16 products.  The other side passes through LDS in
@@ -86,19 +86,16 @@ __device__ inline float dpp(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL,
                                                                0xf, 0xf, true));
 }
-// largest of N = 4, 8, 16 or 32 neighbouring lanes (values >= 0)
-template <int N>
-__device__ inline float max_of_lanes(float x) {
-  x = fmaxf(x, dpp<0xb1>(x));                        // quad_perm 1 0 3 2
-  x = fmaxf(x, dpp<0x4e>(x));                        // quad_perm 2 3 0 1
-  if constexpr (N >= 8) x = fmaxf(x, dpp<0x141>(x)); // mirrored within 8
-  if constexpr (N >= 16) x = fmaxf(x, dpp<0x140>(x));// mirrored within 16
-  if constexpr (N >= 32) x = fmaxf(x, __shfl_xor(x, 16, 64));
-  return x;
-}
-__device__ inline float wave_max(float v) {
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+// largest of the wave's values (>= 0)
+__device__ inline float wave_max(float x) {
+  x = fmaxf(x, dpp<0xb1>(x));    // quad_perm 1 0 3 2
+  x = fmaxf(x, dpp<0x4e>(x));    // quad_perm 2 3 0 1
+  x = fmaxf(x, dpp<0x141>(x));   // mirrored within 8
+  x = fmaxf(x, dpp<0x140>(x));   // mirrored within 16
+  const uint32_t v = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const uint32_t a = r[0], b = r[1];
+  return max_of_halves(fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
 }
 
 // ---------------------------------------------------------------- scaled pieces
@@ -112,18 +109,40 @@ __device__ inline int exponent(float x) {
 struct Pieces {
   half8v h, l;
 };
-__device__ inline void split2(float x, float y, uint32_t& h, uint32_t& l) {
-  const half2v hh = __builtin_convertvector((floatx2){x, y}, half2v);
-  const half2v ll = __builtin_convertvector((floatx2){x - (float)hh[0], y - (float)hh[1]}, half2v);
+// x scale = h + l.  The remainders are single instructions (fma of fp32 and fp16 operands, rounded
+// to fp16); as a literal, a factor of 1 would be folded into a conversion and a subtraction.
+__device__ inline void split2(float x, float y, float scale, uint32_t& h, uint32_t& l) {
+  const half2v hh = __builtin_convertvector((floatx2){x * scale, y * scale}, half2v);
+  half2v ll;
+  ll[0] = (_Float16)__builtin_fmaf(x, scale, -(float)hh[0]);
+  ll[1] = (_Float16)__builtin_fmaf(y, scale, -(float)hh[1]);
   h = __builtin_bit_cast(uint32_t, hh);
   l = __builtin_bit_cast(uint32_t, ll);
 }
 __device__ inline Pieces split8(const float* v, float scale) {
   uint4 h, l;
-  split2(v[0] * scale, v[1] * scale, h.x, l.x);
-  split2(v[2] * scale, v[3] * scale, h.y, l.y);
-  split2(v[4] * scale, v[5] * scale, h.z, l.z);
-  split2(v[6] * scale, v[7] * scale, h.w, l.w);
+  split2(v[0], v[1], scale, h.x, l.x);
+  split2(v[2], v[3], scale, h.y, l.y);
+  split2(v[4], v[5], scale, h.z, l.z);
+  split2(v[6], v[7], scale, h.w, l.w);
+  return {__builtin_bit_cast(half8v, h), __builtin_bit_cast(half8v, l)};
+}
+// the same of values in fp16's range
+__device__ inline Pieces split8(const float* v) {
+  float one = 1.f;
+  asm("" : "+s"(one));
+  uint4 h, l;
+  uint32_t* hp[4] = {&h.x, &h.y, &h.z, &h.w};
+  uint32_t* lp[4] = {&l.x, &l.y, &l.z, &l.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const half2v hh = __builtin_convertvector((floatx2){v[2 * i], v[2 * i + 1]}, half2v);
+    half2v ll;
+    ll[0] = (_Float16)__builtin_fmaf(v[2 * i], one, -(float)hh[0]);
+    ll[1] = (_Float16)__builtin_fmaf(v[2 * i + 1], one, -(float)hh[1]);
+    *hp[i] = __builtin_bit_cast(uint32_t, hh);
+    *lp[i] = __builtin_bit_cast(uint32_t, ll);
+  }
   return {__builtin_bit_cast(half8v, h), __builtin_bit_cast(half8v, l)};
 }
 __device__ inline float max_abs(const float* v, int n) {
@@ -269,6 +288,60 @@ struct Flight {
   }
 };
 
+// Splits the two tiles in flight into LDS and returns the exponents of their largest values, e.x of
+// the first and e.y of the second; `choose` may raise the second's.  The waves' largest values meet
+// in `tops` across the barrier that frees the tiles of the last round, so each round has two.  Where
+// a tile holds an infinity, the largest finite value counts: the others keep their pieces, and the
+// infinity's remainder is a NaN that reaches whatever reads it.
+template <int DH, int T, class F>
+__device__ inline int2 settle(const Flight<DH, T>& f, char* first, char* second, floatx2* tops,
+                              F choose) {
+  using Wd = Width<DH>;
+  constexpr int U = Flight<DH, T>::kUnits;
+  const auto largest = [&](float ma, float mb) -> floatx2 {
+    ma = wave_max(ma);
+    mb = wave_max(mb);
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = {ma, mb};
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      ma = fmaxf(ma, tops[k][0]);
+      mb = fmaxf(mb, tops[k][1]);
+    }
+    return {ma, mb};
+  };
+  float ma = 0.f, mb = 0.f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) (u < U / 2 ? ma : mb) = fmaxf(u < U / 2 ? ma : mb, max_abs(f.v[u], 8));
+  floatx2 top = largest(ma, mb);
+  if (top[0] == INFINITY || top[1] == INFINITY) {
+    ma = mb = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float v = fabsf(f.v[u][k]);
+        (u < U / 2 ? ma : mb) = fmaxf(u < U / 2 ? ma : mb, v < INFINITY ? v : 0.f);
+      }
+    __syncthreads();
+    top = largest(ma, mb);
+  }
+  ma = top[0];
+  mb = top[1];
+  const int2 e = {exponent(ma), choose(exponent(mb))};
+  const float sa = exp2_of(14 - e.x), sb = exp2_of(14 - e.y);
+  const int c = f.chunk();
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const bool b = u >= U / 2;
+    const Pieces p = split8(f.v[u], b ? sb : sa);
+    if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks)
+      Rows<DH, T>::store(b ? second : first, f.row(u) - (b ? T : 0), c, p);
+  }
+  __syncthreads();
+  return e;
+}
+
 // The workgroup's place: pairs (b, key head), tiles of columns, slices of the other side.  The
 // tiles of a pair run on one die, whose L2 then holds the pair's states (or queries).
 struct Place {
@@ -308,10 +381,11 @@ __device__ inline float pick(const float4& v, int e) {
   return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
 }
 
-// 16 values of a column, scaled, as the B operands of two 16-row steps
-__device__ inline void split_values(const float (&p)[16], float scale, Pieces (&o)[2]) {
-  o[0] = split8(p, scale);
-  o[1] = split8(p + 8, scale);
+// What a masked row's score becomes, for the last tile of a sequence: rows at and past `left`.
+__device__ inline void mask_rows(floatx16& a, int r0, int left) {
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) a[i] = r0 + 8 * (i / 4) + 4 * half + i % 4 < left ? a[i] : -INFINITY;
 }
 
 // ---------------------------------------------------------------- forward
@@ -327,7 +401,7 @@ __global__ __launch_bounds__(TPB, 2) void fwd_kernel(const float* __restrict__ q
   using Rw = Rows<DH, T>;
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
-  __shared__ __attribute__((aligned(16))) float kf[T], ve[T], vi[T];
+  __shared__ floatx2 tops[kWaves];
   const Place at = place(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
@@ -360,58 +434,24 @@ __global__ __launch_bounds__(TPB, 2) void fwd_kernel(const float* __restrict__ q
   };
   if (k0 < k1) fetch(k0);
   for (int j0 = k0; j0 < k1; j0 += T) {
-    constexpr int U = Flight<DH, T>::kUnits;
-    int e[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      e[u] = exponent(max_of_lanes<Wd::kLanes>(max_abs(next.v[u], 8)));
-    const int c = next.chunk();
-    __syncthreads();
-    if (j0 == k0) {   // base: the largest exponent of the first tile's values
-      if (c == 0)
-#pragma unroll
-        for (int u = U / 2; u < U; ++u) ve[next.row(u) - T] = (float)e[u];
-      __syncthreads();
-      const float top = wave_max(lane < T ? ve[lane] : -112.f);
-      base = top <= -112.f || top >= 128.f ? 0 : __builtin_amdgcn_readfirstlane((int)top);
-      __syncthreads();
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool value = u >= U / 2;
-      const int r = next.row(u) - (value ? T : 0);
-      // values far below base keep a common exponent; rows of zeros count as base
-      if (value) e[u] = e[u] <= -112 ? base : max(e[u], base - 40);
-      const Pieces p = split8(next.v[u], exp2_of(14 - e[u]));
-      if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks) Rw::store(value ? vs : ks, r, c, p);
-      if (c == 0) {
-        if (value) {
-          const bool there = j0 + r < k1;
-          ve[r] = there ? (float)(e[u] - base) : -INFINITY;
-          vi[r] = there ? exp2_of(max(base - e[u], -126)) : 0.f;
-        } else {
-          kf[r] = exp2_of(e[u] - 14);
-        }
-      }
-    }
-    __syncthreads();
+    const int2 e = settle<DH, T>(next, ks, vs, tops, [&](int x) {
+      if (j0 == k0) base = x <= -112 ? 0 : x;
+      return x <= -112 ? base : max(x, base - 40);   // zeros count as base
+    });
     if (j0 + T < k1) fetch(j0 + T);
-#pragma unroll
+    // (no smaller than the normal numbers: a masked score stays -inf)
+    const float c = fmaxf(qc * exp2_of(e.x - 14), 0x1p-126f);
+    const float ve = (float)(e.y - base), vi = exp2_of(max(base - e.y, -126));
+#pragma unroll 1
     for (int r0 = 0; r0 < T; r0 += 32) {
       floatx16 a = {};
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(ks, r0, t), qp[t], a);
-      float p[16], top = -INFINITY;
+      if (r0 + 32 > k1 - j0) mask_rows(a, r0, k1 - j0);
+      float top = -INFINITY;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 f = at4(kf, r0 + 8 * g + 4 * half), x = at4(ve, r0 + 8 * g + 4 * half);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[4 * g + i] = fmaf(a[4 * g + i] * pick(f, i), qc, pick(x, i));
-          top = fmaxf(top, p[4 * g + i]);
-        }
-      }
-      top = max_of_halves(top);
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, a[i]);
+      top = fmaf(max_of_halves(top), c, ve);
       if (__any(top > m + 7.f)) {
         const float up = fmaxf(m, top), f = m == up ? 1.f : exp2f(m - up);
         m = up;
@@ -421,20 +461,15 @@ __global__ __launch_bounds__(TPB, 2) void fwd_kernel(const float* __restrict__ q
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[t][i] *= f;
       }
-      float part = 0.f;
-      const float off = 8.f - m;
+      const float off = ve + 8.f - m;
+      float p[16], part = 0.f;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 x = at4(vi, r0 + 8 * g + 4 * half);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[4 * g + i] = __builtin_amdgcn_exp2f(p[4 * g + i] + off);
-          part = fmaf(p[4 * g + i], pick(x, i), part);
-        }
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, off));
+        part += p[i];
       }
-      sum += part;
-      Pieces pp[2];
-      split_values(p, 1.f, pp);
+      sum = fmaf(part, vi, sum);
+      const Pieces pp[2] = {split8(p), split8(p + 8)};
 #pragma unroll
       for (int t = 0; t < Wd::kSums; ++t)
 #pragma unroll
@@ -498,7 +533,7 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dq_kernel(
   using Rw = Rows<DH, T>;
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
-  __shared__ __attribute__((aligned(16))) float kf[T], vf[T], off[T];
+  __shared__ floatx2 tops[kWaves];
   const Place at = place(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
@@ -537,44 +572,25 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dq_kernel(
   };
   if (k0 < k1) fetch(k0);
   for (int j0 = k0; j0 < k1; j0 += T) {
-    constexpr int U = Flight<DH, T>::kUnits;
-    const int c = next.chunk();
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool value = u >= U / 2;
-      const int r = next.row(u) - (value ? T : 0);
-      const int e = exponent(max_of_lanes<Wd::kLanes>(max_abs(next.v[u], 8)));
-      const Pieces p = split8(next.v[u], exp2_of(14 - e));
-      if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks) Rw::store(value ? vs : ks, r, c, p);
-      if (c == 0) {
-        (value ? vf : kf)[r] = exp2_of(e - 14);
-        if (value) off[r] = j0 + r < k1 ? 0.f : -INFINITY;
-      }
-    }
-    __syncthreads();
+    const int2 e = settle<DH, T>(next, ks, vs, tops, [](int x) { return x; });
     if (j0 + T < k1) fetch(j0 + T);
-#pragma unroll
+    const float kf = exp2_of(e.x - 14), c = fmaxf(qc * kf, 0x1p-126f), cv = gf * exp2_of(e.y - 14);
+#pragma unroll 1
     for (int r0 = 0; r0 < T; r0 += 32) {
       floatx16 a = {}, b = {};
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(ks, r0, t), qp[t], a);
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) b = mma(Rw::by_row(vs, r0, t), gp[t], b);
+      if (r0 + 32 > k1 - j0) mask_rows(a, r0, k1 - j0);
       float x[16], top = 0.f;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int row = r0 + 8 * g + 4 * half;
-        const float4 fk = at4(kf, row), fv = at4(vf, row), z = at4(off, row);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(a[4 * g + i] * pick(fk, i), qc, nl + pick(z, i)));
-          const float d = fmaf(b[4 * g + i] * pick(fv, i), gf, -dl);
-          x[4 * g + i] = p * d * pick(fk, i);
-          top = fmaxf(top, fabsf(x[4 * g + i]));
-        }
+      for (int i = 0; i < 16; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, nl)) * fmaf(b[i], cv, -dl);
+        top = fmaxf(top, fabsf(x[i]));
       }
-      top = max_of_halves(top);
+      // x 2^(e.x - 14) is what meets the pieces of k: the factor f keeps is for that
+      top = max_of_halves(top) * kf;
       if (__any(top * f > 0x1p15f)) {
         const float g = top * f > 0x1p15f ? exp2_of(max(8 - exponent(top), -126)) : f;
         const float up = g / f;
@@ -584,8 +600,7 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dq_kernel(
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[t][i] *= up;
       }
-      Pieces xp[2];
-      split_values(x, f, xp);
+      const Pieces xp[2] = {split8(x, f * kf), split8(x + 8, f * kf)};
 #pragma unroll
       for (int t = 0; t < Wd::kSums; ++t)
 #pragma unroll
@@ -610,7 +625,8 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dkv_kernel(
   using Rw = Rows<DH, T>;
   __shared__ __attribute__((aligned(16))) char qs[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char gs[Rw::kBytes];
-  __shared__ __attribute__((aligned(16))) float qf[T], gf[T], nl[T], dl[T];
+  __shared__ __attribute__((aligned(16))) float nl[T], dl[T];
+  __shared__ floatx2 tops[kWaves];
   const Place at = place(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
@@ -675,26 +691,18 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dkv_kernel(
   const auto step = [&](int i) { return packed ? i + T : min(i + T, i - i % s.Tq + s.Tq); };
   if (i0 < i1) fetch(i0);
   for (int i = i0; i < i1;) {
-    constexpr int U = Flight<DH, T>::kUnits;
-    const int c = next.chunk();
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool second = u >= U / 2;
-      const int r = next.row(u) - (second ? T : 0);
-      const int e = exponent(max_of_lanes<Wd::kLanes>(max_abs(next.v[u], 8)));
-      const Pieces p = split8(next.v[u], exp2_of(14 - e));
-      if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks) Rw::store(second ? gs : qs, r, c, p);
-      if (c == 0) (second ? gf : qf)[r] = exp2_of(e - 14);
-    }
-    if ((int)threadIdx.x < T) {
-      nl[threadIdx.x] = ll;
-      dl[threadIdx.x] = dd;
-    }
-    __syncthreads();
+    const float l0 = ll, d0 = dd;
+    const int2 e = settle<DH, T>(next, qs, gs, tops, [&](int x) {
+      if ((int)threadIdx.x < T) {   // between the barriers, as the tiles themselves
+        nl[threadIdx.x] = l0;
+        dl[threadIdx.x] = d0;
+      }
+      return x;
+    });
     i = step(i);
     if (i < i1) fetch(i);
-#pragma unroll
+    const float qf = exp2_of(e.x - 14), gf = exp2_of(e.y - 14), c = kc * qf, cv = vf * gf;
+#pragma unroll 1
     for (int r0 = 0; r0 < T; r0 += 32) {
       floatx16 a = {}, b = {};
 #pragma unroll
@@ -705,19 +713,17 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dkv_kernel(
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int row = r0 + 8 * g + 4 * half;
-        const float4 fq = at4(qf, row), fg = at4(gf, row), l4 = at4(nl, row), d4 = at4(dl, row);
+        const float4 l4 = at4(nl, row), d4 = at4(dl, row);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float pr = __builtin_amdgcn_exp2f(fmaf(a[4 * g + e] * pick(fq, e), kc, pick(l4, e)));
-          const float d = fmaf(b[4 * g + e] * pick(fg, e), vf, -pick(d4, e));
-          p[4 * g + e] = pr * pick(fg, e);
-          x[4 * g + e] = pr * d * pick(fq, e);
-          ptop = fmaxf(ptop, p[4 * g + e]);
-          xtop = fmaxf(xtop, fabsf(x[4 * g + e]));
+        for (int k = 0; k < 4; ++k) {
+          p[4 * g + k] = __builtin_amdgcn_exp2f(fmaf(a[4 * g + k], c, pick(l4, k)));
+          x[4 * g + k] = p[4 * g + k] * fmaf(b[4 * g + k], cv, -pick(d4, k));
+          ptop = fmaxf(ptop, p[4 * g + k]);
+          xtop = fmaxf(xtop, fabsf(x[4 * g + k]));
         }
       }
-      ptop = max_of_halves(ptop);
-      xtop = max_of_halves(xtop);
+      ptop = max_of_halves(ptop) * gf;
+      xtop = max_of_halves(xtop) * qf;
       if (__any(ptop * fv > 0x1p15f || xtop * fk > 0x1p15f)) {
         const float gv = ptop * fv > 0x1p15f ? exp2_of(max(8 - exponent(ptop), -126)) : fv;
         const float gk = xtop * fk > 0x1p15f ? exp2_of(max(8 - exponent(xtop), -126)) : fk;
@@ -727,21 +733,23 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dkv_kernel(
 #pragma unroll
         for (int t = 0; t < Wd::kSums; ++t)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            dv[t][e] *= uv;
-            dk[t][e] *= uk;
+          for (int k = 0; k < 16; ++k) {
+            dv[t][k] *= uv;
+            dk[t][k] *= uk;
           }
       }
-      Pieces pp[2], xp[2];
-      split_values(p, fv, pp);
-      split_values(x, fk, xp);
+      {
+        const Pieces pp[2] = {split8(p, fv * gf), split8(p + 8, fv * gf)};
+#pragma unroll
+        for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) dv[t] = mma(Rw::by_column(gs, r0 + 16 * h, first + t), pp[h], dv[t]);
+      }
+      const Pieces xp[2] = {split8(x, fk * qf), split8(x + 8, fk * qf)};
 #pragma unroll
       for (int t = 0; t < Wd::kSums; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          dv[t] = mma(Rw::by_column(gs, r0 + 16 * h, first + t), pp[h], dv[t]);
-          dk[t] = mma(Rw::by_column(qs, r0 + 16 * h, first + t), xp[h], dk[t]);
-        }
+        for (int h = 0; h < 2; ++h) dk[t] = mma(Rw::by_column(qs, r0 + 16 * h, first + t), xp[h], dk[t]);
     }
   }
   if (!mine) return;

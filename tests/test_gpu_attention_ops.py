@@ -237,6 +237,39 @@ def test_cross_attention_nan_stays_in_its_sequence_and_head():
     assert np.array_equal(bad, want) and np.array_equal(np.isnan(lse), want.transpose(0, 2, 1))
 
 
+def test_cross_attention_infinite_value_stays_in_its_column():
+    """A value of infinity: its head column is not finite, the other columns are what they are."""
+    a, q, kv, klen, dy = au.cross_case(39, 1, 70, 100, 2, 2, 32, [100])
+    clean = kv.copy()
+    kv[41, 64 + 7], clean[41, 64 + 7] = np.inf, 0      # key head 0, column 7
+    y, _ = cross_fwd(a, q, kv, klen)
+    f = np.float64
+    want, _ = ops.cross_attention_fwd(q.astype(f), clean.astype(f), klen, a)
+    bound = au.cross_bounds(q, clean, klen, dy, a)[0]
+    bad = np.zeros(64, bool)
+    bad[7] = True
+    assert not np.isfinite(y[:, bad]).any()
+    au.within("y", y[:, ~bad], want[:, ~bad], bound[:, ~bad])
+
+
+def test_cross_attention_scales():
+    """Values of any size, and sequences whose states differ in size by 2^20 along the keys: the
+    sums are accurate relative to what they sum."""
+    for i, (sq, sk, sv, sg) in enumerate(((1e-20, 1e20, 1e-15, 1e15), (1e10, 1e-10, 1e25, 1e-25),
+                                          (1e-30, 1.0, 1e-30, 1e-3), (1.0, 1.0, 1e30, 1e-30))):
+        a, q, kv, klen, dy = au.cross_case(70 + i, 2, 40, 150, 2, 1, 40, [150, 33])
+        n = kv.shape[1] // 2
+        kv[:, :n] *= np.float32(sk)
+        kv[:, n:] *= np.float32(sv)
+        check_cross(a, q * np.float32(sq), kv, klen, dy * np.float32(sg))
+    a, q, kv, klen, dy = au.cross_case(75, 1, 40, 256, 2, 1, 64, [256])
+    kv[:128, 64:] *= np.float32(2.0 ** 20)             # values; and a softmax that looks at the others
+    kv[:128, :64], kv[128:, :64] = 0, kv[128:, :64]
+    kv[128:, 0] = 60 * np.sign(kv[128:, 0])
+    q[:, ::64] = 20
+    check_cross(a, q, kv, klen, dy)
+
+
 def test_cross_attention_gradient_of_the_forward_by_differences():
     """The device's gradients against differences of the device's own forward, at a step where
     truncation and rounding of the sum stay below a percent."""
