@@ -41,8 +41,6 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int kWaves = 4;
-constexpr int TPB = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kUnit = 0x1p-14f;    // a scaled row's largest value is 2^14 .. 2^15 of its exponent
 constexpr uint32_t kNone = 0x80000000u;   // past the length of every descriptor
@@ -58,11 +56,22 @@ struct Width {
   static constexpr int kChunks = DH / 8;
   static constexpr int kLanes = DH == 32 ? 4 : DH == 64 ? 8 : DH <= 128 ? 16 : 32;   // that load a row
   static constexpr int kRow = (DH == 32 ? 7 : DH == 64 ? 9 : DH == 96 ? 13 : DH == 128 ? 19 : 35) * 16;
-  static constexpr int kTile = DH <= 64 ? 64 : 32;        // rows of a tile
-  // waves that share 32 columns, each with its part of the sums (registers hold no more)
+  // The forward: rows of a tile, waves of a workgroup, sets of 32 columns a wave, waves that share
+  // columns, each with its part of the sums (where registers hold no more), blocks it then sums.
+  static constexpr int kTile = DH <= 64 ? 64 : 32;
+  static constexpr int kFwdWaves = DH <= 64 ? 4 : DH <= 128 ? 8 : 4;
+  static constexpr int kSets = DH <= 64 ? 2 : 1;
   static constexpr int kParts = DH <= 128 ? 1 : 2;
-  static constexpr int kCols = 32 * kWaves / kParts;      // columns of a workgroup
-  static constexpr int kSums = kBlocks / kParts;          // blocks of head columns a wave sums
+  static constexpr int kSums = kBlocks / kParts;
+  static constexpr int kFwdCols = 32 * kFwdWaves * kSets / kParts;
+  // The backward up to 64 head columns: rows of a tile, waves of a workgroup.
+  static constexpr int kBackTile = 64, kBackWaves = 4;
+  // The backward above, by pairs of waves: waves of a workgroup, tile buffers, waves a SIMD holds.
+  static constexpr int kPairWaves = DH <= 128 ? 8 : 4;
+  static constexpr int kBuffers = DH <= 128 ? 2 : 1;
+  static constexpr int kOccupancy = DH <= 128 ? 2 : 1;
+  static constexpr int kBackCols = DH <= 64 ? 32 * kBackWaves : 16 * kPairWaves;
+  static constexpr int kBackRows = DH <= 64 ? kBackTile : 32;
 };
 
 // ---------------------------------------------------------------- exchange between lanes
@@ -202,17 +211,26 @@ __device__ inline int64_t stat_row(const Shape& s, int b, int hk) {
 }
 
 // A wave's own columns: lane l holds column l mod 32, head columns 16 s + 8 (l / 32) .. + 8 of every
-// step s.  p: the column's row; nothing is read unless `valid`.
+// step s.  p: the column's row (a column past the last takes the last one's; it is not stored).
 template <int DH, bool EXACT>
-__device__ inline void load_column(const float* p, bool valid, int dh, float (&v)[DH / 2]) {
+__device__ inline void load_column(const float* p, int dh, float (&v)[DH / 2]) {
   const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-  for (int s = 0; s < DH / 16; ++s)
+  for (int s = 0; s < DH / 16; ++s) {
+    if constexpr (EXACT) {
+      const float4 a = *reinterpret_cast<const float4*>(p + 16 * s + 8 * half);
+      const float4 b = *reinterpret_cast<const float4*>(p + 16 * s + 8 * half + 4);
+      v[8 * s] = a.x; v[8 * s + 1] = a.y; v[8 * s + 2] = a.z; v[8 * s + 3] = a.w;
+      v[8 * s + 4] = b.x; v[8 * s + 5] = b.y; v[8 * s + 6] = b.z; v[8 * s + 7] = b.w;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int d = 16 * s + 8 * half + e;
-      v[8 * s + e] = valid && (EXACT || d < dh) ? p[d] : 0.f;
+      for (int e = 0; e < 8; ++e) {
+        const int d = 16 * s + 8 * half + e;
+        const float x = p[min(d, dh - 1)];
+        v[8 * s + e] = d < dh ? x : 0.f;
+      }
     }
+  }
 }
 // Returns the inverse scale.
 template <int DH>
@@ -259,89 +277,6 @@ struct Rows {
   }
 };
 
-// The values of two matrices' next tile on their way from memory: unit u of a thread is 8 head
-// columns of row u / lanes of the two tiles on top of each other.
-template <int DH, int T>
-struct Flight {
-  using Wd = Width<DH>;
-  static constexpr int kUnits = 2 * T * Wd::kLanes / TPB;
-  static_assert(kUnits >= 1 && 2 * T * Wd::kLanes % TPB == 0, "units per thread");
-  float v[kUnits][8];
-  static __device__ int row(int u) { return ((int)threadIdx.x + u * TPB) / Wd::kLanes; }
-  static __device__ int chunk() { return (int)threadIdx.x % Wd::kLanes; }
-  // a, b: the two matrices from the tile's first row on, n values a row's distance, `rows` of them
-  // there.  The matrix of a unit is uniform over the thread block's unit index.
-  template <bool EXACT>
-  __device__ void load(const float* a, const float* b, int64_t lda, int64_t ldb, int rows, int dh) {
-    const auto ra = buffer(a, rows > 0 ? (int64_t)(rows - 1) * lda + dh : 0);
-    const auto rb = buffer(b, rows > 0 ? (int64_t)(rows - 1) * ldb + dh : 0);
-    const int c = chunk();
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const bool second = u >= kUnits / 2;
-      const int r = row(u) - (second ? T : 0);
-      uint32_t off = (uint32_t)(r * (second ? ldb : lda) + 8 * c) * 4u;
-      if (r >= rows || 8 * c >= dh) off = kNone;
-      load8(second ? rb : ra, off, v[u]);
-      trim<EXACT>(v[u], 8 * c, dh);
-    }
-  }
-};
-
-// Splits the two tiles in flight into LDS and returns the exponents of their largest values, e.x of
-// the first and e.y of the second; `choose` may raise the second's.  The waves' largest values meet
-// in `tops` across the barrier that frees the tiles of the last round, so each round has two.  Where
-// a tile holds an infinity, the largest finite value counts: the others keep their pieces, and the
-// infinity's remainder is a NaN that reaches whatever reads it.
-template <int DH, int T, class F>
-__device__ inline int2 settle(const Flight<DH, T>& f, char* first, char* second, floatx2* tops,
-                              F choose) {
-  using Wd = Width<DH>;
-  constexpr int U = Flight<DH, T>::kUnits;
-  const auto largest = [&](float ma, float mb) -> floatx2 {
-    ma = wave_max(ma);
-    mb = wave_max(mb);
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = {ma, mb};
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-      ma = fmaxf(ma, tops[k][0]);
-      mb = fmaxf(mb, tops[k][1]);
-    }
-    return {ma, mb};
-  };
-  float ma = 0.f, mb = 0.f;
-#pragma unroll
-  for (int u = 0; u < U; ++u) (u < U / 2 ? ma : mb) = fmaxf(u < U / 2 ? ma : mb, max_abs(f.v[u], 8));
-  floatx2 top = largest(ma, mb);
-  if (top[0] == INFINITY || top[1] == INFINITY) {
-    ma = mb = 0.f;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float v = fabsf(f.v[u][k]);
-        (u < U / 2 ? ma : mb) = fmaxf(u < U / 2 ? ma : mb, v < INFINITY ? v : 0.f);
-      }
-    __syncthreads();
-    top = largest(ma, mb);
-  }
-  ma = top[0];
-  mb = top[1];
-  const int2 e = {exponent(ma), choose(exponent(mb))};
-  const float sa = exp2_of(14 - e.x), sb = exp2_of(14 - e.y);
-  const int c = f.chunk();
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const bool b = u >= U / 2;
-    const Pieces p = split8(f.v[u], b ? sb : sa);
-    if (Wd::kLanes == Wd::kChunks || c < Wd::kChunks)
-      Rows<DH, T>::store(b ? second : first, f.row(u) - (b ? T : 0), c, p);
-  }
-  __syncthreads();
-  return e;
-}
-
 // The workgroup's place: pairs (b, key head), tiles of columns, slices of the other side.  The
 // tiles of a pair run on one die, whose L2 then holds the pair's states (or queries).
 struct Place {
@@ -355,11 +290,11 @@ __device__ inline Place place(const Shape& s, int tiles) {
 }
 
 // Sum t of a lane holds, in r, head column 32 (first + t) + 8 (r / 4) + 4 half + r % 4 of its column.
-template <int DH, bool EXACT, class F>
+template <int N, bool EXACT, class F>
 __device__ inline void store_column(float* p, int first, int dh, F value) {
   const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-  for (int t = 0; t < Width<DH>::kSums; ++t)
+  for (int t = 0; t < N; ++t)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int d = 32 * (first + t) + 8 * q + 4 * half;
@@ -388,106 +323,234 @@ __device__ inline void mask_rows(floatx16& a, int r0, int left) {
   for (int i = 0; i < 16; ++i) a[i] = r0 + 8 * (i / 4) + 4 * half + i % 4 < left ? a[i] : -INFINITY;
 }
 
+// The values of two matrices' next tile of T rows on their way from memory to LDS, W waves a
+// workgroup: a thread holds units of 8 head columns, of the rows of the first matrix, then of the
+// second.  The matrix of a unit is uniform over a wave, as T rows are whole waves' worth.
+template <int DH, int W, int T>
+struct Raw {
+  using Wd = Width<DH>;
+  static constexpr int kThreads = 64 * W;
+  static constexpr int kLanes = Wd::kLanes;
+  static constexpr int kUnits = (2 * T * kLanes + kThreads - 1) / kThreads;
+  static_assert(T * kLanes % 64 == 0, "a wave's units are of one matrix");
+  float v[kUnits][8];
+  static __device__ int row(int u) { return ((int)threadIdx.x + u * kThreads) / kLanes; }
+  static __device__ bool second(int u) { return __builtin_amdgcn_readfirstlane(row(u)) >= T; }
+  static __device__ bool idle(int u) {
+    return 2 * T * kLanes % kThreads && __builtin_amdgcn_readfirstlane(row(u)) >= 2 * T;
+  }
+  static __device__ int chunk() { return (int)threadIdx.x % kLanes; }
+  // a, b: the matrices from the tile's first row on, ld values a row's distance, `rows` of them there
+  template <bool EXACT>
+  __device__ void load(const float* a, const float* b, int64_t ld, int rows, int dh) {
+    const int64_t len = rows > 0 ? (int64_t)(min(rows, T) - 1) * ld + dh : 0;
+    const auto ra = buffer(a, len), rb = buffer(b, len);
+    const int c = chunk();
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int r = row(u) % T;
+      uint32_t off = (uint32_t)(r * ld + 8 * c) * 4u;
+      if (r >= rows || 8 * c >= dh || idle(u)) off = kNone;
+      load8(second(u) ? rb : ra, off, v[u]);
+      trim<EXACT>(v[u], 8 * c, dh);
+    }
+  }
+  // rows i .. of the group's heads, numbered g Tq + position; a, b: position 0 of its first head
+  template <bool EXACT>
+  __device__ void load_packed(const float* a, const float* b, const Shape& s, int i, int rows) {
+    const int64_t len = (int64_t)(s.Tq - 1) * s.ldq + (int64_t)s.G * s.dh;
+    const auto ra = buffer(a, len), rb = buffer(b, len);
+    const int c = chunk();
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int r = row(u) % T, g = (i + r) / s.Tq, k = i + r - g * s.Tq;
+      uint32_t off = (uint32_t)(k * s.ldq + (int64_t)g * s.dh + 8 * c) * 4u;
+      if (r >= rows || 8 * c >= s.dh || idle(u)) off = kNone;
+      load8(second(u) ? rb : ra, off, v[u]);
+      trim<EXACT>(v[u], 8 * c, s.dh);
+    }
+  }
+  // The wave's largest finite values of the two matrices.  An infinity does not count: the other
+  // values keep their pieces, and its remainder is a NaN that reaches whatever reads it.
+  __device__ void publish(floatx2* tops) const {
+    float ma = 0.f, mb = 0.f;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const float m = max_abs(v[u], 8);
+      if (second(u)) mb = fmaxf(mb, m);
+      else ma = fmaxf(ma, m);
+    }
+    if (__any(fmaxf(ma, mb) == INFINITY)) {
+      ma = mb = 0.f;
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float x = fabsf(v[u][k]), m = x < INFINITY ? x : 0.f;
+          if (second(u)) mb = fmaxf(mb, m);
+          else ma = fmaxf(ma, m);
+        }
+    }
+    ma = wave_max(ma);
+    mb = wave_max(mb);
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = {ma, mb};
+  }
+  // The exponents of the tiles' largest values, from what every wave has published.
+  static __device__ int2 exponents(const floatx2* tops) {
+    float ma = 0.f, mb = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      ma = fmaxf(ma, tops[k][0]);
+      mb = fmaxf(mb, tops[k][1]);
+    }
+    return {exponent(ma), exponent(mb)};
+  }
+  __device__ void store(char* a, char* b, int2 e) const {
+    const float sa = exp2_of(14 - e.x), sb = exp2_of(14 - e.y);
+    const int c = chunk();
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const Pieces p = split8(v[u], second(u) ? sb : sa);
+      if ((kLanes == Wd::kChunks || c < Wd::kChunks) && !idle(u))
+        Rows<DH, T>::store(second(u) ? b : a, row(u) % T, c, p);
+    }
+  }
+};
+
 // ---------------------------------------------------------------- forward
 template <int DH, bool EXACT>
-__global__ __launch_bounds__(TPB, 2) void fwd_kernel(const float* __restrict__ q,
-                                                     const float* __restrict__ kv,
-                                                     const int32_t* __restrict__ klen,
-                                                     float* __restrict__ y, float* __restrict__ lse,
-                                                     Shape s, int tiles, int slice_len,
-                                                     int64_t y_slice, int64_t lse_slice) {
+__global__ __launch_bounds__(64 * Width<DH>::kFwdWaves, DH <= 128 ? 2 : 1) void fwd_kernel(
+    const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
+    float* __restrict__ y, float* __restrict__ lse, Shape s, int tiles, int slice_len,
+    int64_t y_slice, int64_t lse_slice) {
   using Wd = Width<DH>;
-  constexpr int T = Wd::kTile;
+  constexpr int T = Wd::kTile, W = Wd::kFwdWaves, C = Wd::kSets;
   using Rw = Rows<DH, T>;
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
-  __shared__ floatx2 tops[kWaves];
+  __shared__ floatx2 tops[W];
   const Place at = place(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-  const int col = at.tile * Wd::kCols + w / Wd::kParts * 32 + (lane & 31);
+  const int col0 = at.tile * Wd::kFwdCols + w / Wd::kParts * 32 * C + (lane & 31);
   const int first = w % Wd::kParts * Wd::kSums;
-  const bool mine = col < s.R;
   const int n = klen[at.b];
   const bool bad = n < 0 || n > s.Tk;
   const int k0 = bad ? 0 : min(n, at.slice * slice_len), k1 = bad ? 0 : min(n, k0 + slice_len);
 
-  Pieces qp[Wd::kSteps];
-  float qc;
-  const int64_t qrow = mine ? query_row(s, at.b, at.hk, col) : 0;
-  {
-    float v[DH / 2];
-    load_column<DH, EXACT>(q + qrow, mine, s.dh, v);
-    qc = split_column<DH>(v, qp) * s.scale * kLog2e;
-  }
-  floatx16 o[Wd::kSums];
+  Pieces qp[C][Wd::kSteps];
+  float qc[C];
 #pragma unroll
-  for (int t = 0; t < Wd::kSums; ++t) o[t] = floatx16{};
+  for (int x = 0; x < C; ++x) {
+    float v[DH / 2];
+    load_column<DH, EXACT>(q + query_row(s, at.b, at.hk, min(col0 + 32 * x, s.R - 1)), s.dh, v);
+    qc[x] = split_column<DH>(v, qp[x]) * s.scale * kLog2e;
+  }
+  floatx16 o[C][Wd::kSums];
   // Powers of two: m above the largest score plus value exponent so far (less base), and the sums
   // of 2^(score - m + 8) and of that times the values.  m stays while no term passes 2^15.
-  float m = -INFINITY, sum = 0.f;
+  float m[C], sum[C];
+#pragma unroll
+  for (int x = 0; x < C; ++x) {
+    m[x] = -INFINITY;
+    sum[x] = 0.f;
+#pragma unroll
+    for (int t = 0; t < Wd::kSums; ++t) o[x][t] = floatx16{};
+  }
   int base = 0;
-  Flight<DH, T> next;
+  Raw<DH, W, T> raw;
   const auto fetch = [&](int j) {
     const int64_t r = key_row(s, at.b, at.hk, j);
-    next.template load<EXACT>(kv + r, kv + r + (int64_t)s.Hkv * s.dh, s.ldk, s.ldk, min(T, k1 - j), s.dh);
+    raw.template load<EXACT>(kv + r, kv + r + (int64_t)s.Hkv * s.dh, s.ldk, k1 - j, s.dh);
   };
   if (k0 < k1) fetch(k0);
   for (int j0 = k0; j0 < k1; j0 += T) {
-    const int2 e = settle<DH, T>(next, ks, vs, tops, [&](int x) {
-      if (j0 == k0) base = x <= -112 ? 0 : x;
-      return x <= -112 ? base : max(x, base - 40);   // zeros count as base
-    });
+    raw.publish(tops);
+    __syncthreads();
+    int2 e = raw.exponents(tops);
+    if (j0 == k0) base = e.y <= -112 ? 0 : e.y;
+    e.y = e.y <= -112 ? base : max(e.y, base - 40);   // zeros count as base
+    raw.store(ks, vs, e);
+    __syncthreads();
     if (j0 + T < k1) fetch(j0 + T);
-    // (no smaller than the normal numbers: a masked score stays -inf)
-    const float c = fmaxf(qc * exp2_of(e.x - 14), 0x1p-126f);
     const float ve = (float)(e.y - base), vi = exp2_of(max(base - e.y, -126));
 #pragma unroll 1
     for (int r0 = 0; r0 < T; r0 += 32) {
-      floatx16 a = {};
+      if (r0 && j0 + r0 >= k1) break;
+      floatx16 a[C];
 #pragma unroll
-      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(ks, r0, t), qp[t], a);
-      if (r0 + 32 > k1 - j0) mask_rows(a, r0, k1 - j0);
-      float top = -INFINITY;
+      for (int x = 0; x < C; ++x) a[x] = floatx16{};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, a[i]);
-      top = fmaf(max_of_halves(top), c, ve);
-      if (__any(top > m + 7.f)) {
-        const float up = fmaxf(m, top), f = m == up ? 1.f : exp2f(m - up);
-        m = up;
-        sum *= f;
+      for (int t = 0; t < Wd::kSteps; ++t) {
+        const Pieces k = Rw::by_row(ks, r0, t);
 #pragma unroll
-        for (int t = 0; t < Wd::kSums; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[t][i] *= f;
+        for (int x = 0; x < C; ++x) a[x] = mma(k, qp[x][t], a[x]);
       }
-      const float off = ve + 8.f - m;
-      float p[16], part = 0.f;
+      if (j0 + r0 + 32 > k1)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, off));
-        part += p[i];
+        for (int x = 0; x < C; ++x) mask_rows(a[x], r0, k1 - j0);
+      float c[C], top[C];
+      bool past = false;
+#pragma unroll
+      for (int x = 0; x < C; ++x) {
+        // (no smaller than the normal numbers: a masked score stays -inf)
+        c[x] = fmaxf(qc[x] * exp2_of(e.x - 14), 0x1p-126f);
+        top[x] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top[x] = fmaxf(top[x], a[x][i]);
+        top[x] = fmaf(max_of_halves(top[x]), c[x], ve);
+        past |= top[x] > m[x] + 7.f;
       }
-      sum = fmaf(part, vi, sum);
-      const Pieces pp[2] = {split8(p), split8(p + 8)};
+      if (__any(past))
+#pragma unroll
+        for (int x = 0; x < C; ++x) {
+          const float up = fmaxf(m[x], top[x]), f = m[x] == up ? 1.f : exp2f(m[x] - up);
+          m[x] = up;
+          sum[x] *= f;
+#pragma unroll
+          for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[x][t][i] *= f;
+        }
+      Pieces pp[C][2];
+#pragma unroll
+      for (int x = 0; x < C; ++x) {
+        const float off = ve + 8.f - m[x];
+        float p[16], part = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(fmaf(a[x][i], c[x], off));
+          part += p[i];
+        }
+        sum[x] = fmaf(part, vi, sum[x]);
+        pp[x][0] = split8(p);
+        pp[x][1] = split8(p + 8);
+      }
 #pragma unroll
       for (int t = 0; t < Wd::kSums; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) o[t] = mma(Rw::by_column(vs, r0 + 16 * h, first + t), pp[h], o[t]);
+        for (int h = 0; h < 2; ++h) {
+          const Pieces v = Rw::by_column(vs, r0 + 16 * h, first + t);
+#pragma unroll
+          for (int x = 0; x < C; ++x) o[x][t] = mma(v, pp[x][h], o[x][t]);
+        }
     }
   }
-  sum = sum_of_halves(sum);
-  if (!mine) return;
-  float f = 0.f, l = -INFINITY;
-  if (bad) f = l = NAN;
-  else if (k0 < k1) {
-    f = kUnit * exp2_of(base) / sum;
-    l = (m - 8.f + log2f(sum)) * kLn2;
+#pragma unroll
+  for (int x = 0; x < C; ++x) {
+    const float total = sum_of_halves(sum[x]);
+    const int col = col0 + 32 * x;
+    if (col >= s.R) continue;
+    float f = 0.f, l = -INFINITY;
+    if (bad) f = l = NAN;
+    else if (k0 < k1) {
+      f = kUnit * exp2_of(base) / total;
+      l = (m[x] - 8.f + log2f(total)) * kLn2;
+    }
+    store_column<Wd::kSums, EXACT>(y + at.slice * y_slice + query_row(s, at.b, at.hk, col), first, s.dh,
+                                   [&](int t, int i) { return k0 < k1 ? o[x][t][i] * f : f; });
+    if (half == 0 && first == 0) lse[at.slice * lse_slice + stat_row(s, at.b, at.hk) + col] = l;
   }
-  store_column<DH, EXACT>(y + at.slice * y_slice + qrow, first, s.dh, [&](int t, int i) {
-    return k0 < k1 ? o[t][i] * f : f;
-  });
-  if (half == 0 && first == 0) lse[at.slice * lse_slice + stat_row(s, at.b, at.hk) + col] = l;
 }
 
 // y and lse of a row from its slices': the slices' outputs weighted by exp(lse_s - lse)
@@ -521,189 +584,198 @@ __global__ void join_kernel(const float* __restrict__ part, float* __restrict__ 
   }
 }
 
-// ---------------------------------------------------------------- backward over the states: dq
+// ---------------------------------------------------------------- backward
+// The scale f of a column's values before they are split, which keeps them within 2^15, where a
+// tile with the largest value `top` needs a smaller one; the sums follow.
+__device__ inline bool passes(float top, float f) { return top * f > 0x1p15f; }
+template <int N>
+__device__ inline void rescale(float top, float& f, floatx16 (&acc)[N]) {
+  const float g = passes(top, f) ? exp2_of(max(8 - exponent(top), -126)) : f, up = g / f;
+  f = g;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[t][i] *= up;
+}
+constexpr float kFirst = 0x1p126f;   // f before the first values
+
+// Loads the row tiles of the pass over the queries: rows i .. of the group's heads, numbered g Tq +
+// position.  A tile stays within a head where a head fills one, else it packs the group's heads.
+struct QueryTiles {
+  const float *q, *dy, *lse, *delta;   // lse, delta: of the group's first head
+  int b, hk, i1, T;
+  __device__ bool packed(const Shape& s) const { return s.Tq < T; }
+  __device__ int rows_at(const Shape& s, int i) const {
+    return packed(s) ? min(T, i1 - i) : min(min(T, i1 - i), s.Tq - i % s.Tq);
+  }
+  // nl, dl: of row threadIdx.x, -lse in powers of two and delta; a row that is not there gets a
+  // probability of 0
+  template <bool EXACT, class R>
+  __device__ void load(const Shape& s, int i, R& raw, float& nl, float& dl) const {
+    const int rows = i < i1 ? rows_at(s, i) : 0;
+    if (!packed(s)) {
+      const int64_t r = query_row(s, b, hk, min(i, s.R - 1));
+      raw.template load<EXACT>(q + r, dy + r, s.ldq, rows, s.dh);
+    } else {
+      const int64_t to = (int64_t)b * s.Tq * s.ldq + (int64_t)hk * s.G * s.dh;
+      raw.template load_packed<EXACT>(q + to, dy + to, s, i, rows);
+    }
+    if ((int)threadIdx.x < T) {
+      const bool there = (int)threadIdx.x < rows;
+      nl = there ? -lse[i + threadIdx.x] * kLog2e : -INFINITY;
+      dl = there ? delta[i + threadIdx.x] : 0.f;
+    }
+  }
+};
+
+// Up to 64 head columns a wave holds both matrices of its columns and all its sums: four waves a
+// workgroup, two workgroups a CU.
+
+// Over the states: dq.  Columns are queries.
 template <int DH, bool EXACT>
-__global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dq_kernel(
+__global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dq_kernel(
     const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
     const float* __restrict__ y, const float* __restrict__ lse, const float* __restrict__ dy,
     float* __restrict__ dq, float* __restrict__ delta, Shape s, int tiles, int slice_len,
     int64_t dq_slice) {
   using Wd = Width<DH>;
-  constexpr int T = Wd::kTile;
+  constexpr int T = Wd::kBackTile, W = Wd::kBackWaves;
   using Rw = Rows<DH, T>;
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
-  __shared__ floatx2 tops[kWaves];
+  __shared__ floatx2 tops[W];
   const Place at = place(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-  const int col = at.tile * Wd::kCols + w / Wd::kParts * 32 + (lane & 31);
-  const int first = w % Wd::kParts * Wd::kSums;
-  const bool mine = col < s.R;
+  const int col = (at.tile * W + w) * 32 + (lane & 31), here = min(col, s.R - 1);
   const int n = klen[at.b];
   const bool bad = n < 0 || n > s.Tk;
   const int k0 = bad ? 0 : min(n, at.slice * slice_len), k1 = bad ? 0 : min(n, k0 + slice_len);
 
+  const int64_t qrow = query_row(s, at.b, at.hk, here), st = stat_row(s, at.b, at.hk) + here;
   Pieces qp[Wd::kSteps], gp[Wd::kSteps];
   float qc, gf, dl = 0.f;
-  const int64_t qrow = mine ? query_row(s, at.b, at.hk, col) : 0;
-  const int64_t st = stat_row(s, at.b, at.hk) + col;
   {
     float v[DH / 2], u[DH / 2];
-    load_column<DH, EXACT>(q + qrow, mine, s.dh, v);
+    load_column<DH, EXACT>(q + qrow, s.dh, v);
     qc = split_column<DH>(v, qp) * s.scale * kLog2e;
-    load_column<DH, EXACT>(dy + qrow, mine, s.dh, v);
+    load_column<DH, EXACT>(dy + qrow, s.dh, v);
     gf = split_column<DH>(v, gp);
-    load_column<DH, EXACT>(y + qrow, mine, s.dh, u);
+    load_column<DH, EXACT>(y + qrow, s.dh, u);
 #pragma unroll
     for (int i = 0; i < DH / 2; ++i) dl = fmaf(v[i], u[i], dl);
     dl = sum_of_halves(dl);
   }
-  if (mine && half == 0 && first == 0 && at.slice == 0) delta[st] = dl;
-  const float nl = mine ? -lse[st] * kLog2e : -INFINITY;
-  floatx16 o[Wd::kSums];
+  if (col < s.R && half == 0 && at.slice == 0) delta[st] = dl;
+  const float nl = -lse[st] * kLog2e;
+  floatx16 acc[Wd::kBlocks];
 #pragma unroll
-  for (int t = 0; t < Wd::kSums; ++t) o[t] = floatx16{};
-  float f = 0x1p126f;   // scale of the score gradients: they stay within 2^15
-  Flight<DH, T> next;
+  for (int t = 0; t < Wd::kBlocks; ++t) acc[t] = floatx16{};
+  float f = kFirst;
+  Raw<DH, W, T> raw;
   const auto fetch = [&](int j) {
     const int64_t r = key_row(s, at.b, at.hk, j);
-    next.template load<EXACT>(kv + r, kv + r + (int64_t)s.Hkv * s.dh, s.ldk, s.ldk, min(T, k1 - j), s.dh);
+    raw.template load<EXACT>(kv + r, kv + r + (int64_t)s.Hkv * s.dh, s.ldk, k1 - j, s.dh);
   };
   if (k0 < k1) fetch(k0);
   for (int j0 = k0; j0 < k1; j0 += T) {
-    const int2 e = settle<DH, T>(next, ks, vs, tops, [](int x) { return x; });
+    raw.publish(tops);
+    __syncthreads();
+    const int2 e = raw.exponents(tops);
+    raw.store(ks, vs, e);
+    __syncthreads();
     if (j0 + T < k1) fetch(j0 + T);
+    // (no smaller than the normal numbers: a masked score stays -inf)
     const float kf = exp2_of(e.x - 14), c = fmaxf(qc * kf, 0x1p-126f), cv = gf * exp2_of(e.y - 14);
 #pragma unroll 1
-    for (int r0 = 0; r0 < T; r0 += 32) {
+    for (int r0 = 0; r0 < T && j0 + r0 < k1; r0 += 32) {
       floatx16 a = {}, b = {};
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(ks, r0, t), qp[t], a);
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) b = mma(Rw::by_row(vs, r0, t), gp[t], b);
-      if (r0 + 32 > k1 - j0) mask_rows(a, r0, k1 - j0);
+      if (j0 + r0 + 32 > k1) mask_rows(a, r0, k1 - j0);
       float x[16], top = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         x[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, nl)) * fmaf(b[i], cv, -dl);
         top = fmaxf(top, fabsf(x[i]));
       }
-      // x 2^(e.x - 14) is what meets the pieces of k: the factor f keeps is for that
+      // dS 2^(e.x - 14) is what meets the pieces of k
       top = max_of_halves(top) * kf;
-      if (__any(top * f > 0x1p15f)) {
-        const float g = top * f > 0x1p15f ? exp2_of(max(8 - exponent(top), -126)) : f;
-        const float up = g / f;
-        f = g;
-#pragma unroll
-        for (int t = 0; t < Wd::kSums; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[t][i] *= up;
-      }
+      if (__any(passes(top, f))) rescale(top, f, acc);
       const Pieces xp[2] = {split8(x, f * kf), split8(x + 8, f * kf)};
 #pragma unroll
-      for (int t = 0; t < Wd::kSums; ++t)
+      for (int t = 0; t < Wd::kBlocks; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) o[t] = mma(Rw::by_column(ks, r0 + 16 * h, first + t), xp[h], o[t]);
+        for (int h = 0; h < 2; ++h) acc[t] = mma(Rw::by_column(ks, r0 + 16 * h, t), xp[h], acc[t]);
     }
   }
-  if (!mine) return;
+  if (col >= s.R) return;
   const float out = s.scale / f;
-  store_column<DH, EXACT>(dq + at.slice * dq_slice + qrow, first, s.dh, [&](int t, int i) {
-    return bad ? NAN : o[t][i] * out;
+  store_column<Wd::kBlocks, EXACT>(dq + at.slice * dq_slice + qrow, 0, s.dh, [&](int t, int i) {
+    return bad ? NAN : acc[t][i] * out;
   });
 }
 
-// ---------------------------------------------------------------- backward over the queries: dk, dv
+// Over the queries: dk and dv.  Columns are states.
 template <int DH, bool EXACT>
-__global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dkv_kernel(
+__global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
     const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
     const float* __restrict__ lse, const float* __restrict__ dy, const float* __restrict__ delta,
     float* __restrict__ dkv, Shape s, int tiles, int slice_len, int64_t dkv_slice) {
   using Wd = Width<DH>;
-  constexpr int T = Wd::kTile;
+  constexpr int T = Wd::kBackTile, W = Wd::kBackWaves;
   using Rw = Rows<DH, T>;
   __shared__ __attribute__((aligned(16))) char qs[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char gs[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) float nl[T], dl[T];
-  __shared__ floatx2 tops[kWaves];
+  __shared__ floatx2 tops[W];
   const Place at = place(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-  const int j = at.tile * Wd::kCols + w / Wd::kParts * 32 + (lane & 31);
-  const int first = w % Wd::kParts * Wd::kSums;
+  const int j = (at.tile * W + w) * 32 + (lane & 31);
   const int n = klen[at.b];
-  const bool bad = n < 0 || n > s.Tk, mine = j < s.Tk, live = mine && j < n && !bad;
+  const bool bad = n < 0 || n > s.Tk;
   // rows of this slice; a workgroup without states has nothing to add
-  const bool any = !bad && at.tile * Wd::kCols < n;
+  const bool any = !bad && at.tile * W * 32 < n;
   const int i0 = any ? min(s.R, at.slice * slice_len) : 0, i1 = any ? min(s.R, i0 + slice_len) : 0;
 
-  const int64_t krow = mine ? key_row(s, at.b, at.hk, j) : 0, to_v = (int64_t)s.Hkv * s.dh;
+  const int64_t krow = key_row(s, at.b, at.hk, min(j, s.Tk - 1)), to_v = (int64_t)s.Hkv * s.dh;
   Pieces kp[Wd::kSteps], vp[Wd::kSteps];
   float kc, vf;
   {
     float v[DH / 2];
-    load_column<DH, EXACT>(kv + krow, live, s.dh, v);
+    load_column<DH, EXACT>(kv + krow, s.dh, v);
     kc = split_column<DH>(v, kp) * s.scale * kLog2e;
-    load_column<DH, EXACT>(kv + krow + to_v, live, s.dh, v);
+    load_column<DH, EXACT>(kv + krow + to_v, s.dh, v);
     vf = split_column<DH>(v, vp);
   }
-  floatx16 dk[Wd::kSums], dv[Wd::kSums];
+  floatx16 dk[Wd::kBlocks], dv[Wd::kBlocks];
 #pragma unroll
-  for (int t = 0; t < Wd::kSums; ++t) dk[t] = dv[t] = floatx16{};
-  float fk = 0x1p126f, fv = 0x1p126f;
+  for (int t = 0; t < Wd::kBlocks; ++t) dk[t] = dv[t] = floatx16{};
+  float fk = kFirst, fv = kFirst;
   const int64_t st = stat_row(s, at.b, at.hk);
-  Flight<DH, T> next;
+  const QueryTiles rows{q, dy, lse + st, delta + st, at.b, at.hk, i1, T};
+  Raw<DH, W, T> raw;
   float ll = 0.f, dd = 0.f;
-  // tiles of rows stay within a head where a head fills one, else they pack the group's heads
-  const bool packed = s.Tq < T;
-  const auto fetch = [&](int i) {
-    if (!packed) {
-      const int64_t r = query_row(s, at.b, at.hk, i);
-      const int rows = min(min(T, i1 - i), s.Tq - i % s.Tq);
-      next.template load<EXACT>(q + r, dy + r, s.ldq, s.ldq, rows, s.dh);
-      if ((int)threadIdx.x < T) {
-        const bool there = (int)threadIdx.x < rows;
-        ll = there ? -lse[st + i + threadIdx.x] * kLog2e : -INFINITY;
-        dd = there ? delta[st + i + threadIdx.x] : 0.f;
-      }
-    } else {
-      const int rows = min(T, i1 - i), c = next.chunk();
-      const int64_t first = (int64_t)at.b * s.Tq * s.ldq + (int64_t)at.hk * s.G * s.dh;
-      const int64_t values = (int64_t)(s.Tq - 1) * s.ldq + (int64_t)s.G * s.dh;
-      const auto rq = buffer(q + first, values), rg = buffer(dy + first, values);
-#pragma unroll
-      for (int u = 0; u < Flight<DH, T>::kUnits; ++u) {
-        const bool second = u >= Flight<DH, T>::kUnits / 2;
-        const int r = next.row(u) - (second ? T : 0), g = (i + r) / s.Tq, k = i + r - g * s.Tq;
-        uint32_t o = (uint32_t)(k * s.ldq + (int64_t)g * s.dh + 8 * c) * 4u;
-        if (r >= rows || 8 * c >= s.dh) o = kNone;
-        load8(second ? rg : rq, o, next.v[u]);
-        trim<EXACT>(next.v[u], 8 * c, s.dh);
-      }
-      if ((int)threadIdx.x < T) {
-        const bool there = (int)threadIdx.x < rows;
-        ll = there ? -lse[st + i + threadIdx.x] * kLog2e : -INFINITY;
-        dd = there ? delta[st + i + threadIdx.x] : 0.f;
-      }
-    }
-  };
-  const auto step = [&](int i) { return packed ? i + T : min(i + T, i - i % s.Tq + s.Tq); };
-  if (i0 < i1) fetch(i0);
+  if (i0 < i1) rows.load<EXACT>(s, i0, raw, ll, dd);
   for (int i = i0; i < i1;) {
-    const float l0 = ll, d0 = dd;
-    const int2 e = settle<DH, T>(next, qs, gs, tops, [&](int x) {
-      if ((int)threadIdx.x < T) {   // between the barriers, as the tiles themselves
-        nl[threadIdx.x] = l0;
-        dl[threadIdx.x] = d0;
-      }
-      return x;
-    });
-    i = step(i);
-    if (i < i1) fetch(i);
+    raw.publish(tops);
+    __syncthreads();
+    const int2 e = raw.exponents(tops);
+    raw.store(qs, gs, e);
+    if ((int)threadIdx.x < T) {
+      nl[threadIdx.x] = ll;
+      dl[threadIdx.x] = dd;
+    }
+    __syncthreads();
+    const int there = rows.rows_at(s, i);
+    i += there;
+    if (i < i1) rows.load<EXACT>(s, i, raw, ll, dd);
     const float qf = exp2_of(e.x - 14), gf = exp2_of(e.y - 14), c = kc * qf, cv = vf * gf;
 #pragma unroll 1
-    for (int r0 = 0; r0 < T; r0 += 32) {
+    for (int r0 = 0; r0 < there; r0 += 32) {
       floatx16 a = {}, b = {};
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(qs, r0, t), kp[t], a);
@@ -724,43 +796,298 @@ __global__ __launch_bounds__(TPB, DH <= 64 ? 2 : 1) void dkv_kernel(
       }
       ptop = max_of_halves(ptop) * gf;
       xtop = max_of_halves(xtop) * qf;
-      if (__any(ptop * fv > 0x1p15f || xtop * fk > 0x1p15f)) {
-        const float gv = ptop * fv > 0x1p15f ? exp2_of(max(8 - exponent(ptop), -126)) : fv;
-        const float gk = xtop * fk > 0x1p15f ? exp2_of(max(8 - exponent(xtop), -126)) : fk;
-        const float uv = gv / fv, uk = gk / fk;
-        fv = gv;
-        fk = gk;
-#pragma unroll
-        for (int t = 0; t < Wd::kSums; ++t)
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            dv[t][k] *= uv;
-            dk[t][k] *= uk;
-          }
+      if (__any(passes(ptop, fv) || passes(xtop, fk))) {
+        rescale(ptop, fv, dv);
+        rescale(xtop, fk, dk);
       }
       {
         const Pieces pp[2] = {split8(p, fv * gf), split8(p + 8, fv * gf)};
 #pragma unroll
-        for (int t = 0; t < Wd::kSums; ++t)
+        for (int t = 0; t < Wd::kBlocks; ++t)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) dv[t] = mma(Rw::by_column(gs, r0 + 16 * h, first + t), pp[h], dv[t]);
+          for (int h = 0; h < 2; ++h) dv[t] = mma(Rw::by_column(gs, r0 + 16 * h, t), pp[h], dv[t]);
       }
       const Pieces xp[2] = {split8(x, fk * qf), split8(x + 8, fk * qf)};
 #pragma unroll
-      for (int t = 0; t < Wd::kSums; ++t)
+      for (int t = 0; t < Wd::kBlocks; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) dk[t] = mma(Rw::by_column(qs, r0 + 16 * h, first + t), xp[h], dk[t]);
+        for (int h = 0; h < 2; ++h) dk[t] = mma(Rw::by_column(qs, r0 + 16 * h, t), xp[h], dk[t]);
     }
   }
-  if (!mine) return;
+  if (j >= s.Tk) return;
   const float ok = s.scale / fk, ov = 1.f / fv;
+  const bool live = j < n;
   float* out = dkv + at.slice * dkv_slice + krow;
-  store_column<DH, EXACT>(out, first, s.dh, [&](int t, int e) {
-    return bad ? NAN : live ? dk[t][e] * ok : 0.f;
+  store_column<Wd::kBlocks, EXACT>(out, 0, s.dh, [&](int t, int k) {
+    return bad ? NAN : live ? dk[t][k] * ok : 0.f;
   });
-  store_column<DH, EXACT>(out + to_v, first, s.dh, [&](int t, int e) {
-    return bad ? NAN : live ? dv[t][e] * ov : 0.f;
+  store_column<Wd::kBlocks, EXACT>(out + to_v, 0, s.dh, [&](int t, int k) {
+    return bad ? NAN : live ? dv[t][k] * ov : 0.f;
   });
+}
+
+// Above 64 head columns both matrices and all sums of a column set take more than the 256 registers
+// of a lane with which a SIMD holds two waves.  A pair of waves shares 32 columns instead: role 0
+// holds a first matrix and forms the scores and probabilities, role 1 a second and forms dP; they
+// exchange values through LDS, and each then multiplies on.  The waves of a pair sit on one SIMD:
+// while one computes exponentials or splits the next tiles, the other multiplies.  2 x 4096 x 4096,
+// 16 heads of 128: dk and dv 3.24 -> 1.65 ms, dq 1.56 -> 1.34.  At 64 columns, where one wave's
+// registers suffice, pairs are slower (24 x 512 x 512: 0.22 against 0.20 ms and 0.19 against 0.15).
+
+// Over the states: dq.  Columns are queries; role 0 holds q, role 1 dy; each multiplies half of the
+// rows of dS and k.
+template <int DH, bool EXACT>
+__global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) void dq_pair_kernel(
+    const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
+    const float* __restrict__ y, const float* __restrict__ lse, const float* __restrict__ dy,
+    float* __restrict__ dq, float* __restrict__ delta, Shape s, int tiles, int slice_len,
+    int64_t dq_slice) {
+  using Wd = Width<DH>;
+  constexpr int T = 32, W = Wd::kPairWaves, kPairs = W / 2, NB = Wd::kBuffers;
+  using Rw = Rows<DH, T>;
+  __shared__ __attribute__((aligned(16))) char mats[NB][2][Rw::kBytes];   // tiles of k and v
+  __shared__ float4 meet[kPairs][2][2][64];
+  __shared__ floatx2 tops[W];
+  const Place at = place(s, tiles);
+  if (at.none) return;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
+  const int col = (at.tile * kPairs + pair) * 32 + (lane & 31), here = min(col, s.R - 1);
+  const int n = klen[at.b];
+  const bool bad = n < 0 || n > s.Tk;
+  const int k0 = bad ? 0 : min(n, at.slice * slice_len), k1 = bad ? 0 : min(n, k0 + slice_len);
+
+  const int64_t qrow = query_row(s, at.b, at.hk, here), st = stat_row(s, at.b, at.hk) + here;
+  Pieces own[Wd::kSteps];   // q, or dy
+  float cf, row = 0.f;      // row: -lse in powers of two, or -delta
+  {
+    float v[DH / 2];
+    load_column<DH, EXACT>((role ? dy : q) + qrow, s.dh, v);
+    cf = split_column<DH>(v, own);
+    if (role) {
+      float u[DH / 2];
+      load_column<DH, EXACT>(y + qrow, s.dh, u);
+#pragma unroll
+      for (int i = 0; i < DH / 2; ++i) row = fmaf(v[i], u[i], row);
+      row = -sum_of_halves(row);
+      if (col < s.R && half == 0 && at.slice == 0) delta[st] = -row;
+    } else {
+      cf *= s.scale * kLog2e;
+      row = -lse[st] * kLog2e;
+    }
+  }
+  floatx16 acc[Wd::kBlocks];
+#pragma unroll
+  for (int t = 0; t < Wd::kBlocks; ++t) acc[t] = floatx16{};
+  float f = kFirst;
+  Raw<DH, W, T> raw;
+  const auto fetch = [&](int j) {
+    const int64_t r = key_row(s, at.b, at.hk, min(j, s.Tk - 1));
+    raw.template load<EXACT>(kv + r, kv + r + (int64_t)s.Hkv * s.dh, s.ldk, k1 - j, s.dh);
+  };
+  const auto stage = [&](int buf) -> int2 {
+    const int2 e = raw.exponents(tops);
+    raw.store(mats[buf][0], mats[buf][1], e);
+    return e;
+  };
+  if (k0 < k1) {
+    fetch(k0);
+    raw.publish(tops);
+    __syncthreads();
+    int2 e = stage(0);
+    int buf = 0;
+    fetch(k0 + T);
+    __syncthreads();
+    for (int j0 = k0;; j0 += T) {
+      const bool more = j0 + T < k1;
+      floatx16 a = {};
+      const char* z = mats[buf][role];
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(z, 0, t), own[t], a);
+      float c = cf * exp2_of((role ? e.y : e.x) - 14);
+      if (!role) {
+        c = fmaxf(c, 0x1p-126f);   // a masked score stays -inf
+        if (j0 + T > k1) mask_rows(a, 0, k1 - j0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, row));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a[i] = fmaf(a[i], c, row);
+      }
+      // the half of the rows that the other wave multiplies
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int i = 4 * g;
+        meet[pair][role][g][lane] = role ? make_float4(a[i], a[i + 1], a[i + 2], a[i + 3])
+                                         : make_float4(a[i + 8], a[i + 9], a[i + 10], a[i + 11]);
+      }
+      raw.publish(tops);
+      __syncthreads();
+      // dS 2^(e.x - 14) is what meets the pieces of k
+      const float kf = exp2_of(e.x - 14);
+      float p[8], top = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float4 o = meet[pair][1 - role][g][lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[4 * g + i] = pick(o, i) * (role ? a[8 + 4 * g + i] : a[4 * g + i]);
+          top = fmaxf(top, fabsf(p[4 * g + i]));
+        }
+      }
+      top = max_of_halves(top) * kf;
+      if (__any(passes(top, f))) rescale(top, f, acc);
+      const Pieces pp = split8(p, f * kf);
+      const auto advance = [&] {
+        e = stage(NB - 1 - buf);
+        fetch(j0 + 2 * T);
+      };
+      if (NB == 2 && role && more) advance();
+#pragma unroll
+      for (int t = 0; t < Wd::kBlocks; ++t) acc[t] = mma(Rw::by_column(mats[buf][0], 16 * role, t), pp, acc[t]);
+      if (!more) break;
+      if (NB == 1) __syncthreads();
+      if (NB == 1 || !role) advance();
+      buf = NB - 1 - buf;
+      __syncthreads();
+    }
+  }
+  // the pair's halves together, through the tiles' memory
+  float* join = reinterpret_cast<float*>(&mats[0][0][0]) + pair * (Wd::kBlocks * 16 * 64);
+  static_assert(kPairs * Wd::kBlocks * 16 * 64 * 4 <= (int)sizeof(mats), "room to join");
+  const float out = s.scale / f;
+  __syncthreads();
+  if (role)
+#pragma unroll
+    for (int t = 0; t < Wd::kBlocks; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) join[(t * 16 + i) * 64 + lane] = acc[t][i] * out;
+  __syncthreads();
+  if (role || col >= s.R) return;
+  store_column<Wd::kBlocks, EXACT>(dq + at.slice * dq_slice + qrow, 0, s.dh, [&](int t, int i) {
+    return bad ? NAN : fmaf(acc[t][i], out, join[(t * 16 + i) * 64 + lane]);
+  });
+}
+
+// Over the queries: dk and dv.  Columns are states; role 0 holds k and sums dv, role 1 holds v and
+// sums dk.
+template <int DH, bool EXACT>
+__global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) void dkv_pair_kernel(
+    const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
+    const float* __restrict__ lse, const float* __restrict__ dy, const float* __restrict__ delta,
+    float* __restrict__ dkv, Shape s, int tiles, int slice_len, int64_t dkv_slice) {
+  using Wd = Width<DH>;
+  constexpr int T = 32, W = Wd::kPairWaves, kPairs = W / 2, NB = Wd::kBuffers;
+  using Rw = Rows<DH, T>;
+  __shared__ __attribute__((aligned(16))) char mats[NB][2][Rw::kBytes];   // tiles of q and dy
+  __shared__ __attribute__((aligned(16))) float nl[NB][T], dl[NB][T];
+  __shared__ float4 meet[kPairs][4][64];
+  __shared__ floatx2 tops[W];
+  const Place at = place(s, tiles);
+  if (at.none) return;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
+  const int j = (at.tile * kPairs + pair) * 32 + (lane & 31);
+  const int n = klen[at.b];
+  const bool bad = n < 0 || n > s.Tk;
+  // rows of this slice; a workgroup without states has nothing to add
+  const bool any = !bad && at.tile * kPairs * 32 < n;
+  const int i0 = any ? min(s.R, at.slice * slice_len) : 0, i1 = any ? min(s.R, i0 + slice_len) : 0;
+
+  const int64_t krow = key_row(s, at.b, at.hk, min(j, s.Tk - 1)), to_v = (int64_t)s.Hkv * s.dh;
+  Pieces own[Wd::kSteps];   // k, or v
+  float cf;
+  {
+    float v[DH / 2];
+    load_column<DH, EXACT>(kv + krow + (role ? to_v : 0), s.dh, v);
+    cf = split_column<DH>(v, own);
+    if (!role) cf *= s.scale * kLog2e;
+  }
+  floatx16 acc[Wd::kBlocks];   // dv, or dk
+#pragma unroll
+  for (int t = 0; t < Wd::kBlocks; ++t) acc[t] = floatx16{};
+  float f = kFirst;
+  const int64_t st = stat_row(s, at.b, at.hk);
+  const QueryTiles rows{q, dy, lse + st, delta + st, at.b, at.hk, i1, T};
+  Raw<DH, W, T> raw;
+  float ll = 0.f, dd = 0.f;
+  const auto stage = [&](int buf) -> int2 {
+    const int2 e = raw.exponents(tops);
+    raw.store(mats[buf][0], mats[buf][1], e);
+    if ((int)threadIdx.x < T) {
+      nl[buf][threadIdx.x] = ll;
+      dl[buf][threadIdx.x] = dd;
+    }
+    return e;
+  };
+  if (i0 < i1) {
+    rows.load<EXACT>(s, i0, raw, ll, dd);
+    raw.publish(tops);
+    __syncthreads();
+    int2 e = stage(0);
+    int i = i0 + rows.rows_at(s, i0), buf = 0;
+    rows.load<EXACT>(s, i, raw, ll, dd);
+    __syncthreads();
+    while (true) {
+      const bool more = i < i1;
+      floatx16 a = {};
+      const char* z = mats[buf][role];
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(z, 0, t), own[t], a);
+      const float c = cf * exp2_of((role ? e.y : e.x) - 14);
+      float v[16], top = 0.f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 r4 = at4(role ? dl[buf] : nl[buf], 8 * g + 4 * half);
+        if (!role) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            v[4 * g + k] = __builtin_amdgcn_exp2f(fmaf(a[4 * g + k], c, pick(r4, k)));
+          meet[pair][g][lane] = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[4 * g + k] = fmaf(a[4 * g + k], c, -pick(r4, k));
+        }
+      }
+      raw.publish(tops);
+      __syncthreads();
+      if (role)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 p4 = meet[pair][g][lane];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[4 * g + k] *= pick(p4, k);
+        }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) top = fmaxf(top, fabsf(v[k]));
+      // the values meet dy's pieces, or q's: times the scale of those
+      const float other = exp2_of((role ? e.x : e.y) - 14);
+      top = max_of_halves(top) * other;
+      if (__any(passes(top, f))) rescale(top, f, acc);
+      const Pieces pp[2] = {split8(v, f * other), split8(v + 8, f * other)};
+      const auto advance = [&] {
+        e = stage(NB - 1 - buf);
+        i += rows.rows_at(s, i);
+        rows.load<EXACT>(s, i, raw, ll, dd);
+      };
+      if (NB == 2 && role && more) advance();
+#pragma unroll
+      for (int t = 0; t < Wd::kBlocks; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) acc[t] = mma(Rw::by_column(mats[buf][1 - role], 16 * h, t), pp[h], acc[t]);
+      if (!more) break;
+      if (NB == 1) __syncthreads();
+      if (NB == 1 || !role) advance();
+      buf = NB - 1 - buf;
+      __syncthreads();
+    }
+  }
+  if (j >= s.Tk) return;
+  const float out = (role ? s.scale : 1.f) / f;   // dk goes where k is, dv where v is
+  const bool live = j < n;
+  store_column<Wd::kBlocks, EXACT>(
+      dkv + at.slice * dkv_slice + krow + (role ? 0 : to_v), 0, s.dh,
+      [&](int t, int k) { return bad ? NAN : live ? acc[t][k] * out : 0.f; });
 }
 
 // out = the slices' partial sums added in order
@@ -787,8 +1114,14 @@ Shape shape_of(const AttendShape& a) {
   return s;
 }
 
-int tile_rows(int64_t dh) { return dh <= 64 ? 64 : 32; }
-int columns(int64_t dh) { return dh <= 128 ? 32 * kWaves : 16 * kWaves; }
+int tile_rows(int64_t dh) { return dh <= 64 ? Width<64>::kTile : 32; }
+int fwd_columns(int64_t dh) {
+  return dh <= 64 ? Width<64>::kFwdCols : dh <= 128 ? Width<128>::kFwdCols : Width<256>::kFwdCols;
+}
+int back_columns(int64_t dh) {
+  return dh <= 64 ? Width<64>::kBackCols : dh <= 128 ? Width<128>::kBackCols : Width<256>::kBackCols;
+}
+int back_rows(int64_t dh) { return dh <= 64 ? Width<64>::kBackRows : Width<128>::kBackRows; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 dim3 grid_of(const Shape& s, int tiles, int64_t slices) {
   return dim3((unsigned)(ceil_div((int64_t)s.B * s.Hkv, kXcds) * kXcds * tiles), (unsigned)slices);
@@ -806,42 +1139,48 @@ int64_t slices_for(int64_t groups, int64_t tiles) {
                                                   kMaxAttentionSlices}));
 }
 
-#define WIDTHS(CALL)                                            \
-  if (s.dh == 32) CALL(32, true);                               \
-  else if (s.dh < 32) CALL(32, false);                          \
-  else if (s.dh == 64) CALL(64, true);                          \
-  else if (s.dh < 64) CALL(64, false);                          \
-  else if (s.dh == 96) CALL(96, true);                          \
-  else if (s.dh < 96) CALL(96, false);                          \
-  else if (s.dh == 128) CALL(128, true);                        \
-  else if (s.dh < 128) CALL(128, false);                        \
-  else if (s.dh == 256) CALL(256, true);                        \
+#define UP_TO_64(CALL)                     \
+  if (s.dh == 32) CALL(32, true);          \
+  else if (s.dh < 32) CALL(32, false);     \
+  else if (s.dh == 64) CALL(64, true);     \
+  else CALL(64, false)
+#define ABOVE_64(CALL)                     \
+  if (s.dh == 96) CALL(96, true);          \
+  else if (s.dh < 96) CALL(96, false);     \
+  else if (s.dh == 128) CALL(128, true);   \
+  else if (s.dh < 128) CALL(128, false);   \
+  else if (s.dh == 256) CALL(256, true);   \
   else CALL(256, false)
+#define LAUNCH(KERNEL, WAVES, TILES, SLICES, ...) \
+  hipLaunchKernelGGL(KERNEL, grid_of(s, TILES, SLICES), dim3(64 * WAVES), 0, st, __VA_ARGS__)
 
 }  // namespace
 
-int64_t attention_key_slices(const AttendShape& a, bool) {
-  return slices_for(a.B * a.Hkv * ceil_div(a.Tq * (a.H / a.Hkv), columns(a.dh)),
-                    ceil_div(a.Tk, tile_rows(a.dh)));
+int64_t attention_key_slices(const AttendShape& a, bool fwd) {
+  const int64_t tiles = ceil_div(a.Tq * (a.H / a.Hkv), fwd ? fwd_columns(a.dh) : back_columns(a.dh));
+  return slices_for(a.B * a.Hkv * tiles, ceil_div(a.Tk, fwd ? tile_rows(a.dh) : back_rows(a.dh)));
 }
 int64_t attention_query_slices(const AttendShape& a) {
-  return slices_for(a.B * a.Hkv * ceil_div(a.Tk, columns(a.dh)),
-                    ceil_div(a.Tq * (a.H / a.Hkv), tile_rows(a.dh)));
+  return slices_for(a.B * a.Hkv * ceil_div(a.Tk, back_columns(a.dh)), ceil_div(a.Tq * (a.H / a.Hkv), back_rows(a.dh)));
 }
 
 hipError_t cross_attention_fwd(const float* q, const float* kv, const int32_t* klen, float* y,
                                float* lse, float* part, const AttendShape& a, int64_t slices,
                                hipStream_t st) {
   const Shape s = shape_of(a);
-  const int tiles = (int)ceil_div(s.R, columns(s.dh));
+  const int tiles = (int)ceil_div(s.R, fwd_columns(s.dh));
   const int len = (int)slice_of(s.Tk, slices, tile_rows(s.dh));
   const int64_t size = a.B * a.Tq * s.ldq, rows = a.B * a.H * a.Tq;
   float* yo = slices > 1 ? part : y;
   float* lo = slices > 1 ? part + slices * size : lse;
-#define FWD(D, X)                                                                                 \
-  hipLaunchKernelGGL((fwd_kernel<D, X>), grid_of(s, tiles, slices), dim3(TPB), 0, st, q, kv, klen, \
-                     yo, lo, s, tiles, len, size, rows)
-  WIDTHS(FWD);
+#define FWD(D, X)                                                                              \
+  LAUNCH((fwd_kernel<D, X>), Width<D>::kFwdWaves, tiles, slices, q, kv, klen, yo, lo, s, tiles, len, \
+         size, rows)
+  if (s.dh <= 64) {
+    UP_TO_64(FWD);
+  } else {
+    ABOVE_64(FWD);
+  }
 #undef FWD
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || slices == 1) return e;
@@ -857,14 +1196,20 @@ hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* k
   const Shape s = shape_of(a);
   const int64_t q_size = a.B * a.Tq * s.ldq, kv_size = a.B * a.Tk * s.ldk;
   {
-    const int tiles = (int)ceil_div(s.R, columns(s.dh));
-    const int len = (int)slice_of(s.Tk, q_slices, tile_rows(s.dh));
+    const int tiles = (int)ceil_div(s.R, back_columns(s.dh));
+    const int len = (int)slice_of(s.Tk, q_slices, back_rows(s.dh));
     float* out = q_slices > 1 ? part : dq;
-#define DQ(D, X)                                                                                   \
-  hipLaunchKernelGGL((dq_kernel<D, X>), grid_of(s, tiles, q_slices), dim3(TPB), 0, st, q, kv, klen, \
-                     y, lse, dy, out, delta, s, tiles, len, q_size)
-    WIDTHS(DQ);
+#define ARGS q, kv, klen, y, lse, dy, out, delta, s, tiles, len, q_size
+#define DQ(D, X) LAUNCH((dq_kernel<D, X>), Width<D>::kBackWaves, tiles, q_slices, ARGS)
+#define DQ_PAIR(D, X) LAUNCH((dq_pair_kernel<D, X>), Width<D>::kPairWaves, tiles, q_slices, ARGS)
+    if (s.dh <= 64) {
+      UP_TO_64(DQ);
+    } else {
+      ABOVE_64(DQ_PAIR);
+    }
+#undef DQ_PAIR
 #undef DQ
+#undef ARGS
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (q_slices > 1) {
@@ -873,14 +1218,20 @@ hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* k
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
-  const int tiles = (int)ceil_div(s.Tk, columns(s.dh));
-  const int len = (int)slice_of(s.R, kv_slices, tile_rows(s.dh));
+  const int tiles = (int)ceil_div(s.Tk, back_columns(s.dh));
+  const int len = (int)slice_of(s.R, kv_slices, back_rows(s.dh));
   float* out = kv_slices > 1 ? part : dkv;
-#define DKV(D, X)                                                                                    \
-  hipLaunchKernelGGL((dkv_kernel<D, X>), grid_of(s, tiles, kv_slices), dim3(TPB), 0, st, q, kv, klen, \
-                     lse, dy, delta, out, s, tiles, len, kv_size)
-  WIDTHS(DKV);
+#define ARGS q, kv, klen, lse, dy, delta, out, s, tiles, len, kv_size
+#define DKV(D, X) LAUNCH((dkv_kernel<D, X>), Width<D>::kBackWaves, tiles, kv_slices, ARGS)
+#define DKV_PAIR(D, X) LAUNCH((dkv_pair_kernel<D, X>), Width<D>::kPairWaves, tiles, kv_slices, ARGS)
+  if (s.dh <= 64) {
+    UP_TO_64(DKV);
+  } else {
+    ABOVE_64(DKV_PAIR);
+  }
+#undef DKV_PAIR
 #undef DKV
+#undef ARGS
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || kv_slices == 1) return e;
   hipLaunchKernelGGL(sum_kernel, dim3(flat_grid(kv_size)), dim3(256), 0, st, part, dkv,
