@@ -4,13 +4,15 @@
 // columns by the angle pos table[i] of their row; the norm divides a head by its root mean square
 // and scales it by a gain, before the rotation.
 //
-// All of this is bound by the rows' traffic.  An angle belongs to a row and a pair, not to a head:
-// a workgroup takes a tile of rows, computes the tile's cosines and sines once into LDS and uses
-// them for every head.
+// All of this is bound by the rows' traffic (8 bytes a value forward, 12 backward).  An angle
+// belongs to a row and a pair, not to a head: a workgroup takes a tile of rows, computes the tile's
+// cosines and sines once into LDS and uses them for every head.  Rows whose heads, rotated width and
+// length come in fours go in 16-byte loads (V = 4), others value by value (V = 1).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 
+#include "fastdiv.h"
 #include "kernels.h"
 
 namespace ooc {
@@ -21,8 +23,8 @@ constexpr int TPB = 256;
 
 // m cos a and m sin a of a = pos f.  Positions far out need the angle in 64 bits: at a million
 // positions an fp32 angle is off by 0.06.  The product is rounded to a double as in the definition,
-// a multiple of pi / 2 (in two doubles) taken off exactly, and the rest, within +-pi/4, goes through
-// the Taylor series in fp32: the first term left out is below 2e-9.
+// a multiple of pi / 2 (in two doubles) taken off, and the rest, within +-pi/4, goes through the
+// Taylor series in fp32: the first term left out is below 2e-9.
 __device__ inline float2 turn(int32_t pos, double f, float m) {
   const double a = (double)pos * f;
   const double n = rint(a * 0.63661977236758134308);
@@ -36,227 +38,419 @@ __device__ inline float2 turn(int32_t pos, double f, float m) {
   return make_float2(m * (q == 1 || q == 2 ? -cs : cs), m * (q >= 2 ? -sn : sn));
 }
 
-// Rows a workgroup takes at once.
-constexpr int kMaxTile = 8;
+// What a launch knows of its rows.
+struct Rows {
+  int64_t rows;
+  int cols, dh, heads, used, half, layout;   // used = heads dh, half = rot / 2
+  int h1;                                    // heads of the first gain
+  int tile;                                  // rows a workgroup takes at once
+  FastDiv by_half, by_dh, by_heads, by_items;
+  int items;                                 // of a row: V columns each
+};
 
 // The pairs' (m cos, m sin) of rows r0 .. r0 + n into cs [n][half].
-__device__ inline void turns(float2* cs, const int32_t* pos, const double* table, int64_t r0, int n,
-                             int half) {
-  const float m = (float)table[half];
-  for (int t = threadIdx.x; t < n * half; t += TPB) cs[t] = turn(pos[r0 + t / half], table[t % half], m);
+__device__ inline void turns(float2* cs, const int32_t* __restrict__ pos,
+                             const double* __restrict__ table, int64_t r0, int n, const Rows& r) {
+  const float m = (float)table[r.half];
+  for (int t = threadIdx.x; t < n * r.half; t += TPB) {
+    const int row = r.by_half.div(t);
+    cs[t] = turn(pos[r0 + row], table[t - row * r.half], m);
+  }
 }
 
-// What column d of a head becomes: own x[d] + sign x[partner].
-struct Pair {
-  int partner, i;
-  float sign;
+// V neighbouring values.
+template <int V>
+struct Val {
+  float v[V];
 };
-__device__ inline Pair pair_of(int d, int half, int layout, bool back) {
-  const bool second = layout == 0 ? d & 1 : d >= half;
-  Pair p;
-  p.partner = layout == 0 ? d ^ 1 : second ? d - half : d + half;
-  p.i = layout == 0 ? d >> 1 : second ? d - half : d;
-  p.sign = second != back ? 1.f : -1.f;
-  return p;
+template <int V>
+__device__ inline Val<V> load(const float* p) {
+  Val<V> x;
+  if constexpr (V == 4) {
+    const float4 t = *reinterpret_cast<const float4*>(p);
+    x.v[0] = t.x; x.v[1] = t.y; x.v[2] = t.z; x.v[3] = t.w;
+  } else {
+    x.v[0] = *p;
+  }
+  return x;
+}
+template <int V>
+__device__ inline void store(float* p, const Val<V>& x) {
+  if constexpr (V == 4) *reinterpret_cast<float4*>(p) = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
+  else *p = x.v[0];
 }
 
+// Where the other ends of the pairs of columns d .. d + V - 1 lie (the same V columns where pairs
+// are neighbours and V = 4), and those pairs' turns.
+template <int V>
+__device__ inline int partner(int d, int half, int layout) {
+  if (layout) return d < half ? d + half : d - half;
+  return V == 4 ? d : d ^ 1;
+}
+// The columns d .. turned: own their values, other their partners', cs the row's turns.
+template <int V>
+__device__ inline Val<V> turned(const Val<V>& own, const Val<V>& other, int d, const float2* cs,
+                                int half, int layout, bool back) {
+  Val<V> y;
+  const float to = back ? -1.f : 1.f;
+  if (V == 4 && layout == 0) {
+    const float4 t = *reinterpret_cast<const float4*>(cs + d / 2);   // two pairs
+    const float s0 = to * t.y, s1 = to * t.w;
+    y.v[0] = own.v[0] * t.x - own.v[1 % V] * s0;
+    y.v[1 % V] = own.v[1 % V] * t.x + own.v[0] * s0;
+    y.v[2 % V] = own.v[2 % V] * t.z - own.v[3 % V] * s1;
+    y.v[3 % V] = own.v[3 % V] * t.z + own.v[2 % V] * s1;
+    return y;
+  }
+  const bool second = layout ? d >= half : d & 1;
+  const int i = layout ? (second ? d - half : d) : d >> 1;
+  const float sign = second ? to : -to;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float2 t = cs[i + e];
+    y.v[e] = own.v[e] * t.x + sign * (other.v[e] * t.y);
+  }
+  return y;
+}
+
+// ---------------------------------------------------------------- rotation
+// A thread has kFlight items' loads in flight.
+constexpr int kFlight = 4;
+
+template <int V>
 __global__ __launch_bounds__(TPB) void rope_kernel(const float* __restrict__ x,
                                                    const int32_t* __restrict__ pos,
                                                    const double* __restrict__ table,
-                                                   float* __restrict__ y, RopeShape r, int tile,
-                                                   bool back) {
-  extern __shared__ float2 cs[];
-  const int64_t r0 = (int64_t)blockIdx.x * tile;
-  const int n = (int)min((int64_t)tile, r.rows - r0), half = (int)r.rot / 2;
-  turns(cs, pos, table, r0, n, half);
+                                                   float* __restrict__ y, Rows r, bool back) {
+  extern __shared__ float4 lds[];
+  float2* cs = reinterpret_cast<float2*>(lds);
+  const int64_t r0 = (int64_t)blockIdx.x * r.tile;
+  const int n = (int)min((int64_t)r.tile, r.rows - r0);
+  turns(cs, pos, table, r0, n, r);
   __syncthreads();
-  const int cols = (int)r.cols, dh = (int)r.dh, used = (int)(r.heads * r.dh);
-  for (int row = 0; row < n; ++row) {
-    const float* xr = x + (r0 + row) * r.cols;
-    float* yr = y + (r0 + row) * r.cols;
-    for (int c = threadIdx.x; c < cols; c += TPB) {
-      const int d = c % dh;
-      float v = xr[c];
-      if (c < used && d < (int)r.rot) {
-        const Pair p = pair_of(d, half, (int)r.layout, back);
-        const float2 w = cs[row * half + p.i];
-        v = v * w.x + p.sign * xr[c - d + p.partner] * w.y;
-      }
-      yr[c] = v;
+  const float* xt = x + r0 * r.cols;
+  float* yt = y + r0 * r.cols;
+  const int total = n * r.items, step = TPB * gridDim.y;
+  for (int i0 = blockIdx.y * TPB + threadIdx.x; i0 < total; i0 += kFlight * step) {
+    Val<V> own[kFlight], other[kFlight];
+    int row[kFlight], c[kFlight], d[kFlight];
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+      const int i = min(i0 + u * step, total - 1);
+      row[u] = r.by_items.div(i);
+      c[u] = (i - row[u] * r.items) * V;
+      d[u] = c[u] - r.by_dh.div(c[u]) * r.dh;
+      if (c[u] >= r.used || d[u] >= 2 * r.half) d[u] = -1;   // copied
+      const float* p = xt + (int64_t)row[u] * r.cols + c[u];
+      own[u] = load<V>(p);
+      other[u] = own[u];
+      if (d[u] >= 0 && (V == 1 || r.layout)) other[u] = load<V>(p - d[u] + partner<V>(d[u], r.half, r.layout));
+    }
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+      if (i0 + u * step >= total) break;
+      if (d[u] >= 0)
+        own[u] = turned<V>(own[u], other[u], d[u], cs + row[u] * r.half, r.half, r.layout, back);
+      store<V>(yt + (int64_t)row[u] * r.cols + c[u], own[u]);
     }
   }
 }
 
-__device__ inline float wave_sum(float v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// ---------------------------------------------------------------- per-head norms
+// A group of G neighbouring lanes holds one head of one row, lane l of it the V columns from
+// V (l + G k) on, k < K.
+template <int G>
+__device__ inline float group_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
 
-// One wave per (row, head), lane l owning the columns l, l + 64, ...
+// The columns behind the heads of a tile's rows are copied.
+template <int V>
+__device__ inline void copy_rest(const float* __restrict__ x, float* __restrict__ y, int64_t r0, int n,
+                                 const Rows& r) {
+  const int rest = (r.cols - r.used) / V;
+  for (int row = 0; row < n; ++row) {
+    const int64_t at = (r0 + row) * r.cols + r.used;
+    for (int c = threadIdx.x; c < rest; c += TPB) store<V>(y + at + V * c, load<V>(x + at + V * c));
+  }
+}
+
+template <int V, int G, int K>
 __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict__ x,
                                                          const float* __restrict__ gain,
                                                          const int32_t* __restrict__ pos,
                                                          const double* __restrict__ table,
-                                                         float* __restrict__ y, RopeShape r,
-                                                         int h1, int tile) {
-  extern __shared__ float2 cs[];
-  const int64_t r0 = (int64_t)blockIdx.x * tile;
-  const int n = (int)min((int64_t)tile, r.rows - r0), half = (int)r.rot / 2, dh = (int)r.dh;
-  if (half) turns(cs, pos, table, r0, n, half);
-  __syncthreads();
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, heads = (int)r.heads;
-  for (int u = w; u < n * heads; u += TPB / 64) {
-    const int row = u / heads, h = u % heads;
-    const float* xr = x + (r0 + row) * r.cols + h * dh;
-    float* yr = y + (r0 + row) * r.cols + h * dh;
-    const float* g = gain + (h < h1 ? 0 : dh);
+                                                         float* __restrict__ y, Rows r) {
+  extern __shared__ float4 lds[];
+  float2* cs = reinterpret_cast<float2*>(lds);
+  const int64_t r0 = (int64_t)blockIdx.x * r.tile;
+  const int n = (int)min((int64_t)r.tile, r.rows - r0);
+  if (r.half) {
+    turns(cs, pos, table, r0, n, r);
+    __syncthreads();
+  }
+  const int lane = threadIdx.x % G, step = TPB / G * gridDim.y, total = n * r.heads;
+  for (int u = blockIdx.y * (TPB / G) + threadIdx.x / G; u < total; u += step) {
+    const int row = r.by_heads.div(u), h = u - row * r.heads;
+    const int64_t at = (r0 + row) * r.cols + h * r.dh;
+    const float* g = gain + (h < r.h1 ? 0 : r.dh);
+    Val<V> own[K], other[K];
     float q = 0.f;
-    for (int d = lane; d < dh; d += 64) q += xr[d] * xr[d];
-    const float rs = 1.f / sqrtf(wave_sum(q) / (float)dh + 1e-5f);
-    for (int d = lane; d < dh; d += 64) {
-      float v = g[d] * (xr[d] * rs);
-      if (d < 2 * half) {
-        const Pair p = pair_of(d, half, (int)r.layout, false);
-        const float2 t = cs[row * half + p.i];
-        v = v * t.x + p.sign * (g[p.partner] * (xr[p.partner] * rs)) * t.y;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int d = V * (lane + G * k);
+      own[k] = {};
+      if (d < r.dh) {
+        own[k] = load<V>(x + at + d);
+        const int p = d < 2 * r.half ? partner<V>(d, r.half, r.layout) : d;
+        other[k] = p == d ? own[k] : load<V>(x + at + p);
       }
-      yr[d] = v;
+#pragma unroll
+      for (int e = 0; e < V; ++e) q += own[k].v[e] * own[k].v[e];
+    }
+    const float rs = 1.f / sqrtf(group_sum<G>(q) / (float)r.dh + 1e-5f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int d = V * (lane + G * k);
+      if (d >= r.dh) continue;
+      const Val<V> gd = load<V>(g + d);
+#pragma unroll
+      for (int e = 0; e < V; ++e) own[k].v[e] = gd.v[e] * (own[k].v[e] * rs);
+      if (d < 2 * r.half) {
+        const int p = partner<V>(d, r.half, r.layout);
+        if (p != d) {
+          const Val<V> gp = load<V>(g + p);
+#pragma unroll
+          for (int e = 0; e < V; ++e) other[k].v[e] = gp.v[e] * (other[k].v[e] * rs);
+        }
+        own[k] = turned<V>(own[k], other[k], d, cs + row * r.half, r.half, r.layout, false);
+      }
+      store<V>(y + at + d, own[k]);
     }
   }
-  const int used = heads * dh, rest = (int)r.cols - used;
-  for (int row = 0; row < n; ++row)
-    for (int c = threadIdx.x; c < rest; c += TPB)
-      y[(r0 + row) * r.cols + used + c] = x[(r0 + row) * r.cols + used + c];
+  if (blockIdx.y == 0) copy_rest<V>(x, y, r0, n, r);
 }
 
-// A workgroup per row slice; its waves' sums of dgain are added in wave order.
-constexpr int kMaxJ = 16;   // columns a lane owns at dh = 1024
+// A workgroup per row slice; its groups' sums of dgain are added in their order.
+template <int V, int G, int K>
 __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
     const float* __restrict__ x, const float* __restrict__ gain, const int32_t* __restrict__ pos,
     const double* __restrict__ table, const float* __restrict__ dy, float* __restrict__ dx,
-    float* __restrict__ part, RopeShape r, int h1, int64_t len, int tile) {
-  extern __shared__ float2 cs[];
-  const int half = (int)r.rot / 2, dh = (int)r.dh, heads = (int)r.heads;
-  const int groups = h1 < heads ? 2 : 1;
-  float* sums = reinterpret_cast<float*>(cs + tile * half);   // [groups][dh]
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  float acc[2][kMaxJ];
+    float* __restrict__ part, Rows r, int64_t len) {
+  extern __shared__ float4 lds[];
+  float2* cs = reinterpret_cast<float2*>(lds);
+  const int lane = threadIdx.x % G, group = threadIdx.x / G;
+  float acc[2][K][V];
 #pragma unroll
-  for (int j = 0; j < kMaxJ; ++j) acc[0][j] = acc[1][j] = 0.f;
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[0][k][e] = acc[1][k][e] = 0.f;
   const int64_t s0 = blockIdx.x * len, s1 = min(r.rows, s0 + len);
-  for (int64_t r0 = s0; r0 < s1; r0 += tile) {
-    const int n = (int)min((int64_t)tile, s1 - r0);
-    __syncthreads();
-    if (half) turns(cs, pos, table, r0, n, half);
-    __syncthreads();
-    for (int u = w; u < n * heads; u += TPB / 64) {
-      const int row = u / heads, h = u % heads;
-      const int64_t at = (r0 + row) * r.cols + h * dh;
-      const int second = h < h1 ? 0 : 1;
-      const float* g = gain + second * dh;
-      float q = 0.f, dot = 0.f, z[kMaxJ];
+  for (int64_t r0 = s0; r0 < s1; r0 += r.tile) {
+    const int n = (int)min((int64_t)r.tile, s1 - r0), total = n * r.heads;
+    if (r.half) {
+      __syncthreads();
+      turns(cs, pos, table, r0, n, r);
+      __syncthreads();
+    }
+    for (int u = group; u < total; u += TPB / G) {
+      const int row = r.by_heads.div(u), h = u - row * r.heads;
+      const int64_t at = (r0 + row) * r.cols + h * r.dh;
+      const bool second = h >= r.h1;
+      const float* g = gain + (second ? r.dh : 0);
+      Val<V> xv[K], z[K], gd[K];
+      float q = 0.f, dot = 0.f;
 #pragma unroll
-      for (int j = 0; j < kMaxJ; ++j) {
-        const int d = lane + 64 * j;
-        z[j] = 0.f;
-        if (d < dh) {
-          z[j] = dy[at + d];
-          if (d < 2 * half) {
-            const Pair p = pair_of(d, half, (int)r.layout, true);
-            const float2 t = cs[row * half + p.i];
-            z[j] = z[j] * t.x + p.sign * dy[at + p.partner] * t.y;
+      for (int k = 0; k < K; ++k) {
+        const int d = V * (lane + G * k);
+        xv[k] = z[k] = gd[k] = {};
+        if (d < r.dh) {
+          xv[k] = load<V>(x + at + d);
+          z[k] = load<V>(dy + at + d);
+          gd[k] = load<V>(g + d);
+          if (d < 2 * r.half) {
+            const int p = partner<V>(d, r.half, r.layout);
+            const Val<V> other = p == d ? z[k] : load<V>(dy + at + p);
+            z[k] = turned<V>(z[k], other, d, cs + row * r.half, r.half, r.layout, true);
           }
-          q += x[at + d] * x[at + d];
-          dot += g[d] * z[j] * x[at + d];
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          q += xv[k].v[e] * xv[k].v[e];
+          dot += gd[k].v[e] * z[k].v[e] * xv[k].v[e];
         }
       }
-      const float rs = 1.f / sqrtf(wave_sum(q) / (float)dh + 1e-5f);
-      const float mean = wave_sum(dot) * rs / (float)dh;   // of gain z xhat
+      q = group_sum<G>(q);
+      dot = group_sum<G>(dot);
+      const float rs = 1.f / sqrtf(q / (float)r.dh + 1e-5f);
+      const float mean = dot * rs / (float)r.dh;   // of gain z xhat
 #pragma unroll
-      for (int j = 0; j < kMaxJ; ++j) {
-        const int d = lane + 64 * j;
-        if (d < dh) {
-          const float xh = x[at + d] * rs, zx = z[j] * xh;
-          acc[0][j] += second ? 0.f : zx;
-          acc[1][j] += second ? zx : 0.f;
-          dx[at + d] = rs * (g[d] * z[j] - xh * mean);
+      for (int k = 0; k < K; ++k) {
+        const int d = V * (lane + G * k);
+        Val<V> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float xh = xv[k].v[e] * rs, zx = z[k].v[e] * xh;
+          acc[0][k][e] += second ? 0.f : zx;
+          acc[1][k][e] += second ? zx : 0.f;
+          o.v[e] = rs * (gd[k].v[e] * z[k].v[e] - xh * mean);
         }
+        if (d < r.dh) store<V>(dx + at + d, o);
       }
     }
-    const int used = heads * dh, rest = (int)r.cols - used;
-    for (int row = 0; row < n; ++row)
-      for (int c = threadIdx.x; c < rest; c += TPB)
-        dx[(r0 + row) * r.cols + used + c] = dy[(r0 + row) * r.cols + used + c];
+    copy_rest<V>(dy, dx, r0, n, r);
   }
-  for (int k = 0; k < TPB / 64; ++k) {
-    __syncthreads();
-    if (w == k) {
-#pragma unroll
-      for (int j = 0; j < kMaxJ; ++j) {
-        const int d = lane + 64 * j;
-        if (d < dh) {
-          sums[d] = (k ? sums[d] : 0.f) + acc[0][j];
-          if (groups == 2) sums[dh + d] = (k ? sums[dh + d] : 0.f) + acc[1][j];
-        }
-      }
-    }
-  }
+  // [groups][2][G K V] in the turns' place
+  float* sums = reinterpret_cast<float*>(lds);
+  constexpr int N = G * K * V;
   __syncthreads();
-  for (int c = threadIdx.x; c < groups * dh; c += TPB) part[blockIdx.x * (int64_t)(groups * dh) + c] = sums[c];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int d = V * (lane + G * k) + e;
+      sums[(group * 2) * N + d] = acc[0][k][e];
+      sums[(group * 2 + 1) * N + d] = acc[1][k][e];
+    }
+  __syncthreads();
+  const int rows = r.h1 < r.heads ? 2 : 1;
+  for (int c = threadIdx.x; c < rows * r.dh; c += TPB) {
+    const int w = c >= r.dh ? 1 : 0, d = c - w * r.dh;
+    float s = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < TPB / G; ++k) s += sums[(k * 2 + w) * N + d];
+    part[(int64_t)blockIdx.x * rows * r.dh + c] = s;
+  }
 }
 
-// dgain = the slices' partials added in order
-__global__ __launch_bounds__(TPB) void qknorm_finalize(const float* __restrict__ part,
-                                                       float* __restrict__ dgain, int n,
-                                                       int64_t slices) {
-  const int c = blockIdx.x * TPB + threadIdx.x;
-  if (c >= n) return;
+// dgain = the slices' partials: a workgroup owns 16 columns, its 64 rows of threads take the slices
+// s = row mod 64 in increasing order, and one row adds the 64 results in order.
+constexpr int kFinCols = 16, kFinRows = 64;
+__global__ __launch_bounds__(kFinCols * kFinRows) void qknorm_finalize(const float* __restrict__ part,
+                                                                       float* __restrict__ dgain,
+                                                                       int n, int64_t slices) {
+  __shared__ float sums[kFinRows][kFinCols];
+  const int c = blockIdx.x * kFinCols + threadIdx.x % kFinCols, row = threadIdx.x / kFinCols;
   float s = 0.f;
-  for (int64_t k = 0; k < slices; ++k) s += part[k * n + c];
-  dgain[c] = s;
+  if (c < n)
+    for (int64_t k = row; k < slices; k += kFinRows) s += part[k * n + c];
+  sums[row][threadIdx.x % kFinCols] = s;
+  __syncthreads();
+  if (row || c >= n) return;
+  float t = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < kFinRows; ++k) t += sums[k][threadIdx.x];
+  dgain[c] = t;
 }
 
-// Rows per workgroup: all of a launch's cosines fit kMaxTile rows, fewer where that would leave
-// compute units without work.
-int row_tile(const RopeShape& r) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxTile, r.rows / 1024));
+// ---------------------------------------------------------------- launches
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// 16-byte items: every head, the rotated width (each half of it where pairs lie half apart) and
+// every row a multiple of four columns.
+bool in_fours(const RopeShape& s, std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return false;
+  return s.dh % 4 == 0 && s.cols % 4 == 0 && s.rot % (s.layout ? 8 : 4) == 0;
 }
 
+Rows rows_of(const RopeShape& s, int64_t h1, int V, int64_t rows_a_group) {
+  Rows r;
+  r.rows = s.rows;
+  r.cols = (int)s.cols;
+  r.dh = (int)s.dh;
+  r.heads = (int)s.heads;
+  r.used = (int)(s.heads * s.dh);
+  r.half = (int)s.rot / 2;
+  r.layout = (int)s.layout;
+  r.h1 = (int)h1;
+  r.items = r.cols / V;
+  // Rows a workgroup takes: their turns keep its threads busy at 8 rows of 64 rotated columns, and
+  // a launch has at least 1024 workgroups where it has the rows for them.
+  r.tile = (int)std::max<int64_t>(1, std::min<int64_t>(8, rows_a_group));
+  r.by_half = FastDiv::make(r.half);
+  r.by_dh = FastDiv::make(r.dh);
+  r.by_heads = FastDiv::make(r.heads);
+  r.by_items = FastDiv::make(r.items);
+  return r;
+}
 unsigned blocks(int64_t rows, int64_t tile) { return (unsigned)((rows + tile - 1) / tile); }
+// Parts a tile's items or heads are cut into where there are few tiles: 512 workgroups in all, and
+// `least` threads' worth of work in each.
+unsigned parts(unsigned tiles, int64_t work, int64_t least) {
+  return (unsigned)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, work / least));
+}
+
+// Lanes a head of q items takes and items a lane: the fewest idle lanes, and of these the fewest items.
+#define GROUPS_TO_256(V, CALL)                         \
+  if (q <= 16) CALL(V, 16, 1);                         \
+  else if (q <= 32) CALL(V, 32, 1);                    \
+  else if (q <= 48) CALL(V, 16, 3);                    \
+  else if (q <= 64) CALL(V, 64, 1);                    \
+  else if (q <= 96) CALL(V, 32, 3);                    \
+  else if (q <= 128) CALL(V, 64, 2);                   \
+  else if (q <= 192) CALL(V, 64, 3);                   \
+  else CALL(V, 64, 4)
+#define GROUPS(CALL)                                   \
+  if (four) {                                          \
+    const int q = r.dh / 4;                            \
+    GROUPS_TO_256(4, CALL);                            \
+  } else if (r.dh <= 256) {                            \
+    const int q = r.dh;                                \
+    GROUPS_TO_256(1, CALL);                            \
+  } else if (r.dh <= 512) CALL(1, 64, 8);              \
+  else CALL(1, 64, 16)
 
 }  // namespace
 
 hipError_t rope(bool back, const float* x, const int32_t* pos, const double* table, float* y,
-                const RopeShape& r, hipStream_t s) {
-  const int tile = row_tile(r);
-  hipLaunchKernelGGL(rope_kernel, dim3(blocks(r.rows, tile)), dim3(TPB),
-                     (unsigned)(tile * r.rot / 2 * sizeof(float2)), s, x, pos, table, y, r, tile,
-                     back);
+                const RopeShape& s, hipStream_t st) {
+  const bool four = in_fours(s, {x, y});
+  const Rows r = rows_of(s, s.heads, four ? 4 : 1, s.rows / 1024);
+  const unsigned nx = blocks(r.rows, r.tile);
+  const dim3 grid(nx, parts(nx, (int64_t)r.tile * r.items, TPB));
+  const unsigned lds = (unsigned)(r.tile * r.half * sizeof(float2));
+  if (four)
+    hipLaunchKernelGGL(rope_kernel<4>, grid, dim3(TPB), lds, st, x, pos, table, y, r, back);
+  else
+    hipLaunchKernelGGL(rope_kernel<1>, grid, dim3(TPB), lds, st, x, pos, table, y, r, back);
   return hipGetLastError();
 }
 
 hipError_t qknorm_fwd(const float* x, const float* gain, const int32_t* pos, const double* table,
-                      float* y, const RopeShape& r, int64_t h1, hipStream_t s) {
-  const int tile = row_tile(r);
-  hipLaunchKernelGGL(qknorm_fwd_kernel, dim3(blocks(r.rows, tile)), dim3(TPB),
-                     (unsigned)(tile * r.rot / 2 * sizeof(float2)), s, x, gain, pos, table, y, r,
-                     (int)h1, tile);
+                      float* y, const RopeShape& s, int64_t h1, hipStream_t st) {
+  const bool four = in_fours(s, {x, gain, y});
+  const Rows r = rows_of(s, h1, four ? 4 : 1, s.rows / 1024);
+  const unsigned nx = blocks(r.rows, r.tile);
+  const unsigned lds = (unsigned)(r.tile * r.half * sizeof(float2));
+#define FWD(V, G, K)                                                                              \
+  hipLaunchKernelGGL((qknorm_fwd_kernel<V, G, K>), dim3(nx, parts(nx, (int64_t)r.tile * r.heads, TPB / G)), \
+                     dim3(TPB), lds, st, x, gain, pos, table, y, r)
+  GROUPS(FWD);
+#undef FWD
   return hipGetLastError();
 }
 
 hipError_t qknorm_bwd(const float* x, const float* gain, const int32_t* pos, const double* table,
-                      const float* dy, float* dx, float* dgain, float* part, const RopeShape& r,
-                      int64_t h1, int64_t slices, hipStream_t s) {
-  const int64_t len = (r.rows + slices - 1) / slices;
-  const int tile = (int)std::min<int64_t>(kMaxTile, len);
-  const int n = (int)((h1 < r.heads ? 2 : 1) * r.dh);
-  hipLaunchKernelGGL(qknorm_bwd_kernel, dim3((unsigned)slices), dim3(TPB),
-                     (unsigned)(tile * r.rot / 2 * sizeof(float2) + n * sizeof(float)), s, x, gain,
-                     pos, table, dy, dx, part, r, (int)h1, len, tile);
+                      const float* dy, float* dx, float* dgain, float* part, const RopeShape& s,
+                      int64_t h1, int64_t slices, hipStream_t st) {
+  const int64_t len = (s.rows + slices - 1) / slices;
+  const bool four = in_fours(s, {x, gain, dy, dx});
+  const Rows r = rows_of(s, h1, four ? 4 : 1, len);
+  const int n = (int)((h1 < s.heads ? 2 : 1) * s.dh);
+#define BWD(V, G, K)                                                                              \
+  hipLaunchKernelGGL((qknorm_bwd_kernel<V, G, K>), dim3((unsigned)slices), dim3(TPB),             \
+                     (unsigned)std::max<size_t>(r.tile * r.half * sizeof(float2),                 \
+                                                TPB * 2 * K * V * sizeof(float)),                 \
+                     st, x, gain, pos, table, dy, dx, part, r, len)
+  GROUPS(BWD);
+#undef BWD
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(qknorm_finalize, dim3((unsigned)((n + TPB - 1) / TPB)), dim3(TPB), 0, s, part,
-                     dgain, n, slices);
+  hipLaunchKernelGGL(qknorm_finalize, dim3((unsigned)((n + kFinCols - 1) / kFinCols)),
+                     dim3(kFinCols * kFinRows), 0, st, part, dgain, n, slices);
   return hipGetLastError();
 }
 

@@ -371,7 +371,7 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
       const int64_t rows = a[0], cols = a[1], heads = a[2], dh = a[3], rot = a[4], layout = a[5];
       const int64_t used = product({heads, dh});
       if (rows <= 0 || rows > INT32_MAX || heads <= 0 || dh <= 0 || used < 0 || cols < used ||
-          cols > INT32_MAX / 4 || rot < 2 || rot % 2 || rot > dh || rot > 1024 || (layout != 0 && layout != 1))
+          cols > (1 << 24) || rot < 2 || rot % 2 || rot > dh || rot > 1024 || (layout != 0 && layout != 1))
         return nm + ": bad attributes";
       const int64_t xb = product({rows, cols, 4});
       NEED(0, xb, "rows");
@@ -387,7 +387,7 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
       const int64_t used = product({h1 + h2, dh});
       const bool fwd = fn.op == OOC_OP_QKNORM_FWD;
       if (rows <= 0 || rows > INT32_MAX || h1 <= 0 || dh <= 0 || dh > 1024 || used < 0 || cols < used ||
-          cols > INT32_MAX / 4 || rot % 2 || rot > dh || (layout != 0 && layout != 1))
+          cols > (1 << 24) || rot % 2 || rot > dh || (layout != 0 && layout != 1))
         return nm + ": bad attributes";
       const int w = rot > 0 ? 2 : 0;   // pos and table
       if (nv != (fwd ? 3 : 6) + w) return nm + ": takes pos and table iff rot > 0";
