@@ -553,34 +553,177 @@ __global__ __launch_bounds__(64 * Width<DH>::kFwdWaves, DH <= 128 ? 2 : 1) void 
   }
 }
 
-// y and lse of a row from its slices': the slices' outputs weighted by exp(lse_s - lse)
-__global__ void join_kernel(const float* __restrict__ part, float* __restrict__ y,
-                            float* __restrict__ lse, Shape s, int slices, int64_t y_size,
-                            int64_t rows) {
-  const float* pl = part + slices * y_size;
-  const int64_t stride = (int64_t)gridDim.x * blockDim.x;
-  for (int64_t u = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u < y_size; u += stride) {
-    const int64_t row = u / s.dh, d = u - row * s.dh;   // row (b, i, h)
-    const int64_t h = row % s.H, bi = row / s.H, i = bi % s.Tq, b = bi / s.Tq;
-    const int64_t st = (b * s.H + h) * s.Tq + i;
-    float top = -INFINITY;
-    bool nan = false;
-    for (int k = 0; k < slices; ++k) {
-      const float l = pl[k * rows + st];
-      top = fmaxf(top, l);
-      nan |= l != l;
+// ---------------------------------------------------------------- forward of a few queries
+// A key head with at most 32 query rows (a token of each sequence and its group's heads) is bound by
+// reading the states once.  They go from memory into registers: each wave takes tiles of 32 states
+// of its own, without barriers, and a workgroup's waves and then the slices join their results.
+constexpr int kFewWaves = 4, kFewRows = 32;
+template <int DH, bool EXACT>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(
+    const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
+    float* __restrict__ y, float* __restrict__ lse, Shape s, int tiles, int slice_len,
+    int64_t y_slice, int64_t lse_slice) {
+  using Wd = Width<DH>;
+  constexpr int T = 32, W = kFewWaves;
+  __shared__ float ys[W][kFewRows][DH + 1], ls[W][kFewRows];
+  const Place at = place(s, tiles);
+  if (at.none) return;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int n = klen[at.b];
+  const bool bad = n < 0 || n > s.Tk;
+  const int k0 = bad ? 0 : min(n, at.slice * slice_len), k1 = bad ? 0 : min(n, k0 + slice_len);
+
+  Pieces qp[Wd::kSteps];
+  float qc;
+  {
+    float v[DH / 2];
+    load_column<DH, EXACT>(q + query_row(s, at.b, at.hk, min(l32, s.R - 1)), s.dh, v);
+    qc = split_column<DH>(v, qp) * s.scale * kLog2e;
+  }
+  floatx16 o[Wd::kBlocks];
+#pragma unroll
+  for (int t = 0; t < Wd::kBlocks; ++t) o[t] = floatx16{};
+  float m = -INFINITY, sum = 0.f;
+  int base = 0;
+  // k: as the A operand of the scores holds it; v: as that of the sums, lane l head column l mod 32
+  // of each block, the rows in the order of a result
+  float k[DH / 2], v[DH / 2];
+  const auto load_k = [&](int j) {
+    const auto r = buffer(kv + key_row(s, at.b, at.hk, min(j, s.Tk - 1)),
+                          j < k1 ? (int64_t)(min(T, k1 - j) - 1) * s.ldk + s.dh : 0);
+#pragma unroll
+    for (int t = 0; t < Wd::kSteps; ++t) {
+      const int d = 16 * t + 8 * half;
+      load8(r, l32 < k1 - j && d < s.dh ? (uint32_t)(l32 * s.ldk + d) * 4u : kNone, k + 8 * t);
+      trim<EXACT>(k + 8 * t, d, s.dh);
     }
-    float sum = 0.f, acc = 0.f;
-    if (top > -INFINITY)
-      for (int k = 0; k < slices; ++k) {
-        const float l = pl[k * rows + st];
-        if (l == -INFINITY) continue;
-        const float f = expf(l - top);
-        sum += f;
-        acc = fmaf(f, part[k * y_size + u], acc);
+  };
+  const auto load_v = [&](int j) {
+    const auto r = buffer(kv + key_row(s, at.b, at.hk, min(j, s.Tk - 1)) + (int64_t)s.Hkv * s.dh,
+                          j < k1 ? (int64_t)(min(T, k1 - j) - 1) * s.ldk + s.dh : 0);
+#pragma unroll
+    for (int t = 0; t < Wd::kBlocks; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = 8 * (i / 4) + 4 * half + i % 4, d = 32 * t + l32;
+        const bool there = row < k1 - j && d < s.dh;
+        v[16 * t + i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
+            r, there ? (int)((uint32_t)(row * s.ldk + d) * 4u) : (int)kNone, 0, 0));
       }
-    y[u] = nan ? NAN : sum > 0.f ? acc / sum : 0.f;
-    if (d == 0) lse[st] = nan ? NAN : sum > 0.f ? top + logf(sum) : -INFINITY;
+  };
+  const auto largest = [&](const float (&x)[DH / 2]) {
+    float top = max_abs(x, DH / 2);
+    if (__any(top == INFINITY)) {   // the largest finite one: see Raw::publish
+      top = 0.f;
+#pragma unroll
+      for (int i = 0; i < DH / 2; ++i) top = fmaxf(top, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.f);
+    }
+    return exponent(wave_max(top));
+  };
+  const int j1 = k0 + w * T;
+  load_k(j1);
+  load_v(j1);
+  for (int j0 = j1; j0 < k1; j0 += W * T) {
+    const int ek = largest(k);
+    int ev = largest(v);
+    if (j0 == j1) base = ev <= -112 ? 0 : ev;
+    ev = ev <= -112 ? base : max(ev, base - 40);   // zeros count as base
+    floatx16 a = {};
+#pragma unroll
+    for (int t = 0; t < Wd::kSteps; ++t) a = mma(split8(k + 8 * t, exp2_of(14 - ek)), qp[t], a);
+    load_k(j0 + W * T);
+    if (j0 + T > k1) mask_rows(a, 0, k1 - j0);
+    const float c = fmaxf(qc * exp2_of(ek - 14), 0x1p-126f);   // a masked score stays -inf
+    const float ve = (float)(ev - base);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, a[i]);
+    top = fmaf(max_of_halves(top), c, ve);
+    if (__any(top > m + 7.f)) {
+      const float up = fmaxf(m, top), f = m == up ? 1.f : exp2f(m - up);
+      m = up;
+      sum *= f;
+#pragma unroll
+      for (int t = 0; t < Wd::kBlocks; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] *= f;
+    }
+    const float off = ve + 8.f - m;
+    float p[16], part = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, off));
+      part += p[i];
+    }
+    sum = fmaf(part, exp2_of(max(base - ev, -126)), sum);
+    const Pieces pp[2] = {split8(p), split8(p + 8)};
+#pragma unroll
+    for (int t = 0; t < Wd::kBlocks; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) o[t] = mma(split8(v + 16 * t + 8 * h, exp2_of(14 - ev)), pp[h], o[t]);
+    load_v(j0 + W * T);
+  }
+  sum = sum_of_halves(sum);
+  const float f = sum == 0.f ? 0.f : kUnit * exp2_of(base) / sum;   // a wave without states: 0
+  if (l32 < s.R) {
+    store_column<Wd::kBlocks, false>(&ys[w][l32][0], 0, DH, [&](int t, int i) { return o[t][i] * f; });
+    if (half == 0) ls[w][l32] = bad ? NAN : sum == 0.f ? -INFINITY : m - 8.f + log2f(sum);
+  }
+  __syncthreads();
+  for (int u = threadIdx.x; u < s.R * DH; u += 64 * W) {
+    const int r = u / DH, d = u % DH;
+    float most = -INFINITY, total = 0.f, acc = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) most = fmaxf(most, ls[k][r]);
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const float l = ls[k][r];
+      if (l == -INFINITY) continue;   // (a NaN goes on)
+      const float g = exp2f(l - most);
+      total += g;
+      acc = fmaf(g, ys[k][r][d], acc);
+    }
+    if (bad) total = NAN;
+    if (d < s.dh)
+      y[at.slice * y_slice + query_row(s, at.b, at.hk, r) + d] = total == 0.f ? 0.f : acc / total;
+    if (d == 0)
+      lse[at.slice * lse_slice + stat_row(s, at.b, at.hk) + r] =
+          total == 0.f ? -INFINITY : (most + log2f(total)) * kLn2;
+  }
+}
+
+// y and lse of a row from its slices': the slices' outputs weighted by exp(lse_s - lse).  A wave a
+// row, lane k holding slice k's weight.
+constexpr int kJoinWaves = 4;
+__global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(const float* __restrict__ part,
+                                                               float* __restrict__ y,
+                                                               float* __restrict__ lse, Shape s,
+                                                               int slices, int64_t y_size,
+                                                               int64_t rows) {
+  const float* pl = part + slices * y_size;
+  const int lane = threadIdx.x & 63;
+  const int64_t stride = (int64_t)gridDim.x * kJoinWaves;
+  for (int64_t row = (int64_t)blockIdx.x * kJoinWaves + (threadIdx.x >> 6); row < rows; row += stride) {
+    const int64_t h = row % s.H, bi = row / s.H, i = bi % s.Tq, b = bi / s.Tq;   // row (b, i, h)
+    const int64_t st = (b * s.H + h) * s.Tq + i;
+    const float l = lane < slices ? pl[lane * rows + st] : -INFINITY;
+    float top = l;
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const float f = l == -INFINITY ? 0.f : expf(l - top);   // a slice with a NaN makes the row one
+    float sum = f;
+    for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, 64);
+    const float g = sum == 0.f ? 0.f : f / sum;
+    for (int d0 = 0; d0 < s.dh; d0 += 64) {
+      const int d = d0 + lane;
+      float acc = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < slices; ++k) {
+        const float x = part[k * y_size + row * s.dh + min(d, s.dh - 1)];
+        acc = fmaf(__shfl(g, k, 64), x, acc);
+      }
+      if (d < s.dh) y[row * s.dh + d] = acc;
+    }
+    if (lane == 0) lse[st] = sum == 0.f ? -INFINITY : top + logf(sum);
   }
 }
 
@@ -1132,31 +1275,39 @@ int64_t slice_of(int64_t n, int64_t slices, int64_t tile) {
 }
 
 // Workgroups to aim for, and the fewest tiles a slice is worth cutting off for.
-constexpr int64_t kWant = 512, kMinTiles = 2;
-int64_t slices_for(int64_t groups, int64_t tiles) {
-  if (groups >= kWant) return 1;
-  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(kWant, groups), tiles / kMinTiles,
+#ifndef FEWW
+#define FEWW 512
+#endif
+constexpr int64_t kWant = 512, kFewWant = FEWW, kMinTiles = 2;
+int64_t slices_for(int64_t groups, int64_t tiles, int64_t want = kWant) {
+  if (groups >= want) return 1;
+  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, groups), tiles / kMinTiles,
                                                   kMaxAttentionSlices}));
 }
+bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows && a.dh <= 128; }
 
 #define UP_TO_64(CALL)                     \
   if (s.dh == 32) CALL(32, true);          \
   else if (s.dh < 32) CALL(32, false);     \
   else if (s.dh == 64) CALL(64, true);     \
   else CALL(64, false)
-#define ABOVE_64(CALL)                     \
+#define TO_128(CALL)                       \
   if (s.dh == 96) CALL(96, true);          \
   else if (s.dh < 96) CALL(96, false);     \
   else if (s.dh == 128) CALL(128, true);   \
-  else if (s.dh < 128) CALL(128, false);   \
-  else if (s.dh == 256) CALL(256, true);   \
-  else CALL(256, false)
+  else CALL(128, false)
+#define ABOVE_64(CALL)                     \
+  if (s.dh == 256) CALL(256, true);        \
+  else if (s.dh > 128) CALL(256, false);   \
+  else TO_128(CALL)
 #define LAUNCH(KERNEL, WAVES, TILES, SLICES, ...) \
   hipLaunchKernelGGL(KERNEL, grid_of(s, TILES, SLICES), dim3(64 * WAVES), 0, st, __VA_ARGS__)
 
 }  // namespace
 
 int64_t attention_key_slices(const AttendShape& a, bool fwd) {
+  if (fwd && few_rows(a))
+    return slices_for(a.B * a.Hkv, ceil_div(a.Tk, 32 * kFewWaves), kFewWant);
   const int64_t tiles = ceil_div(a.Tq * (a.H / a.Hkv), fwd ? fwd_columns(a.dh) : back_columns(a.dh));
   return slices_for(a.B * a.Hkv * tiles, ceil_div(a.Tk, fwd ? tile_rows(a.dh) : back_rows(a.dh)));
 }
@@ -1168,24 +1319,34 @@ hipError_t cross_attention_fwd(const float* q, const float* kv, const int32_t* k
                                float* lse, float* part, const AttendShape& a, int64_t slices,
                                hipStream_t st) {
   const Shape s = shape_of(a);
-  const int tiles = (int)ceil_div(s.R, fwd_columns(s.dh));
-  const int len = (int)slice_of(s.Tk, slices, tile_rows(s.dh));
+  const bool few = few_rows(a);
+  const int tiles = few ? 1 : (int)ceil_div(s.R, fwd_columns(s.dh));
+  const int len = (int)slice_of(s.Tk, slices, few ? 32 : tile_rows(s.dh));
   const int64_t size = a.B * a.Tq * s.ldq, rows = a.B * a.H * a.Tq;
   float* yo = slices > 1 ? part : y;
   float* lo = slices > 1 ? part + slices * size : lse;
 #define FWD(D, X)                                                                              \
   LAUNCH((fwd_kernel<D, X>), Width<D>::kFwdWaves, tiles, slices, q, kv, klen, yo, lo, s, tiles, len, \
          size, rows)
-  if (s.dh <= 64) {
+#define FEW(D, X)                                                                                \
+  LAUNCH((few_kernel<D, X>), kFewWaves, tiles, slices, q, kv, klen, yo, lo, s, tiles, len, size, rows)
+  if (few) {
+    if (s.dh <= 64) {
+      UP_TO_64(FEW);
+    } else {
+      TO_128(FEW);
+    }
+  } else if (s.dh <= 64) {
     UP_TO_64(FWD);
   } else {
     ABOVE_64(FWD);
   }
+#undef FEW
 #undef FWD
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || slices == 1) return e;
-  hipLaunchKernelGGL(join_kernel, dim3(flat_grid(size)), dim3(256), 0, st, part, y, lse, s,
-                     (int)slices, size, rows);
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(rows, kJoinWaves), 8192)),
+                     dim3(64 * kJoinWaves), 0, st, part, y, lse, s, (int)slices, size, rows);
   return hipGetLastError();
 }
 
