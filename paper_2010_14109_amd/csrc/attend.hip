@@ -183,6 +183,9 @@ __device__ inline void load8(__amdgpu_buffer_rsrc_t r, uint32_t off, float* v) {
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
   v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
+// four values at a 4-byte aligned address
+typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
+
 // columns at and past dh of the eight from d on are zero
 template <bool EXACT>
 __device__ inline void trim(float* v, int d, int dh) {
@@ -210,27 +213,29 @@ __device__ inline int64_t stat_row(const Shape& s, int b, int hk) {
   return ((int64_t)b * s.H + (int64_t)hk * s.G) * s.Tq;
 }
 
+// head columns d .. d + 7 of the row at p, zero past the last
+template <bool EXACT>
+__device__ inline void load_eight(const float* p, int d, int dh, float* v) {
+  if (EXACT || d + 8 <= dh) {
+    const floatx4u a = *reinterpret_cast<const floatx4u*>(p + d), b = *reinterpret_cast<const floatx4u*>(p + d + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = a[e];
+      v[4 + e] = b[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = d + e < dh ? p[d + e] : 0.f;
+  }
+}
+
 // A wave's own columns: lane l holds column l mod 32, head columns 16 s + 8 (l / 32) .. + 8 of every
 // step s.  p: the column's row (a column past the last takes the last one's; it is not stored).
 template <int DH, bool EXACT>
 __device__ inline void load_column(const float* p, int dh, float (&v)[DH / 2]) {
   const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-  for (int s = 0; s < DH / 16; ++s) {
-    if constexpr (EXACT) {
-      const float4 a = *reinterpret_cast<const float4*>(p + 16 * s + 8 * half);
-      const float4 b = *reinterpret_cast<const float4*>(p + 16 * s + 8 * half + 4);
-      v[8 * s] = a.x; v[8 * s + 1] = a.y; v[8 * s + 2] = a.z; v[8 * s + 3] = a.w;
-      v[8 * s + 4] = b.x; v[8 * s + 5] = b.y; v[8 * s + 6] = b.z; v[8 * s + 7] = b.w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int d = 16 * s + 8 * half + e;
-        const float x = p[min(d, dh - 1)];
-        v[8 * s + e] = d < dh ? x : 0.f;
-      }
-    }
-  }
+  for (int s = 0; s < DH / 16; ++s) load_eight<EXACT>(p, 16 * s + 8 * half, dh, v + 8 * s);
 }
 // Returns the inverse scale.
 template <int DH>
@@ -275,6 +280,20 @@ struct Rows {
   static __device__ Pieces by_column(const char* lds, int r0, int block) {
     return {transposed(lds, r0, block), transposed(lds + kPiece, r0, block)};
   }
+  // the same for 16 x 16 x 32: head columns 16 block .. + 15 x all 32 rows, quarter g of the wave
+  // having rows 4 g .. + 3 and 16 + 4 g .. + 3
+  static __device__ half8v transposed16(const char* lds, int block) {
+    const int l = threadIdx.x & 63, t = l & 15;
+    const char* p = lds + (4 * (l >> 4) + (t >> 2)) * Wd::kRow + (16 * block + 4 * (t & 3)) * 2;
+    typedef __attribute__((address_space(3))) short4v* Lds;
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
+    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 16 * Wd::kRow));
+    const half4v x = __builtin_bit_cast(half4v, a), y = __builtin_bit_cast(half4v, b);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  static __device__ Pieces by_column16(const char* lds, int block) {
+    return {transposed16(lds, block), transposed16(lds + kPiece, block)};
+  }
 };
 
 // The workgroup's place: pairs (b, key head), tiles of columns, slices of the other side.  The
@@ -298,9 +317,9 @@ __device__ inline void store_column(float* p, int first, int dh, F value) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int d = 32 * (first + t) + 8 * q + 4 * half;
-      if constexpr (EXACT) {
-        *reinterpret_cast<float4*>(p + d) =
-            make_float4(value(t, 4 * q), value(t, 4 * q + 1), value(t, 4 * q + 2), value(t, 4 * q + 3));
+      if (EXACT || d + 4 <= dh) {
+        *reinterpret_cast<floatx4u*>(p + d) =
+            floatx4u{value(t, 4 * q), value(t, 4 * q + 1), value(t, 4 * q + 2), value(t, 4 * q + 3)};
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -554,63 +573,94 @@ __global__ __launch_bounds__(64 * Width<DH>::kFwdWaves, DH <= 128 ? 2 : 1) void 
 }
 
 // ---------------------------------------------------------------- forward of a few queries
-// A key head with at most 32 query rows (a token of each sequence and its group's heads) is bound by
-// reading the states once.  They go from memory into registers: each wave takes tiles of 32 states
-// of its own, without barriers, and a workgroup's waves and then the slices join their results.
-constexpr int kFewWaves = 4, kFewRows = 32;
+// A key head with at most 16 query rows (a token of each sequence and its group's heads) is bound by
+// reading the states once.  Each wave takes tiles of 32 states of its own, without barriers: k goes
+// from memory straight into the A operand, v through the wave's part of LDS.  A workgroup's waves
+// and then the slices join their results.  Products are 16 x 16 x 32: 16 columns are all there is,
+// and half the registers of 32 let a SIMD hold three waves, whose loads are all in flight at once.  One token of 8 sequences against 4096
+// states, 16 heads of 64 on 4 key heads: 33.9 -> 18.6 us
+// (the first kernel 14, the join 4; 17 MB at the rate of a large copy take 3.5) against the kernel
+// for many queries.
+constexpr int kFewWaves = 4, kFewRows = 16;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+__device__ inline floatx4 mma16(const Pieces& a, const Pieces& b, floatx4 c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.l, b.h, c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, b.l, c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, b.h, c, 0, 0, 0);
+}
+// over the four lanes 16 apart
+__device__ inline float max_of_quarters(float x) {
+  const uint32_t v = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const uint32_t a = r[0], b = r[1];
+  return max_of_halves(fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+}
+__device__ inline float sum_of_quarters(float x) {
+  const uint32_t v = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const uint32_t a = r[0], b = r[1];
+  return sum_of_halves(__builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+}
+
 template <int DH, bool EXACT>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(
+__global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
     const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
     float* __restrict__ y, float* __restrict__ lse, Shape s, int tiles, int slice_len,
     int64_t y_slice, int64_t lse_slice) {
-  using Wd = Width<DH>;
-  constexpr int T = 32, W = kFewWaves;
-  __shared__ float ys[W][kFewRows][DH + 1], ls[W][kFewRows];
+  constexpr int T = 32, W = kFewWaves, kSteps = DH / 32, kBlocks = DH / 16;
+  __shared__ __attribute__((aligned(16))) char mine[W][Rows<DH, T>::kBytes];
+  __shared__ float ls[W][kFewRows];
+  // a wave's results take its tile's place
+  constexpr int kYs = DH + 4;
+  static_assert(kFewRows * kYs * 4 <= Rows<DH, T>::kBytes, "room for the results");
+  const auto ys = [&](int wave, int r, int d) -> float* {
+    return reinterpret_cast<float*>(mine[wave]) + r * kYs + d;
+  };
   const Place at = place(s, tiles);
   if (at.none) return;
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, quarter = lane >> 4, l16 = lane & 15;
   const int n = klen[at.b];
   const bool bad = n < 0 || n > s.Tk;
   const int k0 = bad ? 0 : min(n, at.slice * slice_len), k1 = bad ? 0 : min(n, k0 + slice_len);
 
-  Pieces qp[Wd::kSteps];
-  float qc;
-  {
-    float v[DH / 2];
-    load_column<DH, EXACT>(q + query_row(s, at.b, at.hk, min(l32, s.R - 1)), s.dh, v);
-    qc = split_column<DH>(v, qp) * s.scale * kLog2e;
-  }
-  floatx16 o[Wd::kBlocks];
-#pragma unroll
-  for (int t = 0; t < Wd::kBlocks; ++t) o[t] = floatx16{};
-  float m = -INFINITY, sum = 0.f;
-  int base = 0;
-  // k: as the A operand of the scores holds it; v: as that of the sums, lane l head column l mod 32
-  // of each block, the rows in the order of a result
+  // a lane's values of a tile: rows l mod 16 and 16 more, head columns 32 t + 8 (l / 16) .. + 8
   float k[DH / 2], v[DH / 2];
-  const auto load_k = [&](int j) {
-    const auto r = buffer(kv + key_row(s, at.b, at.hk, min(j, s.Tk - 1)),
+  const auto load_tile = [&](int j, int64_t to, float (&x)[DH / 2]) {
+    const auto r = buffer(kv + key_row(s, at.b, at.hk, min(j, s.Tk - 1)) + to,
                           j < k1 ? (int64_t)(min(T, k1 - j) - 1) * s.ldk + s.dh : 0);
 #pragma unroll
-    for (int t = 0; t < Wd::kSteps; ++t) {
-      const int d = 16 * t + 8 * half;
-      load8(r, l32 < k1 - j && d < s.dh ? (uint32_t)(l32 * s.ldk + d) * 4u : kNone, k + 8 * t);
-      trim<EXACT>(k + 8 * t, d, s.dh);
-    }
-  };
-  const auto load_v = [&](int j) {
-    const auto r = buffer(kv + key_row(s, at.b, at.hk, min(j, s.Tk - 1)) + (int64_t)s.Hkv * s.dh,
-                          j < k1 ? (int64_t)(min(T, k1 - j) - 1) * s.ldk + s.dh : 0);
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int t = 0; t < Wd::kBlocks; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = 8 * (i / 4) + 4 * half + i % 4, d = 32 * t + l32;
-        const bool there = row < k1 - j && d < s.dh;
-        v[16 * t + i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
-            r, there ? (int)((uint32_t)(row * s.ldk + d) * 4u) : (int)kNone, 0, 0));
+      for (int t = 0; t < kSteps; ++t) {
+        const int d = 32 * t + 8 * quarter, row = 16 * h + l16;
+        float* o = x + 8 * (h * kSteps + t);
+        load8(r, row < k1 - j && d < s.dh ? (uint32_t)(row * s.ldk + d) * 4u : kNone, o);
+        trim<EXACT>(o, d, s.dh);
       }
   };
+  const int64_t to_v = (int64_t)s.Hkv * s.dh;
+  char* vs = mine[w];
+  const int j1 = k0 + w * T;
+  load_tile(j1, 0, k);
+  load_tile(j1, to_v, v);
+
+  Pieces qp[kSteps];
+  float qc;
+  {
+    const float* p = q + query_row(s, at.b, at.hk, min(l16, s.R - 1));
+    float x[DH / 4];
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) load_eight<EXACT>(p, 32 * t + 8 * quarter, s.dh, x + 8 * t);
+    const int e = exponent(max_of_quarters(max_abs(x, DH / 4)));
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) qp[t] = split8(x + 8 * t, exp2_of(14 - e));
+    qc = exp2_of(e - 14) * s.scale * kLog2e;
+  }
+  floatx4 o[kBlocks];
+#pragma unroll
+  for (int t = 0; t < kBlocks; ++t) o[t] = floatx4{};
+  float m = -INFINITY, sum = 0.f;
+  int base = 0;
   const auto largest = [&](const float (&x)[DH / 2]) {
     float top = max_abs(x, DH / 2);
     if (__any(top == INFINITY)) {   // the largest finite one: see Raw::publish
@@ -620,70 +670,80 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(
     }
     return exponent(wave_max(top));
   };
-  const int j1 = k0 + w * T;
-  load_k(j1);
-  load_v(j1);
   for (int j0 = j1; j0 < k1; j0 += W * T) {
     const int ek = largest(k);
+    floatx4 a[2] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < kSteps; ++t)
+        a[h] = mma16(split8(k + 8 * (h * kSteps + t), exp2_of(14 - ek)), qp[t], a[h]);
+    load_tile(j0 + W * T, 0, k);
     int ev = largest(v);
     if (j0 == j1) base = ev <= -112 ? 0 : ev;
     ev = ev <= -112 ? base : max(ev, base - 40);   // zeros count as base
-    floatx16 a = {};
+    // (the wave's LDS accesses stay in order; the fences keep the compiler from moving them)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int t = 0; t < Wd::kSteps; ++t) a = mma(split8(k + 8 * t, exp2_of(14 - ek)), qp[t], a);
-    load_k(j0 + W * T);
-    if (j0 + T > k1) mask_rows(a, 0, k1 - j0);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < kSteps; ++t)
+        Rows<DH, T>::store(vs, 16 * h + l16, 4 * t + quarter, split8(v + 8 * (h * kSteps + t), exp2_of(14 - ev)));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    load_tile(j0 + W * T, to_v, v);
     const float c = fmaxf(qc * exp2_of(ek - 14), 0x1p-126f);   // a masked score stays -inf
     const float ve = (float)(ev - base);
-    float top = -INFINITY;
+    float p[8], top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, a[i]);
-    top = fmaf(max_of_halves(top), c, ve);
+    for (int i = 0; i < 8; ++i) {
+      const bool there = 16 * (i / 4) + 4 * quarter + i % 4 < k1 - j0;
+      p[i] = there ? a[i / 4][i % 4] : -INFINITY;
+      top = fmaxf(top, p[i]);
+    }
+    top = fmaf(max_of_quarters(top), c, ve);
     if (__any(top > m + 7.f)) {
       const float up = fmaxf(m, top), f = m == up ? 1.f : exp2f(m - up);
       m = up;
       sum *= f;
 #pragma unroll
-      for (int t = 0; t < Wd::kBlocks; ++t)
+      for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] *= f;
+        for (int i = 0; i < 4; ++i) o[t][i] *= f;
     }
     const float off = ve + 8.f - m;
-    float p[16], part = 0.f;
+    float part = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, off));
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, off));
       part += p[i];
     }
     sum = fmaf(part, exp2_of(max(base - ev, -126)), sum);
-    const Pieces pp[2] = {split8(p), split8(p + 8)};
+    const Pieces pp = split8(p);
 #pragma unroll
-    for (int t = 0; t < Wd::kBlocks; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) o[t] = mma(split8(v + 16 * t + 8 * h, exp2_of(14 - ev)), pp[h], o[t]);
-    load_v(j0 + W * T);
+    for (int t = 0; t < kBlocks; ++t) o[t] = mma16(Rows<DH, T>::by_column16(vs, t), pp, o[t]);
   }
-  sum = sum_of_halves(sum);
+  sum = sum_of_quarters(sum);
   const float f = sum == 0.f ? 0.f : kUnit * exp2_of(base) / sum;   // a wave without states: 0
-  if (l32 < s.R) {
-    store_column<Wd::kBlocks, false>(&ys[w][l32][0], 0, DH, [&](int t, int i) { return o[t][i] * f; });
-    if (half == 0) ls[w][l32] = bad ? NAN : sum == 0.f ? -INFINITY : m - 8.f + log2f(sum);
-  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int t = 0; t < kBlocks; ++t)
+    *reinterpret_cast<float4*>(ys(w, l16, 16 * t + 4 * quarter)) =
+        make_float4(o[t][0] * f, o[t][1] * f, o[t][2] * f, o[t][3] * f);
+  if (quarter == 0) ls[w][l16] = bad ? NAN : sum == 0.f ? -INFINITY : m - 8.f + log2f(sum);
   __syncthreads();
   for (int u = threadIdx.x; u < s.R * DH; u += 64 * W) {
     const int r = u / DH, d = u % DH;
     float most = -INFINITY, total = 0.f, acc = 0.f;
 #pragma unroll
-    for (int k = 0; k < W; ++k) most = fmaxf(most, ls[k][r]);
+    for (int x = 0; x < W; ++x) most = fmaxf(most, ls[x][r]);
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      const float l = ls[k][r];
+    for (int x = 0; x < W; ++x) {
+      const float l = ls[x][r];
       if (l == -INFINITY) continue;   // (a NaN goes on)
       const float g = exp2f(l - most);
       total += g;
-      acc = fmaf(g, ys[k][r][d], acc);
+      acc = fmaf(g, *ys(x, r, d), acc);
     }
-    if (bad) total = NAN;
     if (d < s.dh)
       y[at.slice * y_slice + query_row(s, at.b, at.hk, r) + d] = total == 0.f ? 0.f : acc / total;
     if (d == 0)
@@ -716,10 +776,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(const float* __re
     for (int d0 = 0; d0 < s.dh; d0 += 64) {
       const int d = d0 + lane;
       float acc = 0.f;
-#pragma unroll 4
-      for (int k = 0; k < slices; ++k) {
-        const float x = part[k * y_size + row * s.dh + min(d, s.dh - 1)];
-        acc = fmaf(__shfl(g, k, 64), x, acc);
+      for (int k0 = 0; k0 < slices; k0 += 4) {   // four loads in flight
+        float x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          x[k] = part[min(k0 + k, slices - 1) * y_size + row * s.dh + min(d, s.dh - 1)];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc = fmaf(__shfl(g, k0 + k, 64), x[k], acc);   // (0 past the last)
       }
       if (d < s.dh) y[row * s.dh + d] = acc;
     }
@@ -1275,13 +1338,10 @@ int64_t slice_of(int64_t n, int64_t slices, int64_t tile) {
 }
 
 // Workgroups to aim for, and the fewest tiles a slice is worth cutting off for.
-#ifndef FEWW
-#define FEWW 512
-#endif
-constexpr int64_t kWant = 512, kFewWant = FEWW, kMinTiles = 2;
-int64_t slices_for(int64_t groups, int64_t tiles, int64_t want = kWant) {
+constexpr int64_t kWant = 512, kFewWant = 256, kMinTiles = 2;
+int64_t slices_for(int64_t groups, int64_t tiles, int64_t want = kWant, int64_t least = kMinTiles) {
   if (groups >= want) return 1;
-  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, groups), tiles / kMinTiles,
+  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, groups), tiles / least,
                                                   kMaxAttentionSlices}));
 }
 bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows && a.dh <= 128; }
@@ -1307,7 +1367,7 @@ bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows &&
 
 int64_t attention_key_slices(const AttendShape& a, bool fwd) {
   if (fwd && few_rows(a))
-    return slices_for(a.B * a.Hkv, ceil_div(a.Tk, 32 * kFewWaves), kFewWant);
+    return slices_for(a.B * a.Hkv, ceil_div(a.Tk, 32 * kFewWaves), kFewWant, 1);
   const int64_t tiles = ceil_div(a.Tq * (a.H / a.Hkv), fwd ? fwd_columns(a.dh) : back_columns(a.dh));
   return slices_for(a.B * a.Hkv * tiles, ceil_div(a.Tk, fwd ? tile_rows(a.dh) : back_rows(a.dh)));
 }
