@@ -56,14 +56,11 @@ struct Width {
   static constexpr int kChunks = DH / 8;
   static constexpr int kLanes = DH == 32 ? 4 : DH == 64 ? 8 : DH <= 128 ? 16 : 32;   // that load a row
   static constexpr int kRow = (DH == 32 ? 7 : DH == 64 ? 9 : DH == 96 ? 13 : DH == 128 ? 19 : 35) * 16;
-  // The forward: rows of a tile, waves of a workgroup, sets of 32 columns a wave, waves that share
-  // columns, each with its part of the sums (where registers hold no more), blocks it then sums.
+  // The forward: rows of a tile, waves that share columns, each with its part of the sums (where
+  // registers hold no more), blocks it then sums.
   static constexpr int kTile = DH <= 64 ? 64 : 32;
-  static constexpr int kFwdWaves = DH <= 64 ? 4 : DH <= 128 ? 8 : 4;
-  static constexpr int kSets = DH <= 64 ? 2 : 1;
   static constexpr int kParts = DH <= 128 ? 1 : 2;
   static constexpr int kSums = kBlocks / kParts;
-  static constexpr int kFwdCols = 32 * kFwdWaves * kSets / kParts;
   // The backward up to 64 head columns: rows of a tile, waves of a workgroup.
   static constexpr int kBackTile = 64, kBackWaves = 4;
   // The backward above, by pairs of waves: waves of a workgroup, tile buffers, waves a SIMD holds.
@@ -437,13 +434,22 @@ struct Raw {
 };
 
 // ---------------------------------------------------------------- forward
-template <int DH, bool EXACT>
-__global__ __launch_bounds__(64 * Width<DH>::kFwdWaves, DH <= 128 ? 2 : 1) void fwd_kernel(
+// A workgroup of wide() has 256 columns: up to 64 head columns two sets of 32 a wave, so that each
+// A operand is read for both; above, eight waves, so that a tile is split once for all. Others have
+// 128 (above 128 head columns, 64).
+template <int DH, bool WIDE>
+struct Forward {
+  static constexpr int kWaves = WIDE && DH > 64 ? 8 : 4;
+  static constexpr int kSets = WIDE && DH <= 64 ? 2 : 1;
+  static constexpr int kCols = 32 * kWaves * kSets / Width<DH>::kParts;
+};
+template <int DH, bool EXACT, bool WIDE>
+__global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1) void fwd_kernel(
     const float* __restrict__ q, const float* __restrict__ kv, const int32_t* __restrict__ klen,
     float* __restrict__ y, float* __restrict__ lse, Shape s, int tiles, int slice_len,
     int64_t y_slice, int64_t lse_slice) {
   using Wd = Width<DH>;
-  constexpr int T = Wd::kTile, W = Wd::kFwdWaves, C = Wd::kSets;
+  constexpr int T = Wd::kTile, W = Forward<DH, WIDE>::kWaves, C = Forward<DH, WIDE>::kSets;
   using Rw = Rows<DH, T>;
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
@@ -451,7 +457,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kFwdWaves, DH <= 128 ? 2 : 1) void 
   const Place at = place(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-  const int col0 = at.tile * Wd::kFwdCols + w / Wd::kParts * 32 * C + (lane & 31);
+  const int col0 = at.tile * Forward<DH, WIDE>::kCols + w / Wd::kParts * 32 * C + (lane & 31);
   const int first = w % Wd::kParts * Wd::kSums;
   const int n = klen[at.b];
   const bool bad = n < 0 || n > s.Tk;
@@ -1301,8 +1307,14 @@ __global__ void sum_kernel(const float* __restrict__ part, float* __restrict__ o
                            int64_t size) {
   const int64_t stride = (int64_t)gridDim.x * blockDim.x;
   for (int64_t u = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u < size; u += stride) {
-    float acc = part[u];
-    for (int k = 1; k < slices; ++k) acc += part[k * size + u];
+    float acc = 0.f;
+    for (int k0 = 0; k0 < slices; k0 += 8) {   // eight loads in flight
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = k0 + k < slices ? part[(k0 + k) * size + u] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc += x[k];
+    }
     out[u] = acc;
   }
 }
@@ -1321,9 +1333,6 @@ Shape shape_of(const AttendShape& a) {
 }
 
 int tile_rows(int64_t dh) { return dh <= 64 ? Width<64>::kTile : 32; }
-int fwd_columns(int64_t dh) {
-  return dh <= 64 ? Width<64>::kFwdCols : dh <= 128 ? Width<128>::kFwdCols : Width<256>::kFwdCols;
-}
 int back_columns(int64_t dh) {
   return dh <= 64 ? Width<64>::kBackCols : dh <= 128 ? Width<128>::kBackCols : Width<256>::kBackCols;
 }
@@ -1332,6 +1341,16 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 dim3 grid_of(const Shape& s, int tiles, int64_t slices) {
   return dim3((unsigned)(ceil_div((int64_t)s.B * s.Hkv, kXcds) * kXcds * tiles), (unsigned)slices);
 }
+// Whether the forward's workgroups have 256 columns, not 128: where that leaves less than a tenth
+// more columns idle, which is what the wide ones gain (4096 x 4096: 0.79 against 0.87 ms at 2 x 16
+// heads of 128, 0.93 against 1.03 at 4 x 16 heads of 64; 333 queries, 12 heads of 85: 87 us wide,
+// 63 narrow), and there are two of them for each CU (77 states, 2 x 4096 queries, 8 heads of 64:
+// 17.4 us wide, 16.4 narrow).
+bool wide(const AttendShape& a) {
+  const int64_t halves = ceil_div(a.Tq * (a.H / a.Hkv), 128);
+  return a.dh <= 128 && (halves % 2 == 0 || halves >= 10) && a.B * a.Hkv * ceil_div(halves, 2) >= 512;
+}
+int fwd_columns(const AttendShape& a) { return wide(a) ? 256 : a.dh <= 128 ? 128 : 64; }
 unsigned flat_grid(int64_t n) { return (unsigned)std::min<int64_t>(ceil_div(n, 256), 4096); }
 int64_t slice_of(int64_t n, int64_t slices, int64_t tile) {
   return ceil_div(ceil_div(n, slices), tile) * tile;
@@ -1346,20 +1365,31 @@ int64_t slices_for(int64_t groups, int64_t tiles, int64_t want = kWant, int64_t 
 }
 bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows && a.dh <= 128; }
 
-#define UP_TO_64(CALL)                     \
+#define TO_64(CALL)                        \
   if (s.dh == 32) CALL(32, true);          \
   else if (s.dh < 32) CALL(32, false);     \
   else if (s.dh == 64) CALL(64, true);     \
   else CALL(64, false)
-#define TO_128(CALL)                       \
+#define FROM_65_TO_128(CALL)               \
   if (s.dh == 96) CALL(96, true);          \
   else if (s.dh < 96) CALL(96, false);     \
   else if (s.dh == 128) CALL(128, true);   \
   else CALL(128, false)
-#define ABOVE_64(CALL)                     \
+#define TO_128(CALL)                       \
+  if (s.dh <= 64) {                        \
+    TO_64(CALL);                           \
+  } else {                                 \
+    FROM_65_TO_128(CALL);                  \
+  }
+#define ABOVE_128(CALL)                    \
   if (s.dh == 256) CALL(256, true);        \
-  else if (s.dh > 128) CALL(256, false);   \
-  else TO_128(CALL)
+  else CALL(256, false)
+#define ABOVE_64(CALL)                     \
+  if (s.dh > 128) {                        \
+    ABOVE_128(CALL);                       \
+  } else {                                 \
+    FROM_65_TO_128(CALL);                  \
+  }
 #define LAUNCH(KERNEL, WAVES, TILES, SLICES, ...) \
   hipLaunchKernelGGL(KERNEL, grid_of(s, TILES, SLICES), dim3(64 * WAVES), 0, st, __VA_ARGS__)
 
@@ -1368,7 +1398,7 @@ bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows &&
 int64_t attention_key_slices(const AttendShape& a, bool fwd) {
   if (fwd && few_rows(a))
     return slices_for(a.B * a.Hkv, ceil_div(a.Tk, 32 * kFewWaves), kFewWant, 1);
-  const int64_t tiles = ceil_div(a.Tq * (a.H / a.Hkv), fwd ? fwd_columns(a.dh) : back_columns(a.dh));
+  const int64_t tiles = ceil_div(a.Tq * (a.H / a.Hkv), fwd ? fwd_columns(a) : back_columns(a.dh));
   return slices_for(a.B * a.Hkv * tiles, ceil_div(a.Tk, fwd ? tile_rows(a.dh) : back_rows(a.dh)));
 }
 int64_t attention_query_slices(const AttendShape& a) {
@@ -1380,29 +1410,28 @@ hipError_t cross_attention_fwd(const float* q, const float* kv, const int32_t* k
                                hipStream_t st) {
   const Shape s = shape_of(a);
   const bool few = few_rows(a);
-  const int tiles = few ? 1 : (int)ceil_div(s.R, fwd_columns(s.dh));
+  const int tiles = few ? 1 : (int)ceil_div(s.R, fwd_columns(a));
   const int len = (int)slice_of(s.Tk, slices, few ? 32 : tile_rows(s.dh));
   const int64_t size = a.B * a.Tq * s.ldq, rows = a.B * a.H * a.Tq;
   float* yo = slices > 1 ? part : y;
   float* lo = slices > 1 ? part + slices * size : lse;
-#define FWD(D, X)                                                                              \
-  LAUNCH((fwd_kernel<D, X>), Width<D>::kFwdWaves, tiles, slices, q, kv, klen, yo, lo, s, tiles, len, \
-         size, rows)
-#define FEW(D, X)                                                                                \
-  LAUNCH((few_kernel<D, X>), kFewWaves, tiles, slices, q, kv, klen, yo, lo, s, tiles, len, size, rows)
+#define ARGS q, kv, klen, yo, lo, s, tiles, len, size, rows
+#define FEW(D, X) LAUNCH((few_kernel<D, X>), kFewWaves, tiles, slices, ARGS)
+#define WIDE(D, X) LAUNCH((fwd_kernel<D, X, true>), (Forward<D, true>::kWaves), tiles, slices, ARGS)
+#define FWD(D, X) LAUNCH((fwd_kernel<D, X, false>), (Forward<D, false>::kWaves), tiles, slices, ARGS)
   if (few) {
-    if (s.dh <= 64) {
-      UP_TO_64(FEW);
-    } else {
-      TO_128(FEW);
-    }
-  } else if (s.dh <= 64) {
-    UP_TO_64(FWD);
+    TO_128(FEW);
+  } else if (wide(a)) {
+    TO_128(WIDE);
+  } else if (s.dh <= 128) {
+    TO_128(FWD);
   } else {
-    ABOVE_64(FWD);
+    ABOVE_128(FWD);
   }
-#undef FEW
 #undef FWD
+#undef WIDE
+#undef FEW
+#undef ARGS
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || slices == 1) return e;
   hipLaunchKernelGGL(join_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(rows, kJoinWaves), 8192)),
@@ -1424,7 +1453,7 @@ hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* k
 #define DQ(D, X) LAUNCH((dq_kernel<D, X>), Width<D>::kBackWaves, tiles, q_slices, ARGS)
 #define DQ_PAIR(D, X) LAUNCH((dq_pair_kernel<D, X>), Width<D>::kPairWaves, tiles, q_slices, ARGS)
     if (s.dh <= 64) {
-      UP_TO_64(DQ);
+      TO_64(DQ);
     } else {
       ABOVE_64(DQ_PAIR);
     }
@@ -1446,7 +1475,7 @@ hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* k
 #define DKV(D, X) LAUNCH((dkv_kernel<D, X>), Width<D>::kBackWaves, tiles, kv_slices, ARGS)
 #define DKV_PAIR(D, X) LAUNCH((dkv_pair_kernel<D, X>), Width<D>::kPairWaves, tiles, kv_slices, ARGS)
   if (s.dh <= 64) {
-    UP_TO_64(DKV);
+    TO_64(DKV);
   } else {
     ABOVE_64(DKV_PAIR);
   }
