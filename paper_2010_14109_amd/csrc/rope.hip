@@ -11,8 +11,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdint>
+#include <initializer_list>
 
-#include "fastdiv.h"
 #include "kernels.h"
 
 namespace ooc {
@@ -38,13 +39,32 @@ __device__ inline float2 turn(int32_t pos, double f, float m) {
   return make_float2(m * (q == 1 || q == 2 ? -cs : cs), m * (q >= 2 ? -sn : sn));
 }
 
+// x / d for 0 <= x < 2^31 and an invariant d >= 1 by one multiply-high (Granlund and Montgomery,
+// 1994): with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, floor(x m / 2^(31 + l)) is the
+// quotient.  d = 1 has l = 0 and would need m = 2^31 + 1 at a shift of -1: it takes m = 2^32 - 1 and
+// x + 1.
+struct Divisor {
+  uint32_t m = 0xffffffffu, shift = 0, add = 1;
+  static Divisor of(int d) {
+    Divisor r;
+    if (d <= 1) return r;
+    uint32_t l = 0;
+    while ((1u << l) < (uint32_t)d) ++l;
+    r.m = (uint32_t)((1ull << (31 + l)) / (uint32_t)d + 1);
+    r.shift = l - 1;
+    r.add = 0;
+    return r;
+  }
+  __device__ int div(int x) const { return (int)(__umulhi((uint32_t)x + add, m) >> shift); }
+};
+
 // What a launch knows of its rows.
 struct Rows {
   int64_t rows;
   int cols, dh, heads, used, half, layout;   // used = heads dh, half = rot / 2
   int h1;                                    // heads of the first gain
   int tile;                                  // rows a workgroup takes at once
-  FastDiv by_half, by_dh, by_heads, by_items;
+  Divisor by_half, by_dh, by_heads, by_items;
   int items;                                 // of a row: V columns each
 };
 
@@ -407,10 +427,10 @@ Rows rows_of(const RopeShape& s, int64_t h1, int V, int64_t rows_a_group) {
   // Rows a workgroup takes: their turns keep its threads busy at 8 rows of 64 rotated columns, and
   // a launch has at least 1024 workgroups where it has the rows for them.
   r.tile = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxTile, rows_a_group));
-  r.by_half = FastDiv::make(r.half);
-  r.by_dh = FastDiv::make(r.dh);
-  r.by_heads = FastDiv::make(r.heads);
-  r.by_items = FastDiv::make(r.items);
+  r.by_half = Divisor::of(r.half);
+  r.by_dh = Divisor::of(r.dh);
+  r.by_heads = Divisor::of(r.heads);
+  r.by_items = Divisor::of(r.items);
   return r;
 }
 unsigned blocks(int64_t rows, int64_t tile) { return (unsigned)((rows + tile - 1) / tile); }
