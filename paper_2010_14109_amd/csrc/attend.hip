@@ -173,10 +173,11 @@ __device__ inline __amdgpu_buffer_rsrc_t buffer(const float* p, int64_t values) 
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), 0, (int)((uint32_t)n * 4u),
                                            0x00020000);
 }
-// eight values at a byte offset (of any 4-byte alignment); what lies past the length is zero
+// eight values at a byte offset (of any 4-byte alignment); what lies past the length is zero.  (Both
+// offsets are the lane's, which the length is compared with.)
 __device__ inline void load8(__amdgpu_buffer_rsrc_t r, uint32_t off, float* v) {
   const float4 a = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
-  const float4 b = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 16, 0));
+  const float4 b = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(off + 16u), 0, 0));
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
   v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
