@@ -441,6 +441,9 @@ class Net:
                    kind=ooc.INPUT)
         self.inputs = {"x"}
         for v in spec.get("inputs", ()):
+            taken = [*self.shape, "labels", *(L["name"] for L in spec["layers"])]
+            if v["name"] in taken:
+                raise ValueError(f"{v['name']}: the name of two tensors")
             self.shape[v["name"]] = tuple(v["shape"])
             self._decl(v["name"], v["shape"], dtype=v["dtype"], kind=ooc.INPUT)
             self.inputs.add(v["name"])
