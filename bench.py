@@ -92,6 +92,14 @@ def fn_work(op, attrs):
         B, T, H, dh, causal = a[:5]
         pairs = T * (T + 1) // 2 if causal else T * T
         return "flop", (2 if op == "attention_fwd" else 5) * 2 * B * H * pairs * dh
+    if op in ("rope_fwd", "rope_bwd", "qknorm_fwd"):
+        return "byte", 8 * a[0] * a[1] + 4 * a[0]
+    if op == "qknorm_bwd":
+        return "byte", 12 * a[0] * a[1] + 4 * a[0]
+    if op in ("cross_attention_fwd", "cross_attention_bwd"):
+        # two products of every query and state forward, five backward
+        B, Tq, Tk, H, Hkv, dh = a[:6]
+        return "flop", (2 if op.endswith("fwd") else 5) * 2 * B * H * Tq * Tk * dh
     return "byte", 0
 
 
@@ -270,6 +278,8 @@ def run_mode(net, spec, x, labels, params, budget, window, chunk, steps, warmup,
         ctx.prepare()
         net.view(ctx, "x")[...] = x
         net.view(ctx, "labels")[...] = labels
+        for name, value in synth.make_extra_inputs(spec).items():
+            net.view(ctx, name)[...] = value
         for name in net.param_names():
             net.view(ctx, name)[...] = params[name]
         for name in net.names:
@@ -362,21 +372,22 @@ def cpu_baseline(name, budget_seconds=15.0):
     from oracle.interp import run as oracle_run
     from oracle.lower import lower
     small = {"mlp": 256, "cnn": 8, "resnet50_b256": 2, "resnet50_b1440": 2,
-             "transformer": 1, "densenet": 2, "unet": 1}[name]
+             "transformer": 1, "seq2seq": 1, "densenet": 2, "unet": 1}[name]
     spec = synth.workload(name, batch=small)
     reg = lower(spec)
     x, labels = synth.make_inputs(spec, 0)
     params = synth.make_params(spec, 1)
+    extra = synth.make_extra_inputs(spec)
     try:
         from threadpoolctl import threadpool_info
         threads = max([p.get("num_threads", 1) for p in threadpool_info()] or [1])
     except Exception:  # noqa: BLE001 - informational only
         threads = len(os.sched_getaffinity(0))
-    oracle_run(reg, x, labels, params, dtype=np.float32)     # warm-up
+    oracle_run(reg, x, labels, params, dtype=np.float32, inputs=extra)     # warm-up
     n = 0
     t0 = time.perf_counter()
     while True:
-        oracle_run(reg, x, labels, params, dtype=np.float32)
+        oracle_run(reg, x, labels, params, dtype=np.float32, inputs=extra)
         n += 1
         el = time.perf_counter() - t0
         if el >= budget_seconds or n >= 1000:

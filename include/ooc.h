@@ -169,7 +169,8 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                for layout 1; all other columns are copied.  pos is one int32 per row,
  *                table rot/2 doubles (radians per position of pair i) then one double, a
  *                magnitude m: with a = pos table[i], a double,
- *                (y0, y1) = m (x0 cos a - x1 sin a, x0 sin a + x1 cos a)
+ *                (y0, y1) = m (x0 cos a - x1 sin a, x0 sin a + x1 cos a);
+ *                |a| < 2^52; rot even, 2..1024; cols at most 2^24
  *                                     X[R] pos[R] table[R] Y[W]    rows cols heads dh rot layout
  *  ROPE_BWD      the transposed rotation: (dx0, dx1) = m (dy0 cos a + dy1 sin a,
  *                dy1 cos a - dy0 sin a)
@@ -177,7 +178,8 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *  QKNORM_FWD    per row, the first h1 heads of dh columns are divided by their root mean
  *                square sqrt(mean x^2 + 1e-5) and scaled by gain row 0, the next h2 heads by
  *                gain row 1 (gain [1 + (h2 > 0)][dh]), then rotated as by ROPE_FWD; all other
- *                columns are copied.  rot = 0: no rotation, and no pos and table
+ *                columns are copied.  rot = 0: no rotation, and no pos and table.  dh at
+ *                most 1024; squares are taken in fp32, so |x| up to 1e18
  *                                     X[R] gain[R] [pos[R] table[R]] Y[W]
  *                                                                  rows cols h1 h2 dh rot layout
  *  QKNORM_BWD    dX and dgain of the above; part = one partial dgain per row slice
@@ -190,8 +192,11 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                in the second; query head h reads key head h Hkv / H (Hkv divides H), dh <= 256:
  *                S = q k^T / sqrt(dh), Y [B Tq][H dh] = softmax(S) v, lse [B][H][Tq] = ln sum
  *                exp S.  klen 0: Y = 0 and lse = -inf; klen outside 0..Tk: NaN.  States at and
- *                past klen may hold anything.  part = partial results, present iff slices > 1
- *                (ooc_attention_slices gives counts and its bytes)
+ *                past klen may hold anything.  Sums are fp32.  Values from 2^-100 to 2^100:
+ *                those more than 2^38 below the largest of the 32 or 64 rows they are read with
+ *                lose their last bits or count as zero; an infinity or a NaN among them gives NaN
+ *                in the results that it reaches.  H dh and Hkv dh at most 2^20.  part = partial
+ *                results, present iff slices > 1 (ooc_attention_slices gives counts and its bytes)
  *                                     q[R] kv[R] klen[R] Y[W] lse[W] [part[W]]
  *                                                                  B Tq Tk H Hkv dh slices
  *  CROSS_ATTENTION_BWD

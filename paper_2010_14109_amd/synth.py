@@ -397,18 +397,21 @@ def make_inputs(spec, seed=0):
     return x, labels
 
 
-def make_extra_inputs(spec, tables, seed=2):
+def make_extra_inputs(spec, tables=None, seed=2):
     """``{name: array}`` of ``spec["inputs"]``: tokens uniform over the vocabulary, lengths uniform
-    over 1 .. the sequence, positions counting up in each sequence, and ``tables`` (name -> table
-    of angles)."""
+    over 1 .. the sequence, positions counting up in each sequence, and tables of angles:
+    ``tables[name]``, or 10000^(-2 i / rot) radians per position and magnitude 1."""
     g = np.random.Generator(np.random.PCG64(seed))
     shapes = {v["name"]: tuple(v["shape"]) for v in spec.get("inputs", ())}
     batch = spec["input"][0]
     out = {}
     for v in spec.get("inputs", ()):
         name, shape = v["name"], tuple(v["shape"])
-        if name in tables:
+        if name in (tables or {}):
             out[name] = np.asarray(tables[name], np.float64).reshape(shape)
+        elif v["dtype"] == "f64":
+            half = shape[0] - 1
+            out[name] = np.append(10000.0 ** (-np.arange(half) / half), 1.0)
         elif name.endswith("_len"):
             out[name] = g.integers(1, shapes[name[:-4]][1] + 1, size=shape).astype(np.int32)
         elif name.endswith("pos"):

@@ -70,10 +70,11 @@ class Stream:
         if getattr(self, "ptr", None):
             hip().hipStreamDestroy(ctypes.c_void_p(self.ptr))
 
-    def record(self, calls):
-        """A graph of what ``calls()`` enqueues on this stream, as a function that replays it."""
+    def record(self, calls, mode=2):
+        """A graph of what ``calls()`` enqueues on this stream, as a function that replays it.
+        ``mode``: hipStreamCaptureMode (0 global, 2 relaxed)."""
         s, graph, run = ctypes.c_void_p(self.ptr), ctypes.c_void_p(), ctypes.c_void_p()
-        check(hip().hipStreamBeginCapture(s, 2), "hipStreamBeginCapture")
+        check(hip().hipStreamBeginCapture(s, mode), "hipStreamBeginCapture")
         try:
             calls()
         finally:

@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 
 import attention_util as au
+import bench
 from oracle import ops
 from oracle import schedule as S
 from oracle.lower import lower
@@ -356,3 +357,37 @@ def test_run_fn_refusals_before_the_device(lib):
     b, a = (C.c_uint64 * 1)(64), (C.c_uint8 * 1)(R)
     assert lib.ooc_run_fn(0, None, 4, p, b, a, 1, None, 3) == ooc.E_INVALID
     assert lib.ooc_qknorm_slices(3, None) == ooc.E_INVALID
+
+
+def test_extra_inputs_of_a_workload():
+    spec = small_seq2seq(layers=1)
+    a, b = synth.make_extra_inputs(spec), synth.make_extra_inputs(spec)
+    assert sorted(a) == sorted(v["name"] for v in spec["inputs"])
+    for v in spec["inputs"]:
+        np.testing.assert_array_equal(a[v["name"]], b[v["name"]])
+        assert list(a[v["name"]].shape) == list(v["shape"])
+    src = a["src"]
+    assert src.min() >= 0 and src.max() < spec["classes"]
+    assert a["src_len"].min() >= 1 and a["src_len"].max() <= src.shape[1]
+    np.testing.assert_array_equal(a["src_pos"], np.tile(np.arange(src.shape[1]), src.shape[0]))
+    half = a["table"].shape[0] - 1
+    np.testing.assert_allclose(a["table"], netdef.rotary_table(2 * half), rtol=1e-14)
+    given = np.full(half + 1, 0.25)
+    np.testing.assert_array_equal(synth.make_extra_inputs(spec, {"table": given})["table"], given)
+
+
+def test_two_tensors_of_one_name_are_refused():
+    spec = small_seq2seq(layers=1)
+    for name in (spec["inputs"][0]["name"], spec["layers"][0]["name"], "x", "labels"):
+        wrong = dict(spec, inputs=spec["inputs"] + [{"name": name, "shape": [4], "dtype": "i32"}])
+        with pytest.raises(ValueError, match="two tensors"):
+            netdef.Net(wrong)
+
+
+def test_work_of_the_operators():
+    assert bench.fn_work("rope_fwd", [6, 32, 2, 16, 8, 0]) == ("byte", 8 * 6 * 32 + 24)
+    assert bench.fn_work("qknorm_bwd", [6, 32, 1, 1, 16, 0, 0, 1]) == ("byte", 12 * 6 * 32 + 24)
+    assert bench.fn_work("cross_attention_fwd", [2, 3, 5, 4, 2, 8, 1]) == \
+        ("flop", 2 * 2 * 2 * 4 * 3 * 5 * 8)
+    assert bench.fn_work("cross_attention_bwd", [2, 3, 5, 4, 2, 8, 1, 1]) == \
+        ("flop", 5 * 2 * 2 * 4 * 3 * 5 * 8)

@@ -351,7 +351,7 @@ def test_streams_and_graphs():
     # the inputs of the attention are themselves rounded: ten times the bound of exact inputs
     by = au.cross_bounds(r.astype(np.float32), kv, klen, dy, a)[0]
     au.within("y of the chain", eager[2], wy, 10 * by)
-    replays = [s.record(d["calls"]) for s, d in zip(streams, sets)]
+    replays = [s.record(d["calls"], mode) for s, d, mode in zip(streams, sets, (0, 2))]
     import ctypes
     for step in range(4):
         src = x if step % 2 == 0 else x2
