@@ -83,7 +83,10 @@ std::string check_attention_shape(const int64_t* a) {
     return "sequence, head or batch count too large";
   // and the bytes from a row to the 64th behind it
   if (product({H, dh}) > (1 << 20) || product({Hkv, dh}) > (1 << 20)) return "rows too wide";
-  if (B * Hkv * (std::max(Tq * (H / Hkv), Tk) / 64 + 1) > (1 << 28)) return "too many tiles";
+  // a launch has fewer than 2^32 threads: workgroups of at most 512, each of 128 columns or more (64
+  // above 128 head columns) of the queries or the states
+  if ((B * Hkv + 7) * (std::max(Tq * (H / Hkv), Tk) / (dh <= 128 ? 128 : 64) + 1) >= (1 << 23))
+    return "too many workgroups";
   if (product({B, Tq, H, dh, 4}) < 0 || product({B, Tk, Hkv, dh, 8}) < 0) return "tensor too large";
   return "";
 }

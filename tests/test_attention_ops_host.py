@@ -285,6 +285,8 @@ def test_signatures(lib, op, attrs):
     ("cross_attention_fwd", [1 << 25, 1, 1, 1, 1, 1, 1]),
     ("cross_attention_fwd", [1, 1, 1 << 29, 1, 1, 1, 1]),
     ("cross_attention_fwd", [1 << 12, 1 << 28, 1 << 28, 16, 16, 256, 1]),
+    ("cross_attention_fwd", [1 << 16, 1 << 14, 64, 8, 8, 16, 1]),
+    ("cross_attention_bwd", [1 << 16, 1, 1 << 14, 8, 8, 200, 1, 1]),
     ("cross_attention_bwd", [2, 3, 70, 4, 2, 10, 5, 7]), ("cross_attention_bwd", [2, 3, 70, 4, 2, 10, 5, 0]),
 ], ids=lambda v: str(v))
 def test_attributes_out_of_their_ranges(lib, op, attrs):
