@@ -584,10 +584,10 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
 // reading the states once.  Each wave takes tiles of 32 states of its own, without barriers: k goes
 // from memory straight into the A operand, v through the wave's part of LDS.  A workgroup's waves
 // and then the slices join their results.  Products are 16 x 16 x 32: 16 columns are all there is,
-// and half the registers of 32 let a SIMD hold three waves, whose loads are all in flight at once.  One token of 8 sequences against 4096
-// states, 16 heads of 64 on 4 key heads: 33.9 -> 18.6 us
-// (the first kernel 14, the join 4; 17 MB at the rate of a large copy take 3.5) against the kernel
-// for many queries.
+// and half the registers of 32 let a SIMD hold three waves, whose loads are all in flight at once.
+// One token of 8 sequences of up to 4096 states, 16 heads of 64 on 4 key heads: 33.9 us with the
+// kernel for many queries, 18 with this one (14, and 4 for the join; reading the 34 MB at the rate of
+// a large copy takes 7).
 constexpr int kFewWaves = 4, kFewRows = 16;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 __device__ inline floatx4 mma16(const Pieces& a, const Pieces& b, floatx4 c) {
@@ -811,6 +811,9 @@ __device__ inline void rescale(float top, float& f, floatx16 (&acc)[N]) {
     for (int i = 0; i < 16; ++i) acc[t][i] *= up;
 }
 constexpr float kFirst = 0x1p126f;   // f before the first values
+// A column's scale times a matrix's, finite: where the product is not, the values are zero or below
+// 2^-111.
+__device__ inline float both(float f, float g) { return fminf(f * g, 0x1p126f); }
 
 // Loads the row tiles of the pass over the queries: rows i .. of the group's heads, numbered g Tq +
 // position.  A tile stays within a head where a head fills one, else it packs the group's heads.
@@ -917,7 +920,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dq_kernel(
       // dS 2^(e.x - 14) is what meets the pieces of k
       top = max_of_halves(top) * kf;
       if (__any(passes(top, f))) rescale(top, f, acc);
-      const Pieces xp[2] = {split8(x, f * kf), split8(x + 8, f * kf)};
+      const Pieces xp[2] = {split8(x, both(f, kf)), split8(x + 8, both(f, kf))};
 #pragma unroll
       for (int t = 0; t < Wd::kBlocks; ++t)
 #pragma unroll
@@ -1014,13 +1017,13 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
         rescale(xtop, fk, dk);
       }
       {
-        const Pieces pp[2] = {split8(p, fv * gf), split8(p + 8, fv * gf)};
+        const Pieces pp[2] = {split8(p, both(fv, gf)), split8(p + 8, both(fv, gf))};
 #pragma unroll
         for (int t = 0; t < Wd::kBlocks; ++t)
 #pragma unroll
           for (int h = 0; h < 2; ++h) dv[t] = mma(Rw::by_column(gs, r0 + 16 * h, t), pp[h], dv[t]);
       }
-      const Pieces xp[2] = {split8(x, fk * qf), split8(x + 8, fk * qf)};
+      const Pieces xp[2] = {split8(x, both(fk, qf)), split8(x + 8, both(fk, qf))};
 #pragma unroll
       for (int t = 0; t < Wd::kBlocks; ++t)
 #pragma unroll
@@ -1150,7 +1153,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
       }
       top = max_of_halves(top) * kf;
       if (__any(passes(top, f))) rescale(top, f, acc);
-      const Pieces pp = split8(p, f * kf);
+      const Pieces pp = split8(p, both(f, kf));
       const auto advance = [&] {
         e = stage(NB - 1 - buf);
         fetch(j0 + 2 * T);
@@ -1277,7 +1280,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
       const float other = exp2_of((role ? e.x : e.y) - 14);
       top = max_of_halves(top) * other;
       if (__any(passes(top, f))) rescale(top, f, acc);
-      const Pieces pp[2] = {split8(v, f * other), split8(v + 8, f * other)};
+      const Pieces pp[2] = {split8(v, both(f, other)), split8(v + 8, both(f, other))};
       const auto advance = [&] {
         e = stage(NB - 1 - buf);
         i += rows.rows_at(s, i);

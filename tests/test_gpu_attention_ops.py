@@ -270,6 +270,23 @@ def test_cross_attention_scales():
     check_cross(a, q, kv, klen, dy)
 
 
+@pytest.mark.parametrize("dh", [24, 64, 96, 256])
+def test_cross_attention_zero_gradients_of_large_states(dh):
+    """Tiles whose score gradients are all zero (no gradient arrives, or the probabilities vanish)
+    against states, queries and gradients far above 1."""
+    for i, (sq, sk, sv, sg) in enumerate(((2.0 ** -40, 2.0 ** 40, 1.0, 1.0), (2.0 ** 40, 2.0 ** -40, 1.0, 1.0),
+                                          (1.0, 1.0, 2.0 ** -30, 2.0 ** 50), (1.0, 1.0, 2.0 ** 60, 2.0 ** -60))):
+        a, q, kv, klen, dy = au.cross_case(80 + i, 2, 200, 150, 2, 1, dh, [150, 90])
+        n = kv.shape[1] // 2
+        dy[:100] = 0                   # the first rows of sequence 0
+        dy[200:] = 0                   # all of sequence 1
+        kv[:64, :n] *= np.float32(0.01)
+        kv[64:150, 0], q[:, ::dh] = 700 * dh ** 0.5, 1   # scores that leave the first tiles nothing
+        kv[:, :n] *= np.float32(sk)
+        kv[:, n:] *= np.float32(sv)
+        check_cross(a, q * np.float32(sq), kv, klen, dy * np.float32(sg))
+
+
 def test_cross_attention_gradient_of_the_forward_by_differences():
     """The device's gradients against differences of the device's own forward, at a step where
     truncation and rounding of the sum stay below a percent."""
