@@ -193,10 +193,11 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                S = q k^T / sqrt(dh), Y [B Tq][H dh] = softmax(S) v, lse [B][H][Tq] = ln sum
  *                exp S.  klen 0: Y = 0 and lse = -inf; klen outside 0..Tk: NaN.  States at and
  *                past klen may hold anything.  Sums are fp32.  Values from 2^-100 to 2^100 and
- *                their products within fp32's range: values more than 2^38 below the largest of the 32 or 64 rows they are read with
- *                lose their last bits or count as zero; an infinity or a NaN among them gives NaN
- *                in the results that it reaches.  H dh and Hkv dh at most 2^20.  part = partial
- *                results, present iff slices > 1 (ooc_attention_slices gives counts and its bytes)
+ *                their products within fp32's range: what lies more than 2^38 below the largest of
+ *                the 32 or 64 rows that it is read with loses its last bits or counts as zero; an
+ *                infinity or a NaN gives NaN in the results that it reaches.  H dh and Hkv dh at
+ *                most 2^20.  part = partial results, present iff slices > 1
+ *                (ooc_attention_slices gives counts and its bytes)
  *                                     q[R] kv[R] klen[R] Y[W] lse[W] [part[W]]
  *                                                                  B Tq Tk H Hkv dh slices
  *  CROSS_ATTENTION_BWD

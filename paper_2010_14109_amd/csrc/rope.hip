@@ -7,7 +7,8 @@
 // All of this is bound by the rows' traffic (8 bytes a value forward, 12 backward).  An angle
 // belongs to a row and a pair, not to a head: a workgroup takes a tile of rows, computes the tile's
 // cosines and sines once into LDS and uses them for every head.  Rows whose heads, rotated width and
-// length come in fours go in 16-byte loads (V = 4), others value by value (V = 1).
+// length come in fours go in aligned 16-byte loads; of others, the norms take 16 bytes at any
+// alignment, the rotation columns.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -78,57 +79,92 @@ __device__ inline void turns(float2* cs, const int32_t* __restrict__ pos,
   }
 }
 
-// V neighbouring values.
-template <int V>
-struct Val {
-  float v[V];
+// four neighbouring values, aligned to 16 bytes, or to 4
+typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
+struct Four {
+  float v[4];
 };
-template <int V>
-__device__ inline Val<V> load(const float* p) {
-  Val<V> x;
-  if constexpr (V == 4) {
-    const float4 t = *reinterpret_cast<const float4*>(p);
-    x.v[0] = t.x; x.v[1] = t.y; x.v[2] = t.z; x.v[3] = t.w;
-  } else {
-    x.v[0] = *p;
+__device__ inline Four load(const float* p) {
+  const float4 t = *reinterpret_cast<const float4*>(p);
+  return {{t.x, t.y, t.z, t.w}};
+}
+__device__ inline void store(float* p, const Four& x) {
+  *reinterpret_cast<float4*>(p) = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
+}
+// The same of a head of which `left` columns remain: four of them aligned to 16 bytes, or (ODD) as
+// many as there are, at any alignment, and zeros.
+template <bool ODD>
+__device__ inline Four load(const float* p, int left) {
+  if constexpr (!ODD) return load(p);
+  if (left >= 4) {
+    const float4u t = *reinterpret_cast<const float4u*>(p);
+    return {{t[0], t[1], t[2], t[3]}};
   }
+  Four x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x.v[e] = e < left ? p[e] : 0.f;
   return x;
 }
-template <int V>
-__device__ inline void store(float* p, const Val<V>& x) {
-  if constexpr (V == 4) *reinterpret_cast<float4*>(p) = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
-  else *p = x.v[0];
+template <bool ODD>
+__device__ inline void store(float* p, int left, const Four& x) {
+  if constexpr (!ODD) return store(p, x);
+  if (left >= 4) {
+    *reinterpret_cast<float4u*>(p) = float4u{x.v[0], x.v[1], x.v[2], x.v[3]};
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < left) p[e] = x.v[e];
 }
 
-// Where the other ends of the pairs of columns d .. d + V - 1 lie (the same V columns where pairs
-// are neighbours and V = 4), and those pairs' turns.
-template <int V>
+// The other end of the pair of column d < 2 half.
 __device__ inline int partner(int d, int half, int layout) {
-  if (layout) return d < half ? d + half : d - half;
-  return V == 4 ? d : d ^ 1;
+  return !layout ? d ^ 1 : d < half ? d + half : d - half;
 }
-// The columns d .. turned: own their values, other their partners', cs the row's turns.
-template <int V>
-__device__ inline Val<V> turned(const Val<V>& own, const Val<V>& other, int d, const float2* cs,
-                                int half, int layout, bool back) {
-  Val<V> y;
+// The partners of the columns d .. d + 3 of the head at p, for turned(): of pairs half a head apart;
+// neighbours have theirs at hand.
+template <bool ODD>
+__device__ inline Four partners(const float* p, int d, const Four& own, int half, int layout) {
+  if (!layout) return own;
+  if (!ODD || d + 4 <= half || (d >= half && d + 4 <= 2 * half))
+    return load<ODD>(p + partner(d, half, 1), 4);
+  Four x;   // columns of both halves, or of the last and behind it
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x.v[e] = d + e < 2 * half ? p[partner(d + e, half, 1)] : 0.f;
+  return x;
+}
+// The columns d .. turned (the first of them is; ODD: those at and past 2 half are not): own their
+// values, other their partners', cs the row's turns.
+template <bool ODD>
+__device__ inline Four turned(const Four& own, const Four& other, int d, const float2* cs, int half,
+                              int layout, bool back) {
+  Four y = own;
   const float to = back ? -1.f : 1.f;
-  if (V == 4 && layout == 0) {
-    const float4 t = *reinterpret_cast<const float4*>(cs + d / 2);   // two pairs
-    const float s0 = to * t.y, s1 = to * t.w;
-    y.v[0] = own.v[0] * t.x - own.v[1 % V] * s0;
-    y.v[1 % V] = own.v[1 % V] * t.x + own.v[0] * s0;
-    y.v[2 % V] = own.v[2 % V] * t.z - own.v[3 % V] * s1;
-    y.v[3 % V] = own.v[3 % V] * t.z + own.v[2 % V] * s1;
+  if (!layout) {
+    float2 t[2];
+    if constexpr (ODD) {
+      t[0] = cs[d / 2];
+      t[1] = d + 2 < 2 * half ? cs[d / 2 + 1] : make_float2(1.f, 0.f);
+    } else {
+      const float4 u = *reinterpret_cast<const float4*>(cs + d / 2);
+      t[0] = make_float2(u.x, u.y);
+      t[1] = make_float2(u.z, u.w);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (ODD && d + 2 * j >= 2 * half) break;   // (1 x is x, but 0 x is not always 0)
+      const float s = to * t[j].y;
+      y.v[2 * j] = own.v[2 * j] * t[j].x - own.v[2 * j + 1] * s;
+      y.v[2 * j + 1] = own.v[2 * j + 1] * t[j].x + own.v[2 * j] * s;
+    }
     return y;
   }
-  const bool second = layout ? d >= half : d & 1;
-  const int i = layout ? (second ? d - half : d) : d >> 1;
-  const float sign = second ? to : -to;
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const float2 t = cs[i + e];
-    y.v[e] = own.v[e] * t.x + sign * (other.v[e] * t.y);
+  for (int e = 0; e < 4; ++e) {
+    if (ODD && d + e >= 2 * half) break;
+    const bool second = (ODD ? d + e : d) >= half;
+    const float2 t = cs[d + e - (second ? half : 0)];
+    y.v[e] = own.v[e] * t.x + (second ? to : -to) * (other.v[e] * t.y);
   }
   return y;
 }
@@ -151,7 +187,7 @@ __global__ __launch_bounds__(TPB) void rope_kernel(const float* __restrict__ x,
   float* yt = y + r0 * r.cols;
   const int total = n * r.items, step = TPB * gridDim.y;
   for (int i0 = blockIdx.y * TPB + threadIdx.x; i0 < total; i0 += kFlight * step) {
-    Val<4> own[kFlight], other[kFlight];
+    Four own[kFlight], other[kFlight];
     int row[kFlight], c[kFlight], d[kFlight];
 #pragma unroll
     for (int u = 0; u < kFlight; ++u) {
@@ -161,16 +197,16 @@ __global__ __launch_bounds__(TPB) void rope_kernel(const float* __restrict__ x,
       d[u] = c[u] - r.by_dh.div(c[u]) * r.dh;
       if (c[u] >= r.used || d[u] >= 2 * r.half) d[u] = -1;   // copied
       const float* p = xt + (int64_t)row[u] * r.cols + c[u];
-      own[u] = load<4>(p);
+      own[u] = load(p);
       other[u] = own[u];
-      if (d[u] >= 0 && r.layout) other[u] = load<4>(p - d[u] + partner<4>(d[u], r.half, r.layout));
+      if (d[u] >= 0) other[u] = partners<false>(p - d[u], d[u], own[u], r.half, r.layout);
     }
 #pragma unroll
     for (int u = 0; u < kFlight; ++u) {
       if (i0 + u * step >= total) break;
       if (d[u] >= 0)
-        own[u] = turned<4>(own[u], other[u], d[u], cs + row[u] * r.half, r.half, r.layout, back);
-      store<4>(yt + (int64_t)row[u] * r.cols + c[u], own[u]);
+        own[u] = turned<false>(own[u], other[u], d[u], cs + row[u] * r.half, r.half, r.layout, back);
+      store(yt + (int64_t)row[u] * r.cols + c[u], own[u]);
     }
   }
 }
@@ -192,7 +228,7 @@ __global__ __launch_bounds__(TPB) void rope_columns_kernel(const float* __restri
   for (int c = blockIdx.y * TPB + threadIdx.x; c < r.cols; c += TPB * gridDim.y) {
     const int d = c - r.by_dh.div(c) * r.dh;
     const bool turned = c < r.used && d < 2 * r.half;
-    const int to = turned ? partner<1>(d, r.half, r.layout) - d : 0;
+    const int to = turned ? partner(d, r.half, r.layout) - d : 0;
     const int i = turned ? (r.layout ? min(d, d + to) : d >> 1) : 0;
     const float sign = turned ? ((to < 0) != back ? 1.f : -1.f) : 0.f;
     const float* p = x + r0 * r.cols + c;
@@ -214,8 +250,8 @@ __global__ __launch_bounds__(TPB) void rope_columns_kernel(const float* __restri
 }
 
 // ---------------------------------------------------------------- per-head norms
-// A group of G neighbouring lanes holds one head of one row, lane l of it the V columns from
-// V (l + G k) on, k < K.
+// A group of G neighbouring lanes holds one head of one row, lane l of it the four columns from
+// 4 (l + G k) on, k < K.
 template <int G>
 __device__ inline float group_sum(float v) {
 #pragma unroll
@@ -224,17 +260,18 @@ __device__ inline float group_sum(float v) {
 }
 
 // The columns behind the heads of a tile's rows are copied.
-template <int V>
+template <bool ODD>
 __device__ inline void copy_rest(const float* __restrict__ x, float* __restrict__ y, int64_t r0, int n,
                                  const Rows& r) {
-  const int rest = (r.cols - r.used) / V;
+  const int rest = r.cols - r.used;
   for (int row = 0; row < n; ++row) {
     const int64_t at = (r0 + row) * r.cols + r.used;
-    for (int c = threadIdx.x; c < rest; c += TPB) store<V>(y + at + V * c, load<V>(x + at + V * c));
+    for (int c = 4 * threadIdx.x; c < rest; c += 4 * TPB)
+      store<ODD>(y + at + c, rest - c, load<ODD>(x + at + c, rest - c));
   }
 }
 
-template <int V, int G, int K>
+template <bool ODD, int G, int K>
 __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict__ x,
                                                          const float* __restrict__ gain,
                                                          const int32_t* __restrict__ pos,
@@ -253,45 +290,42 @@ __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict
     const int row = r.by_heads.div(u), h = u - row * r.heads;
     const int64_t at = (r0 + row) * r.cols + h * r.dh;
     const float* g = gain + (h < r.h1 ? 0 : r.dh);
-    Val<V> own[K], other[K];
+    Four own[K], other[K];
     float q = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int d = V * (lane + G * k);
+      const int d = 4 * (lane + G * k);
       own[k] = {};
       if (d < r.dh) {
-        own[k] = load<V>(x + at + d);
-        const int p = d < 2 * r.half ? partner<V>(d, r.half, r.layout) : d;
-        other[k] = p == d ? own[k] : load<V>(x + at + p);
+        own[k] = load<ODD>(x + at + d, r.dh - d);
+        other[k] = own[k];
+        if (d < 2 * r.half) other[k] = partners<ODD>(x + at, d, own[k], r.half, r.layout);
       }
 #pragma unroll
-      for (int e = 0; e < V; ++e) q += own[k].v[e] * own[k].v[e];
+      for (int e = 0; e < 4; ++e) q += own[k].v[e] * own[k].v[e];
     }
     const float rs = 1.f / sqrtf(group_sum<G>(q) / (float)r.dh + 1e-5f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int d = V * (lane + G * k);
+      const int d = 4 * (lane + G * k);
       if (d >= r.dh) continue;
-      const Val<V> gd = load<V>(g + d);
+      const Four gd = load<ODD>(g + d, r.dh - d);
 #pragma unroll
-      for (int e = 0; e < V; ++e) own[k].v[e] = gd.v[e] * (own[k].v[e] * rs);
+      for (int e = 0; e < 4; ++e) own[k].v[e] = gd.v[e] * (own[k].v[e] * rs);
       if (d < 2 * r.half) {
-        const int p = partner<V>(d, r.half, r.layout);
-        if (p != d) {
-          const Val<V> gp = load<V>(g + p);
+        const Four gp = partners<ODD>(g, d, gd, r.half, r.layout);
 #pragma unroll
-          for (int e = 0; e < V; ++e) other[k].v[e] = gp.v[e] * (other[k].v[e] * rs);
-        }
-        own[k] = turned<V>(own[k], other[k], d, cs + row * r.half, r.half, r.layout, false);
+        for (int e = 0; e < 4; ++e) other[k].v[e] = gp.v[e] * (other[k].v[e] * rs);
+        own[k] = turned<ODD>(own[k], other[k], d, cs + row * r.half, r.half, r.layout, false);
       }
-      store<V>(y + at + d, own[k]);
+      store<ODD>(y + at + d, r.dh - d, own[k]);
     }
   }
-  if (blockIdx.y == 0) copy_rest<V>(x, y, r0, n, r);
+  if (blockIdx.y == 0) copy_rest<ODD>(x, y, r0, n, r);
 }
 
 // A workgroup per row slice; its groups' sums of dgain are added in their order.
-template <int V, int G, int K>
+template <bool ODD, int G, int K>
 __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
     const float* __restrict__ x, const float* __restrict__ gain, const int32_t* __restrict__ pos,
     const double* __restrict__ table, const float* __restrict__ dy, float* __restrict__ dx,
@@ -299,11 +333,11 @@ __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
   extern __shared__ float4 lds[];
   float2* cs = reinterpret_cast<float2*>(lds);
   const int lane = threadIdx.x % G, group = threadIdx.x / G;
-  float acc[2][K][V];
+  float acc[2][K][4];
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int e = 0; e < V; ++e) acc[0][k][e] = acc[1][k][e] = 0.f;
+    for (int e = 0; e < 4; ++e) acc[0][k][e] = acc[1][k][e] = 0.f;
   const int64_t s0 = blockIdx.x * len, s1 = min(r.rows, s0 + len);
   for (int64_t r0 = s0; r0 < s1; r0 += r.tile) {
     const int n = (int)min((int64_t)r.tile, s1 - r0), total = n * r.heads;
@@ -317,24 +351,23 @@ __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
       const int64_t at = (r0 + row) * r.cols + h * r.dh;
       const bool second = h >= r.h1;
       const float* g = gain + (second ? r.dh : 0);
-      Val<V> xv[K], z[K], gd[K];
+      Four xv[K], z[K], gd[K];
       float q = 0.f, dot = 0.f;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int d = V * (lane + G * k);
+        const int d = 4 * (lane + G * k);
         xv[k] = z[k] = gd[k] = {};
         if (d < r.dh) {
-          xv[k] = load<V>(x + at + d);
-          z[k] = load<V>(dy + at + d);
-          gd[k] = load<V>(g + d);
+          xv[k] = load<ODD>(x + at + d, r.dh - d);
+          z[k] = load<ODD>(dy + at + d, r.dh - d);
+          gd[k] = load<ODD>(g + d, r.dh - d);
           if (d < 2 * r.half) {
-            const int p = partner<V>(d, r.half, r.layout);
-            const Val<V> other = p == d ? z[k] : load<V>(dy + at + p);
-            z[k] = turned<V>(z[k], other, d, cs + row * r.half, r.half, r.layout, true);
+            const Four other = partners<ODD>(dy + at, d, z[k], r.half, r.layout);
+            z[k] = turned<ODD>(z[k], other, d, cs + row * r.half, r.half, r.layout, true);
           }
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
+        for (int e = 0; e < 4; ++e) {
           q += xv[k].v[e] * xv[k].v[e];
           dot += gd[k].v[e] * z[k].v[e] * xv[k].v[e];
         }
@@ -345,29 +378,29 @@ __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
       const float mean = dot * rs / (float)r.dh;   // of gain z xhat
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int d = V * (lane + G * k);
-        Val<V> o;
+        const int d = 4 * (lane + G * k);
+        Four o;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
+        for (int e = 0; e < 4; ++e) {
           const float xh = xv[k].v[e] * rs, zx = z[k].v[e] * xh;
           acc[0][k][e] += second ? 0.f : zx;
           acc[1][k][e] += second ? zx : 0.f;
           o.v[e] = rs * (gd[k].v[e] * z[k].v[e] - xh * mean);
         }
-        if (d < r.dh) store<V>(dx + at + d, o);
+        if (d < r.dh) store<ODD>(dx + at + d, r.dh - d, o);
       }
     }
-    copy_rest<V>(dy, dx, r0, n, r);
+    copy_rest<ODD>(dy, dx, r0, n, r);
   }
-  // [groups][2][G K V] in the turns' place
+  // [groups][2][4 G K] in the turns' place
   float* sums = reinterpret_cast<float*>(lds);
-  constexpr int N = G * K * V;
+  constexpr int N = 4 * G * K;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int d = V * (lane + G * k) + e;
+    for (int e = 0; e < 4; ++e) {
+      const int d = 4 * (lane + G * k) + e;
       sums[(group * 2) * N + d] = acc[0][k][e];
       sums[(group * 2 + 1) * N + d] = acc[1][k][e];
     }
@@ -405,8 +438,8 @@ __global__ __launch_bounds__(kFinCols * kFinRows) void qknorm_finalize(const flo
 // ---------------------------------------------------------------- launches
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// 16-byte items: every head, the rotated width (each half of it where pairs lie half apart) and
-// every row a multiple of four columns.
+// Aligned 16-byte items: every head, the rotated width (each half of it where pairs lie half apart)
+// and every row a multiple of four columns.
 bool in_fours(const RopeShape& s, std::initializer_list<const void*> ptrs) {
   for (const void* p : ptrs)
     if (!aligned16(p)) return false;
@@ -440,25 +473,28 @@ unsigned parts(unsigned tiles, int64_t work, int64_t least) {
   return (unsigned)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, work / least));
 }
 
-// Lanes a head of q items takes and items a lane: the fewest idle lanes, and of these the fewest items.
-#define GROUPS_TO_256(V, CALL)                         \
-  if (q <= 16) CALL(V, 16, 1);                         \
-  else if (q <= 32) CALL(V, 32, 1);                    \
-  else if (q <= 48) CALL(V, 16, 3);                    \
-  else if (q <= 64) CALL(V, 64, 1);                    \
-  else if (q <= 96) CALL(V, 32, 3);                    \
-  else if (q <= 128) CALL(V, 64, 2);                   \
-  else if (q <= 192) CALL(V, 64, 3);                   \
-  else CALL(V, 64, 4)
-#define GROUPS(CALL)                                   \
-  if (four) {                                          \
-    const int q = r.dh / 4;                            \
-    GROUPS_TO_256(4, CALL);                            \
-  } else if (r.dh <= 256) {                            \
-    const int q = r.dh;                                \
-    GROUPS_TO_256(1, CALL);                            \
-  } else if (r.dh <= 512) CALL(1, 64, 8);              \
-  else CALL(1, 64, 16)
+// Lanes a head of q fours of columns takes and fours a lane: the fewest idle lanes, and of these the
+// fewest fours.  Forward + backward, 20000 rows of 10 heads of 96: 49 + 61 us so, 59 + 64 one four a
+// lane (8 of 32 lanes idle).  Odd widths value by value instead: heads of 85, 32 columns turned, 90 +
+// 76 us, so 45 + 59; of 301: 274 + 151, so 140 + 168.
+#define GROUPS(ODD, CALL)                              \
+  if (q <= 8) CALL(ODD, 8, 1);                         \
+  else if (q <= 16) CALL(ODD, 16, 1);                  \
+  else if (q <= 24) CALL(ODD, 8, 3);                   \
+  else if (q <= 32) CALL(ODD, 32, 1);                  \
+  else if (q <= 48) CALL(ODD, 16, 3);                  \
+  else if (q <= 64) CALL(ODD, 64, 1);                  \
+  else if (q <= 96) CALL(ODD, 32, 3);                  \
+  else if (q <= 128) CALL(ODD, 64, 2);                 \
+  else if (q <= 192) CALL(ODD, 64, 3);                 \
+  else CALL(ODD, 64, 4)
+#define BY_WIDTH(CALL)                                 \
+  const int q = (r.dh + 3) / 4;                        \
+  if (in_fours(s, pointers)) {                         \
+    GROUPS(false, CALL);                               \
+  } else {                                             \
+    GROUPS(true, CALL);                                \
+  }
 
 }  // namespace
 
@@ -478,14 +514,14 @@ hipError_t rope(bool back, const float* x, const int32_t* pos, const double* tab
 
 hipError_t qknorm_fwd(const float* x, const float* gain, const int32_t* pos, const double* table,
                       float* y, const RopeShape& s, int64_t h1, hipStream_t st) {
-  const bool four = in_fours(s, {x, gain, y});
-  const Rows r = rows_of(s, h1, four ? 4 : 1, s.rows / 1024);
+  const std::initializer_list<const void*> pointers = {x, gain, y};
+  const Rows r = rows_of(s, h1, 4, s.rows / 1024);
   const unsigned nx = blocks(r.rows, r.tile);
   const unsigned lds = (unsigned)(r.tile * r.half * sizeof(float2));
-#define FWD(V, G, K)                                                                              \
-  hipLaunchKernelGGL((qknorm_fwd_kernel<V, G, K>), dim3(nx, parts(nx, (int64_t)r.tile * r.heads, TPB / G)), \
+#define FWD(ODD, G, K)                                                                                  \
+  hipLaunchKernelGGL((qknorm_fwd_kernel<ODD, G, K>), dim3(nx, parts(nx, (int64_t)r.tile * r.heads, TPB / G)), \
                      dim3(TPB), lds, st, x, gain, pos, table, y, r)
-  GROUPS(FWD);
+  BY_WIDTH(FWD)
 #undef FWD
   return hipGetLastError();
 }
@@ -494,15 +530,15 @@ hipError_t qknorm_bwd(const float* x, const float* gain, const int32_t* pos, con
                       const float* dy, float* dx, float* dgain, float* part, const RopeShape& s,
                       int64_t h1, int64_t slices, hipStream_t st) {
   const int64_t len = (s.rows + slices - 1) / slices;
-  const bool four = in_fours(s, {x, gain, dy, dx});
-  const Rows r = rows_of(s, h1, four ? 4 : 1, len);
+  const std::initializer_list<const void*> pointers = {x, gain, dy, dx};
+  const Rows r = rows_of(s, h1, 4, len);
   const int n = (int)((h1 < s.heads ? 2 : 1) * s.dh);
-#define BWD(V, G, K)                                                                              \
-  hipLaunchKernelGGL((qknorm_bwd_kernel<V, G, K>), dim3((unsigned)slices), dim3(TPB),             \
+#define BWD(ODD, G, K)                                                                                  \
+  hipLaunchKernelGGL((qknorm_bwd_kernel<ODD, G, K>), dim3((unsigned)slices), dim3(TPB),             \
                      (unsigned)std::max<size_t>(r.tile * r.half * sizeof(float2),                 \
-                                                TPB * 2 * K * V * sizeof(float)),                 \
+                                                TPB * 8 * K * sizeof(float)),                 \
                      st, x, gain, pos, table, dy, dx, part, r, len)
-  GROUPS(BWD);
+  BY_WIDTH(BWD)
 #undef BWD
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

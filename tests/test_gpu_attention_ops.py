@@ -86,6 +86,11 @@ QKNORM = [
     (10, 1, 1, 1024, 1024, 1, 3, True), (10, 1, 2, 1000, 500, 0, 0, True), (2100, 2, 2, 40, 40, 1, 8, True),
     (517, 5, 1, 48, 12, 1, 0, False), (17000, 1, 1, 32, 32, 0, 4, True), (64, 3, 3, 80, 80, 1, 240, False),
     (41, 2, 5, 33, 32, 0, 0, True), (5, 4, 0, 3, 2, 1, 1, False), (12, 2, 2, 300, 40, 1, 12, True),
+    (20, 3, 2, 85, 34, 0, 3, True), (20, 3, 2, 85, 34, 1, 3, True), (33, 2, 1, 18, 14, 1, 7, False),
+    (9, 1, 1, 7, 2, 1, 2, False), (9, 2, 0, 7, 6, 0, 0, True), (12, 2, 1, 6, 6, 1, 0, False),
+    (50, 2, 2, 301, 0, 1, 3, False), (40, 2, 1, 30, 16, 1, 0, True), (64, 8, 2, 96, 32, 0, 192, False),
+    (21, 3, 1, 62, 62, 1, 2, True), (13, 1, 1, 1023, 1022, 1, 1, True), (700, 2, 2, 130, 66, 1, 130, False),
+    (30, 2, 2, 64, 36, 1, 64, False), (30, 2, 2, 64, 22, 0, 64, True),
 ]
 
 
@@ -581,8 +586,11 @@ def rounding_floors(spec, ref, extra):
     """What rounding alone leaves in gradients that are zero in exact arithmetic.  With one state
     to attend to, P = 1 and dP - delta is the difference of two sums of equal value, so dq and dk
     are zero up to the bounds of ``cross_bounds`` (a few u sum |dy| |v| each), and so is everything
-    they alone feed: the gains of both norms and the query projection.  Returns {gradient: bound},
-    the bounds carried through |.| of the exact factors."""
+    they alone feed: the gains of both norms, the query projection, and gamma and beta of the norm
+    before it.  Returns {gradient: bound}, the bounds carried through |.| of the exact factors: of
+    the projection's rows dx, the norm receives dx W, so |d beta| <= sum |dx| |W|, and |d gamma| at
+    most sqrt(d) times that, as no normalised value of d columns with a mean square of at most 1
+    passes sqrt(d)."""
     out = {}
     for L in spec["layers"]:
         if L["op"] != "cross_attention":
@@ -603,6 +611,8 @@ def rounding_floors(spec, ref, extra):
                 dx = (r * (w + u * (w * u).mean(-1, keepdims=True))).reshape(len(x), -1)
                 out[f"d:{b}.q.W"] = dx.T @ np.abs(ref[f"{b}.ln2"])
                 out[f"d:{b}.q.b"] = dx.sum(0)
+                out[f"d:{b}.ln2.beta"] = dx.sum(0) @ np.abs(ref[f"{b}.q.W"]).reshape(dx.shape[1], -1)
+                out[f"d:{b}.ln2.gamma"] = out[f"d:{b}.ln2.beta"] * dx.shape[1] ** 0.5
     return out
 
 
