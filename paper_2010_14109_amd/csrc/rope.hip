@@ -86,7 +86,9 @@ struct Four {
 };
 __device__ inline Four load(const float* p) {
   const float4 t = *reinterpret_cast<const float4*>(p);
-  return {{t.x, t.y, t.z, t.w}};
+  Four x;
+  x.v[0] = t.x; x.v[1] = t.y; x.v[2] = t.z; x.v[3] = t.w;
+  return x;
 }
 __device__ inline void store(float* p, const Four& x) {
   *reinterpret_cast<float4*>(p) = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
@@ -95,43 +97,56 @@ __device__ inline void store(float* p, const Four& x) {
 // many as there are, at any alignment, and zeros.
 template <bool ODD>
 __device__ inline Four load(const float* p, int left) {
-  if constexpr (!ODD) return load(p);
-  if (left >= 4) {
-    const float4u t = *reinterpret_cast<const float4u*>(p);
-    return {{t[0], t[1], t[2], t[3]}};
-  }
-  Four x;
+  if constexpr (!ODD) {
+    return load(p);
+  } else {
+    Four x;
+    if (left >= 4) {
+      const float4u t = *reinterpret_cast<const float4u*>(p);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x.v[e] = e < left ? p[e] : 0.f;
-  return x;
+      for (int e = 0; e < 4; ++e) x.v[e] = t[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.v[e] = e < left ? p[e] : 0.f;
+    }
+    return x;
+  }
 }
 template <bool ODD>
 __device__ inline void store(float* p, int left, const Four& x) {
-  if constexpr (!ODD) return store(p, x);
-  if (left >= 4) {
+  if constexpr (!ODD) {
+    store(p, x);
+  } else if (left >= 4) {
     *reinterpret_cast<float4u*>(p) = float4u{x.v[0], x.v[1], x.v[2], x.v[3]};
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < left) p[e] = x.v[e];
+    for (int e = 0; e < 4; ++e)
+      if (e < left) p[e] = x.v[e];
+  }
 }
 
 // The other end of the pair of column d < 2 half.
 __device__ inline int partner(int d, int half, int layout) {
   return !layout ? d ^ 1 : d < half ? d + half : d - half;
 }
-// The partners of the columns d .. d + 3 of the head at p, for turned(): of pairs half a head apart;
-// neighbours have theirs at hand.
+// Where the partners of columns d .. d + 3 of a head begin, for turned(): of neighbours and of columns
+// that stay, at d.
+__device__ inline int partners_at(int d, int half, int layout) {
+  return layout && d < 2 * half ? partner(d, half, layout) : d;
+}
+// The four values at partners_at(d) of the head at p.  ODD: value by value where the columns are of
+// both halves, or of the last and behind it.
 template <bool ODD>
-__device__ inline Four partners(const float* p, int d, const Four& own, int half, int layout) {
-  if (!layout) return own;
-  if (!ODD || d + 4 <= half || (d >= half && d + 4 <= 2 * half))
-    return load<ODD>(p + partner(d, half, 1), 4);
-  Four x;   // columns of both halves, or of the last and behind it
+__device__ inline Four partners(const float* p, int d, int half) {
+  if constexpr (!ODD) {
+    return load(p + partner(d, half, 1));
+  } else {
+    if (d + 4 <= half || (d >= half && d + 4 <= 2 * half)) return load<true>(p + partner(d, half, 1), 4);
+    Four x;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x.v[e] = d + e < 2 * half ? p[partner(d + e, half, 1)] : 0.f;
-  return x;
+    for (int e = 0; e < 4; ++e) x.v[e] = d + e < 2 * half ? p[partner(d + e, half, 1)] : 0.f;
+    return x;
+  }
 }
 // The columns d .. turned (the first of them is; ODD: those at and past 2 half are not): own their
 // values, other their partners', cs the row's turns.
@@ -159,12 +174,23 @@ __device__ inline Four turned(const Four& own, const Four& other, int d, const f
     }
     return y;
   }
+  if constexpr (ODD) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (ODD && d + e >= 2 * half) break;
-    const bool second = (ODD ? d + e : d) >= half;
-    const float2 t = cs[d + e - (second ? half : 0)];
-    y.v[e] = own.v[e] * t.x + (second ? to : -to) * (other.v[e] * t.y);
+    for (int e = 0; e < 4; ++e) {
+      if (d + e >= 2 * half) break;
+      const bool second = d + e >= half;
+      const float2 t = cs[d + e - (second ? half : 0)];
+      y.v[e] = own.v[e] * t.x + (second ? to : -to) * (other.v[e] * t.y);
+    }
+  } else {
+    const bool second = d >= half;
+    const int i = second ? d - half : d;
+    const float sign = second ? to : -to;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 t = cs[i + e];
+      y.v[e] = own.v[e] * t.x + sign * (other.v[e] * t.y);
+    }
   }
   return y;
 }
@@ -199,7 +225,7 @@ __global__ __launch_bounds__(TPB) void rope_kernel(const float* __restrict__ x,
       const float* p = xt + (int64_t)row[u] * r.cols + c[u];
       own[u] = load(p);
       other[u] = own[u];
-      if (d[u] >= 0) other[u] = partners<false>(p - d[u], d[u], own[u], r.half, r.layout);
+      if (d[u] >= 0 && r.layout) other[u] = load(p - d[u] + partner(d[u], r.half, r.layout));
     }
 #pragma unroll
     for (int u = 0; u < kFlight; ++u) {
@@ -298,8 +324,8 @@ __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict
       own[k] = {};
       if (d < r.dh) {
         own[k] = load<ODD>(x + at + d, r.dh - d);
-        other[k] = own[k];
-        if (d < 2 * r.half) other[k] = partners<ODD>(x + at, d, own[k], r.half, r.layout);
+        const bool at_hand = partners_at(d, r.half, r.layout) == d;
+        other[k] = at_hand ? own[k] : partners<ODD>(x + at, d, r.half);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) q += own[k].v[e] * own[k].v[e];
@@ -313,9 +339,11 @@ __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict
 #pragma unroll
       for (int e = 0; e < 4; ++e) own[k].v[e] = gd.v[e] * (own[k].v[e] * rs);
       if (d < 2 * r.half) {
-        const Four gp = partners<ODD>(g, d, gd, r.half, r.layout);
+        if (partners_at(d, r.half, r.layout) != d) {
+          const Four gp = partners<ODD>(g, d, r.half);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) other[k].v[e] = gp.v[e] * (other[k].v[e] * rs);
+          for (int e = 0; e < 4; ++e) other[k].v[e] = gp.v[e] * (other[k].v[e] * rs);
+        }
         own[k] = turned<ODD>(own[k], other[k], d, cs + row * r.half, r.half, r.layout, false);
       }
       store<ODD>(y + at + d, r.dh - d, own[k]);
@@ -362,7 +390,8 @@ __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
           z[k] = load<ODD>(dy + at + d, r.dh - d);
           gd[k] = load<ODD>(g + d, r.dh - d);
           if (d < 2 * r.half) {
-            const Four other = partners<ODD>(dy + at, d, z[k], r.half, r.layout);
+            const bool at_hand = partners_at(d, r.half, r.layout) == d;
+            const Four other = at_hand ? z[k] : partners<ODD>(dy + at, d, r.half);
             z[k] = turned<ODD>(z[k], other, d, cs + row * r.half, r.half, r.layout, true);
           }
         }
@@ -476,7 +505,7 @@ unsigned parts(unsigned tiles, int64_t work, int64_t least) {
 // Lanes a head of q fours of columns takes and fours a lane: the fewest idle lanes, and of these the
 // fewest fours.  Forward + backward, 20000 rows of 10 heads of 96: 49 + 61 us so, 59 + 64 one four a
 // lane (8 of 32 lanes idle).  Odd widths value by value instead: heads of 85, 32 columns turned, 90 +
-// 76 us, so 45 + 59; of 301: 274 + 151, so 140 + 168.
+// 76 us, so 47 + 69; 12288 rows of 20 heads of 64: 47 + 41 (3.2 and 5.5 TB/s).
 #define GROUPS(ODD, CALL)                              \
   if (q <= 8) CALL(ODD, 8, 1);                         \
   else if (q <= 16) CALL(ODD, 16, 1);                  \
