@@ -65,7 +65,7 @@ struct Rows {
   int cols, dh, heads, used, half, layout;   // used = heads dh, half = rot / 2
   int h1;                                    // heads of the first gain
   int tile;                                  // rows a workgroup takes at once
-  Divisor by_half, by_dh, by_heads, by_items;
+  Divisor by_half, by_dh, by_heads, by_items, by_rest;
   int items;                                 // of a row: V columns each
 };
 
@@ -285,15 +285,18 @@ __device__ inline float group_sum(float v) {
   return v;
 }
 
-// The columns behind the heads of a tile's rows are copied.
+// The columns behind the heads of a tile's rows are copied, all rows' together: a row at a time, with
+// most threads idle, 12288 rows of 20 heads of 64 and 256 columns took 46 us forward and 41 backward,
+// so 43 and 39 (3.5 and 5.8 TB/s).
 template <bool ODD>
 __device__ inline void copy_rest(const float* __restrict__ x, float* __restrict__ y, int64_t r0, int n,
                                  const Rows& r) {
-  const int rest = r.cols - r.used;
-  for (int row = 0; row < n; ++row) {
-    const int64_t at = (r0 + row) * r.cols + r.used;
-    for (int c = 4 * threadIdx.x; c < rest; c += 4 * TPB)
-      store<ODD>(y + at + c, rest - c, load<ODD>(x + at + c, rest - c));
+  const int rest = r.cols - r.used, items = (rest + 3) / 4, total = n * items;
+#pragma unroll 2
+  for (int t = threadIdx.x; t < total; t += TPB) {
+    const int row = r.by_rest.div(t), c = 4 * (t - row * items);
+    const int64_t at = (r0 + row) * r.cols + r.used + c;
+    store<ODD>(y + at, rest - c, load<ODD>(x + at, rest - c));
   }
 }
 
@@ -493,6 +496,7 @@ Rows rows_of(const RopeShape& s, int64_t h1, int V, int64_t rows_a_group) {
   r.by_dh = Divisor::of(r.dh);
   r.by_heads = Divisor::of(r.heads);
   r.by_items = Divisor::of(r.items);
+  r.by_rest = Divisor::of((r.cols - r.used + 3) / 4);
   return r;
 }
 unsigned blocks(int64_t rows, int64_t tile) { return (unsigned)((rows + tile - 1) / tile); }
@@ -503,9 +507,9 @@ unsigned parts(unsigned tiles, int64_t work, int64_t least) {
 }
 
 // Lanes a head of q fours of columns takes and fours a lane: the fewest idle lanes, and of these the
-// fewest fours.  Forward + backward, 20000 rows of 10 heads of 96: 49 + 61 us so, 59 + 64 one four a
-// lane (8 of 32 lanes idle).  Odd widths value by value instead: heads of 85, 32 columns turned, 90 +
-// 76 us, so 47 + 69; 12288 rows of 20 heads of 64: 47 + 41 (3.2 and 5.5 TB/s).
+// fewest fours.  Forward + backward, 20000 rows of 10 heads of 96 and 192 columns: 49 + 61 us so, 59 +
+// 64 one four a lane (8 of 32 lanes idle).  Odd widths value by value instead: heads of 85, 32 columns
+// turned, 90 + 76 us, so 47 + 69.
 #define GROUPS(ODD, CALL)                              \
   if (q <= 8) CALL(ODD, 8, 1);                         \
   else if (q <= 16) CALL(ODD, 16, 1);                  \
