@@ -170,7 +170,7 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                table rot/2 doubles (radians per position of pair i) then one double, a
  *                magnitude m: with a = pos table[i], a double,
  *                (y0, y1) = m (x0 cos a - x1 sin a, x0 sin a + x1 cos a);
- *                |a| < 2^52; rot even, 2..1024; cols at most 2^24
+ *                |a| < 2^52; rot even, 2..1024; cols at most 2^24, rows at most 2^27 - 8
  *                                     X[R] pos[R] table[R] Y[W]    rows cols heads dh rot layout
  *  ROPE_BWD      the transposed rotation: (dx0, dx1) = m (dy0 cos a + dy1 sin a,
  *                dy1 cos a - dy0 sin a)
@@ -178,8 +178,8 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *  QKNORM_FWD    per row, the first h1 heads of dh columns are divided by their root mean
  *                square sqrt(mean x^2 + 1e-5) and scaled by gain row 0, the next h2 heads by
  *                gain row 1 (gain [1 + (h2 > 0)][dh]), then rotated as by ROPE_FWD; all other
- *                columns are copied.  rot = 0: no rotation, and no pos and table.  dh at
- *                most 1024; squares are taken in fp32, so |x| up to 1e18
+ *                columns are copied.  rot = 0: no rotation, and no pos and table.  Limits as
+ *                of ROPE_FWD, dh at most 1024; squares are taken in fp32, so |x| up to 1e18
  *                                     X[R] gain[R] [pos[R] table[R]] Y[W]
  *                                                                  rows cols h1 h2 dh rot layout
  *  QKNORM_BWD    dX and dgain of the above; part = one partial dgain per row slice

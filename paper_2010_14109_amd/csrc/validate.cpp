@@ -61,6 +61,8 @@ const Sig kSig[OOC_OP_COUNT] = {
 };
 
 const int64_t kMaxElems = int64_t(1) << 40;
+// Rows of heads: a launch takes 8 to a workgroup of 256 threads and has fewer than 2^32 threads.
+const int64_t kMaxHeadRows = (int64_t(1) << 27) - 8;
 
 // The product of non-negative factors, or -1 where it passes 2^52 (no variable is that large).
 int64_t product(std::initializer_list<int64_t> factors) {
@@ -373,7 +375,7 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
     case OOC_OP_ROPE_BWD: {
       const int64_t rows = a[0], cols = a[1], heads = a[2], dh = a[3], rot = a[4], layout = a[5];
       const int64_t used = product({heads, dh});
-      if (rows <= 0 || rows > INT32_MAX || heads <= 0 || dh <= 0 || used < 0 || cols < used ||
+      if (rows <= 0 || rows > kMaxHeadRows || heads <= 0 || dh <= 0 || used < 0 || cols < used ||
           cols > (1 << 24) || rot < 2 || rot % 2 || rot > dh || rot > 1024 || (layout != 0 && layout != 1))
         return nm + ": bad attributes";
       const int64_t xb = product({rows, cols, 4});
@@ -389,7 +391,7 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
                     layout = a[6];
       const int64_t used = product({h1 + h2, dh});
       const bool fwd = fn.op == OOC_OP_QKNORM_FWD;
-      if (rows <= 0 || rows > INT32_MAX || h1 <= 0 || dh <= 0 || dh > 1024 || used < 0 || cols < used ||
+      if (rows <= 0 || rows > kMaxHeadRows || h1 <= 0 || dh <= 0 || dh > 1024 || used < 0 || cols < used ||
           cols > (1 << 24) || rot % 2 || rot > dh || (layout != 0 && layout != 1))
         return nm + ": bad attributes";
       const int w = rot > 0 ? 2 : 0;   // pos and table

@@ -274,6 +274,9 @@ def test_signatures(lib, op, attrs):
     ("rope_fwd", [3, 50, 0, 20, 10, 1]), ("rope_fwd", [3, 5000, 1, 5000, 1026, 1]),
     ("rope_fwd", [1 << 31, 2, 1, 2, 2, 0]), ("rope_fwd", [1, 1 << 30, 1, 2, 2, 0]),
     ("rope_fwd", [3, 50, 1 << 39, 1 << 39, 2, 0]),
+    ("rope_bwd", [1 << 27, 2, 1, 2, 2, 0]), ("qknorm_fwd", [1 << 27, 2, 1, 0, 2, 0, 0]),
+    ("qknorm_fwd", [3, 50, 2, -1, 10, 6, 1]), ("qknorm_fwd", [3, 50, 2, 1, 10, -2, 1]),
+    ("qknorm_bwd", [9, 50, 2, 1, 10, -4, 1, 2]), ("qknorm_fwd", [3, 50, 1 << 62, 1 << 62, 10, 6, 1]),
     ("qknorm_fwd", [3, 50, 0, 1, 10, 6, 1]), ("qknorm_fwd", [3, 50, 2, 1, 10, 5, 1]),
     ("qknorm_fwd", [3, 2050, 1, 1, 1025, 6, 1]), ("qknorm_fwd", [3, 29, 2, 1, 10, 6, 1]),
     ("qknorm_fwd", [3, 50, 2, 1, 10, 12, 1]), ("qknorm_fwd", [3, 50, 2, 1, 10, 6, 3]),
