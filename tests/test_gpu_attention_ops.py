@@ -1,6 +1,8 @@
 """Rotation, per-head norms and cross attention on the device against the 64-bit oracle, alone and
 inside training steps.  Error bounds: attention_util."""
 
+import threading
+
 import numpy as np
 import pytest
 
@@ -393,6 +395,54 @@ def test_streams_and_graphs():
         hu.synchronize()
         for u, v in zip(got[0], results(sets[0])):
             assert u.tobytes() == v.tobytes()
+
+
+def test_two_threads_at_once():
+    """Two threads, each on its own stream and memory: the results of one alone."""
+    cases = [au.cross_case(44, 2, 70, 130, 4, 2, 64, [130, 50]), au.cross_case(45, 3, 1, 900, 8, 2, 40)]
+    alone = [cross_fwd(a, q, kv, klen) for a, q, kv, klen, _ in cases]
+    streams, got, errors = [hu.Stream(), hu.Stream()], [[], []], []
+
+    def work(i):
+        try:
+            a, q, kv, klen, _ = cases[i]
+            shape = au.cross_shape(a)
+            slices, nbytes = ooc.attention_slices("cross_attention_fwd", shape)
+            for _ in range(20):
+                d = [hu.Array(v) for v in (q, kv, klen)]
+                out = [hu.empty(q.shape), hu.empty(alone[i][1].shape)]
+                part = [hu.empty(nbytes // 4)] if nbytes else []
+                hu.call("cross_attention_fwd", d + out + part, [R] * 3 + [W] * (2 + len(part)),
+                        shape + slices, streams[i])
+                hu.synchronize()
+                got[i].append([o.get() for o in out])
+        except BaseException as e:  # noqa: BLE001 - reported by the test
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for i in range(2):
+        for pair in got[i]:
+            for u, v in zip(pair, alone[i]):
+                assert u.tobytes() == v.tobytes()
+
+
+def test_one_tensor_read_twice():
+    """The states' own rows as queries, in the same memory."""
+    a, _, kv, klen, dy = au.cross_case(46, 2, 45, 45, 4, 2, 32, [45, 20])
+    q = hu.Array(kv)
+    y, lse, k = hu.empty(kv.shape), hu.empty((2, 4, 45)), hu.Array(klen)
+    shape = au.cross_shape(a)
+    slices, nbytes = ooc.attention_slices("cross_attention_fwd", shape)
+    part = [hu.empty(nbytes // 4)] if nbytes else []
+    hu.call("cross_attention_fwd", [q, q, k, y, lse] + part, [R] * 3 + [W] * (2 + len(part)),
+            shape + slices)
+    hu.synchronize()
+    want = cross_fwd(a, kv, kv, klen)
+    assert y.get().tobytes() == want[0].tobytes() and lse.get().tobytes() == want[1].tobytes()
 
 
 def test_run_fn_refuses_bad_memory():
