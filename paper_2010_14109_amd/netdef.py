@@ -262,8 +262,8 @@ class Net:
         dh = self.shape[q][1] // H
         if self.shape[q][1] != H * dh or self.shape[kv][1] != 2 * Hkv * dh:
             raise ValueError(f"{L['name']}: query and key widths do not fit the heads")
-        if self.meta.get(L["klen"], (None,))[0] != (B,) or L["klen"] not in self.inputs:
-            raise ValueError(f"{L['name']}: {L['klen']} must be an input of one length per sequence")
+        if L["klen"] not in self.inputs or self.meta[L["klen"]][:2] != ((B,), "i32"):
+            raise ValueError(f"{L['name']}: {L['klen']} must be an input of one int32 length per sequence")
         return [B, self.shape[q][0] // B, self.shape[kv][0] // B, H, Hkv, dh]
 
     def _fwd_cross_attention(self, L, X):

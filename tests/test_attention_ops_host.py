@@ -193,6 +193,13 @@ def test_wrong_descriptions_are_refused():
             netdef.Net(broken(change))
 
 
+def test_lengths_that_are_not_integers_are_refused():
+    spec = small_seq2seq(layers=1)
+    spec["inputs"] = [dict(v, dtype="f32") if v["name"] == "src_len" else v for v in spec["inputs"]]
+    with pytest.raises(ValueError, match="length"):
+        netdef.Net(spec)
+
+
 # ---------------------------------------------------------------- refusals of the library
 def add(op, sizes, access, attrs, kinds=None):
     """add_fn on a host context; the error message, or ''."""
