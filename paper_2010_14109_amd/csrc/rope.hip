@@ -287,7 +287,7 @@ __device__ inline float group_sum(float v) {
 
 // The columns behind the heads of a tile's rows are copied, all rows' together: a row at a time, with
 // most threads idle, 12288 rows of 20 heads of 64 and 256 columns took 46 us forward and 41 backward,
-// so 43 and 39 (3.5 and 5.8 TB/s).
+// so 43 and 39.
 template <bool ODD>
 __device__ inline void copy_rest(const float* __restrict__ x, float* __restrict__ y, int64_t r0, int n,
                                  const Rows& r) {
@@ -315,6 +315,24 @@ __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict
     __syncthreads();
   }
   const int lane = threadIdx.x % G, step = TPB / G * gridDim.y, total = n * r.heads;
+  // With one four a lane, both rows' gains of it and of its partners stay in registers: 12288 rows of
+  // 20 heads of 64 and 256 columns took 39 us with their loads for every head, so 31 (4.9 TB/s).
+  Four kept[2] = {}, kept_partners[2] = {};
+  if (K == 1 && 4 * lane < r.dh) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const float* g = gain + (w && r.h1 < r.heads ? r.dh : 0);
+      kept[w] = load<ODD>(g + 4 * lane, r.dh - 4 * lane);
+      if (partners_at(4 * lane, r.half, r.layout) != 4 * lane)
+        kept_partners[w] = partners<ODD>(g, 4 * lane, r.half);
+    }
+  }
+  const auto of_head = [&](const Four (&both)[2], int h) {
+    Four x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x.v[e] = h < r.h1 ? both[0].v[e] : both[1].v[e];
+    return x;
+  };
   for (int u = blockIdx.y * (TPB / G) + threadIdx.x / G; u < total; u += step) {
     const int row = r.by_heads.div(u), h = u - row * r.heads;
     const int64_t at = (r0 + row) * r.cols + h * r.dh;
@@ -338,12 +356,12 @@ __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict
     for (int k = 0; k < K; ++k) {
       const int d = 4 * (lane + G * k);
       if (d >= r.dh) continue;
-      const Four gd = load<ODD>(g + d, r.dh - d);
+      const Four gd = K == 1 ? of_head(kept, h) : load<ODD>(g + d, r.dh - d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) own[k].v[e] = gd.v[e] * (own[k].v[e] * rs);
       if (d < 2 * r.half) {
         if (partners_at(d, r.half, r.layout) != d) {
-          const Four gp = partners<ODD>(g, d, r.half);
+          const Four gp = K == 1 ? of_head(kept_partners, h) : partners<ODD>(g, d, r.half);
 #pragma unroll
           for (int e = 0; e < 4; ++e) other[k].v[e] = gp.v[e] * (other[k].v[e] * rs);
         }
@@ -448,8 +466,8 @@ __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
 }
 
 // dgain = the slices' partials: a workgroup owns 16 columns, its 64 rows of threads take the slices
-// s = row mod 64 in increasing order, and one row adds the 64 results in order.
-constexpr int kFinCols = 16, kFinRows = 64;
+// s = row mod 64 in increasing order, eight loads in flight, and one row adds the 64 results in order.
+constexpr int kFinCols = 16, kFinRows = 64, kFlights = 8;
 __global__ __launch_bounds__(kFinCols * kFinRows) void qknorm_finalize(const float* __restrict__ part,
                                                                        float* __restrict__ dgain,
                                                                        int n, int64_t slices) {
@@ -457,7 +475,17 @@ __global__ __launch_bounds__(kFinCols * kFinRows) void qknorm_finalize(const flo
   const int c = blockIdx.x * kFinCols + threadIdx.x % kFinCols, row = threadIdx.x / kFinCols;
   float s = 0.f;
   if (c < n)
-    for (int64_t k = row; k < slices; k += kFinRows) s += part[k * n + c];
+    for (int64_t k0 = row; k0 < slices; k0 += kFlights * kFinRows) {
+      float x[kFlights];
+#pragma unroll
+      for (int i = 0; i < kFlights; ++i) {
+        const int64_t k = k0 + i * kFinRows;
+        x[i] = part[min(k, slices - 1) * n + c];
+        if (k >= slices) x[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kFlights; ++i) s += x[i];
+    }
   sums[row][threadIdx.x % kFinCols] = s;
   __syncthreads();
   if (row || c >= n) return;
