@@ -42,7 +42,6 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr float kUnit = 0x1p-14f;    // a scaled row's largest value is 2^14 .. 2^15 of its exponent
 constexpr uint32_t kNone = 0x80000000u;   // past the length of every descriptor
 constexpr uint32_t kXcds = 8;
 
@@ -435,6 +434,43 @@ struct Raw {
 };
 
 // ---------------------------------------------------------------- forward
+// The running softmax of a column, in powers of two and apart for the two sums it divides, as a
+// tile's values bring an exponent of their own (ve of Raw::exponents, -112 for zeros).  ms is a whole
+// number no more than kLag below the largest score, and the sum of probabilities is in units of 2^ms.
+// m is a whole number no more than kRoom below the largest score + ve, and a probability meets the
+// values' pieces as p = 2^(score + ve - m + kTop), so that p is at most 2^15 and the largest are above
+// 2^11; of one below 2^-2 its pieces hold what is above 2^-25, 2^-36 of the largest or less.  Both are
+// whole so that changing them is exact.  Where p is too far below the units of the sum (m - ve - ms
+// past kFar: other tiles' values are far larger, or this one's are zero, and p may vanish while the
+// probability counts), the probabilities are computed again for the sum alone.
+constexpr float kTop = 12.f, kRoom = 3.f, kLag = 64.f, kFar = 64.f;
+__device__ inline bool outgrown(float top, float ve, float m, float ms) {
+  return top + ve > m + kRoom || top > ms + kLag;
+}
+// m and ms for a tile with the largest score `top`; returns the factor of the sums with m
+__device__ inline float raise(float top, float ve, float& m, float& ms, float& sum) {
+  const float up = fmaxf(m, ceilf(top + ve)), f = m == up ? 1.f : exp2f(m - up);
+  const float us = fmaxf(ms, ceilf(top));
+  sum *= ms == us ? 1.f : exp2f(ms - us);
+  m = up;
+  ms = us;
+  return f;
+}
+// What turns a column's sum of p times scaled values into its quotient by `total`, a factor, and log2
+// of the sum of 2^score.  The factor is 2^(m - ms - 26) / total, total's power of two taken into the
+// exponent; where that is below the normal numbers' (values below 2^-70 or so), the sum takes kDown of it.
+struct Quotient {
+  static constexpr float kDown = 0x1p-60f;
+  float factor, log;
+  bool low;
+  __device__ Quotient(float total, float m, float ms) {
+    const float l = __builtin_amdgcn_logf(total), whole = rintf(l), e = m - ms - (kTop + 14.f) - whole;
+    low = e < -120.f;
+    factor = __builtin_amdgcn_exp2f(low ? e + 60.f : e) / (total * __builtin_amdgcn_exp2f(-whole));
+    log = ms + l;
+  }
+};
+
 // A workgroup of wide() has 256 columns: up to 64 head columns two sets of 32 a wave, so that each
 // A operand is read for both; above, eight waves, so that a tile is split once for all. Others have
 // 128 (above 128 head columns, 64).
@@ -473,17 +509,14 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
     qc[x] = split_column<DH>(v, qp[x]) * s.scale * kLog2e;
   }
   floatx16 o[C][Wd::kSums];
-  // Powers of two: m above the largest score plus value exponent so far (less base), and the sums
-  // of 2^(score - m + 8) and of that times the values.  m stays while no term passes 2^15.
-  float m[C], sum[C];
+  float m[C], ms[C], sum[C];   // see kTop
 #pragma unroll
   for (int x = 0; x < C; ++x) {
-    m[x] = -INFINITY;
+    m[x] = ms[x] = -INFINITY;
     sum[x] = 0.f;
 #pragma unroll
     for (int t = 0; t < Wd::kSums; ++t) o[x][t] = floatx16{};
   }
-  int base = 0;
   Raw<DH, W, T> raw;
   const auto fetch = [&](int j) {
     const int64_t r = key_row(s, at.b, at.hk, j);
@@ -493,13 +526,11 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
   for (int j0 = k0; j0 < k1; j0 += T) {
     raw.publish(tops);
     __syncthreads();
-    int2 e = raw.exponents(tops);
-    if (j0 == k0) base = e.y <= -112 ? 0 : e.y;
-    e.y = e.y <= -112 ? base : max(e.y, base - 40);   // zeros count as base
+    const int2 e = raw.exponents(tops);
     raw.store(ks, vs, e);
     __syncthreads();
     if (j0 + T < k1) fetch(j0 + T);
-    const float ve = (float)(e.y - base), vi = exp2_of(max(base - e.y, -126));
+    const float ve = (float)e.y;
 #pragma unroll 1
     for (int r0 = 0; r0 < T; r0 += 32) {
       if (r0 && j0 + r0 >= k1) break;
@@ -524,15 +555,13 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
         top[x] = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) top[x] = fmaxf(top[x], a[x][i]);
-        top[x] = fmaf(max_of_halves(top[x]), c[x], ve);
-        past |= top[x] > m[x] + 7.f;
+        top[x] = max_of_halves(top[x]) * c[x];
+        past |= outgrown(top[x], ve, m[x], ms[x]);
       }
-      if (__any(past))
+      if (__builtin_expect(__any(past), 0))
 #pragma unroll
         for (int x = 0; x < C; ++x) {
-          const float up = fmaxf(m[x], top[x]), f = m[x] == up ? 1.f : exp2f(m[x] - up);
-          m[x] = up;
-          sum[x] *= f;
+          const float f = raise(top[x], ve, m[x], ms[x], sum[x]);
 #pragma unroll
           for (int t = 0; t < Wd::kSums; ++t)
 #pragma unroll
@@ -541,14 +570,21 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
       Pieces pp[C][2];
 #pragma unroll
       for (int x = 0; x < C; ++x) {
-        const float off = ve + 8.f - m[x];
+        const float off = ve + kTop - m[x], far = m[x] - ve - ms[x];
         float p[16], part = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           p[i] = __builtin_amdgcn_exp2f(fmaf(a[x][i], c[x], off));
           part += p[i];
         }
-        sum[x] = fmaf(part, vi, sum[x]);
+        float g = __builtin_amdgcn_exp2f(far - kTop);
+        if (__builtin_expect(__any(far > kFar), 0)) {
+          part = 0.f;
+          g = 1.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(a[x][i], c[x], -ms[x]));
+        }
+        sum[x] = fmaf(part, g, sum[x]);
         pp[x][0] = split8(p);
         pp[x][1] = split8(p + 8);
       }
@@ -567,15 +603,18 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
     const float total = sum_of_halves(sum[x]);
     const int col = col0 + 32 * x;
     if (col >= s.R) continue;
-    float f = 0.f, l = -INFINITY;
-    if (bad) f = l = NAN;
-    else if (k0 < k1) {
-      f = kUnit * exp2_of(base) / total;
-      l = (m[x] - 8.f + log2f(total)) * kLn2;
-    }
+    const float none = bad ? NAN : 0.f;
+    const Quotient f(total, m[x], ms[x]);
+    if (__any(f.low))
+#pragma unroll
+      for (int t = 0; t < Wd::kSums; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[x][t][i] *= f.low ? Quotient::kDown : 1.f;
     store_column<Wd::kSums, EXACT>(y + at.slice * y_slice + query_row(s, at.b, at.hk, col), first, s.dh,
-                                   [&](int t, int i) { return k0 < k1 ? o[x][t][i] * f : f; });
-    if (half == 0 && first == 0) lse[at.slice * lse_slice + stat_row(s, at.b, at.hk) + col] = l;
+                                   [&](int t, int i) { return k0 < k1 ? o[x][t][i] * f.factor : none; });
+    if (half == 0 && first == 0)
+      lse[at.slice * lse_slice + stat_row(s, at.b, at.hk) + col] =
+          bad ? NAN : k0 < k1 ? f.log * kLn2 : -INFINITY;
   }
 }
 
@@ -666,8 +705,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
   floatx4 o[kBlocks];
 #pragma unroll
   for (int t = 0; t < kBlocks; ++t) o[t] = floatx4{};
-  float m = -INFINITY, sum = 0.f;
-  int base = 0;
+  float m = -INFINITY, ms = -INFINITY, sum = 0.f;   // see kTop
   const auto largest = [&](const float (&x)[DH / 2]) {
     float top = max_abs(x, DH / 2);
     if (__any(top == INFINITY)) {   // the largest finite one: see Raw::publish
@@ -686,9 +724,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
       for (int t = 0; t < kSteps; ++t)
         a[h] = mma16(split8(k + 8 * (h * kSteps + t), exp2_of(14 - ek)), qp[t], a[h]);
     load_tile(j0 + W * T, 0, k);
-    int ev = largest(v);
-    if (j0 == j1) base = ev <= -112 ? 0 : ev;
-    ev = ev <= -112 ? base : max(ev, base - 40);   // zeros count as base
+    const int ev = largest(v);
     // (the wave's LDS accesses stay in order; the fences keep the compiler from moving them)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -699,7 +735,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     load_tile(j0 + W * T, to_v, v);
     const float c = fmaxf(qc * exp2_of(ek - 14), 0x1p-126f);   // a masked score stays -inf
-    const float ve = (float)(ev - base);
+    const float ve = (float)ev;
     float p[8], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -707,36 +743,44 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
       p[i] = there ? a[i / 4][i % 4] : -INFINITY;
       top = fmaxf(top, p[i]);
     }
-    top = fmaf(max_of_quarters(top), c, ve);
-    if (__any(top > m + 7.f)) {
-      const float up = fmaxf(m, top), f = m == up ? 1.f : exp2f(m - up);
-      m = up;
-      sum *= f;
+    top = max_of_quarters(top) * c;
+    if (__builtin_expect(__any(outgrown(top, ve, m, ms)), 0)) {
+      const float f = raise(top, ve, m, ms, sum);
 #pragma unroll
       for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[t][i] *= f;
     }
-    const float off = ve + 8.f - m;
+    const float off = ve + kTop - m, far = m - ve - ms;
     float part = 0.f;
+    if (__builtin_expect(__any(far > kFar), 0)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part += __builtin_amdgcn_exp2f(fmaf(p[i], c, -ms));
+      sum += part;
+      part = 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, off));
       part += p[i];
     }
-    sum = fmaf(part, exp2_of(max(base - ev, -126)), sum);
+    if (!__any(far > kFar)) sum = fmaf(part, __builtin_amdgcn_exp2f(far - kTop), sum);
     const Pieces pp = split8(p);
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) o[t] = mma16(Rows<DH, T>::by_column16(vs, t), pp, o[t]);
   }
   sum = sum_of_quarters(sum);
-  const float f = sum == 0.f ? 0.f : kUnit * exp2_of(base) / sum;   // a wave without states: 0
+  const Quotient f(sum, m, ms);
+  const bool none = sum == 0.f;   // a wave without states
+  const float down = f.low ? Quotient::kDown : 1.f;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
   for (int t = 0; t < kBlocks; ++t)
     *reinterpret_cast<float4*>(ys(w, l16, 16 * t + 4 * quarter)) =
-        make_float4(o[t][0] * f, o[t][1] * f, o[t][2] * f, o[t][3] * f);
-  if (quarter == 0) ls[w][l16] = bad ? NAN : sum == 0.f ? -INFINITY : m - 8.f + log2f(sum);
+        none ? make_float4(0.f, 0.f, 0.f, 0.f)
+             : make_float4(o[t][0] * down * f.factor, o[t][1] * down * f.factor,
+                           o[t][2] * down * f.factor, o[t][3] * down * f.factor);
+  if (quarter == 0) ls[w][l16] = bad ? NAN : none ? -INFINITY : f.log;
   __syncthreads();
   for (int u = threadIdx.x; u < s.R * DH; u += 64 * W) {
     const int r = u / DH, d = u % DH;
