@@ -192,10 +192,14 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                in the second; query head h reads key head h Hkv / H (Hkv divides H), dh <= 256:
  *                S = q k^T / sqrt(dh), Y [B Tq][H dh] = softmax(S) v, lse [B][H][Tq] = ln sum
  *                exp S.  klen 0: Y = 0 and lse = -inf; klen outside 0..Tk: NaN.  States at and
- *                past klen may hold anything.  Sums are fp32.  Values from 2^-100 to 2^100 and
- *                their products within fp32's range: what lies more than 2^38 below the largest of
- *                the 32 or 64 rows that it is read with loses its last bits or counts as zero; an
- *                infinity or a NaN gives NaN in the results that it reaches.  H dh and Hkv dh at
+ *                past klen may hold anything.  Values from 2^-100 to 2^100 and their products
+ *                within fp32's range; an infinity or a NaN gives NaN in the results that it
+ *                reaches.  Sums are fp32.  Operands of products are rounded: q, kv and dY to 2^-23
+ *                of the value, or to 2^-39 of the largest value that it is read with (those of its
+ *                own row and head, or of a head in 32 or 64 neighbouring rows) where that is more;
+ *                probabilities and their gradients to 2^-23, or to 2^-35 of the largest of their
+ *                query (in dkv: of their state), each times the largest value of the 32 or 64 rows
+ *                it meets.  H dh and Hkv dh at
  *                most 2^20.  part = partial results, present iff slices > 1
  *                (ooc_attention_slices gives counts and its bytes)
  *                                     q[R] kv[R] klen[R] Y[W] lse[W] [part[W]]

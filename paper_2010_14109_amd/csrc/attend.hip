@@ -8,13 +8,20 @@
 // Products.  All of it is fp32, and the fp32 matrix instructions run at a sixteenth of the fp16
 // ones' rate.  A matrix (a column of the wave's own side, a tile of rows of the other) is scaled by
 // a power of two that brings its largest value to 2^14 .. 2^15 and split into fp16 pieces, h =
-// fp16(x), l = fp16(x - h), which keep 23 bits of every value, and of small ones the 40 bits below
-// the largest; x y is the sum of h h, h l and l h, accumulated in fp32 (l l is below 2^-22 of x y).
-// Three instructions where splitting into bfloat16 pieces takes six, two pieces to keep and move
-// instead of three.  The scales are exact and multiply into factors that are applied anyway.  What
-// is computed and multiplied again (probabilities, score gradients) is itself scaled by a running
-// power of two per column: its values lie within 2^15, and sums are rescaled, as for the running
-// maximum, in the rare tiles where one passes it.
+// fp16(x), l = fp16(x - h); x y is the sum of h h, h l and l h, accumulated in fp32.  Three
+// instructions where splitting into bfloat16 pieces takes six, two pieces to keep and move instead of
+// three.  The scales are exact and multiply into factors that are applied anyway.  What is computed
+// and multiplied again (probabilities, score gradients) is itself scaled by a running power of two
+// per column: its values lie within 2^15, and sums are rescaled, as for the running maximum, in the
+// rare tiles where one passes it.
+//
+// What that gives up against fp32, for the speed of three products instead of six: the pieces of a
+// value are off by up to 2^-23 of it (fp32: 2^-24), and l l, up to 2^-22 of x y, is left out.  l has
+// no bits below 2^-25, so a value 2^-16 and more below its matrix's largest is off by up to 2^-39 of
+// that: of a column's own head columns, or of all head columns of a tile's 32 or 64 rows.  Likewise a
+// probability or score gradient is off by up to 2^-35 of its column's largest (each times the power
+// of two of the tile it meets; 2^-36 forward, see kTop): where a state that takes nearly all
+// probability brings nothing itself, the others' part of y is off by 2^-36 / their probability.
 //
 // Tiles.  A wave owns 32 columns: of queries (forward, dq) or of states (dk, dv).  Their pieces stay
 // in registers as the B operands of 32 x 32 x 16 products.  The other side passes through LDS in
@@ -843,11 +850,14 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(const float* __re
 
 // ---------------------------------------------------------------- backward
 // The scale f of a column's values before they are split, which keeps them within 2^15, where a
-// tile with the largest value `top` needs a smaller one; the sums follow.
+// tile with the largest value `top` needs a smaller one; the sums follow.  It brings `top` to 2^10 ..
+// 2^11: lower leaves the pieces of small values fewer bits, higher rescales more often (2^12: 24 x 512 x
+// 512, 121 -> 124 us dk and dv, 89 -> 91 dq; 2^8 is no faster than 2^10).
+constexpr int kFresh = 10;
 __device__ inline bool passes(float top, float f) { return top * f > 0x1p15f; }
 template <int N>
 __device__ inline void rescale(float top, float& f, floatx16 (&acc)[N]) {
-  const float g = passes(top, f) ? exp2_of(max(8 - exponent(top), -126)) : f, up = g / f;
+  const float g = passes(top, f) ? exp2_of(max(kFresh - exponent(top), -126)) : f, up = g / f;
   f = g;
 #pragma unroll
   for (int t = 0; t < N; ++t)

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import attention_util as au
-from test_gpu_attention_ops import check_cross, cross_fwd
+from test_gpu_attention_ops import check_cross, cross_bwd, cross_fwd
 from oracle import ops
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +56,107 @@ def test_gradients_of_unlike_sizes(kernel):
     states[:, :64, 1] = 0
     states[:, 64:, 1] *= np.float32(2.0 ** -50)
     check_cross(a, q, kv, klen, dy * np.float32(2.0 ** 40))
+
+
+# ---------------------------------------------------------------- bits of small terms
+# The bounds below count what include/ooc.h states: two pieces of a value are off by 2^-23 of it (2 u) or
+# 2^-39 of the largest value it is read with, the pieces of a probability by 2^-23 of it or 2^-35 of the
+# largest, and the products of two low pieces, 2^-22 (4 u) at most, are left out.  Each matrix instruction
+# (3 for 16 terms, in two halves) and each addition rounds once more.
+
+def uniform(kernel, seed=93, lengths=None):
+    """A case whose scores are all zero: every probability is 1 / klen."""
+    B, Tq, Tk, H, Hkv, dh, klen = KERNELS[kernel]
+    if lengths is not None:
+        klen = np.resize(lengths, B)
+    a, q, kv, klen, dy = au.cross_case(seed, B, Tq, Tk, H, Hkv, dh, klen)
+    return a, np.zeros_like(q), kv, np.maximum(klen, 1), dy
+
+
+@pytest.mark.parametrize("lengths", [[1], [2, 3], [33, 5], [64, 100, 17], [140]], ids=str)
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_means_of_few_states(kernel, lengths):
+    """y is the mean of klen states and lse their count's logarithm, as exactly as fp32 has them."""
+    a, q, kv, klen, dy = uniform(kernel, lengths=lengths)
+    y, lse = cross_fwd(a, q, kv, klen)
+    f = np.float64
+    wy, wl = ops.cross_attention_fwd(q.astype(f), kv.astype(f), klen, a)
+    size, _ = ops.cross_attention_fwd(q.astype(f), np.abs(kv.astype(f)), klen, a)
+    n = np.repeat(klen, a["Tq"])[:, None]
+    top = np.abs(kv).max()
+    # pieces of the values, instructions, the join's weights, quotient and products
+    au.within("y", y, wy, (2 + 6 * np.ceil(n / 16) + 40) * au.U * size + 2.0 ** -39 * top)
+    au.within("lse", lse, wl, (klen / 16 + 16)[:, None, None] * au.U + 4 * au.U * np.abs(wl))
+    dq, dkv, _ = cross_bwd(a, q, kv, klen, y, lse, dy)
+    _, wk, _ = ops.cross_attention_bwd(q.astype(f), kv.astype(f), klen, dy.astype(f), a)
+    _, size, _ = ops.cross_attention_bwd(q.astype(f), kv.astype(f), klen, np.abs(dy.astype(f)), a)
+    half = kv.shape[1] // 2
+    rows = a["Tq"] * a["H"] // a["Hkv"]
+    assert not dkv[:, :half].any()               # dk sums multiples of q
+    # pieces of dy and of the probabilities, exp(-lse) with its argument's rounding, instructions, joins
+    au.within("dv", dkv[:, half:], wk[:, half:],
+              (2 + 2 + 4 + 40 + 8 * np.log(n.max()) + 6 * rows / 16) * au.U * size[:, half:]
+              + rows * 2.0 ** -39 * np.abs(dy).max())
+
+
+@pytest.mark.parametrize("outlier", [2.0 ** 17, 2.0 ** 24])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_a_large_column_of_values(kernel, outlier):
+    """One head column far above the others: those lose what lies 2^-39 below it."""
+    a, q, kv, klen, _ = uniform(kernel, seed=94)
+    kv.reshape(a["B"], a["Tk"], 2, a["Hkv"], a["dh"])[:, :, 1, :, 5] *= np.float32(outlier)
+    y, _ = cross_fwd(a, q, kv, klen)
+    f = np.float64
+    wy, _ = ops.cross_attention_fwd(q.astype(f), kv.astype(f), klen, a)
+    size, _ = ops.cross_attention_fwd(q.astype(f), np.abs(kv.astype(f)), klen, a)
+    n = np.repeat(klen, a["Tq"])[:, None]
+    au.within("y", y, wy, (2 + 6 * np.ceil(n / 16) + 40) * au.U * size + 2.0 ** -39 * np.abs(kv).max())
+
+
+@pytest.mark.parametrize("ratio", [14.0, 16.0, 18.3, 20.6, 22.7, 24.4])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_a_state_of_zeros_that_takes_the_weight(kernel, ratio):
+    """State 0 has zero values and nearly all probability, every other 2^-ratio of it: y is what the
+    others leave.  (All of one sign, as the pieces of equal probabilities err to one side.)"""
+    B, Tq, Tk, H, Hkv, dh, _ = KERNELS[kernel]
+    a, q, kv, klen, _ = au.cross_case(95, B, Tq, Tk, H, Hkv, dh, Tk)
+    f = np.float64
+    states = kv.reshape(B, Tk, 2, Hkv, dh)
+    q[:] = 0
+    q[:, ::dh] = 1
+    states[:, :, 0] = 0
+    states[:, 0, 0, :, 0] = ratio * np.log(2) * dh ** 0.5
+    states[:, :, 1] = 1 + np.abs(states[:, :, 1])
+    states[:, 0, 1] = 0
+    y, _ = cross_fwd(a, q, kv, klen)
+    wy, _ = ops.cross_attention_fwd(q.astype(f), kv.astype(f), klen, a)
+    # the score's two pieces and three factors (5 u of it, a base-2 logarithm of `ratio`) and the sum
+    # with the maximum (20 u), exp2 and sums, pieces, instructions, quotient and joins
+    c = np.log(2) * (5 * ratio + 20) + 12 + 8 + 6 * np.ceil(Tk / 16) + 40
+    au.within("y", y, wy, (c * au.U + 2.0 ** (ratio - 36)) * wy + 2.0 ** (-39 - ratio) * np.abs(kv).max())
+
+
+@pytest.mark.parametrize("ratio", [6.0, 8.3, 10.6, 12.7, 14.4])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_a_query_without_gradient_that_takes_a_state(kernel, ratio):
+    """Query 0 looks at state 1 alone and has a zero gradient: dv of state 1 is what the other queries
+    leave, whose probabilities there are 2^-ratio / Tk or so."""
+    B, Tq, Tk, H, Hkv, dh, _ = KERNELS[kernel]
+    a, q, kv, klen, dy = au.cross_case(96, B, max(Tq, 2), Tk, H, Hkv, dh, Tk)
+    f = np.float64
+    q[:] = 0
+    heads = q.reshape(B, -1, H, dh)
+    heads[:, :, :, 0] = -1
+    heads[:, 0, :, 0] = 40 / ratio
+    kv.reshape(B, Tk, 2, Hkv, dh)[:, :, 0] = 0
+    kv.reshape(B, Tk, 2, Hkv, dh)[:, 1, 0, :, 0] = ratio * np.log(2) * dh ** 0.5
+    dy[:] = 1 + np.abs(dy)
+    dy.reshape(B, -1, H, dh)[:, 0] = 0
+    wy, wl = ops.cross_attention_fwd(q.astype(f), kv.astype(f), klen, a)
+    _, wk, _ = ops.cross_attention_bwd(q.astype(f), kv.astype(f), klen, dy.astype(f), a)
+    _, dkv, _ = cross_bwd(a, q, kv, klen, wy.astype(np.float32), wl.astype(np.float32), dy)
+    got, want = (t.reshape(B, Tk, 2, -1)[:, 1, 1] for t in (dkv, wk))
+    # score, lse and exp2 with their arguments' roundings, pieces, instructions, joins
+    c = np.log(2) * (5 * ratio + 20) + 8 * np.log(Tk) + 8 + 6 * (a["Tq"] * H // Hkv) / 16 + 40
+    lost = np.abs(dy).reshape(B, -1, Hkv, H // Hkv, dh).sum((1, 3)).reshape(B, -1) * 2.0 ** -35
+    au.within("dv", got, want, c * au.U * want + lost)
