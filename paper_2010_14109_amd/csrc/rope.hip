@@ -67,6 +67,10 @@ struct Rows {
   int tile;                                  // rows a workgroup takes at once
   Divisor by_half, by_dh, by_heads, by_items, by_rest;
   int items;                                 // of a row: V columns each
+  // The norms' squares are of down x, down a power of two with dh down^2 <= 1: their sum is at most
+  // the largest square, where a sum of 1024 squares of 1e18 would pass fp32's range.  The factor is
+  // exact; squares that vanish below 2^-126 are of no account beside 1e-5.
+  float down;
 };
 
 // The pairs' (m cos, m sin) of rows r0 .. r0 + n into cs [n][half].
@@ -349,9 +353,12 @@ __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict
         other[k] = at_hand ? own[k] : partners<ODD>(x + at, d, r.half);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q += own[k].v[e] * own[k].v[e];
+      for (int e = 0; e < 4; ++e) {
+        const float t = r.down * own[k].v[e];
+        q += t * t;
+      }
     }
-    const float rs = 1.f / sqrtf(group_sum<G>(q) / (float)r.dh + 1e-5f);
+    const float rs = 1.f / sqrtf(group_sum<G>(q) / (r.down * r.down * (float)r.dh) + 1e-5f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int d = 4 * (lane + G * k);
@@ -418,14 +425,15 @@ __global__ __launch_bounds__(TPB) void qknorm_bwd_kernel(
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          q += xv[k].v[e] * xv[k].v[e];
-          dot += gd[k].v[e] * z[k].v[e] * xv[k].v[e];
+          const float t = r.down * xv[k].v[e];
+          q += t * t;
+          dot += gd[k].v[e] * z[k].v[e] * t;
         }
       }
       q = group_sum<G>(q);
       dot = group_sum<G>(dot);
-      const float rs = 1.f / sqrtf(q / (float)r.dh + 1e-5f);
-      const float mean = dot * rs / (float)r.dh;   // of gain z xhat
+      const float rs = 1.f / sqrtf(q / (r.down * r.down * (float)r.dh) + 1e-5f);
+      const float mean = dot * rs / (r.down * (float)r.dh);   // of gain z xhat
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int d = 4 * (lane + G * k);
@@ -517,6 +525,7 @@ Rows rows_of(const RopeShape& s, int64_t h1, int V, int64_t rows_a_group) {
   r.layout = (int)s.layout;
   r.h1 = (int)h1;
   r.items = r.cols / V;
+  for (r.down = 1.f; r.down * r.down * (float)s.dh > 1.f;) r.down *= 0.5f;
   // Rows a workgroup takes: their turns keep its threads busy at 8 rows of 64 rotated columns, and
   // a launch has at least 1024 workgroups where it has the rows for them.
   r.tile = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxTile, rows_a_group));
