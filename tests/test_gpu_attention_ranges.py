@@ -18,6 +18,7 @@ KERNELS = {
     "128 columns, pairs": (1, 70, 200, 2, 2, 96, [190]),
     "64 columns": (1, 70, 200, 1, 1, 160, [190]),
     "256 columns": (64, 129, 140, 8, 8, 32, None),
+    "256 columns, eight waves": (64, 129, 140, 8, 8, 72, None),
 }
 #: factors of the values of the first 64 states and of the others, and whether the first have all
 #: probabilities vanish
