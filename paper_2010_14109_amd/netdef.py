@@ -30,7 +30,8 @@ same size; cross attention keeps one logarithm per row and head instead.
 
 ``spec["input"]`` is the shape of the input ``x``; ``spec["inputs"]`` lists
 further INPUT variables, ``{"name", "shape", "dtype"}``: the tokens and lengths
-of a second sequence, positions, tables of angles.
+of a second sequence, positions, tables of angles.  All tokens are of as many
+sequences as ``x``, and attention takes its rows to be theirs in order.
 """
 
 from __future__ import annotations
@@ -183,8 +184,17 @@ class Net:
         self._call("add", [(X, ooc.R), (B, ooc.R), (Y, ooc.W)], [prod(xs)])
         return xs
 
+    def _positions(self, name, rows):
+        """Rows of each of the network's sequences in a tensor of ``rows`` rows."""
+        B = self.spec["input"][0]
+        if rows % B:
+            raise ValueError(f"{name}: {rows} rows do not divide into {B} sequences")
+        return rows // B
+
     def _fwd_embed(self, L, X):
         B, T = self.shape[X]
+        if B != self.spec["input"][0]:
+            raise ValueError(f"{L['name']}: {X} has {B} sequences, the network {self.spec['input'][0]}")
         d = L["d"]
         E = self._decl(L["name"] + ".E", (L["vocab"], d), kind=ooc.PARAM)
         pos = self._decl(L["name"] + ".pos", (T, d), kind=ooc.PARAM)
@@ -214,8 +224,7 @@ class Net:
 
     def _attn_attrs(self, L, X):
         rows, d3 = self.shape[X]
-        B = self.spec["input"][0]
-        T = rows // B
+        B, T = self.spec["input"][0], self._positions(L["name"], rows)
         H = L["heads"]
         return [B, T, H, d3 // 3 // H, 1 if L["causal"] else 0]
 
@@ -264,7 +273,8 @@ class Net:
             raise ValueError(f"{L['name']}: query and key widths do not fit the heads")
         if L["klen"] not in self.inputs or self.meta[L["klen"]][:2] != ((B,), "i32"):
             raise ValueError(f"{L['name']}: {L['klen']} must be an input of one int32 length per sequence")
-        return [B, self.shape[q][0] // B, self.shape[kv][0] // B, H, Hkv, dh]
+        Tq, Tk = (self._positions(L["name"], self.shape[t][0]) for t in (q, kv))
+        return [B, Tq, Tk, H, Hkv, dh]
 
     def _fwd_cross_attention(self, L, X):
         a = self._cross_attrs(L)
