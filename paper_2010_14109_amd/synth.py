@@ -398,9 +398,11 @@ def make_inputs(spec, seed=0):
 
 
 def make_extra_inputs(spec, tables=None, seed=2):
-    """``{name: array}`` of ``spec["inputs"]``: tokens uniform over the vocabulary, lengths uniform
-    over 1 .. the sequence, positions counting up in each sequence, and tables of angles:
-    ``tables[name]``, or 10000^(-2 i / rot) radians per position and magnitude 1."""
+    """``{name: array}`` of ``spec["inputs"]``, by type and name: i32 of two axes are tokens, uniform
+    over the vocabulary; i32 ``<tokens>_len`` their lengths, uniform over 1 .. the sequence; i32
+    ``*pos`` positions counting up in each sequence; f64 tables of angles, ``tables[name]`` or
+    10000^(-2 i / rot) radians per position and magnitude 1; f32 standard normal.  Anything else is a
+    ValueError."""
     g = np.random.Generator(np.random.PCG64(seed))
     shapes = {v["name"]: tuple(v["shape"]) for v in spec.get("inputs", ())}
     batch = spec["input"][0]
@@ -412,12 +414,16 @@ def make_extra_inputs(spec, tables=None, seed=2):
         elif v["dtype"] == "f64":
             half = shape[0] - 1
             out[name] = np.append(10000.0 ** (-np.arange(half) / half), 1.0)
-        elif name.endswith("_len"):
+        elif v["dtype"] == "f32":
+            out[name] = g.standard_normal(shape, np.float32)
+        elif v["dtype"] == "i32" and len(shape) == 2:
+            out[name] = g.integers(0, spec["classes"], size=shape).astype(np.int32)
+        elif v["dtype"] == "i32" and name.endswith("_len") and len(shapes.get(name[:-4], ())) == 2:
             out[name] = g.integers(1, shapes[name[:-4]][1] + 1, size=shape).astype(np.int32)
-        elif name.endswith("pos"):
+        elif v["dtype"] == "i32" and name.endswith("pos") and shape[0] % batch == 0:
             out[name] = (np.arange(shape[0]) % (shape[0] // batch)).astype(np.int32)
         else:
-            out[name] = g.integers(0, spec["classes"], size=shape).astype(np.int32)
+            raise ValueError(f"{name}: no synthetic values for {v['dtype']} {shape} of this name")
     return out
 
 

@@ -1,8 +1,9 @@
 """Network descriptions whose tensors hold other numbers of sequences than the network's input."""
 
+import numpy as np
 import pytest
 
-from paper_2010_14109_amd import netdef
+from paper_2010_14109_amd import netdef, synth
 from test_attention_ops_host import small_seq2seq
 
 
@@ -38,3 +39,17 @@ def test_rows_that_do_not_divide_into_the_sequences_are_refused(lib):
         net(28, op)
         with pytest.raises(ValueError, match="sequences"):
             net(27, op)
+
+
+def test_inputs_without_a_meaning_are_refused():
+    """Synthetic inputs follow names and types; one that fits none is not filled with guesses."""
+    spec = small_seq2seq(layers=1)
+    good = synth.make_extra_inputs(resized(spec))
+    assert good["src"].dtype == np.int32
+    for v in ({"name": "offsets", "shape": [3], "dtype": "i32"}, {"name": "mask", "shape": [3, 7], "dtype": "u8"},
+              {"name": "other_len", "shape": [3], "dtype": "i32"}):
+        with pytest.raises(ValueError, match=v["name"]):
+            synth.make_extra_inputs(dict(spec, inputs=spec["inputs"] + [v]))
+    states = synth.make_extra_inputs(dict(spec, inputs=spec["inputs"] + [
+        {"name": "memory_in", "shape": [21, 6], "dtype": "f32"}]))["memory_in"]
+    assert states.dtype == np.float32 and states.shape == (21, 6) and states.std() > 0.5
