@@ -37,10 +37,11 @@ PEAK_HBM_GBS = 8000.0          # MI355X HBM3E
 PCIE5_X16_GBS = 63.0           # theoretical, per direction
 
 
-def fn_work(op, attrs):
+def fn_work(op, attrs, states=None):
     """Algorithmic work of one function: ('flop', n) for GEMM-shaped ops, ('byte', n) for
     memory-bound ones (compulsory HBM bytes: every operand read once, every result
-    written once)."""
+    written once).  ``states``: of all sequences together, for a cross attention whose sequences
+    are padded."""
     a = attrs
     if op in ("linear_fwd", "linear_bwd_w", "linear_bwd_x"):
         return "flop", 2 * a[0] * a[1] * a[2]
@@ -97,9 +98,10 @@ def fn_work(op, attrs):
     if op == "qknorm_bwd":
         return "byte", 12 * a[0] * a[1] + 4 * a[0]
     if op in ("cross_attention_fwd", "cross_attention_bwd"):
-        # two products of every query and state forward, five backward
+        # two products of every query and state of its sequence forward, five backward
         B, Tq, Tk, H, Hkv, dh = a[:6]
-        return "flop", (2 if op.endswith("fwd") else 5) * 2 * B * H * Tq * Tk * dh
+        pairs = Tq * (B * Tk if states is None else states)
+        return "flop", (2 if op.endswith("fwd") else 5) * 2 * H * pairs * dh
     return "byte", 0
 
 
@@ -310,10 +312,15 @@ def run_mode(net, spec, x, labels, params, budget, window, chunk, steps, warmup,
         ctx.close()
 
 
-def kernel_table(net, fn_ms):
+def kernel_table(net, fn_ms, inputs=None):
+    """Time and work of each operation; ``inputs``: {name: array} of the network's further inputs,
+    whose lengths say how many states a cross attention has."""
     table = {}
     for j, (op, attrs) in enumerate(zip(net.fn_ops, net.fn_attrs)):
-        kind, work = fn_work(op, attrs)
+        states = None
+        if op.startswith("cross_attention") and inputs:
+            states = int(inputs[net.names[net.fn_vars[j][2][0]]].sum())
+        kind, work = fn_work(op, attrs, states)
         if op == "sgd":
             kind, work = "byte", sgd_bytes(net, j)
         e = table.setdefault(op, {"ms": 0.0, "launches": 0, "unit": kind, "work": 0})
@@ -494,7 +501,7 @@ def main():
     st = out["stats"]
     ms = out["elapsed"] / args.steps * 1e3
     value = batch * args.steps / out["elapsed"]
-    table = kernel_table(net, out["fn_ms"])
+    table = kernel_table(net, out["fn_ms"], synth.make_extra_inputs(spec))
     dom_op = max(table, key=lambda o: table[o]["ms"])
     dom = table[dom_op]
     roof = roofline(dom)

@@ -1,0 +1,19 @@
+"""``bench.py``'s figures of the attention-side operators (no GPU)."""
+
+
+import bench
+from paper_2010_14109_amd import netdef, synth
+from test_attention_ops_host import small_seq2seq
+
+
+def test_padding_is_not_work(lib):
+    """A step's cross attention is credited with the states that its sequences have."""
+    spec = small_seq2seq(layers=1)
+    net = netdef.Net(spec)
+    extra = synth.make_extra_inputs(spec)
+    assert extra["src_len"].sum() < 3 * 7
+    table = bench.kernel_table(net, [1.0] * len(net.fn_ops), extra)
+    d, seq = 24, 5                     # all heads' columns, positions of a sequence
+    for op, products in (("cross_attention_fwd", 2), ("cross_attention_bwd", 5)):
+        assert table[op]["work"] == products * 2 * d * seq * int(extra["src_len"].sum())
+    assert bench.fn_work("cross_attention_fwd", [2, 3, 5, 4, 2, 8, 1], 6) == ("flop", 2 * 2 * 4 * 3 * 6 * 8)
