@@ -31,8 +31,9 @@ import numpy as np
 
 from paper_2010_14109_amd import netdef, ooc, synth
 
-PEAK_BF16_TFLOPS = 2500.0      # MI355X dense bf16 matrix instructions
+PEAK_BF16_TFLOPS = 2500.0      # MI355X dense bf16 matrix instructions, and fp16
 PRODUCTS = 6                   # of bf16 pieces for each fp32 product (gemm.hip)
+FP16_PRODUCTS = 3              # of fp16 pieces for each fp32 product (attend.hip)
 PEAK_HBM_GBS = 8000.0          # MI355X HBM3E
 PCIE5_X16_GBS = 63.0           # theoretical, per direction
 
@@ -126,13 +127,16 @@ def algorithmic_bytes(net, op):
     return round(tot / n) if n else None
 
 
-def roofline(dom):
-    """Rate of the dominant function against what bounds it: products against the matrix
+def roofline(dom, op=None):
+    """Rate of the dominant function (``op``) against what bounds it: products against the matrix
     instructions that carry them, everything else against HBM."""
     if dom["unit"] == "flop":
-        peak = PEAK_BF16_TFLOPS / PRODUCTS
+        fp16 = op in ("cross_attention_fwd", "cross_attention_bwd")
+        products = FP16_PRODUCTS if fp16 else PRODUCTS
+        peak = PEAK_BF16_TFLOPS / products
         return {"bound": "mfma", "achieved": round(dom["rate"], 3), "peak": round(peak, 1),
-                "peak_of": f"fp32 products as {PRODUCTS} bf16 products of split operands, "
+                "peak_of": f"fp32 products as {products} {'fp16' if fp16 else 'bf16'} products of "
+                           f"split operands, "
                            f"{PEAK_BF16_TFLOPS:g} TFLOP/s dense",
                 "unit": "TFLOP/s", "frac": round(dom["rate"] / peak, 4), "traffic": None}
     return {"bound": "hbm", "achieved": round(dom["rate"], 1), "peak": PEAK_HBM_GBS,
@@ -504,7 +508,7 @@ def main():
     table = kernel_table(net, out["fn_ms"], synth.make_extra_inputs(spec))
     dom_op = max(table, key=lambda o: table[o]["ms"])
     dom = table[dom_op]
-    roof = roofline(dom)
+    roof = roofline(dom, dom_op)
     roof["traffic"] = measured_traffic(net, dom_op)
     roof["traffic_unit"] = ("bytes per launch fetched and written back by the L2 caches (rocprofv3 "
                             "FETCH_SIZE + WRITE_SIZE, calibrated; last-level-cache hits included)")

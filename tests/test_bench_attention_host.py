@@ -17,3 +17,12 @@ def test_padding_is_not_work(lib):
     for op, products in (("cross_attention_fwd", 2), ("cross_attention_bwd", 5)):
         assert table[op]["work"] == products * 2 * d * seq * int(extra["src_len"].sum())
     assert bench.fn_work("cross_attention_fwd", [2, 3, 5, 4, 2, 8, 1], 6) == ("flop", 2 * 2 * 4 * 3 * 6 * 8)
+
+
+def test_roof_of_fp16_pieces():
+    """Cross attention runs three fp16 products for each fp32 product, everything else six bf16 ones."""
+    dom = {"unit": "flop", "rate": 200.0}
+    r = bench.roofline(dom, "cross_attention_bwd")
+    assert r["peak"] == round(2500 / 3, 1) and "3 fp16" in r["peak_of"] and r["frac"] == round(600 / 2500, 4)
+    for op in ("conv_fwd", "attention_bwd", "linear_bwd_w"):
+        assert bench.roofline(dom, op) == bench.roofline(dom)
