@@ -117,12 +117,12 @@ def sgd_bytes(net, j):
 def algorithmic_bytes(net, op):
     """Mean compulsory bytes per launch of ``op``: every operand read once and every result
     written once (an input gradient reads the filter and the output gradient and writes the
-    input gradient).  Split-K partial sums (``.part``) are not compulsory and are left out."""
+    input gradient).  Partial sums (``.part``, ``.bpart``) are not compulsory and are left out."""
     tot, n = 0, 0
     for j, o in enumerate(net.fn_ops):
         if o == op:
             tot += sum(net.var_bytes[v] for v, _ in net.fn_vars[j]
-                       if not net.names[v].endswith(".part"))
+                       if not net.names[v].endswith((".part", ".bpart")))
             n += 1
     return round(tot / n) if n else None
 

@@ -26,3 +26,15 @@ def test_roof_of_fp16_pieces():
     assert r["peak"] == round(2500 / 3, 1) and "3 fp16" in r["peak_of"] and r["frac"] == round(600 / 2500, 4)
     for op in ("conv_fwd", "attention_bwd", "linear_bwd_w"):
         assert bench.roofline(dom, op) == bench.roofline(dom)
+
+
+def test_partial_results_are_not_algorithmic(lib):
+    """Neither direction's partial results (``.part``, ``.bpart``) count as compulsory bytes."""
+    net = netdef.Net(small_seq2seq(batch=1, src_seq=700, seq=300, layers=1))
+    sizes = dict(zip(net.names, net.var_bytes))
+    assert any(n.endswith("cross.part") for n in sizes) and any(n.endswith("cross.bpart") for n in sizes)
+    q, kv, y = sizes["d1.qn"], sizes["d1.kn"], sizes["d1.cross"]
+    lse = sizes["d1.cross.lse"]
+    assert bench.algorithmic_bytes(net, "cross_attention_fwd") == q + kv + y + 4 + lse
+    # q, kv, lengths, y, lse, dy read; dq, dkv and delta written
+    assert bench.algorithmic_bytes(net, "cross_attention_bwd") == 4 * q + 2 * kv + 4 + 2 * lse
