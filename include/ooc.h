@@ -550,7 +550,10 @@ ooc_status ooc_attention_slices(int32_t op, const int64_t *attrs, int32_t n_attr
  * shorter than bytes[j]; a variable that is written and overlaps another;
  * a stream of another device.  OOC_E_UNSUPPORTED: SGD, whose rates belong to
  * ooc_step.  OOC_E_DEVICE: a launch failed, or there is no such device.
- * Message on ooc_last_error(NULL).  The caller's current device is kept. */
+ * Message on ooc_last_error(NULL).  The caller's current device is kept.  An
+ * error that an earlier HIP call of the same thread left pending is not this
+ * call's and is cleared, as hipGetLastError does: a program that looks for
+ * one looks before. */
 ooc_status ooc_run_fn(int32_t hip_device, void *stream, int32_t op, void *const *ptrs,
                       const uint64_t *bytes, const uint8_t *access, int32_t n,
                       const int64_t *attrs, int32_t n_attrs);

@@ -92,7 +92,9 @@ ooc_status run_fn(int32_t device, hipStream_t stream, int32_t op, void* const* p
       return refuse(OOC_E_INVALID, "variable " + std::to_string(j) + " is longer than its memory");
   }
   const std::vector<uint8_t> dead((size_t)n, 0);   // the caller may read whatever is written
-  (void)hipGetLastError();   // an earlier call's error is not this launch's
+  // The launchers ask hipGetLastError, which would also report an error that an earlier call of the
+  // caller's left pending; there is no way to put one back.
+  (void)hipGetLastError();
   const hipError_t r = launch_fn(fn, ptrs, bytes, dead.data(), Join::kNone, BnBehind{}, 0.f, 0.f,
                                  stream);
   if (r != hipSuccess) return refuse(OOC_E_DEVICE, std::string("launch failed: ") + hipGetErrorString(r));

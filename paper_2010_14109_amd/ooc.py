@@ -205,7 +205,8 @@ def run_fn(op, vars_, access, attrs=(), device=0, stream=0):
     """Runs one operation alone on the caller's device memory (see ooc_run_fn): ``vars_`` are its
     variables as ``(device address, bytes)``, ``access`` and ``attrs`` as ``add_fn`` takes them,
     ``stream`` a HIP stream handle of ``device`` (a PyTorch stream's ``cuda_stream``).  Returns
-    once the kernels are enqueued.  A program that passes PyTorch's memory imports torch before
+    once the kernels are enqueued.  A HIP error that an earlier call of the thread left pending is
+    cleared.  A program that passes PyTorch's memory imports torch before
     the first call here, so that both use one HIP runtime."""
     n = len(vars_)
     p = (ctypes.c_void_p * n)(*[v for v, _ in vars_])
