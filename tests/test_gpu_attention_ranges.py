@@ -161,3 +161,30 @@ def test_a_query_without_gradient_that_takes_a_state(kernel, ratio):
     c = np.log(2) * (5 * ratio + 20) + 8 * np.log(Tk) + 8 + 6 * (a["Tq"] * H // Hkv) / 16 + 40
     lost = np.abs(dy).reshape(B, -1, Hkv, H // Hkv, dh).sum((1, 3)).reshape(B, -1) * 2.0 ** -35
     au.within("dv", got, want, c * au.U * want + lost)
+
+
+#: factors of the keys, of the values (first 64 states, the others), of the queries and of their
+#: gradients (first 64 positions, the others)
+UNLIKE = [((2.0 ** -60, 2.0 ** 30), (1, 1), (2.0 ** -30, 2.0 ** -30), (1, 1)),
+          ((2.0 ** 30, 2.0 ** -60), (1, 1), (2.0 ** -30, 2.0 ** -30), (1, 1)),
+          ((1, 1), (2.0 ** -70, 2.0 ** 70), (1, 1), (2.0 ** -60, 2.0 ** -60)),
+          ((1, 1), (2.0 ** 70, 2.0 ** -70), (1, 1), (2.0 ** -60, 2.0 ** -60)),
+          ((1, 1), (1, 1), (1, 1), (2.0 ** -50, 2.0 ** 50)), ((1, 1), (1, 1), (1, 1), (2.0 ** 50, 2.0 ** -50)),
+          ((1, 1), (1, 1), (1, 1), (0, 2.0 ** -80)), ((0, 1), (0, 1), (0, 1), (0, 1)),
+          ((2.0 ** -90, 2.0 ** -95), (2.0 ** 80, 2.0 ** 90), (2.0 ** 85, 2.0 ** 95), (2.0 ** -90, 2.0 ** -80)),
+          ((2.0 ** -40, 2.0 ** 40), (2.0 ** 40, 2.0 ** -40), (2.0 ** -40, 2.0 ** -100), (2.0 ** -40, 2.0 ** 40))]
+
+
+@pytest.mark.parametrize("sizes", UNLIKE, ids=str)
+@pytest.mark.parametrize("dh", [24, 64, 85, 200])
+def test_whole_gradients_of_unlike_sizes(dh, sizes):
+    """Every operand of unlike sizes along its rows, alike within the 64 that share a scale (from the first
+    of a head or slice on): all gradients relative to what they sum."""
+    a, q, kv, klen, dy = au.cross_case(97, 2, 150, 170, 4, 2, dh, [170, 90])
+    states = kv.reshape(2, 170, 2, 2, dh)
+    for part, t in ((slice(0, 64), 0), (slice(64, None), 1)):
+        states[:, part, 0] *= np.float32(sizes[0][t])
+        states[:, part, 1] *= np.float32(sizes[1][t])
+        q.reshape(2, 150, -1)[:, part] *= np.float32(sizes[2][t])
+        dy.reshape(2, 150, -1)[:, part] *= np.float32(sizes[3][t])
+    check_cross(a, q, kv, klen, dy, slices=(None, (1, 1)))
