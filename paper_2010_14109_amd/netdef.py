@@ -86,6 +86,8 @@ class Net:
 
     # ------------------------------------------------------------ helpers
     def _decl(self, name, shape, dtype="f32", kind=ooc.TEMP):
+        if name in self.meta:
+            raise ValueError(f"{name}: the name of two tensors")
         self.meta[name] = (tuple(int(s) for s in shape), dtype, kind)
         return name
 
