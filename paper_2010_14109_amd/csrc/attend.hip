@@ -449,7 +449,8 @@ struct Raw {
 // 2^11; of one below 2^-2 its pieces hold what is above 2^-25, 2^-36 of the largest or less.  Both are
 // whole so that changing them is exact.  Where p is too far below the units of the sum (m - ve - ms
 // past kFar: other tiles' values are far larger, or this one's are zero, and p may vanish while the
-// probability counts), the probabilities are computed again for the sum alone.
+// probability counts), the probabilities are computed again for the sum alone.  (More room, from 2^8 up,
+// would rescale less often: 1 % of 24 x 512 x 512, nothing elsewhere, for four bits of small p.)
 constexpr float kTop = 12.f, kRoom = 3.f, kLag = 64.f, kFar = 64.f;
 __device__ inline bool outgrown(float top, float ve, float m, float ms) {
   return top + ve > m + kRoom || top > ms + kLag;
@@ -465,7 +466,8 @@ __device__ inline float raise(float top, float ve, float& m, float& ms, float& s
 }
 // What turns a column's sum of p times scaled values into its quotient by `total`, a factor, and log2
 // of the sum of 2^score.  The factor is 2^(m - ms - 26) / total, total's power of two taken into the
-// exponent; where that is below the normal numbers' (values below 2^-70 or so), the sum takes kDown of it.
+// exponent; where that is below the normal numbers' (values below 2^-94 times the states that share the
+// weight), the sum takes kDown of it.
 struct Quotient {
   static constexpr float kDown = 0x1p-60f;
   float factor, log;
@@ -630,7 +632,7 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
 // reading the states once.  Each wave takes tiles of 32 states of its own, without barriers: k goes
 // from memory straight into the A operand, v through the wave's part of LDS.  A workgroup's waves
 // and then the slices join their results.  Products are 16 x 16 x 32: 16 columns are all there is,
-// and half the registers of 32 let a SIMD hold three waves, whose loads are all in flight at once.
+// and half the registers of 32 let a SIMD hold three waves, where there are as many.
 // One token of 8 sequences of up to 4096 states, 16 heads of 64 on 4 key heads: 33.9 us with the
 // kernel for many queries, 18 with this one (14, and 4 for the join; reading the 34 MB at the rate of
 // a large copy takes 7).
@@ -1101,7 +1103,8 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
 // holds a first matrix and forms the scores and probabilities, role 1 a second and forms dP; they
 // exchange values through LDS, and each then multiplies on.  The waves of a pair sit on one SIMD:
 // while one computes exponentials or splits the next tiles, the other multiplies.  2 x 4096 x 4096,
-// 16 heads of 128: dk and dv 3.24 -> 1.65 ms, dq 1.56 -> 1.34.  At 64 columns, where one wave's
+// 16 heads of 128 on 4, on one card: dk and dv 3.24 -> 1.65 ms, dq 1.56 -> 1.34 (over several cards, as
+// their clocks allow: 1.65 .. 1.79 and 1.34 .. 1.45).  At 64 columns, where one wave's
 // registers suffice, pairs are slower (24 x 512 x 512: 0.22 against 0.20 ms and 0.19 against 0.15).
 
 // Over the states: dq.  Columns are queries; role 0 holds q, role 1 dy; each multiplies half of the
@@ -1400,10 +1403,10 @@ dim3 grid_of(const Shape& s, int tiles, int64_t slices) {
   return dim3((unsigned)(ceil_div((int64_t)s.B * s.Hkv, kXcds) * kXcds * tiles), (unsigned)slices);
 }
 // Whether the forward's workgroups have 256 columns, not 128: where that leaves less than a tenth
-// more columns idle, which is what the wide ones gain (4096 x 4096: 0.79 against 0.87 ms at 2 x 16
-// heads of 128, 0.93 against 1.03 at 4 x 16 heads of 64; 333 queries, 12 heads of 85: 87 us wide,
-// 63 narrow), and there are two of them for each CU (77 states, 2 x 4096 queries, 8 heads of 64:
-// 17.4 us wide, 16.4 narrow).
+// more columns idle, which is what the wide ones gain (4096 x 4096: 0.86 against 0.96 ms at 2 x 16
+// heads of 128, 0.89 against 0.98 at 4 x 16 heads of 64; 333 queries, 12 heads of 85: 81 us wide,
+// 60 narrow), and there are two of them for each CU (77 states, 2 x 4096 queries, 8 heads of 64:
+// 18.1 us wide, 16.8 narrow).
 bool wide(const AttendShape& a) {
   const int64_t halves = ceil_div(a.Tq * (a.H / a.Hkv), 128);
   return a.dh <= 128 && (halves % 2 == 0 || halves >= 10) && a.B * a.Hkv * ceil_div(halves, 2) >= 512;

@@ -290,8 +290,7 @@ __device__ inline float group_sum(float v) {
 }
 
 // The columns behind the heads of a tile's rows are copied, all rows' together: a row at a time, with
-// most threads idle, 12288 rows of 20 heads of 64 and 256 columns took 46 us forward and 41 backward,
-// so 43 and 39.
+// most threads idle, 12288 rows of 20 heads of 64 and 256 columns took 3 us more forward, 2 backward (39).
 template <bool ODD>
 __device__ inline void copy_rest(const float* __restrict__ x, float* __restrict__ y, int64_t r0, int n,
                                  const Rows& r) {
@@ -320,7 +319,7 @@ __global__ __launch_bounds__(TPB) void qknorm_fwd_kernel(const float* __restrict
   }
   const int lane = threadIdx.x % G, step = TPB / G * gridDim.y, total = n * r.heads;
   // With one four a lane, both rows' gains of it and of its partners stay in registers: 12288 rows of
-  // 20 heads of 64 and 256 columns took 39 us with their loads for every head, so 31 (4.9 TB/s).
+  // 20 heads of 64 and 256 columns took 39 us with their loads for every head, so 34 (4.4 TB/s).
   Four kept[2] = {}, kept_partners[2] = {};
   if (K == 1 && 4 * lane < r.dh) {
 #pragma unroll
