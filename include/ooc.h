@@ -55,7 +55,7 @@ enum {
   OOC_E_INVALID = -1,     /* bad argument or ill-formed function sequence */
   OOC_E_STATE = -2,       /* call out of order */
   OOC_E_INFEASIBLE = -3,  /* budget below the footprint of one function */
-  OOC_E_HOST_OOM = -4,    /* pinned host memory could not be allocated */
+  OOC_E_HOST_OOM = -4,    /* host memory, pinned or not, could not be allocated */
   OOC_E_DEVICE = -5,      /* a HIP call failed (message names it) */
   OOC_E_UNSUPPORTED = -6  /* valid request this build cannot serve */
 };

@@ -441,17 +441,20 @@ ooc_status ooc_wgrad_slices(int32_t op, const int64_t* attrs, int32_t n_attrs, i
   return OOC_E_INVALID;
 }
 
-ooc_status ooc_qknorm_slices(int64_t rows, int64_t* slices) {
+// A message takes memory: where there is none, the status comes without one.
+ooc_status ooc_qknorm_slices(int64_t rows, int64_t* slices) try {
   if (!slices || rows < 1) {
     g_create_error = "ooc_qknorm_slices: bad argument";
     return OOC_E_INVALID;
   }
   *slices = rows > 8 * 2048 ? 2048 : (rows + 7) / 8;
   return OOC_OK;
+} catch (const std::bad_alloc&) {
+  return OOC_E_HOST_OOM;
 }
 
 ooc_status ooc_attention_slices(int32_t op, const int64_t* attrs, int32_t n_attrs,
-                                int64_t slices[2], uint64_t* part_bytes) {
+                                int64_t slices[2], uint64_t* part_bytes) try {
   if (!slices || !attrs || !part_bytes || n_attrs < 6) {
     g_create_error = "ooc_attention_slices: NULL argument or fewer than 6 attributes";
     return OOC_E_INVALID;
@@ -473,6 +476,8 @@ ooc_status ooc_attention_slices(int32_t op, const int64_t* attrs, int32_t n_attr
   slices[1] = full[7] = fwd ? 1 : attention_query_slices(a);
   *part_bytes = (uint64_t)attention_part_bytes(fwd, full);
   return OOC_OK;
+} catch (const std::bad_alloc&) {
+  return OOC_E_HOST_OOM;
 }
 
 ooc_status ooc_run_fn(int32_t hip_device, void* stream, int32_t op, void* const* ptrs,
