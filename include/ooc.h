@@ -199,14 +199,17 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                own row and head, or of a head in 32 or 64 neighbouring rows) where that is more;
  *                probabilities and their gradients to 2^-23, or to 2^-35 of the largest of their
  *                query (in dkv: of their state), each times the largest value of the 32 or 64 rows
- *                it meets.  H dh and Hkv dh at
- *                most 2^20.  part = partial results, present iff slices > 1
- *                (ooc_attention_slices gives counts and its bytes)
+ *                it meets.  A score is off by up to 2^-21 sum |q k| / sqrt(dh), a probability by as
+ *                much of itself; scores may be of any size.  H dh and Hkv dh at most 2^20.
+ *                part = partial results, present iff slices > 1 (ooc_attention_slices gives counts
+ *                and its bytes)
  *                                     q[R] kv[R] klen[R] Y[W] lse[W] [part[W]]
  *                                                                  B Tq Tk H Hkv dh slices
  *  CROSS_ATTENTION_BWD
  *                dq and dkv (zero at and past klen) of the above; delta [B][H][Tq] receives the
- *                row sums of dY Y.  part = partial sums, present iff a slice count > 1
+ *                row sums of dY Y.  Probabilities are exp(S - lse) of the lse given, whose own
+ *                rounding is 2^-24 of it: |S| at most 2^20 here, gradients of larger scores mean
+ *                nothing.  part = partial sums, present iff a slice count > 1
  *                                     q[R] kv[R] klen[R] Y[R] lse[R] dY[R] dq[W] dkv[W] delta[W]
  *                                     [part[W]]          B Tq Tk H Hkv dh q_slices kv_slices
  *  MIX           swap-integrity test op on uint32 words (sizes multiple of

@@ -444,36 +444,47 @@ struct Raw {
 // The running softmax of a column, in powers of two and apart for the two sums it divides, as a
 // tile's values bring an exponent of their own (ve of Raw::exponents, -112 for zeros).  ms is a whole
 // number no more than kLag below the largest score, and the sum of probabilities is in units of 2^ms.
-// m is a whole number no more than kRoom below the largest score + ve, and a probability meets the
-// values' pieces as p = 2^(score + ve - m + kTop), so that p is at most 2^15 and the largest are above
-// 2^11; of one below 2^-2 its pieces hold what is above 2^-25, 2^-36 of the largest or less.  Both are
-// whole so that changing them is exact.  Where p is too far below the units of the sum (m - ve - ms
-// past kFar: other tiles' values are far larger, or this one's are zero, and p may vanish while the
-// probability counts), the probabilities are computed again for the sum alone.  (More room, from 2^8 up,
-// would rescale less often: 1 % of 24 x 512 x 512, nothing elsewhere, for four bits of small p.)
-constexpr float kTop = 12.f, kRoom = 3.f, kLag = 64.f, kFar = 64.f;
-__device__ inline bool outgrown(float top, float ve, float m, float ms) {
-  return top + ve > m + kRoom || top > ms + kLag;
+// d is a whole number, and ms + d no more than kRoom below the largest score + ve: a probability meets
+// the values' pieces as p = 2^(score - ms - d + ve + kTop), so that p is at most 2^15 and the largest are
+// above 2^11; of one below 2^-2 its pieces hold what is above 2^-25, 2^-36 of the largest or less.  Both are
+// whole so that changing them is exact.  (More room, from 2^8 up, would rescale less often: 1 % of
+// 24 x 512 x 512, nothing elsewhere, for four bits of small p.)
+//
+// Two rare cases take the terms apart: p too far below the units of the sum (d - ve past kFar: other
+// tiles' values are far larger, or this one's are zero, and p may vanish while the probability counts),
+// and scores from kLarge on: a score is a product a c, rounded where the largest is taken and exact in
+// fma(a, c, ..), and the difference could take p out of its room, d and ve be lost beside ms.  There
+// each score is rounded, ms taken off, and the probability computed for the sum alone.
+constexpr float kTop = 12.f, kRoom = 3.f, kLag = 64.f, kFar = 64.f, kLarge = 0x1p22f;
+__device__ inline bool outgrown(float top, float ve, float d, float ms) {
+  const float t = top - ms;
+  return t + ve > d + kRoom || t > kLag;
 }
-// m and ms for a tile with the largest score `top`; returns the factor of the sums with m
-__device__ inline float raise(float top, float ve, float& m, float& ms, float& sum) {
-  const float up = fmaxf(m, ceilf(top + ve)), f = m == up ? 1.f : exp2f(m - up);
-  const float us = fmaxf(ms, ceilf(top));
-  sum *= ms == us ? 1.f : exp2f(ms - us);
-  m = up;
+// d and ms for a tile with the largest score `top`; returns the factor of the sums with d
+__device__ inline float raise(float top, float ve, float& d, float& ms, float& sum) {
+  const float us = fmaxf(ms, ceilf(top)), by = ms == us ? 0.f : ms - us;
+  const float now = d + by, up = fmaxf(now, ceilf(top - us + ve));
+  sum *= exp2f(by);
   ms = us;
-  return f;
+  d = up;
+  return now == up ? 1.f : exp2f(now - up);
+}
+// a c, rounded: without the barrier the compiler makes one fma of the product and a subtraction behind it
+__device__ inline float score(float a, float c) {
+  float t = a * c;
+  asm("" : "+v"(t));
+  return t;
 }
 // What turns a column's sum of p times scaled values into its quotient by `total`, a factor, and log2
-// of the sum of 2^score.  The factor is 2^(m - ms - 26) / total, total's power of two taken into the
+// of the sum of 2^score.  The factor is 2^(d - 26) / total, total's power of two taken into the
 // exponent; where that is below the normal numbers' (values below 2^-94 times the states that share the
 // weight), the sum takes kDown of it.
 struct Quotient {
   static constexpr float kDown = 0x1p-60f;
   float factor, log;
   bool low;
-  __device__ Quotient(float total, float m, float ms) {
-    const float l = __builtin_amdgcn_logf(total), whole = rintf(l), e = m - ms - (kTop + 14.f) - whole;
+  __device__ Quotient(float total, float d, float ms) {
+    const float l = __builtin_amdgcn_logf(total), whole = rintf(l), e = d - (kTop + 14.f) - whole;
     low = e < -120.f;
     factor = __builtin_amdgcn_exp2f(low ? e + 60.f : e) / (total * __builtin_amdgcn_exp2f(-whole));
     log = ms + l;
@@ -518,10 +529,10 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
     qc[x] = split_column<DH>(v, qp[x]) * s.scale * kLog2e;
   }
   floatx16 o[C][Wd::kSums];
-  float m[C], ms[C], sum[C];   // see kTop
+  float d[C], ms[C], sum[C];   // see kTop
 #pragma unroll
   for (int x = 0; x < C; ++x) {
-    m[x] = ms[x] = -INFINITY;
+    d[x] = ms[x] = -INFINITY;
     sum[x] = 0.f;
 #pragma unroll
     for (int t = 0; t < Wd::kSums; ++t) o[x][t] = floatx16{};
@@ -564,13 +575,13 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
         top[x] = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) top[x] = fmaxf(top[x], a[x][i]);
-        top[x] = max_of_halves(top[x]) * c[x];
-        past |= outgrown(top[x], ve, m[x], ms[x]);
+        top[x] = score(max_of_halves(top[x]), c[x]);
+        past |= outgrown(top[x], ve, d[x], ms[x]);
       }
       if (__builtin_expect(__any(past), 0))
 #pragma unroll
         for (int x = 0; x < C; ++x) {
-          const float f = raise(top[x], ve, m[x], ms[x], sum[x]);
+          const float f = raise(top[x], ve, d[x], ms[x], sum[x]);
 #pragma unroll
           for (int t = 0; t < Wd::kSums; ++t)
 #pragma unroll
@@ -579,21 +590,25 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
       Pieces pp[C][2];
 #pragma unroll
       for (int x = 0; x < C; ++x) {
-        const float off = ve + kTop - m[x], far = m[x] - ve - ms[x];
-        float p[16], part = 0.f;
+        const float far = d[x] - ve;
+        const bool apart = __any(far > kFar || fabsf(ms[x]) > kLarge);
+        float base = -ms[x], p[16], part = 0.f, alone = 0.f;
+        if (__builtin_expect(apart, 0)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            a[x][i] = score(a[x][i], c[x]) - ms[x];
+            alone += __builtin_amdgcn_exp2f(a[x][i]);
+          }
+          c[x] = 1.f;
+          base = 0.f;
+        }
+        const float off = base - (far - kTop);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           p[i] = __builtin_amdgcn_exp2f(fmaf(a[x][i], c[x], off));
           part += p[i];
         }
-        float g = __builtin_amdgcn_exp2f(far - kTop);
-        if (__builtin_expect(__any(far > kFar), 0)) {
-          part = 0.f;
-          g = 1.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(a[x][i], c[x], -ms[x]));
-        }
-        sum[x] = fmaf(part, g, sum[x]);
+        sum[x] = apart ? sum[x] + alone : fmaf(part, __builtin_amdgcn_exp2f(far - kTop), sum[x]);
         pp[x][0] = split8(p);
         pp[x][1] = split8(p + 8);
       }
@@ -613,7 +628,7 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
     const int col = col0 + 32 * x;
     if (col >= s.R) continue;
     const float none = bad ? NAN : 0.f;
-    const Quotient f(total, m[x], ms[x]);
+    const Quotient f(total, d[x], ms[x]);
     if (__any(f.low))
 #pragma unroll
       for (int t = 0; t < Wd::kSums; ++t)
@@ -714,7 +729,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
   floatx4 o[kBlocks];
 #pragma unroll
   for (int t = 0; t < kBlocks; ++t) o[t] = floatx4{};
-  float m = -INFINITY, ms = -INFINITY, sum = 0.f;   // see kTop
+  float d = -INFINITY, ms = -INFINITY, sum = 0.f;   // see kTop
   const auto largest = [&](const float (&x)[DH / 2]) {
     float top = max_abs(x, DH / 2);
     if (__any(top == INFINITY)) {   // the largest finite one: see Raw::publish
@@ -743,7 +758,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
         Rows<DH, T>::store(vs, 16 * h + l16, 4 * t + quarter, split8(v + 8 * (h * kSteps + t), exp2_of(14 - ev)));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     load_tile(j0 + W * T, to_v, v);
-    const float c = fmaxf(qc * exp2_of(ek - 14), 0x1p-126f);   // a masked score stays -inf
+    float c = fmaxf(qc * exp2_of(ek - 14), 0x1p-126f);   // a masked score stays -inf
     const float ve = (float)ev;
     float p[8], top = -INFINITY;
 #pragma unroll
@@ -752,34 +767,39 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
       p[i] = there ? a[i / 4][i % 4] : -INFINITY;
       top = fmaxf(top, p[i]);
     }
-    top = max_of_quarters(top) * c;
-    if (__builtin_expect(__any(outgrown(top, ve, m, ms)), 0)) {
-      const float f = raise(top, ve, m, ms, sum);
+    top = score(max_of_quarters(top), c);
+    if (__builtin_expect(__any(outgrown(top, ve, d, ms)), 0)) {
+      const float f = raise(top, ve, d, ms, sum);
 #pragma unroll
       for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[t][i] *= f;
     }
-    const float off = ve + kTop - m, far = m - ve - ms;
-    float part = 0.f;
-    if (__builtin_expect(__any(far > kFar), 0)) {
+    const float far = d - ve;
+    const bool apart = __any(far > kFar || fabsf(ms) > kLarge);
+    float base = -ms, part = 0.f, alone = 0.f;
+    if (__builtin_expect(apart, 0)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) part += __builtin_amdgcn_exp2f(fmaf(p[i], c, -ms));
-      sum += part;
-      part = 0.f;
+      for (int i = 0; i < 8; ++i) {
+        p[i] = score(p[i], c) - ms;
+        alone += __builtin_amdgcn_exp2f(p[i]);
+      }
+      c = 1.f;
+      base = 0.f;
     }
+    const float off = base - (far - kTop);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, off));
       part += p[i];
     }
-    if (!__any(far > kFar)) sum = fmaf(part, __builtin_amdgcn_exp2f(far - kTop), sum);
+    sum = apart ? sum + alone : fmaf(part, __builtin_amdgcn_exp2f(far - kTop), sum);
     const Pieces pp = split8(p);
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) o[t] = mma16(Rows<DH, T>::by_column16(vs, t), pp, o[t]);
   }
   sum = sum_of_quarters(sum);
-  const Quotient f(sum, m, ms);
+  const Quotient f(sum, d, ms);
   const bool none = sum == 0.f;   // a wave without states
   const float down = f.low ? Quotient::kDown : 1.f;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -188,3 +188,33 @@ def test_whole_gradients_of_unlike_sizes(dh, sizes):
         q.reshape(2, 150, -1)[:, part] *= np.float32(sizes[2][t])
         dy.reshape(2, 150, -1)[:, part] *= np.float32(sizes[3][t])
     check_cross(a, q, kv, klen, dy, slices=(None, (1, 1)))
+
+
+@pytest.mark.parametrize("size", [12, 23, 26, 100])
+@pytest.mark.parametrize("later", [2.0 ** -20, 2.0 ** 20])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_scores_of_any_size(kernel, later, size):
+    """Scores that differ by 2^size / sqrt(dh) and more, to both sides of zero: each query has one state, or
+    two of the same key in tiles whose values are unlike, and lse is its score."""
+    a, q, kv, klen, _ = au.cross_case(98, *KERNELS[kernel])
+    B, Tq, Tk, H, Hkv, dh = au.cross_shape(a)
+    g = np.random.default_rng(99)
+    rank = 1.0 + g.permutation(Tk)               # whole numbers: exact in one fp16 piece
+    top, low = np.argmax(rank[:64]), np.argmin(rank[:64])
+    rank[top], rank[low] = Tk + 1, 0.5
+    rank[64 + 6], rank[64 + 7] = rank[top], rank[low]
+    states = kv.reshape(B, Tk, 2, Hkv, dh)
+    states[:, :, 0] = 0
+    states[:, :, 0, :, 0] = (rank * 2.0 ** (size // 2))[None, :, None]
+    states[:, 64:, 1] *= np.float32(later)
+    q[:] = 0
+    q.reshape(B, Tq, H, dh)[..., 0] = g.choice([-1.0, 1.0], (B, Tq, H)) * 2.0 ** (size - size // 2)
+    y, lse = cross_fwd(a, q, kv, klen)
+    f = np.float64
+    wy, wl = ops.cross_attention_fwd(q.astype(f), kv.astype(f), klen, a)
+    abs_v = kv.astype(f).copy()
+    abs_v.reshape(states.shape)[:, :, 1] = np.abs(states[:, :, 1])
+    weight, _ = ops.cross_attention_fwd(q.astype(f), abs_v, klen, a)
+    # pieces, instructions and joins as in the means above; the score's scale is a product of three
+    au.within("y", y, wy, (2 + 6 * np.ceil(Tk / 16) + 40) * au.U * weight + 2.0 ** -39 * np.abs(states[:, :, 1]).max())
+    au.within("lse", lse, wl, 8 * au.U * np.abs(wl) + 16 * au.U)
