@@ -18,8 +18,8 @@
  *    negative ooc_status and sets a message readable with ooc_last_error():
  *    on the context for calls that take one (const queries included), else
  *    (a NULL context, ooc_create, ooc_link_probe, ooc_wgrad_slices,
- *    ooc_qknorm_slices, ooc_attention_slices, ooc_run_fn) on
- *    ooc_last_error(NULL).  A NULL out-pointer, or a NULL buffer with a
+ *    ooc_qknorm_slices, ooc_attention_slices, ooc_join_slices,
+ *    ooc_scan_slices, ooc_run_fn) on ooc_last_error(NULL).  A NULL out-pointer, or a NULL buffer with a
  *    nonzero capacity, is OOC_E_INVALID; a query made before the stage it
  *    needs is OOC_E_STATE.
  *  - A context is driven in this order: create -> add_var / add_fn ->
@@ -212,6 +212,37 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                nothing.  part = partial sums, present iff a slice count > 1
  *                                     q[R] kv[R] klen[R] Y[R] lse[R] dY[R] dq[W] dkv[W] delta[W]
  *                                     [part[W]]          B Tq Tk H Hkv dh q_slices kv_slices
+ *  DROPOUT       Y = X where a random word of 32 bits is `drop` or more, times 2^32 / (2^32 - drop)
+ *                rounded to fp32; 0 elsewhere, whatever X holds.  The words are Philox 4x32-10's
+ *                (Salmon et al., 2011): value i takes word i mod 4 of the counter (i / 4, salt), low
+ *                32 bits first, under the key `seed` (two uint32), so the mask need not be kept: the
+ *                backward is the operation itself on dY, with the same seed and salt.  drop 0: a copy
+ *                                     X[R] seed[R] Y[W]            n drop salt
+ *  JOIN_FWD      a block's output F joins its residual stream X, and the next block's input N leaves:
+ *                H = scale X + gate dropout(post F / rms(F)), N = pre H / rms(H), rms over the d
+ *                columns of a row with 1e-5 added to the mean square; post, pre [d]; gate [groups][d],
+ *                a row of it for each rows / groups consecutive rows; scale one float; dropout as
+ *                above over the whole [rows][d], with a seed iff drop > 0.  stats = 1 / rms of F and of
+ *                H, by row.  d at most 8192, rows below 2^23; |F|, |H| up to 1e17
+ *                                     X[R] F[R] post[R] gate[R] pre[R] scale[R] [seed[R]] H[W] N[W]
+ *                                     stats[W]                     rows d groups drop salt
+ *  JOIN_BWD      dX, dF, dpost, dgate and dpre of the above (scale is a constant); dH, the gradient of
+ *                what else reads H, iff stream = 1; part = three partial rows per slice of a gate's
+ *                rows (ooc_join_slices gives a count)
+ *                                     F[R] H[R] stats[R] post[R] gate[R] pre[R] scale[R] [seed[R]]
+ *                                     [dH[R]] dN[R] dX[W] dF[W] dpost[W] dgate[W] dpre[W] part[W]
+ *                                                       rows d groups drop salt stream slices
+ *  SCAN_FWD      gated recurrence along the T rows of each of B sequences, by column: FX [B T][2 C]
+ *                holds f, then x; a = sigmoid(f), H_t = a_t H_(t-1) + (1 - a_t) x_t.  The state before
+ *                the first row is h0 [B][C] iff carry = 1, else 0; iff fresh = 1, it is 0 too before
+ *                each row whose entry in fresh [B T] (int32) is not 0.  Where a gate, or a product of
+ *                gates, is 0 in fp32, the state before does not count, be it a NaN.  part = partial
+ *                results, present iff slices > 1 (ooc_scan_slices gives a count and its bytes)
+ *                                     FX[R] [h0[R]] [fresh[R]] H[W] [part[W]]
+ *                                                                  B T C carry fresh slices
+ *  SCAN_BWD      dFX, and dh0 iff carry = 1, of the above
+ *                                     FX[R] [h0[R]] [fresh[R]] H[R] dH[R] dFX[W] [dh0[W]] [part[W]]
+ *                                                                  B T C carry fresh slices
  *  MIX           swap-integrity test op on uint32 words (sizes multiple of
  *                4): the last variable y is the only one written (W or RW),
  *                the others are read; y[j] = seed ^ (j * 2654435761) ^ sum
@@ -258,7 +289,12 @@ enum {
   OOC_OP_QKNORM_BWD = 35,
   OOC_OP_CROSS_ATTENTION_FWD = 36,
   OOC_OP_CROSS_ATTENTION_BWD = 37,
-  OOC_OP_COUNT = 38
+  OOC_OP_DROPOUT = 38,
+  OOC_OP_JOIN_FWD = 39,
+  OOC_OP_JOIN_BWD = 40,
+  OOC_OP_SCAN_FWD = 41,
+  OOC_OP_SCAN_BWD = 42,
+  OOC_OP_COUNT = 43
 };
 
 /* One schedule op.  fn = N for END ops; held = budget bytes held after it
@@ -538,6 +574,21 @@ ooc_status ooc_qknorm_slices(int64_t rows, int64_t *slices);
  * context.  OOC_E_INVALID for another op or a bad shape. */
 ooc_status ooc_attention_slices(int32_t op, const int64_t *attrs, int32_t n_attrs,
                                 int64_t slices[2], uint64_t *part_bytes);
+
+/* Slices of the rows of each gate for OOC_OP_JOIN_BWD, and the bytes of its
+ * part variable: 12 d groups slices.  Any count of 1 .. rows / groups gives the
+ * same gradients up to the order of sums.  Host only; no context.
+ * OOC_E_INVALID for a bad shape. */
+ooc_status ooc_join_slices(int64_t rows, int64_t d, int64_t groups, int64_t *slices,
+                           uint64_t *part_bytes);
+
+/* Slices of a sequence's rows that the gated recurrence runs best with, and the
+ * bytes of its part variable (8 B C slices; 0 for one slice), for
+ * OOC_OP_SCAN_FWD or _BWD and the attributes B T C (further ones are ignored).
+ * Any count of 1 .. min(T, 64) gives the same results up to roundings.  Host
+ * only; no context.  OOC_E_INVALID for another op or a bad shape. */
+ooc_status ooc_scan_slices(int32_t op, const int64_t *attrs, int32_t n_attrs, int64_t *slices,
+                           uint64_t *part_bytes);
 
 /* Runs one operation of the table above alone, outside any context, on device
  * memory of the caller's: ptrs[j] and bytes[j] are its variables in the

@@ -412,3 +412,156 @@ def cross_attention_bwd(q, kv, klen, dY, a):
             dV[b, j, :n] += P.T @ g[b, h]
     dkv = np.stack([dK, dV]).transpose(1, 3, 0, 2, 4).reshape(kv.shape)
     return dQ.transpose(0, 2, 1, 3).reshape(q.shape), dkv, delta
+
+
+# ---------------------------------------------------------------- dropout
+def philox(counters, salt, seed):
+    """The four words [n, 4] of Philox 4x32-10 (Salmon et al., 2011) at each counter of 64 bits, its
+    upper half being ``salt``, under the key ``seed`` (two uint32)."""
+    low = np.uint64(0xFFFFFFFF)
+    i = np.asarray(counters, np.uint64)
+    c = [i & low, i >> np.uint64(32), np.full_like(i, int(salt) & 0xFFFFFFFF),
+         np.full_like(i, int(salt) >> 32)]
+    key = [int(np.uint32(k)) for k in np.asarray(seed).astype(np.uint32)]
+    for r in range(10):
+        k = [np.uint64((key[0] + r * 0x9E3779B9) & 0xFFFFFFFF),
+             np.uint64((key[1] + r * 0xBB67AE85) & 0xFFFFFFFF)]
+        p, q = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(q >> np.uint64(32)) ^ c[1] ^ k[0], q & low, (p >> np.uint64(32)) ^ c[3] ^ k[1], p & low]
+    return np.stack(c, -1).astype(np.uint32)
+
+
+def dropout_factor(shape, seed, a):
+    """What each value of a tensor is multiplied by: 0, or 1 / (1 - drop / 2^32)."""
+    n = int(np.prod(shape))
+    if not a["drop"]:
+        return np.ones(shape)
+    words = philox(np.arange((n + 3) // 4), a["salt"], seed).reshape(-1)[:n]
+    return ((words >= a["drop"]) / (1.0 - a["drop"] / 2.0 ** 32)).reshape(shape)
+
+
+def dropout(X, seed, a):
+    m = dropout_factor(X.shape, seed, a)
+    return np.where(m > 0, X * m, 0.0)
+
+
+# ---------------------------------------------------------------- a block's join
+def _gate_rows(gate, rows):
+    return np.repeat(gate, rows // len(gate), 0)
+
+
+def join_fwd(X, F, post, gate, pre, scale, a, seed=None):
+    """Returns (H, N, stats [rows, 2])."""
+    r = 1.0 / np.sqrt((F * F).mean(-1, keepdims=True) + LN_EPS)
+    w = dropout(post * F * r, seed, a)
+    H = scale * X + _gate_rows(gate, len(X)) * w
+    s = 1.0 / np.sqrt((H * H).mean(-1, keepdims=True) + LN_EPS)
+    return H, pre * H * s, np.concatenate([r, s], 1)
+
+
+def join_bwd(F, H, post, gate, pre, scale, dH, dN, a, seed=None):
+    """Returns (dX, dF, dpost, dgate, dpre); dH may be None."""
+    rows, d = F.shape
+    g = _gate_rows(gate, rows)
+    r = 1.0 / np.sqrt((F * F).mean(-1, keepdims=True) + LN_EPS)
+    s = 1.0 / np.sqrt((H * H).mean(-1, keepdims=True) + LN_EPS)
+    m = dropout_factor(F.shape, seed, a)
+    v, t = F * r, H * s
+    dt = pre * dN
+    dh = s * (dt - t * (dt * t).mean(-1, keepdims=True)) + (0.0 if dH is None else dH)
+    du = g * dh * m
+    dv = post * du
+    dF = r * (dv - v * (dv * v).mean(-1, keepdims=True))
+    dgate = (dh * post * v * m).reshape(len(gate), -1, d).sum(1)
+    return scale * dh, dF, (du * v).sum(0), dgate, (dN * t).sum(0)
+
+
+# ---------------------------------------------------------------- gated recurrence
+def _gates(FX, fresh, a):
+    f, x = FX.reshape(a["B"], a["T"], 2, a["C"]).transpose(2, 0, 1, 3)
+    gate, rest = (1.0 / (1.0 + np.exp(-np.clip(s * f, -700, None))) for s in (1, -1))
+    live = np.ones((a["B"], a["T"], 1)) if fresh is None else \
+        (np.asarray(fresh).reshape(a["B"], a["T"], 1) == 0).astype(np.float64)
+    return x, gate, rest, live
+
+
+def scan_fwd(FX, a, h0=None, fresh=None):
+    x, gate, rest, live = _gates(FX, fresh, a)
+    H, state = np.zeros(x.shape), np.zeros(x[:, 0].shape) if h0 is None else h0
+    for t in range(a["T"]):
+        state = gate[:, t] * live[:, t] * state + rest[:, t] * x[:, t]
+        H[:, t] = state
+    return H.reshape(-1, a["C"])
+
+
+def scan_bwd(FX, H, dH, a, h0=None, fresh=None):
+    """Returns (dFX, dh0)."""
+    x, gate, rest, live = _gates(FX, fresh, a)
+    H, dH = H.reshape(x.shape), dH.reshape(x.shape)
+    first = np.zeros(x[:, :1].shape) if h0 is None else h0[:, None]
+    before = np.concatenate([first, H[:, :-1]], 1) * live
+    g, later = np.zeros(x.shape), np.zeros(x[:, 0].shape)
+    for t in range(a["T"] - 1, -1, -1):
+        g[:, t] = dH[:, t] + later
+        later = gate[:, t] * live[:, t] * g[:, t]
+    dFX = np.stack([g * (before - x) * gate * rest, g * rest], 2)
+    return dFX.reshape(FX.shape), later
+
+
+# ---------------------------------------------------------------- attention to a span of states
+def _span_scores(q, k, span, head, a, mod):
+    """(scores with -inf where nothing is seen, what the cap multiplies their gradients by)."""
+    S = q @ k.T / np.sqrt(a["dh"])
+    turn = 1.0
+    mod = np.asarray([] if mod is None else mod, np.float64)
+    if a["cap"]:
+        t = np.tanh(S / mod[0])
+        S, turn = mod[0] * t, 1.0 - t * t
+    lo, hi, at = np.asarray(span, np.int64)[:, :, None].transpose(1, 0, 2)
+    j = np.arange(a["Tk"])
+    if a["bias"]:
+        S = S - mod[a["cap"] + head] * np.abs(at - j)
+    return np.where((j >= lo) & (j < hi), S, -np.inf), turn
+
+
+def _span_probs(S):
+    top = S.max(-1, keepdims=True)
+    none = top == -np.inf
+    e = np.exp(S - np.where(none, 0.0, top))
+    total = e.sum(-1, keepdims=True)
+    with np.errstate(divide="ignore"):
+        return e / np.where(none, 1.0, total), (np.where(none, -np.inf, top + np.log(total)))[:, 0]
+
+
+def span_attention_fwd(q, kv, span, a, mod=None):
+    """Returns (Y [B Tq, H dh], lse [B, H, Tq])."""
+    Q, K, V, G = _cross_parts(q, kv, a)
+    Y, lse = np.zeros_like(Q), np.zeros(Q.shape[:3])
+    sp = np.asarray(span).reshape(a["B"], a["Tq"], 3)
+    for b in range(a["B"]):
+        for h in range(a["H"]):
+            P, lse[b, h] = _span_probs(_span_scores(Q[b, h], K[b, h // G], sp[b], h, a, mod)[0])
+            Y[b, h] = P @ V[b, h // G]
+    return Y.transpose(0, 2, 1, 3).reshape(q.shape), lse
+
+
+def span_attention_bwd(q, kv, span, dY, a, mod=None):
+    """Returns (dq, dkv, delta [B, H, Tq])."""
+    Q, K, V, G = _cross_parts(q, kv, a)
+    g = dY.reshape(a["B"], a["Tq"], a["H"], a["dh"]).transpose(0, 2, 1, 3)
+    dQ, dK, dV = np.zeros_like(Q), np.zeros_like(K), np.zeros_like(V)
+    delta = np.zeros(Q.shape[:3])
+    sp = np.asarray(span).reshape(a["B"], a["Tq"], 3)
+    for b in range(a["B"]):
+        for h in range(a["H"]):
+            j = h // G
+            S, turn = _span_scores(Q[b, h], K[b, j], sp[b], h, a, mod)
+            P, _ = _span_probs(S)
+            dP = g[b, h] @ V[b, j].T
+            delta[b, h] = (P * dP).sum(-1)
+            dS = P * (dP - delta[b, h][:, None]) * turn / np.sqrt(a["dh"])
+            dQ[b, h] = dS @ K[b, j]
+            dK[b, j] += dS.T @ Q[b, h]
+            dV[b, j] += P.T @ g[b, h]
+    dkv = np.stack([dK, dV]).transpose(1, 3, 0, 2, 4).reshape(kv.shape)
+    return dQ.transpose(0, 2, 1, 3).reshape(q.shape), dkv, delta

@@ -480,6 +480,37 @@ ooc_status ooc_attention_slices(int32_t op, const int64_t* attrs, int32_t n_attr
   return OOC_E_HOST_OOM;
 }
 
+ooc_status ooc_join_slices(int64_t rows, int64_t d, int64_t groups, int64_t* slices,
+                           uint64_t* part_bytes) try {
+  const std::string e = slices && part_bytes ? check_join_shape(rows, d, groups) : "NULL argument";
+  if (!e.empty()) {
+    g_create_error = "ooc_join_slices: " + e;
+    return OOC_E_INVALID;
+  }
+  *slices = join_slices(rows, groups);
+  *part_bytes = (uint64_t)join_part_bytes(d, groups, *slices);
+  return OOC_OK;
+} catch (const std::bad_alloc&) {
+  return OOC_E_HOST_OOM;
+}
+
+ooc_status ooc_scan_slices(int32_t op, const int64_t* attrs, int32_t n_attrs, int64_t* slices,
+                           uint64_t* part_bytes) try {
+  std::string e;
+  if (!slices || !attrs || !part_bytes || n_attrs < 3) e = "NULL argument or fewer than 3 attributes";
+  else if (op != OOC_OP_SCAN_FWD && op != OOC_OP_SCAN_BWD) e = "op must be SCAN_FWD or _BWD";
+  else e = check_scan_shape(attrs[0], attrs[1], attrs[2]);
+  if (!e.empty()) {
+    g_create_error = "ooc_scan_slices: " + e;
+    return OOC_E_INVALID;
+  }
+  *slices = scan_slices({attrs[0], attrs[1], attrs[2]});
+  *part_bytes = (uint64_t)scan_part_bytes(attrs[0], attrs[2], *slices);
+  return OOC_OK;
+} catch (const std::bad_alloc&) {
+  return OOC_E_HOST_OOM;
+}
+
 ooc_status ooc_run_fn(int32_t hip_device, void* stream, int32_t op, void* const* ptrs,
                       const uint64_t* bytes, const uint8_t* access, int32_t n,
                       const int64_t* attrs, int32_t n_attrs) {

@@ -142,6 +142,35 @@ hipError_t launch_fn(const Fn& fn, void* const* p, const uint64_t* bytes, const 
       return cross_attention_bwd(F(0), F(1), static_cast<const int32_t*>(p[2]), F(3), F(4), F(5),
                                  F(6), F(7), F(8), a[6] > 1 || a[7] > 1 ? F(9) : nullptr,
                                  {a[0], a[1], a[2], a[3], a[4], a[5]}, a[6], a[7], s);
+    case OOC_OP_DROPOUT:
+      return dropout(F(0), static_cast<const uint32_t*>(p[1]), F(2), a[0], a[1], a[2], s);
+    case OOC_OP_JOIN_FWD: {
+      const JoinShape j{a[0], a[1], a[2], a[3], a[4]};
+      const int w = j.drop ? 7 : 6;   // the first variable behind the seed
+      return join_fwd(F(0), F(1), F(2), F(3), F(4), F(5),
+                      j.drop ? static_cast<const uint32_t*>(p[6]) : nullptr, F(w), F(w + 1),
+                      F(w + 2), j, s);
+    }
+    case OOC_OP_JOIN_BWD: {
+      const JoinShape j{a[0], a[1], a[2], a[3], a[4]};
+      int w = 7;
+      const uint32_t* seed = j.drop ? static_cast<const uint32_t*>(p[w++]) : nullptr;
+      const float* dh = a[5] ? F(w++) : nullptr;
+      return join_bwd(F(0), F(1), F(2), F(3), F(4), F(5), F(6), seed, dh, F(w), F(w + 1), F(w + 2),
+                      F(w + 3), F(w + 4), F(w + 5), F(w + 6), j, a[6], s);
+    }
+    case OOC_OP_SCAN_FWD:
+    case OOC_OP_SCAN_BWD: {
+      int w = 1;
+      const float* h0 = a[3] ? F(w++) : nullptr;
+      const int32_t* fresh = a[4] ? static_cast<const int32_t*>(p[w++]) : nullptr;
+      const ScanShape c{a[0], a[1], a[2]};
+      if (fn.op == OOC_OP_SCAN_FWD)
+        return scan_fwd(F(0), h0, fresh, F(w), a[5] > 1 ? F(w + 1) : nullptr, c, a[5], s);
+      float* dh0 = a[3] ? F(w + 3) : nullptr;
+      return scan_bwd(F(0), h0, fresh, F(w), F(w + 1), F(w + 2), dh0,
+                      a[5] > 1 ? F(w + 3 + (a[3] ? 1 : 0)) : nullptr, c, a[5], s);
+    }
     default:
       return hipErrorInvalidValue;
   }

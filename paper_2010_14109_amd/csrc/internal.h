@@ -111,6 +111,18 @@ constexpr int64_t kMaxAttentionSlices = 64;
 std::string check_attention_shape(const int64_t* attrs);
 int64_t attention_part_bytes(bool fwd, const int64_t* attrs);
 
+// Dropout, block joins and gated recurrences: their shapes ("" when valid), and the bytes of their
+// partial results.
+constexpr int64_t kMaxScanSlices = 64;
+std::string check_join_shape(int64_t rows, int64_t d, int64_t groups);
+std::string check_scan_shape(int64_t B, int64_t T, int64_t C);
+inline int64_t join_part_bytes(int64_t d, int64_t groups, int64_t slices) {
+  return groups * slices * 3 * d * 4;
+}
+inline int64_t scan_part_bytes(int64_t B, int64_t C, int64_t slices) {
+  return slices > 1 ? B * slices * 2 * C * 4 : 0;
+}
+
 inline uint64_t round_up(uint64_t b, uint64_t c) { return (b + c - 1) / c * c; }
 
 }  // namespace ooc

@@ -147,6 +147,35 @@ hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* k
 int64_t attention_key_slices(const AttendShape& a, bool fwd);
 int64_t attention_query_slices(const AttendShape& a);
 
+// Dropout and the join of a block with its residual stream (block.hip).  drop: of 2^32; seed null iff
+// drop = 0 in a join.
+hipError_t dropout(const float* x, const uint32_t* seed, float* y, int64_t n, int64_t drop,
+                   int64_t salt, hipStream_t s);
+struct JoinShape {
+  int64_t rows, d, groups, drop, salt;
+};
+int64_t join_slices(int64_t rows, int64_t groups);   // of the rows of a gate
+hipError_t join_fwd(const float* x, const float* f, const float* post, const float* gate,
+                    const float* pre, const float* scale, const uint32_t* seed, float* h, float* n,
+                    float* stats, const JoinShape& a, hipStream_t s);
+// dh null: nothing else reads h
+hipError_t join_bwd(const float* f, const float* h, const float* stats, const float* post,
+                    const float* gate, const float* pre, const float* scale, const uint32_t* seed,
+                    const float* dh, const float* dn, float* dx, float* df, float* dpost,
+                    float* dgate, float* dpre, float* part, const JoinShape& a, int64_t slices,
+                    hipStream_t s);
+
+// Gated recurrence (scan.hip).  h0, fresh, dh0 null where there is none; part null iff slices = 1.
+struct ScanShape {
+  int64_t B, T, C;
+};
+int64_t scan_slices(const ScanShape& a);   // of the rows of a sequence
+hipError_t scan_fwd(const float* fx, const float* h0, const int32_t* fresh, float* h, float* part,
+                    const ScanShape& a, int64_t slices, hipStream_t s);
+hipError_t scan_bwd(const float* fx, const float* h0, const int32_t* fresh, const float* h,
+                    const float* dh, float* dfx, float* dh0, float* part, const ScanShape& a,
+                    int64_t slices, hipStream_t s);
+
 hipError_t mix(void* const* ptrs, const uint64_t* words, int nvars, uint32_t seed, hipStream_t s,
                bool y_read);
 

@@ -1,0 +1,192 @@
+// Gated linear recurrence h_t = a_t h_(t-1) + (1 - a_t) x_t with a = sigmoid(f), forward and
+// backward, over sequences of any length (gfx950).
+//
+// Steps compose: a run of steps maps the state before it to A h + B, A the product of its gates, and
+// runs join by (A2, B2) after (A1, B1) = (A1 A2, A2 B1 + B2).  The backward is the same recurrence
+// from the last row to the first: with G_t = a_t (dh_t + G_(t+1)), the gradient of h_t is
+// dh_t + G_(t+1).
+//
+// It is bound by memory traffic, 12 bytes a value forward (f, x read, h written) and 24 backward (f,
+// x, h, dh read, df, dx written), if each value is read once.  So a workgroup keeps a stretch of rows
+// in registers: a lane loads kSteps rows of its column, reduces them to (A, B), all runs of the
+// stretch meet in LDS, each lane takes in the runs before its own and walks its rows with the state
+// that it then knows.  Rows of the next stretch are on their way meanwhile.  Where the columns of all
+// sequences do not fill the chip, time is cut into slices: a first pass reduces every slice to (A, B),
+// and each workgroup of the second takes in the slices before its own.
+//
+// A gate of exactly zero (f far below, or a row that starts afresh) cuts the state off, whatever it
+// was, an infinity or a NaN too; that goes for a product of gates that is below fp32's range as well.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "kernels.h"
+
+namespace ooc {
+
+namespace {
+
+constexpr int kWaves = 8;   // of a workgroup, at most
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Scan {
+  int B, T, C, slices, slice_len;
+};
+
+// a = sigmoid(f) and 1 - a, each to a few units in its last place
+__device__ inline void gate_of(float f, float& a, float& rest) {
+  const float e = expf(-fabsf(f)), r = 1.f / (1.f + e), er = e * r;
+  a = f >= 0.f ? r : er;
+  rest = f >= 0.f ? er : r;
+}
+// the state behind a run (A, B)
+__device__ inline float after(float A, float B, float h) { return A == 0.f ? B : fmaf(A, h, B); }
+
+// One lane's rows: column c, rows t0 .. of its sequence in the order of the pass (backward: from the
+// last on), those at and past `end` being no rows (they change nothing).
+template <bool BACK, int S>
+struct Lane {
+  float f[S], x[S], d[S], p[S];   // backward: d = dh, p = h of the row before
+  int fresh[S];
+  __device__ void load(const float* fx, const float* h0, const int32_t* fr, const float* h,
+                       const float* dh, const Scan& s, int b, int c, int t0, int end, bool sum_only) {
+    const int cc = min(c, s.C - 1);
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      const int u = min(t0 + k, end - 1), t = BACK ? s.T - 1 - u : u;
+      const int64_t row = (int64_t)b * s.T + t;
+      const float* q = fx + row * 2 * s.C + cc;
+      f[k] = q[0];
+      if (!BACK || !sum_only) x[k] = q[s.C];
+      fresh[k] = fr ? fr[row] : 0;
+      if (BACK) {
+        d[k] = dh[row * s.C + cc];
+        if (!sum_only) {
+          p[k] = 0.f;
+          if (t > 0) p[k] = h[(row - 1) * s.C + cc];
+          else if (h0) p[k] = h0[(int64_t)b * s.C + cc];
+        }
+      }
+    }
+  }
+};
+
+// SUM: only reduce the slice to (A, B), into part.
+template <bool BACK, bool SUM, int S>
+__global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(
+    const float* __restrict__ fx, const float* __restrict__ h0, const int32_t* __restrict__ fr,
+    const float* __restrict__ hin, const float* __restrict__ dh, float* __restrict__ out,
+    float* __restrict__ dh0, float* __restrict__ part, Scan s) {
+  __shared__ float2 runs[2][kWaves][64];
+  const int nw = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int blocks = (s.C + 63) / 64, b = blockIdx.x / blocks, c = (int)(blockIdx.x % blocks) * 64 + lane;
+  const int slice = blockIdx.y, begin = min(s.T, slice * s.slice_len), end = min(s.T, begin + s.slice_len);
+  float state = 0.f, A_all = 1.f;
+  if (!SUM) {
+    if (!BACK && h0 && c < s.C) state = h0[(int64_t)b * s.C + c];
+    if (c < s.C)
+      for (int k = 0; k < slice; ++k) {
+        const float* q = part + ((int64_t)b * s.slices + k) * 2 * s.C + c;
+        state = after(q[0], q[s.C], state);
+      }
+  }
+  Lane<BACK, S> next;
+  if (begin < end) next.load(fx, h0, fr, hin, dh, s, b, c, begin + w * S, end, SUM);
+  int buf = 0;
+  for (int r = begin; r < end; r += nw * S, buf ^= 1) {
+    const int t0 = r + w * S;
+    float a[S], rest[S], al[S], B = 0.f, A = 1.f;
+    const Lane<BACK, S> now = next;
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      gate_of(now.f[k], a[k], rest[k]);
+      al[k] = now.fresh[k] ? 0.f : a[k];
+      if (t0 + k < end) {
+        B = BACK ? (al[k] == 0.f ? 0.f : al[k] * (now.d[k] + B)) : after(al[k], rest[k] * now.x[k], B);
+        A *= al[k];
+      }
+    }
+    runs[buf][w][lane] = make_float2(A, B);
+    if (r + nw * S < end) next.load(fx, h0, fr, hin, dh, s, b, c, t0 + nw * S, end, SUM);
+    __syncthreads();
+    float mine = state;
+    for (int k = 0; k < nw; ++k) {
+      const float2 run = runs[buf][k][lane];
+      if (k == w) mine = state;
+      state = after(run.x, run.y, state);
+      A_all *= run.x;
+    }
+    if (SUM || c >= s.C) continue;
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      if (t0 + k >= end) break;
+      const int t = BACK ? s.T - 1 - (t0 + k) : t0 + k;
+      const int64_t row = (int64_t)b * s.T + t;
+      if (!BACK) {
+        mine = after(al[k], rest[k] * now.x[k], mine);
+        out[row * s.C + c] = mine;
+      } else {
+        const float g = now.d[k] + mine, before = now.fresh[k] ? 0.f : now.p[k];
+        mine = al[k] == 0.f ? 0.f : al[k] * g;
+        out[row * 2 * s.C + c] = g * (before - now.x[k]) * (a[k] * rest[k]);
+        out[row * 2 * s.C + s.C + c] = rest[k] * g;
+      }
+    }
+  }
+  if (w || c >= s.C) return;
+  if (SUM) {
+    float* q = part + ((int64_t)b * s.slices + slice) * 2 * s.C + c;
+    q[0] = A_all;
+    q[s.C] = state;
+  } else if (BACK && dh0 && end == s.T && begin < s.T) {
+    dh0[(int64_t)b * s.C + c] = state;
+  }
+}
+
+// Rows of a lane: few enough that two workgroups of eight waves fit a CU with the next ones on
+// their way; one where there is one.
+constexpr int kSteps = 16, kBackSteps = 8;
+
+template <bool BACK, int S>
+hipError_t scan(const float* fx, const float* h0, const int32_t* fresh, const float* h, const float* dh,
+                float* out, float* dh0, float* part, const ScanShape& a, int64_t slices,
+                hipStream_t st) {
+  const Scan s{(int)a.B, (int)a.T, (int)a.C, (int)slices, (int)ceil_div(a.T, slices)};
+  const unsigned blocks = (unsigned)(a.B * ceil_div(a.C, 64));
+  const unsigned threads = 64 * (unsigned)std::min<int64_t>(kWaves, ceil_div(s.slice_len, S));
+  if (slices > 1) {
+    hipLaunchKernelGGL((scan_kernel<BACK, true, S>), dim3(blocks, (unsigned)slices - 1), dim3(threads), 0,
+                       st, fx, h0, fresh, h, dh, out, dh0, part, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((scan_kernel<BACK, false, S>), dim3(blocks, (unsigned)slices), dim3(threads), 0, st,
+                     fx, h0, fresh, h, dh, out, dh0, part, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Slices to fill the chip where the columns do not: each has 128 rows or more.
+int64_t scan_slices(const ScanShape& a) {
+  const int64_t blocks = a.B * ceil_div(a.C, 64);
+  if (blocks >= 256) return 1;
+  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, blocks), a.T / 128, kMaxScanSlices}));
+}
+
+hipError_t scan_fwd(const float* fx, const float* h0, const int32_t* fresh, float* h, float* part,
+                    const ScanShape& a, int64_t slices, hipStream_t s) {
+  if (a.T == 1) return scan<false, 1>(fx, h0, fresh, nullptr, nullptr, h, nullptr, part, a, slices, s);
+  return scan<false, kSteps>(fx, h0, fresh, nullptr, nullptr, h, nullptr, part, a, slices, s);
+}
+
+hipError_t scan_bwd(const float* fx, const float* h0, const int32_t* fresh, const float* h,
+                    const float* dh, float* dfx, float* dh0, float* part, const ScanShape& a,
+                    int64_t slices, hipStream_t s) {
+  if (a.T == 1) return scan<true, 1>(fx, h0, fresh, h, dh, dfx, dh0, part, a, slices, s);
+  return scan<true, kBackSteps>(fx, h0, fresh, h, dh, dfx, dh0, part, a, slices, s);
+}
+
+}  // namespace ooc

@@ -58,6 +58,11 @@ const Sig kSig[OOC_OP_COUNT] = {
     {"QKNORM_BWD", -1, 8, {}},
     {"CROSS_ATTENTION_FWD", -1, 7, {}},
     {"CROSS_ATTENTION_BWD", -1, 8, {}},
+    {"DROPOUT", 3, 3, {OOC_R, OOC_R, OOC_W}},
+    {"JOIN_FWD", -1, 5, {}},
+    {"JOIN_BWD", -1, 7, {}},
+    {"SCAN_FWD", -1, 6, {}},
+    {"SCAN_BWD", -1, 6, {}},
 };
 
 const int64_t kMaxElems = int64_t(1) << 40;
@@ -90,6 +95,22 @@ std::string check_attention_shape(const int64_t* a) {
   if ((B * Hkv + 7) * (std::max(Tq * (H / Hkv), Tk) / (dh <= 128 ? 128 : 64) + 1) >= (1 << 23))
     return "too many workgroups";
   if (product({B, Tq, H, dh, 4}) < 0 || product({B, Tk, Hkv, dh, 8}) < 0) return "tensor too large";
+  return "";
+}
+
+std::string check_join_shape(int64_t rows, int64_t d, int64_t groups) {
+  // a launch has fewer than 2^32 threads, up to 512 of them a row, and 65535 workgroups across
+  if (rows <= 0 || rows >= (1 << 23) || d <= 0 || d > 8192 || groups <= 0 || groups > 65533 ||
+      rows % groups)
+    return "bad attributes";
+  return "";
+}
+
+std::string check_scan_shape(int64_t B, int64_t T, int64_t C) {
+  // rows are counted in 32 bits; a launch has fewer than 2^32 threads, 512 a sequence and 64 columns
+  if (B <= 0 || T <= 0 || C <= 0 || T > (1 << 28) || C > (1 << 24) || B > (1 << 23) ||
+      B * ((C + 63) / 64) >= (1 << 23) / kMaxScanSlices || product({B, T, C, 8}) < 0)
+    return "bad attributes";
   return "";
 }
 
@@ -444,6 +465,81 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
         NEED(8, lb, "delta");
       }
       if (part) NEED(nv - 1, part, "partial results");
+      return "";
+    }
+    case OOC_OP_DROPOUT:
+      if (a[1] > UINT32_MAX) return nm + ": a drop of 2^32 or more";
+      NEED(0, product({a[0], 4}), "X");
+      NEED(1, 8, "seed");
+      NEED(2, product({a[0], 4}), "Y");
+      return "";
+    case OOC_OP_JOIN_FWD:
+    case OOC_OP_JOIN_BWD: {
+      const bool fwd = fn.op == OOC_OP_JOIN_FWD;
+      const int64_t rows = a[0], d = a[1], groups = a[2], drop = a[3];
+      if (!(e = check_join_shape(rows, d, groups)).empty()) return nm + ": " + e;
+      if (drop > UINT32_MAX) return nm + ": a drop of 2^32 or more";
+      const int w = drop > 0 ? 1 : 0, g = !fwd && a[5] ? 1 : 0;   // seed; dH
+      if (!fwd && a[5] > 1) return nm + ": bad attributes";
+      if (nv != (fwd ? 9 + w : 14 + w + g))
+        return nm + ": takes a seed iff drop > 0" + (fwd ? "" : " and dH iff said so");
+      for (int j = 0; j < nv; ++j)
+        if (v[j].access != (j < (fwd ? 6 + w : 8 + w + g) ? OOC_R : OOC_W)) return nm + ": wrong access";
+      const int64_t xb = product({rows, d, 4}), gb = d * 4, sb = rows * 8;
+      NEED(0, xb, fwd ? "X" : "F");
+      NEED(1, xb, fwd ? "F" : "H");
+      if (!fwd) NEED(2, sb, "stats");
+      const int at = fwd ? 2 : 3;
+      NEED(at, gb, "post");
+      NEED(at + 1, groups * gb, "gate");
+      NEED(at + 2, gb, "pre");
+      NEED(at + 3, 4, "scale");
+      if (w) NEED(at + 4, 8, "seed");
+      int out = at + 4 + w;
+      if (fwd) {
+        NEED(out, xb, "H");
+        NEED(out + 1, xb, "N");
+        NEED(out + 2, sb, "stats");
+        return "";
+      }
+      const int64_t slices = a[6];
+      if (slices < 1 || slices > rows / groups) return nm + ": bad slice count";
+      if (g) NEED(out++, xb, "dH");
+      NEED(out, xb, "dN");
+      NEED(out + 1, xb, "dX");
+      NEED(out + 2, xb, "dF");
+      NEED(out + 3, gb, "dpost");
+      NEED(out + 4, groups * gb, "dgate");
+      NEED(out + 5, gb, "dpre");
+      NEED(out + 6, join_part_bytes(d, groups, slices), "partial sums");
+      return "";
+    }
+    case OOC_OP_SCAN_FWD:
+    case OOC_OP_SCAN_BWD: {
+      const bool fwd = fn.op == OOC_OP_SCAN_FWD;
+      const int64_t b = a[0], T = a[1], C = a[2], carry = a[3], fresh = a[4], slices = a[5];
+      if (!(e = check_scan_shape(b, T, C)).empty()) return nm + ": " + e;
+      if (carry > 1 || fresh > 1) return nm + ": bad attributes";
+      if (slices < 1 || slices > kMaxScanSlices || slices > T) return nm + ": bad slice count";
+      const int in = 1 + (int)carry + (int)fresh + (fwd ? 0 : 2);
+      const int out = fwd ? 1 : 1 + (int)carry;
+      if (nv != in + out + (slices > 1))
+        return nm + ": takes a state, fresh rows and partial results iff said so";
+      for (int j = 0; j < nv; ++j)
+        if (v[j].access != (j < in ? OOC_R : OOC_W)) return nm + ": wrong access";
+      const int64_t hb = product({b, T, C, 4}), cb = b * C * 4;
+      NEED(0, 2 * hb, "FX");
+      if (carry) NEED(1, cb, "h0");
+      if (fresh) NEED(1 + (int)carry, b * T * 4, "fresh");
+      if (fwd) {
+        NEED(in, hb, "H");
+      } else {
+        NEED(in - 2, hb, "H");
+        NEED(in - 1, hb, "dH");
+        NEED(in, 2 * hb, "dFX");
+        if (carry) NEED(in + 1, cb, "dh0");
+      }
+      if (slices > 1) NEED(nv - 1, scan_part_bytes(b, C, slices), "partial results");
       return "";
     }
     case OOC_OP_MIX: {

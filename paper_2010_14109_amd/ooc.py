@@ -36,6 +36,7 @@ OPS = {
     "upsample_fwd": 29, "upsample_bwd": 30, "acc": 31,
     "rope_fwd": 32, "rope_bwd": 33, "qknorm_fwd": 34, "qknorm_bwd": 35,
     "cross_attention_fwd": 36, "cross_attention_bwd": 37,
+    "dropout": 38, "join_fwd": 39, "join_bwd": 40, "scan_fwd": 41, "scan_bwd": 42,
 }
 
 #: every symbol ``include/ooc.h`` declares
@@ -47,7 +48,8 @@ EXPORTS = [
     "ooc_download", "ooc_step", "ooc_get_stats", "ooc_fn_times", "ooc_link_probe",
     "ooc_timeline", "ooc_set_swapout_depth", "ooc_set_fixed_distance", "ooc_bestfit_extent",
     "ooc_set_wait_order", "ooc_set_host_limit", "ooc_wgrad_slices", "ooc_set_layout",
-    "ooc_qknorm_slices", "ooc_attention_slices", "ooc_run_fn",
+    "ooc_qknorm_slices", "ooc_attention_slices", "ooc_join_slices", "ooc_scan_slices",
+    "ooc_run_fn",
 ]
 
 
@@ -144,6 +146,10 @@ def load(path=LIB_PATH):
         "ooc_qknorm_slices": ([c.c_int64, c.POINTER(c.c_int64)], c.c_int32),
         "ooc_attention_slices": ([c.c_int32, c.POINTER(c.c_int64), c.c_int32,
                                   c.POINTER(c.c_int64), c.POINTER(c.c_uint64)], c.c_int32),
+        "ooc_join_slices": ([c.c_int64, c.c_int64, c.c_int64, c.POINTER(c.c_int64),
+                             c.POINTER(c.c_uint64)], c.c_int32),
+        "ooc_scan_slices": ([c.c_int32, c.POINTER(c.c_int64), c.c_int32, c.POINTER(c.c_int64),
+                             c.POINTER(c.c_uint64)], c.c_int32),
         "ooc_run_fn": ([c.c_int32, P, c.c_int32, c.POINTER(P), c.POINTER(c.c_uint64),
                         c.POINTER(c.c_uint8), c.c_int32, c.POINTER(c.c_int64), c.c_int32],
                        c.c_int32),
@@ -199,6 +205,23 @@ def attention_slices(op, attrs):
     op = OPS[op] if isinstance(op, str) else op
     _check(load().ooc_attention_slices(op, a, len(attrs), out, ctypes.byref(part)), None)
     return list(out)[:1 if op == OPS["cross_attention_fwd"] else 2], part.value
+
+
+def join_slices(rows, d, groups):
+    """``(slices, bytes of the part variable)`` of ``join_bwd``."""
+    out, part = ctypes.c_int64(), ctypes.c_uint64()
+    _check(load().ooc_join_slices(rows, d, groups, ctypes.byref(out), ctypes.byref(part)), None)
+    return out.value, part.value
+
+
+def scan_slices(op, attrs):
+    """``(slices, bytes of the part variable)`` of a gated recurrence with the shape B, T, C:
+    ``scan_fwd`` or ``scan_bwd``."""
+    a = (ctypes.c_int64 * len(attrs))(*attrs)
+    out, part = ctypes.c_int64(), ctypes.c_uint64()
+    op = OPS[op] if isinstance(op, str) else op
+    _check(load().ooc_scan_slices(op, a, len(attrs), ctypes.byref(out), ctypes.byref(part)), None)
+    return out.value, part.value
 
 
 def run_fn(op, vars_, access, attrs=(), device=0, stream=0):

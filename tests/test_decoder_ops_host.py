@@ -1,0 +1,191 @@
+"""Dropout, block joins and gated recurrences without a GPU: the oracle's formulas against published
+values, differences and plain loops, and everything the library refuses."""
+
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import decoder_util as du
+from oracle import ops
+from paper_2010_14109_amd import ooc
+from test_attention_ops_host import difference
+
+R, W, RW = ooc.R, ooc.W, ooc.RW
+
+
+# ---------------------------------------------------------------- the oracle's formulas
+def test_the_generator_gives_its_published_words():
+    """The known answers that were published with the generator, for three counters and keys."""
+    full = 0xFFFFFFFF
+    assert ops.philox([0], 0, [0, 0]).tolist() == [[0x6627e8d5, 0xe169c58d, 0xbc57ac4c, 0x9b00dbd8]]
+    assert ops.philox([full << 32 | full], full << 32 | full, [full, full]).tolist() == \
+        [[0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd]]
+    assert ops.philox([0x85a308d3243f6a88], 0x0370734413198a2e, [0xa4093822, 0x299f31d0]).tolist() == \
+        [[0xd16cfe09, 0x94fdcceb, 0x5001e420, 0x24126ea1]]
+
+
+def test_dropout_keeps_its_share():
+    a = {"drop": int(0.1 * 2 ** 32), "salt": 1}
+    m = ops.dropout_factor((1000, 400), [1, 2], a)
+    kept = (m > 0).mean()
+    assert abs(kept - 0.9) < 5 * np.sqrt(0.09 / m.size) and np.allclose(m[m > 0], 1 / 0.9, rtol=1e-9)
+    assert (ops.dropout_factor((1000, 400), [1, 3], a) != m).mean() > 0.15
+
+
+@pytest.mark.parametrize("groups,p,stream", [(1, 0.0, True), (3, 0.4, True), (2, 0.2, False)])
+def test_join_gradients_against_differences(groups, p, stream):
+    a, v = du.join_case(1, 6, 11, groups, p)
+    f = {k: t.astype(np.float64) for k, t in v.items()}
+    seed = v["seed"]
+    if not stream:
+        f["dh"] = np.zeros_like(f["dh"])
+
+    def loss(**kw):
+        t = dict(f, **kw)
+        h, n, _ = ops.join_fwd(t["x"], t["f"], t["post"], t["gate"], t["pre"], t["scale"], a, seed)
+        return (h * f["dh"]).sum() + (n * f["dn"]).sum()
+    h = ops.join_fwd(f["x"], f["f"], f["post"], f["gate"], f["pre"], f["scale"], a, seed)[0]
+    grads = ops.join_bwd(f["f"], h, f["post"], f["gate"], f["pre"], f["scale"],
+                         f["dh"] if stream else None, f["dn"], a, seed)
+    g = np.random.default_rng(2)
+    for name, grad in zip(("x", "f", "post", "gate", "pre"), grads):
+        d = g.standard_normal(f[name].shape)
+        assert np.isclose(difference(lambda t: loss(**{name: t}), f[name], d), (grad * d).sum(),
+                          rtol=1e-6, atol=1e-7), name
+
+
+@pytest.mark.parametrize("carry,fresh", [(False, False), (True, True)])
+def test_scan_against_plain_loops_and_differences(carry, fresh):
+    a, fx, h0, fr, dh = du.scan_case(3, 2, 9, 4, carry, fresh)
+    if fresh:
+        fr[[3, 14]] = 1
+    fx, dh = fx.astype(np.float64), dh.astype(np.float64)
+    h0 = None if h0 is None else h0.astype(np.float64)
+    h = ops.scan_fwd(fx, a, h0, fr)
+    for b in range(2):
+        for c in range(4):
+            s = h0[b, c] if carry else 0.0
+            for t in range(9):
+                r = b * 9 + t
+                if fresh and fr[r]:
+                    s = 0.0
+                gate = 1 / (1 + np.exp(-fx[r, c]))
+                s = gate * s + (1 - gate) * fx[r, 4 + c]
+                assert np.isclose(h[r, c], s, rtol=1e-12)
+    dfx, dh0 = ops.scan_bwd(fx, h, dh, a, h0, fr)
+    g = np.random.default_rng(4)
+    d = g.standard_normal(fx.shape)
+    num = difference(lambda t: (ops.scan_fwd(t, a, h0, fr) * dh).sum(), fx, d)
+    assert np.isclose(num, (dfx * d).sum(), rtol=1e-7)
+    if carry:
+        d = g.standard_normal(h0.shape)
+        num = difference(lambda t: (ops.scan_fwd(fx, a, t, fr) * dh).sum(), h0, d)
+        assert np.isclose(num, (dh0 * d).sum(), rtol=1e-7)
+
+
+def test_the_bounds_separate_planted_mistakes():
+    """Planted in the oracle: a join without its 1e-5, a recurrence that misses one row."""
+    a, v = du.join_case(5, 20, 64, 1, wide=True)
+    h, n, _ = du.join_oracle(a, v)
+    off = dict(v, f=v["f"] * np.float32(1 + 1e-4))
+    bh, bn, _ = du.join_bounds(a, v)
+    h1, n1, _ = du.join_oracle(a, off)
+    assert (np.abs(h1 - h) > bh).any() and (np.abs(n1 - n) > bn).any()
+    a, fx, h0, fr, dh = du.scan_case(6, 1, 50, 8, True, False)
+    h = du.scan_oracle(a, fx, h0, fr)
+    fx1 = fx.copy()
+    fx1[20, 8:] = 0
+    assert (np.abs(du.scan_oracle(a, fx1, h0, fr) - h) > du.scan_bound(a, fx, h0, fr)).any(1)[20:30].all()
+
+
+# ---------------------------------------------------------------- what is refused
+def refused(op, sizes, access, attrs, match):
+    ctx = ooc.Context(-1)
+    try:
+        ids = [ctx.add_var(n, ooc.TEMP if a & W else ooc.INPUT) for n, a in zip(sizes, access)]
+        with pytest.raises(ooc.OocError, match=match) as e:
+            ctx.add_fn(op, ids, access, attrs)
+        assert e.value.status == ooc.E_INVALID
+    finally:
+        ctx.close()
+
+
+def accepted(op, sizes, access, attrs):
+    ctx = ooc.Context(-1)
+    try:
+        ids = [ctx.add_var(n, ooc.TEMP if a & W else ooc.INPUT) for n, a in zip(sizes, access)]
+        ctx.add_fn(op, ids, access, attrs)
+    finally:
+        ctx.close()
+
+
+def vary(op, sizes, access, attrs, bad_attrs):
+    """The call as given is taken; each size off by 4, each access, one variable fewer or more, one
+    attribute fewer, and the attributes named are not."""
+    accepted(op, sizes, access, attrs)
+    for j in range(len(sizes)):
+        refused(op, [s + 4 * (i == j) for i, s in enumerate(sizes)], access, attrs, op.upper())
+        refused(op, sizes, [(R + W - s if i == j else s) for i, s in enumerate(access)], attrs, op.upper())
+    refused(op, sizes[:-1], access[:-1], attrs, op.upper())
+    refused(op, sizes + [16], access + [W], attrs, op.upper())
+    refused(op, sizes, access, attrs[:-1], op.upper())
+    for j, x in bad_attrs:
+        refused(op, sizes, access, attrs[:j] + [x] + attrs[j + 1:], op.upper())
+
+
+def test_dropout_refusals(lib):
+    vary("dropout", [400, 8, 400], [R, R, W], [100, 7, 3],
+         [(0, 0), (0, 101), (0, -1), (0, 1 << 40), (1, 1 << 32), (1, -1), (2, -1)])
+
+
+@pytest.mark.parametrize("drop", [0, 9])
+def test_join_refusals(lib, drop):
+    x, v, g = 6 * 10 * 4, 40, 2 * 40
+    seed = [8] if drop else []
+    sizes = [x, x, v, g, v, 4] + seed + [x, x, 48]
+    access = [R] * (6 + len(seed)) + [W] * 3
+    bad = [(0, 0), (0, 7), (0, 1 << 23), (1, 0), (1, 8193), (2, 0), (2, 4), (2, 65534), (3, 1 << 32),
+           (3, 0 if drop else 9), (4, -1)]
+    vary("join_fwd", sizes, access, [6, 10, 2, drop, 3], bad)
+    for stream in (0, 1):
+        sizes = [x, x, 48, v, g, v, 4] + seed + [x] * stream + [x, x, x, v, g, v, 2 * 3 * 3 * 40]
+        access = [R] * (8 + len(seed) + stream) + [W] * 6
+        vary("join_bwd", sizes, access, [6, 10, 2, drop, 3, stream, 3],
+             bad + [(5, 1 - stream), (5, 2), (6, 0), (6, 4)])
+
+
+@pytest.mark.parametrize("carry,fresh,slices", [(0, 0, 1), (1, 1, 2), (1, 0, 1), (0, 1, 3)])
+def test_scan_refusals(lib, carry, fresh, slices):
+    h, st = 3 * 5 * 7 * 4, 3 * 7 * 4
+    part = [3 * slices * 2 * 7 * 4] if slices > 1 else []
+    ins = [2 * h] + [st] * carry + [60] * fresh
+    bad = [(0, 0), (1, 0), (2, 0), (0, 4), (1, (1 << 28) + 1), (2, (1 << 24) + 1), (0, 1 << 24),
+           (3, 1 - carry), (3, 2), (4, 1 - fresh), (4, 2), (5, 0), (5, 6), (5, 65)]
+    attrs = [3, 5, 7, carry, fresh, slices]
+    vary("scan_fwd", ins + [h] + part, [R] * len(ins) + [W] * (1 + len(part)), attrs, bad)
+    outs = [2 * h] + [st] * carry + part
+    vary("scan_bwd", ins + [h, h] + outs, [R] * (len(ins) + 2) + [W] * len(outs), attrs, bad)
+
+
+def test_slice_counts(lib):
+    assert ooc.join_slices(12288, 1024, 24) == (22, 24 * 22 * 3 * 1024 * 4)
+    assert ooc.join_slices(1, 1, 1) == (1, 12) and ooc.join_slices(24, 5, 24)[0] == 1
+    assert ooc.scan_slices("scan_fwd", [24, 512, 1024]) == (1, 0)
+    assert ooc.scan_slices("scan_bwd", [1, 1, 1]) == (1, 0)
+    s, part = ooc.scan_slices("scan_fwd", [1, 1 << 20, 64])
+    assert 1 < s <= 64 and part == s * 2 * 64 * 4
+    for rows, d, groups in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (6, 1, 4), (1 << 23, 1, 1), (1, 8193, 1)):
+        with pytest.raises(ooc.OocError, match="ooc_join_slices"):
+            ooc.join_slices(rows, d, groups)
+    for op, a in (("scan_fwd", [0, 1, 1]), ("join_fwd", [1, 1, 1]), ("scan_bwd", [1, 1]),
+                  ("scan_fwd", [1 << 23, 1, 1])):
+        with pytest.raises(ooc.OocError, match="ooc_scan_slices"):
+            ooc.scan_slices(op, a)
+    n, b = C.c_int64(), C.c_uint64()
+    a = (C.c_int64 * 3)(1, 1, 1)
+    assert lib.ooc_join_slices(1, 1, 1, None, C.byref(b)) == ooc.E_INVALID
+    assert lib.ooc_join_slices(1, 1, 1, C.byref(n), None) == ooc.E_INVALID
+    assert lib.ooc_scan_slices(41, None, 3, C.byref(n), C.byref(b)) == ooc.E_INVALID
+    assert lib.ooc_scan_slices(41, a, 3, None, C.byref(b)) == ooc.E_INVALID
+    assert lib.ooc_scan_slices(41, a, 3, C.byref(n), None) == ooc.E_INVALID
