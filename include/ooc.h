@@ -212,6 +212,26 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                nothing.  part = partial sums, present iff a slice count > 1
  *                                     q[R] kv[R] klen[R] Y[R] lse[R] dY[R] dq[W] dkv[W] delta[W]
  *                                     [part[W]]          B Tq Tk H Hkv dh q_slices kv_slices
+ *  SPAN_ATTENTION_FWD
+ *                as CROSS_ATTENTION_FWD, but query i of a sequence attends to the states lo <= j < hi of
+ *                its own entry in span [B Tq][3] (int32: lo, hi, at): causal, a sliding window,
+ *                documents packed into a sequence, a prefix that all see, a token behind a cache.
+ *                Scores S = q k^T / sqrt(dh) become cap tanh(S / cap) iff cap = 1, then lose slope |at - j|
+ *                iff bias = 1; mod holds the cap (above 0), then a slope for each of the H heads (as
+ *                many of the two as there are).  lo >= hi: Y = 0, lse = -inf; a span that reaches
+ *                outside 0..Tk sees nothing, and its Y and lse are NaN.  A state with an infinity or a
+ *                NaN makes Y and lse NaN for the queries that see it, and reaches no other.  Values,
+ *                roundings and limits as of CROSS_ATTENTION_FWD; a capped score is off by 2^-21 of itself
+ *                more, a biased one by 2^-23; |at| at most 2^24
+ *                                     q[R] kv[R] span[R] [mod[R]] Y[W] lse[W] [part[W]]
+ *                                                         B Tq Tk H Hkv dh cap bias slices
+ *  SPAN_ATTENTION_BWD
+ *                dq and dkv (zero for what sees or is seen by nothing) of the above; a query whose q
+ *                or dY holds an infinity or a NaN makes the gradients NaN of the states that it sees.
+ *                delta as of CROSS_ATTENTION_BWD; bounds [B][ceil(Tq / 32)][2] (int32) is scratch
+ *                                     q[R] kv[R] span[R] [mod[R]] Y[R] lse[R] dY[R] dq[W] dkv[W]
+ *                                     delta[W] bounds[W] [part[W]]
+ *                                              B Tq Tk H Hkv dh cap bias q_slices kv_slices
  *  DROPOUT       Y = X where a random word of 32 bits is `drop` or more, times 2^32 / (2^32 - drop)
  *                rounded to fp32; 0 elsewhere, whatever X holds.  The words are Philox 4x32-10's
  *                (Salmon et al., 2011): value i takes word i mod 4 of the counter (i / 4, salt), low
@@ -294,7 +314,9 @@ enum {
   OOC_OP_JOIN_BWD = 40,
   OOC_OP_SCAN_FWD = 41,
   OOC_OP_SCAN_BWD = 42,
-  OOC_OP_COUNT = 43
+  OOC_OP_SPAN_ATTENTION_FWD = 43,
+  OOC_OP_SPAN_ATTENTION_BWD = 44,
+  OOC_OP_COUNT = 45
 };
 
 /* One schedule op.  fn = N for END ops; held = budget bytes held after it
@@ -563,11 +585,11 @@ ooc_status ooc_wgrad_slices(int32_t op, const int64_t *attrs, int32_t n_attrs, i
  * Host only; no context.  OOC_E_INVALID for rows < 1. */
 ooc_status ooc_qknorm_slices(int64_t rows, int64_t *slices);
 
-/* Slice counts the cross attention runs best with, and the bytes of its part
+/* Slice counts the cross or span attention runs best with, and the bytes of its part
  * variable (0: none), for the attributes B Tq Tk H Hkv dh (further ones are
- * ignored).  OOC_OP_CROSS_ATTENTION_FWD: slices[0] parts of the keys
- * (slices[1] = 1).  OOC_OP_CROSS_ATTENTION_BWD: slices[0] parts of the keys
- * for dq, slices[1] parts of the queries for dkv.  Any counts that ooc_add_fn
+ * ignored).  OOC_OP_CROSS_ATTENTION_FWD and OOC_OP_SPAN_ATTENTION_FWD:
+ * slices[0] parts of the keys (slices[1] = 1).  The backwards: slices[0] parts
+ * of the keys for dq, slices[1] parts of the queries for dkv.  Any counts that ooc_add_fn
  * accepts give the same results up to the order of sums; part then has
  * slices (B Tq H dh + B H Tq) floats forward and max(q_slices B Tq H dh,
  * kv_slices 2 B Tk Hkv dh) backward, a count of 1 taking none.  Host only; no

@@ -459,9 +459,9 @@ ooc_status ooc_attention_slices(int32_t op, const int64_t* attrs, int32_t n_attr
     g_create_error = "ooc_attention_slices: NULL argument or fewer than 6 attributes";
     return OOC_E_INVALID;
   }
-  const bool fwd = op == OOC_OP_CROSS_ATTENTION_FWD;
-  if (!fwd && op != OOC_OP_CROSS_ATTENTION_BWD) {
-    g_create_error = "ooc_attention_slices: op must be CROSS_ATTENTION_FWD or _BWD";
+  const bool fwd = op == OOC_OP_CROSS_ATTENTION_FWD || op == OOC_OP_SPAN_ATTENTION_FWD;
+  if (!fwd && op != OOC_OP_CROSS_ATTENTION_BWD && op != OOC_OP_SPAN_ATTENTION_BWD) {
+    g_create_error = "ooc_attention_slices: op must be CROSS_ATTENTION_FWD or _BWD or SPAN_ATTENTION_FWD or _BWD";
     return OOC_E_INVALID;
   }
   const std::string e = check_attention_shape(attrs);
@@ -470,11 +470,9 @@ ooc_status ooc_attention_slices(int32_t op, const int64_t* attrs, int32_t n_attr
     return OOC_E_INVALID;
   }
   const AttendShape a{attrs[0], attrs[1], attrs[2], attrs[3], attrs[4], attrs[5]};
-  int64_t full[8];
-  for (int j = 0; j < 6; ++j) full[j] = attrs[j];
-  slices[0] = full[6] = attention_key_slices(a, fwd);
-  slices[1] = full[7] = fwd ? 1 : attention_query_slices(a);
-  *part_bytes = (uint64_t)attention_part_bytes(fwd, full);
+  slices[0] = attention_key_slices(a, fwd);
+  slices[1] = fwd ? 1 : attention_query_slices(a);
+  *part_bytes = (uint64_t)attention_part_bytes(fwd, attrs, slices);
   return OOC_OK;
 } catch (const std::bad_alloc&) {
   return OOC_E_HOST_OOM;

@@ -142,6 +142,20 @@ hipError_t launch_fn(const Fn& fn, void* const* p, const uint64_t* bytes, const 
       return cross_attention_bwd(F(0), F(1), static_cast<const int32_t*>(p[2]), F(3), F(4), F(5),
                                  F(6), F(7), F(8), a[6] > 1 || a[7] > 1 ? F(9) : nullptr,
                                  {a[0], a[1], a[2], a[3], a[4], a[5]}, a[6], a[7], s);
+    case OOC_OP_SPAN_ATTENTION_FWD:
+    case OOC_OP_SPAN_ATTENTION_BWD: {
+      const AttendShape t{a[0], a[1], a[2], a[3], a[4], a[5]};
+      const bool cap = a[6] != 0, bias = a[7] != 0;
+      const int w = cap || bias ? 4 : 3;   // the first variable behind mod
+      const int32_t* span = static_cast<const int32_t*>(p[2]);
+      const float* mod = w == 4 ? F(3) : nullptr;
+      if (fn.op == OOC_OP_SPAN_ATTENTION_FWD)
+        return span_attention_fwd(F(0), F(1), span, mod, cap, bias, F(w), F(w + 1),
+                                  a[8] > 1 ? F(w + 2) : nullptr, t, a[8], s);
+      return span_attention_bwd(F(0), F(1), span, mod, cap, bias, F(w), F(w + 1), F(w + 2), F(w + 3),
+                                F(w + 4), F(w + 5), static_cast<int32_t*>(p[w + 6]),
+                                a[8] > 1 || a[9] > 1 ? F(w + 7) : nullptr, t, a[8], a[9], s);
+    }
     case OOC_OP_DROPOUT:
       return dropout(F(0), static_cast<const uint32_t*>(p[1]), F(2), a[0], a[1], a[2], s);
     case OOC_OP_JOIN_FWD: {

@@ -109,7 +109,8 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn);
 // for these attributes with their slice counts (0: none).
 constexpr int64_t kMaxAttentionSlices = 64;
 std::string check_attention_shape(const int64_t* attrs);
-int64_t attention_part_bytes(bool fwd, const int64_t* attrs);
+// attrs: the shape; counts: the slice counts
+int64_t attention_part_bytes(bool fwd, const int64_t* attrs, const int64_t* counts);
 
 // Dropout, block joins and gated recurrences: their shapes ("" when valid), and the bytes of their
 // partial results.

@@ -142,6 +142,15 @@ hipError_t cross_attention_bwd(const float* q, const float* kv, const int32_t* k
                                const float* y, const float* lse, const float* dy, float* dq,
                                float* dkv, float* delta, float* part, const AttendShape& a,
                                int64_t q_slices, int64_t kv_slices, hipStream_t s);
+// Span attention (span.hip); mod null iff neither cap nor bias.
+hipError_t span_attention_fwd(const float* q, const float* kv, const int32_t* span, const float* mod,
+                              bool cap, bool bias, float* y, float* lse, float* part,
+                              const AttendShape& a, int64_t slices, hipStream_t s);
+hipError_t span_attention_bwd(const float* q, const float* kv, const int32_t* span, const float* mod,
+                              bool cap, bool bias, const float* y, const float* lse, const float* dy,
+                              float* dq, float* dkv, float* delta, int32_t* bounds, float* part,
+                              const AttendShape& a, int64_t q_slices, int64_t kv_slices,
+                              hipStream_t s);
 // Slice counts the launchers run best with: of the keys for a pass over query rows (forward, dq),
 // of the query rows for the pass over keys (dkv).
 int64_t attention_key_slices(const AttendShape& a, bool fwd);

@@ -1,0 +1,28 @@
+// Span attention: each query against a span of the states of its sequence (gfx950): causal, a sliding
+// window, documents packed into a sequence, a prefix, a token behind a cache are all such spans.  The
+// kernels are those of cross attention (attend_kernels.h) with another view of what is seen.
+//
+// Tiles of states that no query of a workgroup sees are not loaded, blocks of 32 x 32 that a wave does
+// not see not multiplied, and only blocks that a span cuts compare states with spans.  The pass for dk
+// and dv finds the queries that see its states by the bounds of every 32 queries, which the pass for dq
+// leaves.
+#include "attend_kernels.h"
+
+namespace ooc {
+
+hipError_t span_attention_fwd(const float* q, const float* kv, const int32_t* span, const float* mod,
+                              bool cap, bool bias, float* y, float* lse, float* part,
+                              const AttendShape& a, int64_t slices, hipStream_t s) {
+  return attend_fwd(q, kv, Spans{span, mod, nullptr, cap, bias}, y, lse, part, a, slices, s);
+}
+
+hipError_t span_attention_bwd(const float* q, const float* kv, const int32_t* span, const float* mod,
+                              bool cap, bool bias, const float* y, const float* lse, const float* dy,
+                              float* dq, float* dkv, float* delta, int32_t* bounds, float* part,
+                              const AttendShape& a, int64_t q_slices, int64_t kv_slices,
+                              hipStream_t s) {
+  return attend_bwd(q, kv, Spans{span, mod, bounds, cap, bias}, y, lse, dy, dq, dkv, delta, part, a,
+                    q_slices, kv_slices, s);
+}
+
+}  // namespace ooc

@@ -63,6 +63,8 @@ const Sig kSig[OOC_OP_COUNT] = {
     {"JOIN_BWD", -1, 7, {}},
     {"SCAN_FWD", -1, 6, {}},
     {"SCAN_BWD", -1, 6, {}},
+    {"SPAN_ATTENTION_FWD", -1, 9, {}},
+    {"SPAN_ATTENTION_BWD", -1, 10, {}},
 };
 
 const int64_t kMaxElems = int64_t(1) << 40;
@@ -114,11 +116,11 @@ std::string check_scan_shape(int64_t B, int64_t T, int64_t C) {
   return "";
 }
 
-int64_t attention_part_bytes(bool fwd, const int64_t* a) {
+int64_t attention_part_bytes(bool fwd, const int64_t* a, const int64_t* n) {
   const int64_t B = a[0], Tq = a[1], Tk = a[2], H = a[3], Hkv = a[4], dh = a[5];
   const int64_t q = B * Tq * H * dh * 4, kv = B * Tk * Hkv * dh * 8, rows = B * H * Tq * 4;
-  if (fwd) return a[6] > 1 ? a[6] * (q + rows) : 0;
-  return std::max(a[6] > 1 ? a[6] * q : 0, a[7] > 1 ? a[7] * kv : 0);
+  if (fwd) return n[0] > 1 ? n[0] * (q + rows) : 0;
+  return std::max(n[0] > 1 ? n[0] * q : 0, n[1] > 1 ? n[1] * kv : 0);
 }
 
 std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
@@ -439,30 +441,40 @@ std::string check_fn(const std::vector<Var>& vars, const Fn& fn) {
       return "";
     }
     case OOC_OP_CROSS_ATTENTION_FWD:
-    case OOC_OP_CROSS_ATTENTION_BWD: {
-      const bool fwd = fn.op == OOC_OP_CROSS_ATTENTION_FWD;
+    case OOC_OP_CROSS_ATTENTION_BWD:
+    case OOC_OP_SPAN_ATTENTION_FWD:
+    case OOC_OP_SPAN_ATTENTION_BWD: {
+      const bool fwd = fn.op == OOC_OP_CROSS_ATTENTION_FWD || fn.op == OOC_OP_SPAN_ATTENTION_FWD;
+      const bool spans = fn.op == OOC_OP_SPAN_ATTENTION_FWD || fn.op == OOC_OP_SPAN_ATTENTION_BWD;
+      const int64_t* counts = a.data() + (spans ? 8 : 6);
+      if (spans && (a[6] > 1 || a[7] > 1)) return nm + ": bad attributes";
+      const int w = spans && (a[6] || a[7]) ? 1 : 0;   // mod
       e = check_attention_shape(a.data());
       if (!e.empty()) return nm + ": " + e;
       const int64_t B = a[0], Tq = a[1], Tk = a[2], H = a[3], Hkv = a[4], dh = a[5];
       const int64_t qb = product({B, Tq, H, dh, 4}), kb = product({B, Tk, Hkv, dh, 8}),
                     lb = product({B, H, Tq, 4});
-      if (a[6] < 1 || a[6] > kMaxAttentionSlices || a[6] > Tk || (!fwd && (a[7] < 1 ||
-          a[7] > kMaxAttentionSlices || a[7] > product({Tq, H / Hkv}))))
+      if (counts[0] < 1 || counts[0] > kMaxAttentionSlices || counts[0] > Tk || (!fwd && (counts[1] < 1 ||
+          counts[1] > kMaxAttentionSlices || counts[1] > product({Tq, H / Hkv}))))
         return nm + ": bad slice count";
-      const int64_t part = attention_part_bytes(fwd, a.data());
-      if (nv != (fwd ? 5 : 9) + (part > 0)) return nm + ": partial variable iff a slice count > 1";
+      const int64_t part = attention_part_bytes(fwd, a.data(), counts);
+      if (nv != (fwd ? 5 : 9) + w + (spans && !fwd) + (part > 0))
+        return nm + (spans ? ": takes mod iff capped or biased, a" : ":") +
+               std::string(" partial variable iff a slice count > 1");
       for (int j = 0; j < nv; ++j)
-        if (v[j].access != (j < (fwd ? 3 : 6) ? OOC_R : OOC_W)) return nm + ": wrong access";
+        if (v[j].access != (j < (fwd ? 3 : 6) + w ? OOC_R : OOC_W)) return nm + ": wrong access";
       NEED(0, qb, "q");
       NEED(1, kb, "kv");
-      NEED(2, B * 4, "klen");
-      NEED(3, qb, "Y");
-      NEED(4, lb, "lse");
+      NEED(2, spans ? product({B, Tq, 12}) : B * 4, spans ? "span" : "klen");
+      if (w) NEED(3, 4 * (a[6] + (a[7] ? H : 0)), "mod");
+      NEED(3 + w, qb, "Y");
+      NEED(4 + w, lb, "lse");
       if (!fwd) {
-        NEED(5, qb, "dY");
-        NEED(6, qb, "dq");
-        NEED(7, kb, "dkv");
-        NEED(8, lb, "delta");
+        NEED(5 + w, qb, "dY");
+        NEED(6 + w, qb, "dq");
+        NEED(7 + w, kb, "dkv");
+        NEED(8 + w, lb, "delta");
+        if (spans) NEED(9 + w, product({B, (Tq + 31) / 32, 8}), "bounds");
       }
       if (part) NEED(nv - 1, part, "partial results");
       return "";

@@ -37,6 +37,7 @@ OPS = {
     "rope_fwd": 32, "rope_bwd": 33, "qknorm_fwd": 34, "qknorm_bwd": 35,
     "cross_attention_fwd": 36, "cross_attention_bwd": 37,
     "dropout": 38, "join_fwd": 39, "join_bwd": 40, "scan_fwd": 41, "scan_bwd": 42,
+    "span_attention_fwd": 43, "span_attention_bwd": 44,
 }
 
 #: every symbol ``include/ooc.h`` declares
@@ -197,14 +198,15 @@ def qknorm_slices(rows):
 
 
 def attention_slices(op, attrs):
-    """``(slice counts, bytes of the part variable)`` of a cross attention with the shape B, Tq,
-    Tk, H, Hkv, dh, as the library's kernels want them: one count for ``cross_attention_fwd``,
-    two for ``cross_attention_bwd``.  They follow the shape in the operation's attributes."""
+    """``(slice counts, bytes of the part variable)`` of a cross or span attention with the shape B,
+    Tq, Tk, H, Hkv, dh, as the library's kernels want them: one count for ``cross_attention_fwd`` and
+    ``span_attention_fwd``, two for the backwards.  They are the operation's last attributes."""
     a = (ctypes.c_int64 * len(attrs))(*attrs)
     out, part = (ctypes.c_int64 * 2)(), ctypes.c_uint64()
     op = OPS[op] if isinstance(op, str) else op
     _check(load().ooc_attention_slices(op, a, len(attrs), out, ctypes.byref(part)), None)
-    return list(out)[:1 if op == OPS["cross_attention_fwd"] else 2], part.value
+    fwd = op in (OPS["cross_attention_fwd"], OPS["span_attention_fwd"])
+    return list(out)[:1 if fwd else 2], part.value
 
 
 def join_slices(rows, d, groups):

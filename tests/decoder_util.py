@@ -161,3 +161,93 @@ def scan_ins(fx, h0, fr):
 
 
 R, W = ooc.R, ooc.W
+
+
+# ---------------------------------------------------------------- span attention
+# A score's error is that of attention_util, and: under the cap 8 u of itself and 4 u of the cap (its
+# tangent is off by 2^-21 of itself, the cap's quotient and product round); the bias rounds the distance's
+# product and the sum, 2 u of each.  The cap's factor 1 - tanh^2 is off by 8 u, and by the score's error
+# over the cap, as its slope is less than 1.
+def spans(kind, g, B, Tq, Tk):
+    i = np.broadcast_to(np.arange(Tq), (B, Tq)) + (Tk - Tq)
+    lo, hi, at = np.zeros((B, Tq), int), i + 1, i
+    if kind == "window":
+        lo = hi - max(1, Tk // 5)
+    elif kind == "docs":
+        cuts = np.sort(g.integers(0, Tk, (B, 3)), 1)
+        lo = np.where(i[:, :, None] >= cuts[:, None], cuts[:, None], 0).max(-1)
+        hi = np.where(i < Tk - Tk // 7, hi, lo)
+    elif kind == "prefix":
+        hi = np.maximum(hi, g.integers(0, Tk + 1, (B, 1)))
+    elif kind == "any":            # spans of any order and length, a quarter of them empty
+        lo = g.integers(0, Tk + 1, (B, Tq))
+        hi = np.where(g.random((B, Tq)) < 0.25, lo - g.integers(0, 3, (B, Tq)),
+                      g.integers(0, Tk + 1, (B, Tq)))
+        at = g.integers(-5, Tk + 5, (B, Tq))
+    elif kind == "all":
+        lo, hi = np.zeros((B, Tq), int), np.full((B, Tq), Tk)
+    elif kind == "none":
+        hi = lo
+    return np.stack([np.maximum(lo, 0), hi, at], -1).reshape(B * Tq, 3).astype(np.int32)
+
+
+def span_case(seed, B, Tq, Tk, H, Hkv, dh, kind, cap=0.0, bias=False, spread=1.0):
+    g = np.random.default_rng(seed)
+    a = {"B": B, "Tq": Tq, "Tk": Tk, "H": H, "Hkv": Hkv, "dh": dh, "cap": int(cap > 0), "bias": int(bias)}
+    q = (spread * g.standard_normal((B * Tq, H * dh))).astype(np.float32)
+    kv, dy = (g.standard_normal(s, np.float32) for s in ((B * Tk, 2 * Hkv * dh), q.shape))
+    mod = ([cap] if cap else []) + (list(2.0 ** -g.uniform(0, 8, H)) if bias else [])
+    return a, q, kv, spans(kind, g, B, Tq, Tk), np.array(mod, np.float32), dy
+
+
+def span_attrs(a):
+    return [a[k] for k in ("B", "Tq", "Tk", "H", "Hkv", "dh", "cap", "bias")]
+
+
+def span_bounds(q, kv, span, mod, dy, a):
+    """Bounds of y, lse, dq, dkv."""
+    f = np.float64
+    Q, K, V, G = ops._cross_parts(q.astype(f), kv.astype(f), a)
+    D = dy.astype(f).reshape(a["B"], a["Tq"], a["H"], a["dh"]).transpose(0, 2, 1, 3)
+    ey, el = np.zeros_like(Q), np.zeros(Q.shape[:3])
+    eq, ek, ev = np.zeros_like(Q), np.zeros_like(K), np.zeros_like(V)
+    scale, es = 1 / np.sqrt(a["dh"]), (a["dh"] / 2 + 16) * U
+    sp = span.reshape(a["B"], a["Tq"], 3)
+    cap = float(mod[0]) if a["cap"] else np.inf
+    sums = (6 * a["Tk"] / 16 + 32) * U
+    rows = (6 * a["Tq"] * G / 16 + 32) * U
+    for b in range(a["B"]):
+        for h in range(a["H"]):
+            j = h // G
+            k, v, qq, d = K[b, j], V[b, j], Q[b, h], D[b, h]
+            S, turn = ops._span_scores(qq, k, sp[b], h, a, mod)
+            seen = S > -np.inf
+            P, lse = ops._span_probs(S)
+            mag = np.where(seen, np.abs(S), 0.0)
+            raw = es * scale * np.abs(qq) @ np.abs(k).T
+            e_turn = raw / cap + 8 * U if a["cap"] else 0.0
+            if a["bias"]:
+                far = np.abs(np.arange(a["Tk"]) - sp[b][:, 2:]) * float(mod[a["cap"] + h])
+            else:
+                far = 0.0
+            eS = raw + ((8 * U * (mag + far) + 4 * U * cap) if a["cap"] else 0.0) + 2 * U * (far + mag)
+            eS = np.where(seen, eS, 0.0)
+            some = np.where(seen.any(1), lse, 0.0)
+            reach = np.where(seen, np.abs(np.where(seen, S, 0.0) - some[:, None]), 0.0) + 8
+            eP = eS + eS.max(-1, keepdims=True) + 2 * U * reach + sums     # relative
+            eP = eP + 4 * U * (np.abs(some) + mag.max(-1))[:, None]
+            el[b, h] = eS.max(-1) + sums + 4 * U * (np.abs(some) + mag.max(-1))
+            ey[b, h] = (P * (eP + sums)) @ np.abs(v)
+            dP = d @ v.T
+            y = P @ v
+            delta = (d * y).sum(-1, keepdims=True)
+            e_dP = es * np.abs(d) @ np.abs(v).T
+            e_delta = (np.abs(d) * (ey[b, h] + (a["dh"] / 16 + 16) * U * np.abs(y))).sum(-1, keepdims=True)
+            dS = P * np.abs(dP - delta) * scale
+            e_dS = dS * turn * (eP + 4 * U) + P * scale * turn * (e_dP + e_delta) + dS * e_turn
+            dS = dS * turn
+            eq[b, h] = (e_dS + sums * dS) @ np.abs(k)
+            ek[b, j] += (e_dS + rows * dS).T @ np.abs(qq)
+            ev[b, j] += (P * (eP + rows)).T @ np.abs(d)
+    return (ey.transpose(0, 2, 1, 3).reshape(q.shape), el, eq.transpose(0, 2, 1, 3).reshape(q.shape),
+            np.stack([ek, ev]).transpose(1, 3, 0, 2, 4).reshape(kv.shape))

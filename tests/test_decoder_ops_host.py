@@ -189,3 +189,72 @@ def test_slice_counts(lib):
     assert lib.ooc_scan_slices(41, None, 3, C.byref(n), C.byref(b)) == ooc.E_INVALID
     assert lib.ooc_scan_slices(41, a, 3, None, C.byref(b)) == ooc.E_INVALID
     assert lib.ooc_scan_slices(41, a, 3, C.byref(n), None) == ooc.E_INVALID
+
+
+# ---------------------------------------------------------------- span attention
+@pytest.mark.parametrize("kind,cap,bias", [("causal", 0, False), ("any", 1.5, True), ("docs", 0, True),
+                                           ("none", 2.0, False)])
+def test_span_attention_against_plain_loops_and_differences(kind, cap, bias):
+    a, q, kv, span, mod, dy = du.span_case(7, 2, 5, 7, 4, 2, 3, kind, cap, bias)
+    q, kv, dy, mod = (t.astype(np.float64) for t in (q, kv, dy, mod))
+    y, lse = ops.span_attention_fwd(q, kv, span, a, mod)
+    for b in range(2):
+        for h in range(4):
+            for i in range(5):
+                lo, hi, at = span[b * 5 + i]
+                e = {}
+                for j in range(max(lo, 0), min(hi, 7)):
+                    s = q[b * 5 + i, 3 * h:3 * h + 3] @ kv[b * 7 + j, 3 * (h // 2):3 * (h // 2) + 3] / np.sqrt(3)
+                    s = mod[0] * np.tanh(s / mod[0]) if cap else s
+                    e[j] = np.exp(s - (mod[-4 + h] * abs(at - j) if bias else 0))
+                want = sum((w * kv[b * 7 + j, 6 + 3 * (h // 2):9 + 3 * (h // 2)] for j, w in e.items()),
+                           np.zeros(3)) / (sum(e.values()) or 1)
+                assert np.allclose(y[b * 5 + i, 3 * h:3 * h + 3], want, rtol=1e-11, atol=1e-13)
+                assert np.isclose(lse[b, h, i], np.log(sum(e.values())) if e else -np.inf)
+    dq, dkv, delta = ops.span_attention_bwd(q, kv, span, dy, a, mod)
+    assert np.allclose(delta.transpose(0, 2, 1).reshape(10, 4), (dy * y).reshape(10, 4, 3).sum(-1), atol=1e-13)
+    g = np.random.default_rng(8)
+    for _ in range(3):
+        vq, vk = g.standard_normal(q.shape), g.standard_normal(kv.shape)
+        num = difference(lambda t: (ops.span_attention_fwd(t, kv, span, a, mod)[0] * dy).sum(), q, vq)
+        assert np.isclose(num, (dq * vq).sum(), rtol=1e-6, atol=1e-8)
+        num = difference(lambda t: (ops.span_attention_fwd(q, t, span, a, mod)[0] * dy).sum(), kv, vk)
+        assert np.isclose(num, (dkv * vk).sum(), rtol=1e-6, atol=1e-8)
+
+
+def test_the_span_bounds_separate_planted_mistakes():
+    """Planted in the oracle: a state more or fewer in each span, a cap and slopes 0.1 % off."""
+    a, q, kv, span, mod, dy = du.span_case(9, 1, 60, 60, 2, 1, 16, "causal", 2.0, True)
+    mod[1:] = 1 / 64      # far states count
+    f = np.float64
+    q64, kv64, d64 = q.astype(f), kv.astype(f), dy.astype(f)
+    y, lse = ops.span_attention_fwd(q64, kv64, span, a, mod)
+    dq, dkv, _ = ops.span_attention_bwd(q64, kv64, span, d64, a, mod)
+    by, bl, bq, bk = du.span_bounds(q, kv, span, mod, dy, a)
+    for other, m in ((span - [0, 1, 0], mod), (span + [1, 0, 0], mod), (span, mod * np.float32(1.001))):
+        y1, l1 = ops.span_attention_fwd(q64, kv64, other, a, m)
+        g1 = ops.span_attention_bwd(q64, kv64, other, d64, a, m)
+        for got, want, bound in ((y1, y, by), (g1[0], dq, bq), (g1[1], dkv, bk)):
+            assert (np.abs(got - want) > bound).mean() > 0.5
+
+
+@pytest.mark.parametrize("cap,bias", [(0, 0), (1, 0), (0, 1), (1, 1)])
+@pytest.mark.parametrize("slices", [(1, 1, 1), (2, 1, 3)], ids=str)
+def test_span_attention_refusals(lib, cap, bias, slices):
+    B, Tq, Tk, H, Hkv, dh = shape = [2, 5, 7, 4, 2, 8]
+    q, kv, lse = B * Tq * H * dh * 4, B * Tk * 2 * Hkv * dh * 4, B * H * Tq * 4
+    mod = [4 * (cap + bias * H)] if cap or bias else []
+    sf, sq, sk = slices
+    bad = [(0, 0), (1, 0), (2, 0), (3, 0), (4, 3), (5, 257), (6, 1 - cap), (6, 2), (7, 1 - bias), (7, 2), (8, 0), (8, 65)]
+    if not (cap and bias):      # one flag for the other needs another mod
+        bad = [(j, x) for j, x in bad if not (j in (6, 7) and x < 2 and not mod)]
+    ins = [q, kv, B * Tq * 12] + mod
+    part = [sf * (q + lse)] if sf > 1 else []
+    vary("span_attention_fwd", ins + [q, lse] + part, [R] * len(ins) + [W] * (2 + len(part)),
+         shape + [cap, bias, sf], bad + [(8, 8)])
+    n = max(sq * q if sq > 1 else 0, sk * kv if sk > 1 else 0)
+    outs = [q, kv, lse, B * 8] + ([n] if n else [])
+    vary("span_attention_bwd", ins + [q, lse, q] + outs, [R] * (len(ins) + 3) + [W] * len(outs),
+         shape + [cap, bias, sq, sk], bad + [(8, 8), (9, 0), (9, 11)])
+    assert ooc.attention_slices("span_attention_fwd", shape) == ooc.attention_slices("cross_attention_fwd", shape)
+    assert ooc.attention_slices("span_attention_bwd", shape) == ooc.attention_slices("cross_attention_bwd", shape)
