@@ -103,6 +103,17 @@ def fn_work(op, attrs, states=None):
         B, Tq, Tk, H, Hkv, dh = a[:6]
         pairs = Tq * (B * Tk if states is None else states)
         return "flop", (2 if op.endswith("fwd") else 5) * 2 * H * pairs * dh
+    if op in ("span_attention_fwd", "span_attention_bwd"):
+        # the same products, of the pairs that spans show
+        B, Tq, Tk, H, Hkv, dh = a[:6]
+        pairs = B * Tq * Tk if states is None else states
+        return "flop", (2 if op.endswith("fwd") else 5) * 2 * H * pairs * dh
+    if op == "dropout":
+        return "byte", 8 * a[0]
+    if op in ("join_fwd", "join_bwd"):
+        return "byte", (16 if op == "join_fwd" else 24 if a[5] else 20) * a[0] * a[1]
+    if op in ("scan_fwd", "scan_bwd"):
+        return "byte", (12 if op == "scan_fwd" else 24) * a[0] * a[1] * a[2]
     return "byte", 0
 
 
@@ -131,7 +142,7 @@ def roofline(dom, op=None):
     """Rate of the dominant function (``op``) against what bounds it: products against the matrix
     instructions that carry them, everything else against HBM."""
     if dom["unit"] == "flop":
-        fp16 = op in ("cross_attention_fwd", "cross_attention_bwd")
+        fp16 = op.startswith(("cross_attention", "span_attention")) if op else False
         products = FP16_PRODUCTS if fp16 else PRODUCTS
         peak = PEAK_BF16_TFLOPS / products
         return {"bound": "mfma", "achieved": round(dom["rate"], 3), "peak": round(peak, 1),
@@ -324,6 +335,9 @@ def kernel_table(net, fn_ms, inputs=None):
         states = None
         if op.startswith("cross_attention") and inputs:
             states = int(inputs[net.names[net.fn_vars[j][2][0]]].sum())
+        if op.startswith("span_attention") and inputs:
+            span = inputs[net.names[net.fn_vars[j][2][0]]]
+            states = int((span[:, 1] - span[:, 0]).clip(min=0).sum())
         kind, work = fn_work(op, attrs, states)
         if op == "sgd":
             kind, work = "byte", sgd_bytes(net, j)
@@ -383,7 +397,7 @@ def cpu_baseline(name, budget_seconds=15.0):
     from oracle.interp import run as oracle_run
     from oracle.lower import lower
     small = {"mlp": 256, "cnn": 8, "resnet50_b256": 2, "resnet50_b1440": 2,
-             "transformer": 1, "seq2seq": 1, "densenet": 2, "unet": 1}[name]
+             "transformer": 1, "seq2seq": 1, "densenet": 2, "unet": 1, "packed": 1}[name]
     spec = synth.workload(name, batch=small)
     reg = lower(spec)
     x, labels = synth.make_inputs(spec, 0)

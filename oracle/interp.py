@@ -183,6 +183,40 @@ def run(reg, x, labels, params, state=None, dtype=np.float64, decisions=None, in
         elif op == "cross_attention_bwd":
             q, kv, n, Y, lse, dY, dq, dkv, delta = vs[:9]
             env[dq], env[dkv], env[delta] = ops.cross_attention_bwd(g(q), g(kv), g(n), g(dY), a)
+        elif op in ("span_attention_fwd", "span_attention_bwd"):
+            q, kv, span = vs[:3]
+            mod = g(vs[3]) if a["cap"] or a["bias"] else None
+            rest = vs[3 + (mod is not None):]
+            if op == "span_attention_fwd":
+                env[rest[0]], env[rest[1]] = ops.span_attention_fwd(g(q), g(kv), g(span), a, mod)
+            else:
+                dY, dq, dkv, delta = rest[2:6]
+                env[dq], env[dkv], env[delta] = ops.span_attention_bwd(g(q), g(kv), g(span), g(dY), a, mod)
+        elif op == "dropout":
+            X, seed, Y = vs
+            env[Y] = ops.dropout(g(X), g(seed), a)
+        elif op == "join_fwd":
+            ins, (H, N, st) = [g(v) for v in vs[:-3]], vs[-3:]
+            env[H], env[N], env[st] = ops.join_fwd(*ins[:6], a, *ins[6:])
+        elif op == "join_bwd":
+            F, H, _, post, gate, pre, scale = (g(v) for v in vs[:7])
+            w = 7 + (a["drop"] > 0)
+            dH = g(vs[w]) if a["stream"] else None
+            w += a["stream"]
+            seed = g(vs[7]) if a["drop"] else None
+            grads = ops.join_bwd(F, H, post, gate, pre, scale, dH, g(vs[w]), a, seed)
+            env.update(zip(vs[w + 1:], grads))
+        elif op in ("scan_fwd", "scan_bwd"):
+            FX, w = vs[0], 1 + a["carry"]
+            h0 = g(vs[1]) if a["carry"] else None
+            fresh = g(vs[w]) if a["fresh"] else None
+            rest = vs[w + a["fresh"]:]
+            if op == "scan_fwd":
+                env[rest[0]] = ops.scan_fwd(g(FX), a, h0, fresh)
+            else:
+                env[rest[2]], dh0 = ops.scan_bwd(g(FX), g(rest[0]), g(rest[1]), a, h0, fresh)
+                if a["carry"]:
+                    env[rest[3]] = dh0
         else:
             raise ValueError(f"unknown function {op}")
     return env

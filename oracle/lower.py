@@ -56,6 +56,14 @@ qknorm_fwd     X R, gain R [, pos R, table R], Y W          (pos, table when it 
 qknorm_bwd     X R, gain R [, pos R, table R], dY R, dX W, dgain W, part W
 cross_attention_fwd  q R, kv R, klen R, Y W, lse W [, part W]
 cross_attention_bwd  q R, kv R, klen R, Y R, lse R, dY R, dq W, dkv W, delta W [, part W]
+span_attention_fwd  q R, kv R, span R [, mod R], Y W, lse W [, part W]
+span_attention_bwd  q R, kv R, span R [, mod R], Y R, lse R, dY R, dq W, dkv W, delta W, bounds W [, part W]
+dropout        X R, seed R, Y W           (its backward: dY R, seed R, dX W)
+join_fwd       X R, F R, post R, gate R, pre R, scale R [, seed R], H W, N W, stats W
+join_bwd       F R, H R, stats R, post R, gate R, pre R, scale R [, seed R] [, dH R], dN R, dX W, dF W,
+               dpost W, dgate W, dpre W, part W  (dH where something else reads H)
+scan_fwd       FX R [, h0 R] [, fresh R], H W [, part W]
+scan_bwd       FX R [, h0 R] [, fresh R], H R, dH R, dFX W [, dh0 W] [, part W]
 =============  ======================================================================
 
 The backward of an addition is the identity, so both inputs receive the
@@ -73,7 +81,9 @@ S_w slices of db, S_w being given per layer by the caller (``lower``'s
 ``slices``); a per-head norm's ``part`` holds S partial gains, S = min(ceil(rows
 / 8), 2048); a cross attention's, S partial outputs and row logarithms forward
 and the larger of S_q partial dq and S_kv partial dkv backward, counts of 1
-taking nothing, ``slices`` giving (S, S_q, S_kv).
+taking nothing, ``slices`` giving (S, S_q, S_kv), and a span attention's alike; a join's three rows
+for each of S slices of the rows of each gate; a recurrence's two rows per slice of a sequence, ``slices``
+giving (S forward, S backward).
 
 Kinds: x and labels INPUT, parameters PARAM, momentum buffers STATE, loss
 OUTPUT (parameter gradients too when ``keep_grads``), everything else TEMP.
@@ -134,6 +144,30 @@ def lower(spec, keep_grads=False, slices=None):
         Bt = spec["input"][0]
         return {"B": Bt, "Tq": q[0] // Bt, "Tk": kv[0] // Bt, "H": L["heads"],
                 "Hkv": L["kv_heads"], "dh": q[1] // L["heads"]}
+
+    def spanned(L):
+        cap, bias = int(bool(L.get("cap"))), int(bool(L.get("bias")))
+        return (dict(cross(L), cap=cap, bias=bias),
+                [(L["span"], R)] + ([(L["mod"], R)] if cap or bias else []))
+
+    def dropped(L):
+        drop = int(L.get("p", 0) * 2 ** 32)
+        return {"drop": drop, "salt": L.get("salt", 0)}, [(L["seed"], R)] if drop else []
+
+    def joined(L):
+        name = L["name"]
+        rows, d = shapes[L["in"][0]]
+        a, seed = dropped(L)
+        gate = L.get("gate", name + ".gate")
+        groups = shapes[gate][0] if "gate" in L else 1
+        return (dict(a, rows=rows, d=d, groups=groups),
+                [(n, R) for n in (name + ".post", gate, name + ".pre", L["scale"])] + seed)
+
+    def scanned(L):
+        rows, c2 = shapes[L["in"][0]]
+        Bt = spec["input"][0]
+        a = {"B": Bt, "T": rows // Bt, "C": c2 // 2, "carry": int("state" in L), "fresh": int("fresh" in L)}
+        return a, [(L[k], R) for k in ("state", "fresh") if k in L]
 
     params_of = {}
 
@@ -270,6 +304,42 @@ def lower(spec, keep_grads=False, slices=None):
             if S > 1:
                 vs.append((var(name + ".part", (S * (math.prod(xs) + rows_h),)), W))
             fns.append(("cross_attention_fwd", vs, a))
+        elif op == "span_attention":
+            a, where = spanned(L)
+            rows_h = a["B"] * a["H"] * a["Tq"]
+            shapes[name] = xs
+            var(name, xs)
+            lse = var(name + ".lse", (a["B"], a["H"], a["Tq"]))
+            S = (slices or {}).get(name, (1, 1, 1))[0]
+            vs = [(X, R), (ins[1], R)] + where + [(name, W), (lse, W)]
+            if S > 1:
+                vs.append((var(name + ".part", (S * (math.prod(xs) + rows_h),)), W))
+            fns.append(("span_attention_fwd", vs, a))
+        elif op == "dropout":
+            a, seed = dropped(L)
+            shapes[name] = xs
+            var(name, xs)
+            fns.append(("dropout", [(X, R)] + seed + [(name, W)], a))
+        elif op == "join":
+            params_of[name] = [var(name + ".post", (xs[1],), kind=PARAM)]
+            if "gate" not in L:
+                params_of[name].append(var(name + ".gate", (1, xs[1]), kind=PARAM))
+            params_of[name].append(var(name + ".pre", (xs[1],), kind=PARAM))
+            a, parts = joined(L)
+            shapes[name] = shapes[name + ".h"] = xs
+            H = var(name + ".h", xs)
+            var(name, xs)
+            st_ = var(name + ".stats", (xs[0], 2))
+            fns.append(("join_fwd", [(X, R), (ins[1], R)] + parts + [(H, W), (name, W), (st_, W)], a))
+        elif op == "scan":
+            a, where = scanned(L)
+            shapes[name] = (xs[0], a["C"])
+            var(name, shapes[name])
+            S = (slices or {}).get(name, (1, 1))[0]
+            vs = [(X, R)] + where + [(name, W)]
+            if S > 1:
+                vs.append((var(name + ".part", (S * a["B"] * 2 * a["C"],)), W))
+            fns.append(("scan_fwd", vs, a))
         else:
             raise ValueError(f"unknown layer kind {op}")
 
@@ -473,7 +543,56 @@ def lower(spec, keep_grads=False, slices=None):
             fns.append(("cross_attention_bwd", vs, a))
             contribute(X, dq, pending)
             contribute(kv, dkv, pending)
-        done.add(name)
+        elif op == "span_attention":
+            (a, where), kv = spanned(L), L["in"][1]
+            dq = var(f"d:{X}@{name}", xs)
+            dkv = var(f"d:{kv}@{name}", shapes[kv])
+            delta = var(name + ".delta", (a["B"], a["H"], a["Tq"]))
+            bounds = var(name + ".bounds", (a["B"], math.ceil(a["Tq"] / 32), 2), dtype="i32")
+            _, Sq, Skv = (slices or {}).get(name, (1, 1, 1))
+            n = max(Sq * math.prod(xs) if Sq > 1 else 0,
+                    Skv * math.prod(shapes[kv]) if Skv > 1 else 0)
+            vs = [(X, R), (kv, R)] + where + [(name, R), (name + ".lse", R), (dY, R),
+                                              (dq, W), (dkv, W), (delta, W), (bounds, W)]
+            if n:
+                vs.append((var(name + ".bpart", (n,)), W))
+            fns.append(("span_attention_bwd", vs, a))
+            contribute(X, dq, pending)
+            contribute(kv, dkv, pending)
+        elif op == "dropout":
+            a, seed = dropped(L)
+            dX = var(f"d:{X}@{name}", xs)
+            fns.append(("dropout", [(dY, R)] + seed + [(dX, W)], a))
+            contribute(X, dX, pending)
+        elif op == "join":
+            a, parts = joined(L)
+            Fn = L["in"][1]
+            dH = grad.get(name + ".h")
+            S = (slices or {}).get(name, 1)
+            dX, dF = var(f"d:{X}@{name}", xs), var(f"d:{Fn}@{name}", xs)
+            shape = (a["groups"], a["d"])
+            dg = (var(f"d:{L['gate']}@{name}", shape) if "gate" in L else
+                  var(f"d:{name}.gate", shape, kind=grad_kind))
+            dpost, dpre = (var(f"d:{name}.{k}", (a["d"],), kind=grad_kind) for k in ("post", "pre"))
+            part = var(name + ".part", (a["groups"] * S * 3 * a["d"],))
+            fns.append(("join_bwd", [(Fn, R), (name + ".h", R), (name + ".stats", R)] + parts +
+                        ([(dH, R)] if dH else []) + [(dY, R)] +
+                        [(o, W) for o in (dX, dF, dpost, dg, dpre, part)], dict(a, stream=dH is not None)))
+            contribute(X, dX, pending)
+            contribute(Fn, dF, pending)
+            if "gate" in L:
+                contribute(L["gate"], dg, pending)
+            update(name)
+        elif op == "scan":
+            a, where = scanned(L)
+            dX = var(f"d:{X}@{name}", xs)
+            outs = [dX] + ([var(f"d:{L['state']}@{name}", (a["B"], a["C"]))] if a["carry"] else [])
+            S = (slices or {}).get(name, (1, 1))[1]
+            if S > 1:
+                outs.append(var(name + ".bpart", (S * a["B"] * 2 * a["C"],)))
+            fns.append(("scan_bwd", [(X, R)] + where + [(name, R), (dY, R)] + [(o, W) for o in outs], a))
+            contribute(X, dX, pending)
+        done.update((name, name + ".h"))
         settle(pending)
 
     # ---------------- number variables by first appearance

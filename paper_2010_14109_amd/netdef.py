@@ -26,7 +26,12 @@ S_w > 1; a LayerNorm keeps mean and 1/std per row and 2 S floats per feature
 with S = min(ceil(rows / 32), 2048) (its rows are d floats wide); attention
 writes its probabilities [B, H, T, T] in the forward, where they die, and its
 backward recomputes them into a variable of its own beside a scratch of the
-same size; cross attention keeps one logarithm per row and head instead.
+same size; cross and span attention keep one logarithm per row and head instead;
+a block join keeps two floats per row, a gated recurrence and dropout nothing.
+
+A join's output ``name`` is the next block's input; ``name + ".h"`` is the residual
+stream, for the next join.  Its gate is a parameter, or the tensor ``gate`` names, a
+row for each rows / groups rows.
 
 ``spec["input"]`` is the shape of the input ``x``; ``spec["inputs"]`` lists
 further INPUT variables, ``{"name", "shape", "dtype"}``: the tokens and lengths
@@ -291,6 +296,105 @@ class Net:
         self.slices[L["name"]] = slices + ooc.attention_slices("cross_attention_bwd", a)[0]
         return self.shape[X]
 
+    def _input(self, L, name, shape, dtype):
+        """The named input of a layer, checked."""
+        if name not in self.inputs or self.meta[name][:2] != (tuple(shape), dtype):
+            raise ValueError(f"{L['name']}: {name} must be an input of {tuple(shape)} {dtype}")
+        return (name, ooc.R)
+
+    def _span_attrs(self, L):
+        q, kv = L["in"]
+        B, H, Hkv = self.spec["input"][0], L["heads"], L["kv_heads"]
+        dh = self.shape[q][1] // H
+        if self.shape[q][1] != H * dh or self.shape[kv][1] != 2 * Hkv * dh:
+            raise ValueError(f"{L['name']}: query and key widths do not fit the heads")
+        Tq, Tk = (self._positions(L["name"], self.shape[t][0]) for t in (q, kv))
+        cap, bias = int(bool(L.get("cap"))), int(bool(L.get("bias")))
+        where = [self._input(L, L["span"], (B * Tq, 3), "i32")]
+        if cap or bias:
+            where.append(self._input(L, L["mod"], (cap + bias * H,), "f32"))
+        return [B, Tq, Tk, H, Hkv, dh, cap, bias], where
+
+    def _fwd_span_attention(self, L, X):
+        a, where = self._span_attrs(L)
+        slices, part = ooc.attention_slices("span_attention_fwd", a)
+        Y = self._decl(L["name"], self.shape[X])
+        lse = self._decl(L["name"] + ".lse", (a[0], a[3], a[1]))
+        pairs = [(X, ooc.R), (L["in"][1], ooc.R)] + where + [(Y, ooc.W), (lse, ooc.W)]
+        if part:
+            pairs.append((self._decl(L["name"] + ".part", (part // FLOAT,)), ooc.W))
+        self._call("span_attention_fwd", pairs, a + slices)
+        self.slices[L["name"]] = slices + ooc.attention_slices("span_attention_bwd", a)[0]
+        return self.shape[X]
+
+    def _dropped(self, L):
+        """drop of 2^32 and salt of a layer's dropout, and its seed where it drops."""
+        if not 0 <= L.get("p", 0) < 1:
+            raise ValueError(f"{L['name']}: p must lie in [0, 1)")
+        drop = int(L.get("p", 0) * 2 ** 32)
+        return [drop, L.get("salt", 0)], [self._input(L, L["seed"], (2,), "i32")] if drop else []
+
+    def _fwd_dropout(self, L, X):
+        xs = self.shape[X]
+        attrs, seed = self._dropped(L)
+        if not seed:
+            raise ValueError(f"{L['name']}: nothing is dropped")
+        Y = self._decl(L["name"], xs)
+        self._call("dropout", [(X, ooc.R)] + seed + [(Y, ooc.W)], [prod(xs)] + attrs)
+        return xs
+
+    def _join_parts(self, L):
+        """Attributes and the variables from post to seed."""
+        rows, d = self.shape[L["in"][0]]
+        gate = L.get("gate", L["name"] + ".gate")
+        attrs, seed = self._dropped(L)
+        scale = self._input(L, L["scale"], (1,), "f32")
+        names = [L["name"] + ".post", gate, L["name"] + ".pre"]
+        groups = self.shape[gate][0] if "gate" in L else 1
+        return [rows, d, groups] + attrs, [(n, ooc.R) for n in names] + [scale] + seed
+
+    def _fwd_join(self, L, X):
+        xs, name = self.shape[X], L["name"]
+        if self.shape[L["in"][1]] != xs:
+            raise ValueError(f"{name}: the stream and the block's output differ in shape")
+        own = [name + ".post"] + ([] if "gate" in L else [name + ".gate"]) + [name + ".pre"]
+        if "gate" in L and (len(self.shape[L["gate"]]) != 2 or self.shape[L["gate"]][1] != xs[1]
+                            or xs[0] % self.shape[L["gate"]][0]):
+            raise ValueError(f"{name}: the gate's rows must be as wide and divide the rows")
+        for p in own:
+            self._decl(p, (1, xs[1]) if p.endswith(".gate") else (xs[1],), kind=ooc.PARAM)
+        self.params[name] = own
+        attrs, parts = self._join_parts(L)
+        H = self._decl(name + ".h", xs)
+        N, st = self._decl(name, xs), self._decl(name + ".stats", (xs[0], 2))
+        self.shape[H] = xs
+        self._call("join_fwd", [(X, ooc.R), (L["in"][1], ooc.R)] + parts +
+                   [(H, ooc.W), (N, ooc.W), (st, ooc.W)], attrs)
+        return xs
+
+    def _scan_parts(self, L, X):
+        rows, c2 = self.shape[X]
+        B, T = self.spec["input"][0], self._positions(L["name"], rows)
+        if c2 % 2:
+            raise ValueError(f"{L['name']}: rows of f and x have an even width")
+        where = []
+        if "state" in L:
+            where.append(self._input(L, L["state"], (B, c2 // 2), "f32"))
+        if "fresh" in L:
+            where.append(self._input(L, L["fresh"], (rows,), "i32"))
+        return [B, T, c2 // 2, int("state" in L), int("fresh" in L)], where
+
+    def _fwd_scan(self, L, X):
+        a, where = self._scan_parts(L, X)
+        slices, part = ooc.scan_slices("scan_fwd", a)
+        H = self._decl(L["name"], (a[0] * a[1], a[2]))
+        pairs = [(X, ooc.R)] + where + [(H, ooc.W)]
+        if part:
+            pairs.append((self._decl(L["name"] + ".part", (part // FLOAT,)), ooc.W))
+        self._call("scan_fwd", pairs, a + [slices])
+        self.slices[L["name"]] = [slices, ooc.scan_slices("scan_bwd", a)[0]]
+        return (a[0] * a[1], a[2])
+
     # ------------------------------------------------------------ backward
     def _grad_of_param(self, p):
         return self._decl("d:" + p, self.meta[p][0],
@@ -444,6 +548,57 @@ class Net:
                 pairs.append((self._decl(name + ".bpart", (part // FLOAT,)), ooc.W))
             self._call("cross_attention_bwd", pairs, a + slices)
             out += [(X, dq), (kv, dkv)]
+        elif op == "span_attention":
+            a, where = self._span_attrs(L)
+            B, Tq, _, H = a[:4]
+            kv = L["in"][1]
+            slices, part = ooc.attention_slices("span_attention_bwd", a)
+            dq = self._decl(f"d:{X}@{name}", xs)
+            dkv = self._decl(f"d:{kv}@{name}", self.shape[kv])
+            delta = self._decl(name + ".delta", (B, H, Tq))
+            bounds = self._decl(name + ".bounds", (B, ceil(Tq / 32), 2), dtype="i32")
+            pairs = [(X, ooc.R), (kv, ooc.R)] + where + [
+                (name, ooc.R), (name + ".lse", ooc.R), (dY, ooc.R), (dq, ooc.W), (dkv, ooc.W),
+                (delta, ooc.W), (bounds, ooc.W)]
+            if part:
+                pairs.append((self._decl(name + ".bpart", (part // FLOAT,)), ooc.W))
+            self._call("span_attention_bwd", pairs, a + slices)
+            out += [(X, dq), (kv, dkv)]
+        elif op == "dropout":
+            attrs, seed = self._dropped(L)
+            dX = self._decl(f"d:{X}@{name}", xs)
+            self._call("dropout", [(dY, ooc.R)] + seed + [(dX, ooc.W)], [prod(xs)] + attrs)
+            out.append((X, dX))
+        elif op == "join":
+            attrs, parts = self._join_parts(L)
+            rows, d, groups = attrs[:3]
+            F = L["in"][1]
+            dH = self.grads.get(name + ".h")
+            slices, part = ooc.join_slices(rows, d, groups)
+            self.slices[name] = slices
+            dX = self._decl(f"d:{X}@{name}", xs)
+            dF = self._decl(f"d:{F}@{name}", xs)
+            dgate = (self._decl(f"d:{L['gate']}@{name}", (groups, d)) if "gate" in L
+                     else self._grad_of_param(name + ".gate"))
+            outs = [dX, dF, self._grad_of_param(name + ".post"), dgate,
+                    self._grad_of_param(name + ".pre"), self._decl(name + ".part", (part // FLOAT,))]
+            self._call("join_bwd", [(F, ooc.R), (name + ".h", ooc.R), (name + ".stats", ooc.R)] + parts +
+                       ([(dH, ooc.R)] if dH else []) + [(dY, ooc.R)] + [(o, ooc.W) for o in outs],
+                       attrs + [int(dH is not None), slices])
+            out += [(X, dX), (F, dF)]
+            if "gate" in L:
+                out.append((L["gate"], dgate))
+            self._sgd(name)
+        elif op == "scan":
+            a, where = self._scan_parts(L, X)
+            slices, part = ooc.scan_slices("scan_bwd", a)
+            dX = self._decl(f"d:{X}@{name}", xs)
+            outs = [dX] + ([self._decl(f"d:{L['state']}@{name}", (a[0], a[2]))] if a[3] else [])
+            if part:
+                outs.append(self._decl(name + ".bpart", (part // FLOAT,)))
+            self._call("scan_bwd", [(X, ooc.R)] + where + [(name, ooc.R), (dY, ooc.R)] +
+                       [(o, ooc.W) for o in outs], a + [slices])
+            out.append((X, dX))
 
     # ------------------------------------------------------------ whole step
     def _lower(self):
@@ -465,7 +620,9 @@ class Net:
                "layernorm": self._fwd_layernorm, "gelu": self._fwd_gelu,
                "attention": self._fwd_attention, "concat": self._fwd_concat,
                "upsample": self._fwd_upsample, "rope": self._fwd_rope,
-               "qknorm": self._fwd_qknorm, "cross_attention": self._fwd_cross_attention}
+               "qknorm": self._fwd_qknorm, "cross_attention": self._fwd_cross_attention,
+               "span_attention": self._fwd_span_attention, "dropout": self._fwd_dropout,
+               "join": self._fwd_join, "scan": self._fwd_scan}
         for L in spec["layers"]:
             self.shape[L["name"]] = fwd[L["op"]](L, L["in"][0])
         logits = spec["logits"]
@@ -476,15 +633,17 @@ class Net:
         dlogits = self._decl("d:" + logits, ls)
         self._call("softmax_ce", [(logits, ooc.R), ("labels", ooc.R), ("loss", ooc.W),
                                   (dlogits, ooc.W)], [n, classes])
-        grads = {logits: dlogits}
+        grads = self.grads = {logits: dlogits}
         sums = {}
         visited = set()      # layers whose backward has been emitted
         for L in reversed(spec["layers"]):
             if L["name"] not in grads:
+                if L["name"] + ".h" in grads:
+                    raise ValueError(f"{L['name']}: nothing reads the join but its stream")
                 continue
             contributions = []
             self._bwd(L, grads[L["name"]], contributions)
-            visited.add(L["name"])
+            visited.update((L["name"], L["name"] + ".h"))
             for tensor, g in contributions:
                 if tensor in self.inputs:
                     continue

@@ -218,6 +218,62 @@ def seq2seq(batch=24, src_seq=512, seq=512, d=1024, heads=16, kv_heads=4, ffn=40
             "init": "normal", "optimizer": {"lr": lr, "momentum": momentum}}
 
 
+def packed(batch=24, seq=512, d=1024, heads=16, kv_heads=4, ffn=4096, layers=8, vocab=8192, p=0.1,
+           cap=30.0, lr=0.01, momentum=0.9):
+    """Decoder over documents packed into its sequences: blocks of a gated recurrence and of attention
+    in turn, each with a feed-forward block behind it.  The recurrence starts afresh where a document
+    does; attention sees a token's own document up to it, its scores capped and falling with distance
+    (no positions are added to them).  Each block's output joins the residual stream through a norm, a
+    gate and dropout, and the next norm's output is the next block's input; the feed-forward's hidden
+    values are dropped too.  Inputs beside the tokens: spans, fresh rows, mod, a seed and a scale."""
+    dh = d // heads
+    L = [{"name": "embed", "op": "embed", "in": ["x"], "vocab": vocab, "d": d},
+         {"name": "norm", "op": "layernorm", "in": ["embed"]}]
+    stream, prev, salt = "embed", "norm", 0
+
+    def lin(name, src, fin, fout):
+        L.append({"name": name, "op": "linear", "in": [src], "in_features": fin,
+                  "out_features": fout})
+        return name
+
+    def join(name, out):
+        nonlocal stream, prev, salt
+        salt += 1
+        L.append({"name": name, "op": "join", "in": [stream, out], "d": d, "p": p, "salt": salt,
+                  "seed": "seed", "scale": "scale"})
+        stream, prev = name + ".h", name
+
+    for i in range(layers):
+        b = f"b{i + 1}"
+        if i % 2 == 0:
+            L.append({"name": f"{b}.scan", "op": "scan", "in": [lin(f"{b}.fx", prev, d, 2 * d)],
+                      "fresh": "fresh"})
+            mixed = f"{b}.scan"
+        else:
+            q, kv = lin(f"{b}.q", prev, d, d), lin(f"{b}.kv", prev, d, 2 * kv_heads * dh)
+            L.append({"name": f"{b}.attn", "op": "span_attention", "in": [q, kv], "heads": heads,
+                      "kv_heads": kv_heads, "span": "span", "cap": cap > 0, "bias": True, "mod": "mod"})
+            mixed = f"{b}.attn"
+        join(f"{b}.join1", lin(f"{b}.out", mixed, d, d))
+        L.append({"name": f"{b}.gelu", "op": "gelu", "in": [lin(f"{b}.fc1", prev, d, ffn)]})
+        hidden = f"{b}.gelu"
+        if p:
+            salt += 1
+            L.append({"name": f"{b}.drop", "op": "dropout", "in": [hidden], "p": p, "salt": salt,
+                      "seed": "seed"})
+            hidden = f"{b}.drop"
+        join(f"{b}.join2", lin(f"{b}.fc2", hidden, ffn, d))
+    lin("head", prev, d, vocab)
+    inputs = [{"name": "span", "shape": [batch * seq, 3], "dtype": "i32"},
+              {"name": "fresh", "shape": [batch * seq], "dtype": "i32"},
+              {"name": "mod", "shape": [(cap > 0) + heads], "dtype": "f32"},
+              {"name": "seed", "shape": [2], "dtype": "i32"},
+              {"name": "scale", "shape": [1], "dtype": "f32"}]
+    return {"name": f"packed{layers}_d{d}_b{batch}_t{seq}", "input": [batch, seq], "inputs": inputs,
+            "tokens": True, "classes": vocab, "layers": L, "logits": "head", "init": "normal",
+            "cap": cap, "optimizer": {"lr": lr, "momentum": momentum}}
+
+
 def densenet(batch=64, hw=64, growth=32, blocks=(6, 12, 24, 16), stem=64, classes=10,
              lr=0.01, momentum=0.9):
     """DenseNet-shaped network (no bottleneck): inside a block every layer reads the channel
@@ -314,8 +370,8 @@ def unet(batch=8, hw=256, base=64, depth=4, classes=8, lr=0.01, momentum=0.9):
 
 
 #: The workloads: name -> (network description, budget as a fraction of the
-#: in-core peak).  seq2seq is an encoder-decoder transformer; densenet and unet
-#: are long-skip networks whose feature maps are read many times; the others are
+#: in-core peak).  seq2seq is an encoder-decoder transformer; packed is a decoder
+#: over packed documents; densenet and unet are long-skip networks whose feature maps are read many times; the others are
 #: the benchmark configurations.
 WORKLOADS = {
     "mlp": (lambda: mlp(), 0.40),
@@ -326,6 +382,7 @@ WORKLOADS = {
     "seq2seq": (lambda: seq2seq(), 0.20),
     "densenet": (lambda: densenet(), 0.25),
     "unet": (lambda: unet(), 0.25),
+    "packed": (lambda: packed(), 0.20),
 }
 
 
@@ -333,7 +390,7 @@ def workload(name, **overrides):
     """Network description of a named workload, with keyword overrides (e.g. ``batch=8``)."""
     builders = {"mlp": mlp, "cnn": plain_cnn, "resnet50_b256": resnet,
                 "resnet50_b1440": resnet, "transformer": transformer, "densenet": densenet,
-                "unet": unet, "seq2seq": seq2seq}
+                "unet": unet, "seq2seq": seq2seq, "packed": packed}
     defaults = {"resnet50_b256": {"batch": 256}, "resnet50_b1440": {"batch": 1440}}
     kw = dict(defaults.get(name, {}))
     kw.update(overrides)
@@ -363,6 +420,11 @@ def param_shapes(spec):
             out.append((L["name"] + ".pos", (length[L["in"][0]], L["d"])))
         elif L["op"] == "qknorm":
             out.append((L["name"] + ".gain", (2 if L["h2"] else 1, L["dh"])))
+        elif L["op"] == "join":
+            out.append((L["name"] + ".post", (L["d"],)))
+            if "gate" not in L:
+                out.append((L["name"] + ".gate", (1, L["d"])))
+            out.append((L["name"] + ".pre", (L["d"],)))
         elif L["op"] == "layernorm":
             out.append((L["name"] + ".gamma", (_width(spec, L),)))
             out.append((L["name"] + ".beta", (_width(spec, L),)))
@@ -400,16 +462,40 @@ def make_inputs(spec, seed=0):
 def make_extra_inputs(spec, tables=None, seed=2):
     """``{name: array}`` of ``spec["inputs"]``, by type and name: i32 of two axes are tokens, uniform
     over the vocabulary; i32 ``<tokens>_len`` their lengths, uniform over 1 .. the sequence; i32
-    ``*pos`` positions counting up in each sequence; f64 tables of angles, ``tables[name]`` or
+    ``*pos`` positions counting up in each sequence; i32 ``*fresh`` the first rows of some four documents
+    a sequence, i32 ``*span`` of three columns what each row sees of its own; i32 ``*seed`` two words; f32
+    ``*mod`` the network's cap, where it has one, then falling slopes; f32 ``*scale`` 1; f64 tables of angles, ``tables[name]`` or
     10000^(-2 i / rot) radians per position and magnitude 1; f32 standard normal.  Anything else is a
     ValueError."""
     g = np.random.Generator(np.random.PCG64(seed))
     shapes = {v["name"]: tuple(v["shape"]) for v in spec.get("inputs", ())}
     batch = spec["input"][0]
     out = {}
+
+    def first_rows(rows):
+        """Each row's document's first row, by sequence; the same for every input."""
+        T = rows // batch
+        cuts = np.random.Generator(np.random.PCG64([seed, rows])).integers(0, T, (batch, 3, 1))
+        at = np.arange(T)
+        return np.where(at >= cuts, cuts, 0).max(1), np.broadcast_to(at, (batch, T))
+
     for v in spec.get("inputs", ()):
         name, shape = v["name"], tuple(v["shape"])
-        if name in (tables or {}):
+        if v["dtype"] == "i32" and name.endswith("span") and shape[1:] == (3,) and shape[0] % batch == 0:
+            first, at = first_rows(shape[0])
+            out[name] = np.stack([first, at + 1, at], -1).reshape(shape).astype(np.int32)
+        elif v["dtype"] == "i32" and name.endswith("fresh") and len(shape) == 1 and shape[0] % batch == 0:
+            first, at = first_rows(shape[0])
+            out[name] = (first == at).astype(np.int32).reshape(shape)
+        elif v["dtype"] == "i32" and name.endswith("seed") and shape == (2,):
+            out[name] = g.integers(-2 ** 31, 2 ** 31, 2).astype(np.int32)
+        elif v["dtype"] == "f32" and name.endswith("mod") and len(shape) == 1:
+            cap = [spec["cap"]] if spec.get("cap") else []
+            n = shape[0] - len(cap)
+            out[name] = np.array(cap + [2.0 ** (-8.0 * (h + 1) / n) for h in range(n)], np.float32)
+        elif v["dtype"] == "f32" and name.endswith("scale") and shape == (1,):
+            out[name] = np.ones(1, np.float32)
+        elif name in (tables or {}):
             out[name] = np.asarray(tables[name], np.float64).reshape(shape)
         elif v["dtype"] == "f64":
             half = shape[0] - 1
@@ -441,7 +527,7 @@ def make_params(spec, seed=1):
             fan_in = int(np.prod(shape[1:]))
             std = np.float32(np.sqrt(2.0 / fan_in))
             params[name] = (g.standard_normal(size=shape, dtype=np.float32) * std).astype(np.float32)
-        elif kind in ("gamma", "gain"):
+        elif kind in ("gamma", "gain", "post", "gate", "pre"):
             params[name] = np.ones(shape, np.float32)
         else:  # bias or beta
             params[name] = np.zeros(shape, np.float32)

@@ -6,9 +6,11 @@ import ctypes as C
 import numpy as np
 import pytest
 
+import bench
 import decoder_util as du
 from oracle import ops
-from paper_2010_14109_amd import ooc
+from oracle.lower import lower
+from paper_2010_14109_amd import netdef, ooc, synth
 from test_attention_ops_host import difference
 
 R, W, RW = ooc.R, ooc.W, ooc.RW
@@ -258,3 +260,137 @@ def test_span_attention_refusals(lib, cap, bias, slices):
          shape + [cap, bias, sq, sk], bad + [(8, 8), (9, 0), (9, 11)])
     assert ooc.attention_slices("span_attention_fwd", shape) == ooc.attention_slices("cross_attention_fwd", shape)
     assert ooc.attention_slices("span_attention_bwd", shape) == ooc.attention_slices("cross_attention_bwd", shape)
+
+
+# ---------------------------------------------------------------- networks
+def small_packed(**kw):
+    args = dict(batch=2, seq=11, d=24, heads=4, kv_heads=2, ffn=20, layers=2, vocab=13, p=0.2, cap=2.0)
+    args.update(kw)
+    return synth.packed(**args)
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("kw", [{}, dict(p=0.0, cap=0.0, layers=3), dict(batch=1, seq=1), dict(batch=1, seq=700)],
+                         ids=str)
+def test_sequence_matches_the_oracle(lib, kw, keep):
+    spec = small_packed(**kw)
+    mine = netdef.Net(spec, keep_grads=keep)
+    ref = lower(spec, keep_grads=keep, slices=mine.slices)
+    assert mine.names == [v["name"] for v in ref["vars"]]
+    assert mine.var_bytes == [v["bytes"] for v in ref["vars"]]
+    assert mine.var_kinds == [v["kind"] for v in ref["vars"]]
+    opname = {"add_fwd": "add", "add_grad": "add", "acc_grad": "acc"}
+    assert mine.fn_ops == [opname.get(f["op"], f["op"]) for f in ref["fns"]]
+    assert mine.fn_vars == [f["vars"] for f in ref["fns"]]
+    ctx = ooc.Context(-1)
+    mine.register(ctx)
+    ctx.build_schedule()
+    ctx.close()
+
+
+def gated_and_carried():
+    """A network with what ``packed`` leaves out: a gate from another layer, states handed in."""
+    spec = small_packed(layers=1)
+    for L in spec["layers"]:
+        if L["op"] == "scan":
+            L["state"] = "state"
+        if L["name"] == "b1.join2":
+            L["gate"] = "gates"
+    i = next(i for i, L in enumerate(spec["layers"]) if L["name"] == "b1.join2")
+    spec["layers"].insert(i, {"name": "gates", "op": "linear", "in": ["cond"], "in_features": 3,
+                              "out_features": 24})
+    spec["inputs"] += [{"name": "state", "shape": [2, 24], "dtype": "f32"},
+                       {"name": "cond", "shape": [2, 3], "dtype": "f32"}]
+    return spec
+
+
+@pytest.mark.parametrize("build", [lambda: small_packed(), gated_and_carried], ids=["packed", "gated"])
+def test_oracle_gradients_by_differences(lib, build):
+    """The wiring: the loss's change along a direction of every parameter is the gradients'."""
+    from oracle.interp import run
+    spec = build()
+    mine = netdef.Net(spec, keep_grads=True)
+    reg = lower(spec, keep_grads=True, slices=mine.slices)
+    assert mine.names == [v["name"] for v in reg["vars"]]
+    x, labels = synth.make_inputs(spec, 0)
+    extra = synth.make_extra_inputs(spec)
+    g = np.random.default_rng(4)
+    shapes = {n: mine.meta[n][0] for n in mine.param_names()}
+    start = synth.make_params(spec, 1)
+    assert {n: v.shape for n, v in start.items()} == shapes
+    params = {n: start[n].astype(np.float64) + 0.3 * g.standard_normal(s) for n, s in shapes.items()}
+    out = run(reg, x, labels, params, inputs=extra)
+    for name in params:
+        v = g.standard_normal(params[name].shape)
+
+        def loss(t):
+            return run(reg, x, labels, dict(params, **{name: params[name] + t * v}),
+                       inputs=extra)["loss"][-1]
+        num = (loss(1e-5) - loss(-1e-5)) / 2e-5
+        assert np.isclose(num, (out["d:" + name] * v).sum(), rtol=1e-4, atol=1e-8), name
+
+
+def test_wrong_descriptions_are_refused():
+    def broken(change, inputs=None):
+        spec = small_packed()
+        for L in spec["layers"]:
+            change(L)
+        for v in spec["inputs"]:
+            if inputs and v["name"] in inputs:
+                v.update(inputs[v["name"]])
+        return spec
+
+    def of(op, **kw):
+        return lambda L: L.update(kw) if L["op"] == op else None
+
+    def nothing(L):
+        pass
+    for change, inputs, what in (
+            (of("span_attention", span="fresh"), None, "must be an input"),
+            (of("span_attention", span="embed"), None, "must be an input"),
+            (of("span_attention", mod="scale"), None, "must be an input"),
+            (of("span_attention", kv_heads=4), None, "widths"),
+            (of("span_attention", cap=False), None, "must be an input"),
+            (of("scan", fresh="span"), None, "must be an input"),
+            (of("scan", state="mod"), None, "must be an input"),
+            (of("dropout", p=1.0), None, "p must lie"), (of("dropout", p=-0.1), None, "p must lie"),
+            (of("dropout", p=0.0), None, "nothing is dropped"),
+            (of("dropout", seed="scale"), None, "must be an input"),
+            (of("join", p=1.0), None, "p must lie"), (of("join", scale="mod"), None, "must be an input"),
+            (of("join", gate="mod"), None, "gate"), (of("join", gate="b1.fx"), None, "gate"),
+            (lambda L: L.update({"in": [L["in"][0], "b1.fx"]}) if L["op"] == "join" else None, None, "shape"),
+            (nothing, {"seed": {"dtype": "f32"}}, "must be an input"),
+            (nothing, {"fresh": {"shape": [21]}}, "must be an input"),
+            (nothing, {"span": {"shape": [22, 2]}}, "must be an input")):
+        with pytest.raises(ValueError, match=what):
+            netdef.Net(broken(change, inputs))
+    spec = small_packed(layers=1)
+    spec["logits"] = "head2"
+    spec["layers"].append({"name": "head2", "op": "linear", "in": ["b1.join2.h"], "in_features": 24,
+                           "out_features": 13})
+    with pytest.raises(ValueError, match="but its stream"):
+        netdef.Net(spec)
+
+
+def test_extra_inputs_and_the_benchmark_s_work(lib):
+    spec = small_packed(batch=3, seq=40)
+    e = synth.make_extra_inputs(spec)
+    span, fresh = e["span"].reshape(3, 40, 3), e["fresh"].reshape(3, 40)
+    assert fresh[:, 0].all() and 3 <= fresh.sum() <= 12
+    for b in range(3):
+        start = 0
+        for t in range(40):
+            start = t if fresh[b, t] else start
+            assert span[b, t].tolist() == [start, t + 1, t]
+    assert e["mod"][0] == 2 and len(e["mod"]) == 5 and (np.diff(e["mod"][1:]) < 0).all()
+    assert e["seed"].dtype == np.int32 and e["scale"].tolist() == [1.0]
+    net = netdef.Net(spec)
+    table = bench.kernel_table(net, [1.0] * len(net.fn_ops), e)
+    pairs = int((span[..., 1] - span[..., 0]).sum())
+    assert table["span_attention_fwd"]["work"] == 4 * 4 * pairs * 6
+    assert table["span_attention_bwd"]["work"] == 10 * 4 * pairs * 6
+    rows = 120
+    assert table["dropout"]["work"] == 4 * 8 * rows * 20 and table["join_fwd"]["work"] == 4 * 16 * rows * 24
+    assert table["join_bwd"]["work"] == (3 * 24 + 20) * rows * 24
+    assert table["scan_fwd"]["work"] == 12 * rows * 24 and table["scan_bwd"]["work"] == 24 * rows * 24
+    assert "fp16" in bench.roofline(table["span_attention_bwd"], "span_attention_bwd")["peak_of"]
