@@ -470,7 +470,8 @@ ooc_status ooc_attention_slices(int32_t op, const int64_t* attrs, int32_t n_attr
     return OOC_E_INVALID;
   }
   const AttendShape a{attrs[0], attrs[1], attrs[2], attrs[3], attrs[4], attrs[5]};
-  slices[0] = attention_key_slices(a, fwd);
+  const bool spans = op == OOC_OP_SPAN_ATTENTION_FWD || op == OOC_OP_SPAN_ATTENTION_BWD;
+  slices[0] = attention_key_slices(a, fwd, spans);
   slices[1] = fwd ? 1 : attention_query_slices(a);
   *part_bytes = (uint64_t)attention_part_bytes(fwd, attrs, slices);
   return OOC_OK;

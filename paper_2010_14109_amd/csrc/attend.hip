@@ -4,14 +4,16 @@
 
 namespace ooc {
 
-int64_t attention_key_slices(const AttendShape& a, bool fwd) {
+int64_t attention_key_slices(const AttendShape& a, bool fwd, bool spans) {
   if (fwd && few_rows(a))
     return slices_for(a.B * a.Hkv, ceil_div(a.Tk, 32 * kFewWaves), kFewWant, 1);
-  const int64_t tiles = ceil_div(a.Tq * (a.H / a.Hkv), fwd ? fwd_columns(a) : back_columns(a.dh));
-  return slices_for(a.B * a.Hkv * tiles, ceil_div(a.Tk, fwd ? tile_rows(a.dh) : back_rows(a.dh)));
+  const int64_t tiles = ceil_div(a.Tq * (a.H / a.Hkv), fwd ? fwd_columns(a, spans) : back_columns(a.dh));
+  return slices_for(a.B * a.Hkv * tiles, ceil_div(a.Tk, fwd ? tile_rows(a.dh) : back_rows(a.dh)),
+                    spans && fwd && a.dh <= 64 ? kSpanWant : kWant);
 }
 int64_t attention_query_slices(const AttendShape& a) {
-  return slices_for(a.B * a.Hkv * ceil_div(a.Tk, back_columns(a.dh)), ceil_div(a.Tq * (a.H / a.Hkv), back_rows(a.dh)));
+  return slices_for(a.B * a.Hkv * ceil_div(a.Tk, back_columns(a.dh)),
+                    ceil_div(a.Tq * (a.H / a.Hkv), back_rows(a.dh)));
 }
 
 hipError_t cross_attention_fwd(const float* q, const float* kv, const int32_t* klen, float* y,

@@ -54,7 +54,7 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint32_t kNone = 0x80000000u;   // past the length of every descriptor
-constexpr uint32_t kXcds = 8;
+constexpr uint32_t kXcds = 8, kCus = 256;
 
 // A width of head columns, padded to DH: a piece's row is DH / 8 chunks of 16 bytes in kRow bytes.
 // The odd number of chunks a row is long spreads the 16 rows of 256 bytes' worth of row reads over
@@ -285,6 +285,7 @@ struct Shape {
   int R;                // G Tq
   int64_t ldq, ldk;     // H dh, 2 Hkv dh
   float scale;          // 1 / sqrt(dh)
+  bool flat;            // see Place
 };
 __device__ inline int64_t query_row(const Shape& s, int b, int hk, int r) {
   const int g = r / s.Tq, i = r - g * s.Tq;
@@ -386,10 +387,20 @@ struct Place {
   int b, hk, tile, slice;
   bool none;
 };
+// Fewer than kFlatPairs of them (Shape::flat) would leave dies without work: theirs take turns, tile by
+// tile.  LAST_FIRST: from the last tile of columns on, which under causal spans has the most to do.
+template <bool LAST_FIRST>
 __device__ inline Place place(const Shape& s, int tiles) {
   const uint32_t pairs = (uint32_t)s.B * s.Hkv, id = blockIdx.x;
+  if (s.flat) {
+    const uint32_t rank = id / kCus % 2 && id / kCus * kCus + kCus <= gridDim.x ? (id / kCus * 2 + 1) * kCus - 1 - id : id;
+    const uint32_t pair = rank % pairs, t = rank / pairs, heads = tiles % s.G ? 1 : s.G;
+    const int tile = LAST_FIRST ? (int)(t % heads * (tiles / heads) + tiles / heads - 1 - t / heads) : (int)t;
+    return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), tile, (int)blockIdx.y, false};
+  }
   const uint32_t idx = id / kXcds, pair = idx / tiles * kXcds + id % kXcds;
-  return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), (int)(idx % tiles), (int)blockIdx.y, pair >= pairs};
+  const int tile = LAST_FIRST ? tiles - 1 - (int)(idx % tiles) : (int)(idx % tiles);
+  return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), tile, (int)blockIdx.y, pair >= pairs};
 }
 
 // Sum t of a lane holds, in r, head column 32 (first + t) + 8 (r / 4) + 4 half + r % 4 of its column.
@@ -729,7 +740,7 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
   __shared__ floatx2 tops[W];
-  const Place at = place(s, tiles);
+  const Place at = place<V::kSpan>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int col0 = at.tile * Forward<DH, WIDE>::kCols + w / Wd::kParts * 32 * C + (lane & 31);
@@ -924,7 +935,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
   const auto ys = [&](int wave, int r, int d) -> float* {
     return reinterpret_cast<float*>(mine[wave]) + r * kYs + d;
   };
-  const Place at = place(s, tiles);
+  const Place at = place<V::kSpan>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, quarter = lane >> 4, l16 = lane & 15;
   int k0, k1;
@@ -1194,6 +1205,11 @@ struct RowSeen {   // what a row of the tile sees
   int lo, len;
   float at, slope;
 };
+template <int T>
+struct RowsOf {   // the same of all its rows
+  int lo[T], len[T];
+  float at[T], slope[T];
+};
 struct QueryTiles {
   const float *q, *dy, *lse, *delta;   // lse, delta: of the group's first head
   int b, hk, i1, T;
@@ -1262,20 +1278,30 @@ __device__ inline void leave_bounds(const Spans& v, const Shape& s, const Place&
     reinterpret_cast<int2*>(v.bounds)[(int64_t)at.b * blocks + first / kBoundRows] = make_int2(lo, hi);
 }
 
-// The rows of a tile from a column's place, state j: their scores with what their spans change.
+// The rows of a tile from a column's place, state j: what sees it, and their scores' bias.
+template <int T>
 struct RowsSeen {
-  const RowSeen* rows;   // in LDS
-  int j, first;          // the column; the wave's first
+  const RowsOf<T>* rows;   // in LDS
+  int j, first;            // the column; the wave's first
   // bit 0: a row of r0 .. r0 + 31 sees a column of the wave, bit 1: all see all
   __device__ int look(int r0) const {
-    const RowSeen& r = rows[r0 + (int)(threadIdx.x & 31)];
-    const int hi = r.lo + r.len;
-    return (__any(r.len && r.lo < first + 32 && hi > first) ? 1 : 0) |
-           (__all(r.lo <= first && hi >= first + 32) ? 2 : 0);
+    const int r = r0 + (int)(threadIdx.x & 31), lo = rows->lo[r], hi = lo + rows->len[r];
+    return (__any(lo < hi && lo < first + 32 && hi > first) ? 1 : 0) |
+           (__all(lo <= first && hi >= first + 32) ? 2 : 0);
   }
-  __device__ bool sees(int r) const { return (uint32_t)(j - rows[r].lo) < (uint32_t)rows[r].len; }
-  __device__ float bias(float z, int r) const {
-    return fmaf(-rows[r].slope, fabsf(rows[r].at - (float)j), z);
+  __device__ bool sees(int r) const { return (uint32_t)(j - rows->lo[r]) < (uint32_t)rows->len[r]; }
+  // of rows r .. r + 3 (r a multiple of 4)
+  __device__ void see(int r, bool (&x)[4]) const {
+    const int4 lo = *reinterpret_cast<const int4*>(rows->lo + r), len = *reinterpret_cast<const int4*>(rows->len + r);
+    x[0] = (uint32_t)(j - lo.x) < (uint32_t)len.x;
+    x[1] = (uint32_t)(j - lo.y) < (uint32_t)len.y;
+    x[2] = (uint32_t)(j - lo.z) < (uint32_t)len.z;
+    x[3] = (uint32_t)(j - lo.w) < (uint32_t)len.w;
+  }
+  __device__ void bias(int r, float (&z)[4]) const {
+    const float4 at = at4(rows->at, r), slope = at4(rows->slope, r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z[k] = fmaf(-pick(slope, k), fabsf(pick(at, k) - (float)j), z[k]);
   }
   // whether one of the rows of `bits` from r0 on, which are not finite, sees the column
   __device__ bool odd(uint32_t bits, int r0) const {
@@ -1284,6 +1310,19 @@ struct RowsSeen {
     return x;
   }
 };
+
+// Scores of rows r .. r + 3, of group g of a's, with what spans change; curve: what the cap multiplies
+// gradients by.
+template <class Rows>
+__device__ inline void shape_states(float (&z)[4], float (&curve)[4], const floatx16& a, int g, float c,
+                                    const Cap& cap, const Spans& v, const Rows& rows, int r) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) z[k] = a[4 * g + k] * c;
+  if (v.cap)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z[k] = cap.apply<true>(z[k], curve[k]);
+  if (v.bias) rows.bias(r, z);
+}
 
 // Up to 64 head columns a wave holds both matrices of its columns and all its sums: four waves a
 // workgroup, two workgroups a CU.
@@ -1307,10 +1346,10 @@ template <int W, int T, int B>
 struct States<W, T, Spans, B> {
   Cap cap;
   int j, first;
-  RowSeen* rows;
+  RowsOf<T>* rows;
   uint32_t* odd_bits;
   __device__ States(const Spans& v, const Shape&, const Place&, int j) : cap(v), j(j) {
-    __shared__ RowSeen seen[B * T];
+    __shared__ __attribute__((aligned(16))) RowsOf<T> seen[B];
     __shared__ uint32_t odd[4];
     rows = seen;
     odd_bits = odd;
@@ -1321,8 +1360,13 @@ struct States<W, T, Spans, B> {
   __device__ bool any(int) const { return true; }
   __device__ bool bad() const { return false; }
   __device__ bool live(int) const { return true; }
-  __device__ void put(const RowSeen& r, int buf) const { rows[buf * T + threadIdx.x] = r; }
-  __device__ RowsSeen at(int buf) const { return {rows + buf * T, j, first}; }
+  __device__ void put(const RowSeen& r, int buf) const {
+    rows[buf].lo[threadIdx.x] = r.lo;
+    rows[buf].len[threadIdx.x] = r.len;
+    rows[buf].at[threadIdx.x] = r.at;
+    rows[buf].slope[threadIdx.x] = r.slope;
+  }
+  __device__ RowsSeen<T> at(int buf) const { return {rows + buf, j, first}; }
   __device__ uint32_t* odd_rows(int turn) const { return odd_bits + 2 * turn; }
   __device__ void clear(int turn) const {
     if (threadIdx.x < 2) odd_bits[2 * turn + threadIdx.x] = 0;
@@ -1341,7 +1385,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dq_kernel(
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
   __shared__ floatx2 tops[W];
-  const Place at = place(s, tiles);
+  const Place at = place<V::kSpan>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int col = (at.tile * W + w) * 32 + (lane & 31), here = min(col, s.R - 1);
@@ -1452,7 +1496,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
   __shared__ __attribute__((aligned(16))) char gs[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) float nl[T], dl[T];
   __shared__ floatx2 tops[W];
-  const Place at = place(s, tiles);
+  const Place at = place<false>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int j = (at.tile * W + w) * 32 + (lane & 31);
@@ -1528,23 +1572,30 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
       for (int g = 0; g < 4; ++g) {
         const int row = r0 + 8 * g + 4 * half;
         const float4 l4 = at4(nl, row), d4 = at4(dl, row);
+        [[maybe_unused]] float z[4], curve[4];
+        if constexpr (V::kSpan) shape_states(z, curve, a, g, c, states.cap, view, states.at(0), row);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          if constexpr (V::kSpan) {
-            float curve = 1.f, z = a[4 * g + k] * c;
-            if (view.cap) z = states.cap.template apply<true>(z, curve);
-            if (view.bias) z = states.at(0).bias(z, row + k);
-            p[4 * g + k] = __builtin_amdgcn_exp2f(z + pick(l4, k));
-            x[4 * g + k] = p[4 * g + k] * fmaf(b[4 * g + k], cv, -pick(d4, k)) * curve;
-            if (!(seen & 2)) {
-              const bool sees = states.at(0).sees(row + k);
-              p[4 * g + k] = sees ? p[4 * g + k] : 0.f;
-              x[4 * g + k] = sees ? x[4 * g + k] : 0.f;
+          if constexpr (V::kSpan) p[4 * g + k] = __builtin_amdgcn_exp2f(z[k] + pick(l4, k));
+          else p[4 * g + k] = __builtin_amdgcn_exp2f(fmaf(a[4 * g + k], c, pick(l4, k)));
+          x[4 * g + k] = p[4 * g + k] * fmaf(b[4 * g + k], cv, -pick(d4, k));
+        }
+        if constexpr (V::kSpan) {
+          if (view.cap)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[4 * g + k] *= curve[k];
+          if (!(seen & 2)) {
+            bool sees[4];
+            states.at(0).see(row, sees);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              p[4 * g + k] = sees[k] ? p[4 * g + k] : 0.f;
+              x[4 * g + k] = sees[k] ? x[4 * g + k] : 0.f;
             }
-          } else {
-            p[4 * g + k] = __builtin_amdgcn_exp2f(fmaf(a[4 * g + k], c, pick(l4, k)));
-            x[4 * g + k] = p[4 * g + k] * fmaf(b[4 * g + k], cv, -pick(d4, k));
           }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
           ptop = fmaxf(ptop, p[4 * g + k]);
           xtop = fmaxf(xtop, fabsf(x[4 * g + k]));
         }
@@ -1603,7 +1654,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   __shared__ __attribute__((aligned(16))) char mats[NB][2][Rw::kBytes];   // tiles of k and v
   __shared__ float4 meet[kPairs][2][2][64];
   __shared__ floatx2 tops[W];
-  const Place at = place(s, tiles);
+  const Place at = place<V::kSpan>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
@@ -1761,7 +1812,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   __shared__ __attribute__((aligned(16))) float nl[NB][T], dl[NB][T];
   __shared__ float4 meet[kPairs][4][64];
   __shared__ floatx2 tops[W];
-  const Place at = place(s, tiles);
+  const Place at = place<false>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
@@ -1842,19 +1893,23 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
         const float4 r4 = at4(role ? dl[buf] : nl[buf], 8 * g + 4 * half);
         if (!role) {
           if constexpr (V::kSpan) {
-            float x[4];   // what role 1 multiplies: the cap's factor comes with it
+            float z[4], curve[4];
+            const int r = 8 * g + 4 * half;
+            shape_states(z, curve, a, g, c, states.cap, view, states.at(buf), r);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int r = 8 * g + 4 * half + k;
-              float curve = 1.f, z = a[4 * g + k] * c;
-              if (view.cap) z = states.cap.template apply<true>(z, curve);
-              if (view.bias) z = states.at(buf).bias(z, r);
-              z = __builtin_amdgcn_exp2f(z + pick(r4, k));
-              if (!(seen & 2)) z = states.at(buf).sees(r) ? z : 0.f;
-              v[4 * g + k] = z;
-              x[k] = z * curve;
+            for (int k = 0; k < 4; ++k) z[k] = __builtin_amdgcn_exp2f(z[k] + pick(r4, k));
+            if (!(seen & 2)) {
+              bool sees[4];
+              states.at(buf).see(r, sees);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) z[k] = sees[k] ? z[k] : 0.f;
             }
-            meet[pair][g][lane] = make_float4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[4 * g + k] = z[k];
+            if (view.cap)   // role 1 multiplies by it
+#pragma unroll
+              for (int k = 0; k < 4; ++k) z[k] *= curve[k];
+            meet[pair][g][lane] = make_float4(z[0], z[1], z[2], z[3]);
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -1927,7 +1982,8 @@ __global__ void sum_kernel(const float* __restrict__ part, float* __restrict__ o
 }
 
 // ---------------------------------------------------------------- launches
-Shape shape_of(const AttendShape& a) {
+constexpr int64_t kFlatPairs = 32;
+Shape shape_of(const AttendShape& a, bool spans) {
   Shape s;
   s.B = (int)a.B; s.Tq = (int)a.Tq; s.Tk = (int)a.Tk; s.H = (int)a.H; s.Hkv = (int)a.Hkv;
   s.G = (int)(a.H / a.Hkv);
@@ -1936,6 +1992,7 @@ Shape shape_of(const AttendShape& a) {
   s.ldq = a.H * a.dh;
   s.ldk = 2 * a.Hkv * a.dh;
   s.scale = 1.f / sqrtf((float)a.dh);
+  s.flat = spans && a.B * a.Hkv < kFlatPairs;
   return s;
 }
 
@@ -1946,18 +2003,20 @@ int back_columns(int64_t dh) {
 int back_rows(int64_t dh) { return dh <= 64 ? Width<64>::kBackRows : Width<128>::kBackRows; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 dim3 grid_of(const Shape& s, int tiles, int64_t slices) {
-  return dim3((unsigned)(ceil_div((int64_t)s.B * s.Hkv, kXcds) * kXcds * tiles), (unsigned)slices);
+  const int64_t pairs = (int64_t)s.B * s.Hkv;
+  return dim3((unsigned)((s.flat ? pairs : ceil_div(pairs, kXcds) * kXcds) * tiles), (unsigned)slices);
 }
 // Whether the forward's workgroups have 256 columns, not 128: where that leaves less than a tenth
 // more columns idle, which is what the wide ones gain (4096 x 4096: 0.86 against 0.96 ms at 2 x 16
 // heads of 128, 0.89 against 0.98 at 4 x 16 heads of 64; 333 queries, 12 heads of 85: 81 us wide,
 // 60 narrow), and there are two of them for each CU (77 states, 2 x 4096 queries, 8 heads of 64:
 // 18.1 us wide, 16.8 narrow).
-bool wide(const AttendShape& a) {
+bool wide(const AttendShape& a, bool spans) {
+  if (spans && a.dh <= 64) return false;
   const int64_t halves = ceil_div(a.Tq * (a.H / a.Hkv), 128);
   return a.dh <= 128 && (halves % 2 == 0 || halves >= 10) && a.B * a.Hkv * ceil_div(halves, 2) >= 512;
 }
-int fwd_columns(const AttendShape& a) { return wide(a) ? 256 : a.dh <= 128 ? 128 : 64; }
+int fwd_columns(const AttendShape& a, bool spans) { return wide(a, spans) ? 256 : a.dh <= 128 ? 128 : 64; }
 unsigned flat_grid(int64_t n) { return (unsigned)std::min<int64_t>(ceil_div(n, 256), 4096); }
 int64_t slice_of(int64_t n, int64_t slices, int64_t tile) {
   return ceil_div(ceil_div(n, slices), tile) * tile;
@@ -1965,6 +2024,9 @@ int64_t slice_of(int64_t n, int64_t slices, int64_t tile) {
 
 // Workgroups to aim for, and the fewest tiles a slice is worth cutting off for.
 constexpr int64_t kWant = 512, kFewWant = 256, kMinTiles = 2;
+// The forward of spans up to 64 head columns: 512 workgroups are all there at once, and the time is that
+// of the one that sees most (8192 causal queries, 8 heads of 64 on 2: 400 us, 322 in two slices).
+constexpr int64_t kSpanWant = 768;
 int64_t slices_for(int64_t groups, int64_t tiles, int64_t want = kWant, int64_t least = kMinTiles) {
   if (groups >= want) return 1;
   return std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, groups), tiles / least,
@@ -2003,9 +2065,9 @@ bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows &&
 template <class V>
 hipError_t attend_fwd(const float* q, const float* kv, const V& view, float* y, float* lse, float* part,
                       const AttendShape& a, int64_t slices, hipStream_t st) {
-  const Shape s = shape_of(a);
+  const Shape s = shape_of(a, V::kSpan);
   const bool few = few_rows(a);
-  const int tiles = few ? 1 : (int)ceil_div(s.R, fwd_columns(a));
+  const int tiles = few ? 1 : (int)ceil_div(s.R, fwd_columns(a, V::kSpan));
   const int len = (int)slice_of(s.Tk, slices, few ? 32 : tile_rows(s.dh));
   const int64_t size = a.B * a.Tq * s.ldq, rows = a.B * a.H * a.Tq;
   float* yo = slices > 1 ? part : y;
@@ -2016,7 +2078,7 @@ hipError_t attend_fwd(const float* q, const float* kv, const V& view, float* y, 
 #define FWD(D, X) LAUNCH((fwd_kernel<D, X, false, V>), (Forward<D, false>::kWaves), tiles, slices, ARGS)
   if (few) {
     TO_128(FEW);
-  } else if (wide(a)) {
+  } else if (wide(a, V::kSpan)) {
     TO_128(WIDE);
   } else if (s.dh <= 128) {
     TO_128(FWD);
@@ -2038,7 +2100,7 @@ template <class V>
 hipError_t attend_bwd(const float* q, const float* kv, const V& view, const float* y, const float* lse,
                       const float* dy, float* dq, float* dkv, float* delta, float* part,
                       const AttendShape& a, int64_t q_slices, int64_t kv_slices, hipStream_t st) {
-  const Shape s = shape_of(a);
+  const Shape s = shape_of(a, V::kSpan);
   const int64_t q_size = a.B * a.Tq * s.ldq, kv_size = a.B * a.Tk * s.ldk;
   {
     const int tiles = (int)ceil_div(s.R, back_columns(s.dh));

@@ -153,7 +153,7 @@ hipError_t span_attention_bwd(const float* q, const float* kv, const int32_t* sp
                               hipStream_t s);
 // Slice counts the launchers run best with: of the keys for a pass over query rows (forward, dq),
 // of the query rows for the pass over keys (dkv).
-int64_t attention_key_slices(const AttendShape& a, bool fwd);
+int64_t attention_key_slices(const AttendShape& a, bool fwd, bool spans);
 int64_t attention_query_slices(const AttendShape& a);
 
 // Dropout and the join of a block with its residual stream (block.hip).  drop: of 2^32; seed null iff
