@@ -248,10 +248,21 @@ struct Seen {
   }
 };
 // the smallest and the largest of a wave's values, the same in every lane
+template <int CTRL>
+__device__ inline int dpp(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true);
+}
 __device__ inline int wave_least(int x) {
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) x = min(x, __shfl_xor(x, s, 64));
-  return __builtin_amdgcn_readfirstlane(x);
+  x = min(x, dpp<0xb1>(x));    // quad_perm 1 0 3 2
+  x = min(x, dpp<0x4e>(x));    // quad_perm 2 3 0 1
+  x = min(x, dpp<0x141>(x));   // mirrored within 8
+  x = min(x, dpp<0x140>(x));   // mirrored within 16
+  const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+  const uint32_t a = r[0], b = r[1];
+  x = min((int)a, (int)b);
+  const auto t = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+  const uint32_t c = t[0], d = t[1];
+  return __builtin_amdgcn_readfirstlane(min((int)c, (int)d));
 }
 __device__ inline int wave_most(int x) { return -wave_least(-x); }
 
@@ -285,7 +296,6 @@ struct Shape {
   int R;                // G Tq
   int64_t ldq, ldk;     // H dh, 2 Hkv dh
   float scale;          // 1 / sqrt(dh)
-  bool flat;            // see Place
 };
 __device__ inline int64_t query_row(const Shape& s, int b, int hk, int r) {
   const int g = r / s.Tq, i = r - g * s.Tq;
@@ -387,20 +397,25 @@ struct Place {
   int b, hk, tile, slice;
   bool none;
 };
-// Fewer than kFlatPairs of them (Shape::flat) would leave dies without work: theirs take turns, tile by
-// tile.  LAST_FIRST: from the last tile of columns on, which under causal spans has the most to do.
-template <bool LAST_FIRST>
+template <class V, bool LAST_FIRST, bool FOLD>
 __device__ inline Place place(const Shape& s, int tiles) {
   const uint32_t pairs = (uint32_t)s.B * s.Hkv, id = blockIdx.x;
-  if (s.flat) {
-    const uint32_t rank = id / kCus % 2 && id / kCus * kCus + kCus <= gridDim.x ? (id / kCus * 2 + 1) * kCus - 1 - id : id;
-    const uint32_t pair = rank % pairs, t = rank / pairs, heads = tiles % s.G ? 1 : s.G;
+  if constexpr (V::kSpan) {
+    // Workgroups differ in what they see, the most under causal spans: the last tiles of queries, the
+    // first of states (LAST_FIRST: from the last tile on).  They start by that, tiles before pairs, so
+    // that short ones fill in at the end (24 x 512 causal, 16 heads of 64, with gradients: 406 us pair by
+    // pair, 325 so; where all see all, 468 and 480).  FOLD, where a CU holds two at a time: every second
+    // round of CUs backwards, as two that start together stay together (8192 causal, 8 heads of 64 on 2,
+    // with gradients: 1.60 ms unfolded, 1.48; where a CU holds one, 2.2 ms became 2.7).
+    const uint32_t at = blockIdx.y * gridDim.x + id, round = at / kCus, last = gridDim.x * gridDim.y;
+    const uint32_t rank = FOLD && round % 2 && (round + 1) * kCus <= last ? (2 * round + 1) * kCus - 1 - at : at;
+    const uint32_t slice = rank / gridDim.x, idx = rank % gridDim.x;
+    const uint32_t pair = idx % pairs, t = idx / pairs, heads = tiles % s.G ? 1 : s.G;
     const int tile = LAST_FIRST ? (int)(t % heads * (tiles / heads) + tiles / heads - 1 - t / heads) : (int)t;
-    return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), tile, (int)blockIdx.y, false};
+    return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), tile, (int)slice, false};
   }
   const uint32_t idx = id / kXcds, pair = idx / tiles * kXcds + id % kXcds;
-  const int tile = LAST_FIRST ? tiles - 1 - (int)(idx % tiles) : (int)(idx % tiles);
-  return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), tile, (int)blockIdx.y, pair >= pairs};
+  return {(int)(pair / s.Hkv), (int)(pair % s.Hkv), (int)(idx % tiles), (int)blockIdx.y, pair >= pairs};
 }
 
 // Sum t of a lane holds, in r, head column 32 (first + t) + 8 (r / 4) + 4 half + r % 4 of its column.
@@ -731,7 +746,7 @@ struct Forward {
   static constexpr int kCols = 32 * kWaves * kSets / Width<DH>::kParts;
 };
 template <int DH, bool EXACT, bool WIDE, class V>
-__global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1) void fwd_kernel(
+__global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), V::kSpan && DH <= 64 ? 3 : DH <= 128 ? 2 : 1) void fwd_kernel(
     const float* __restrict__ q, const float* __restrict__ kv, V view, float* __restrict__ y, float* __restrict__ lse, Shape s, int tiles, int slice_len,
     int64_t y_slice, int64_t lse_slice) {
   using Wd = Width<DH>;
@@ -740,7 +755,7 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), DH <= 128 ? 2 : 1
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
   __shared__ floatx2 tops[W];
-  const Place at = place<V::kSpan>(s, tiles);
+  const Place at = place<V, true, (DH <= 64)>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int col0 = at.tile * Forward<DH, WIDE>::kCols + w / Wd::kParts * 32 * C + (lane & 31);
@@ -935,7 +950,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
   const auto ys = [&](int wave, int r, int d) -> float* {
     return reinterpret_cast<float*>(mine[wave]) + r * kYs + d;
   };
-  const Place at = place<V::kSpan>(s, tiles);
+  const Place at = place<V, true, (DH <= 64)>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, quarter = lane >> 4, l16 = lane & 15;
   int k0, k1;
@@ -1201,10 +1216,11 @@ __device__ inline float both(float f, float g) { return fminf(f * g, 0x1p126f); 
 
 // Loads the row tiles of the pass over the queries: rows i .. of the group's heads, numbered g Tq +
 // position.  A tile stays within a head where a head fills one, else it packs the group's heads.
-struct RowSeen {   // what a row of the tile sees
-  int lo, len;
-  float at, slope;
+struct RowSeen {   // what a row of the tile sees, as given
+  int lo, hi, at;
+  float slope;
 };
+struct Walk;
 template <int T>
 struct RowsOf {   // the same of all its rows
   int lo[T], len[T];
@@ -1213,35 +1229,6 @@ struct RowsOf {   // the same of all its rows
 struct QueryTiles {
   const float *q, *dy, *lse, *delta;   // lse, delta: of the group's first head
   int b, hk, i1, T;
-  // The first row from i on in whose 32 queries, by the bounds that the pass for dq left, one sees a
-  // state of j0 .. j1: at 512 queries of four documents a workgroup then passes over three quarters of
-  // them.  64 bounds at a time; packed rows are not looked at.
-  __device__ int next(const Shape& s, const Spans& v, int i, int j0, int j1) const {
-    if (packed(s)) return i;
-    const int blocks = (s.Tq + kBoundRows - 1) / kBoundRows;
-    const int2* bounds = reinterpret_cast<const int2*>(v.bounds) + (int64_t)b * blocks;
-    while (i < i1) {
-      const int g = i / s.Tq, first = (i - g * s.Tq) / kBoundRows;
-      for (int at = first; at < blocks; at += 64) {
-        const int k = at + (int)(threadIdx.x & 63);
-        const int2 r = bounds[min(k, blocks - 1)];
-        const uint64_t some = __ballot(k < blocks && r.x < j1 && r.y > j0);
-        if (some) {
-          const int k0 = at + __builtin_ctzll(some);
-          return k0 == first ? i : g * s.Tq + k0 * kBoundRows;
-        }
-      }
-      i = (g + 1) * s.Tq;
-    }
-    return i;
-  }
-  __device__ RowSeen seen(const Shape& s, const Spans& v, int i) const {
-    const int r = i + (int)threadIdx.x;
-    if (i >= i1 || (int)threadIdx.x >= rows_at(s, i)) return {0, 0, 0.f, 0.f};
-    const int g = r / s.Tq;
-    const Seen x(v, (int64_t)b * s.Tq + (r - g * s.Tq), hk * s.G + g, s.Tk);
-    return {x.lo, x.len, (float)x.at, x.slope};
-  }
   __device__ bool packed(const Shape& s) const { return s.Tq < T; }
   __device__ int rows_at(const Shape& s, int i) const {
     return packed(s) ? min(T, i1 - i) : min(min(T, i1 - i), s.Tq - i % s.Tq);
@@ -1263,6 +1250,115 @@ struct QueryTiles {
       nl = there ? -lse[i + threadIdx.x] * kLog2e : -INFINITY;
       dl = there ? delta[i + threadIdx.x] : 0.f;
     }
+  }
+  // the same of a walk's tile, with lse itself
+  template <bool EXACT, class R>
+  __device__ void load(const Shape& s, const Walk& at, R& raw, float& nl, float& dl) const;
+};
+
+// The walk of a workgroup over the tiles of rows that see its states j0 .. j1: a tile without any row
+// that sees one, by the bounds of every 32 queries that the pass for dq left, is passed over (at 512
+// queries of four documents, half of them).  64 bounds are looked at together, once where they are all.
+// Packed rows are not looked at.
+struct Walk {
+  int i, i1, g, pos;        // the tile's first row; the last one's end; its head and query
+  uint64_t some = 0;        // of blocks first .. first + 63: seen
+  int first = -64;
+  int b, j0, j1, T;
+  const Spans& v;
+  __device__ Walk(const Spans& v, const Shape& s, int b, int i0, int i1, int j0, int j1, int T)
+      : i(i0), i1(i1), g(i0 / s.Tq), b(b), j0(j0), j1(j1), T(T), v(v) {
+    pos = i0 - g * s.Tq;
+    find(s);
+  }
+  __device__ bool packed(const Shape& s) const { return s.Tq < T; }
+  __device__ int rows(const Shape& s) const {
+    return packed(s) ? min(T, i1 - i) : min(min(T, i1 - i), s.Tq - pos);
+  }
+  __device__ void find(const Shape& s) {
+    if (packed(s)) return;
+    const int blocks = (s.Tq + kBoundRows - 1) / kBoundRows;
+    while (i < i1) {
+      const int block = pos / kBoundRows;
+      if (block < first || block >= first + 64) {
+        first = block;
+        const int k = block + (int)(threadIdx.x & 63);
+        const int2 r = reinterpret_cast<const int2*>(v.bounds)[(int64_t)b * blocks + min(k, blocks - 1)];
+        some = __ballot(k < blocks && r.x < j1 && r.y > j0);
+      }
+      const uint64_t left = some >> (block - first);
+      if (left & 1) return;
+      pos = left ? (block + __builtin_ctzll(left)) * kBoundRows : (first + 64) * kBoundRows;
+      if (pos >= s.Tq) {
+        ++g;
+        pos = 0;
+      }
+      i = g * s.Tq + pos;
+    }
+  }
+  __device__ void step(const Shape& s) {
+    const int n = rows(s);
+    i += n;
+    pos += n;
+    if (!packed(s) && pos >= s.Tq) {
+      ++g;
+      pos = 0;
+    }
+    find(s);
+  }
+  // what row threadIdx.x sees, as it is in memory
+  __device__ RowSeen seen(const Shape& s, int hk) const {
+    if (i >= i1 || (int)threadIdx.x >= rows(s)) return {0, 0, 0, 0.f};
+    int head = g, q = pos + (int)threadIdx.x;
+    if (packed(s)) {
+      head = (i + (int)threadIdx.x) / s.Tq;
+      q = i + (int)threadIdx.x - head * s.Tq;
+    }
+    const int32_t* p = v.span + 3 * ((int64_t)b * s.Tq + q);
+    return {p[0], p[1], p[2], v.bias ? v.mod[(v.cap ? 1 : 0) + hk * s.G + head] : 0.f};
+  }
+};
+template <bool EXACT, class R>
+__device__ void QueryTiles::load(const Shape& s, const Walk& at, R& raw, float& nl, float& dl) const {
+  const int rows = at.i < i1 ? at.rows(s) : 0;
+  if (!packed(s)) {
+    const int64_t r = ((int64_t)b * s.Tq + at.pos) * s.ldq + (int64_t)min(hk * s.G + at.g, s.H - 1) * s.dh;
+    raw.template load<EXACT>(q + r, dy + r, s.ldq, rows, s.dh);
+  } else {
+    const int64_t to = (int64_t)b * s.Tq * s.ldq + (int64_t)hk * s.G * s.dh;
+    raw.template load_packed<EXACT>(q + to, dy + to, s, at.i, rows);
+  }
+  if ((int)threadIdx.x < T) {
+    const bool there = (int)threadIdx.x < rows;
+    nl = there ? lse[at.i + threadIdx.x] : INFINITY;
+    dl = there ? delta[at.i + threadIdx.x] : 0.f;
+  }
+}
+
+// The tiles of rows that a workgroup of the pass over the queries works through.
+template <class V, int T>
+struct Tiles {
+  int i, i1;
+  __device__ Tiles(const V&, const Shape&, int, int i0, int i1, int, int) : i(i0), i1(i1) {}
+  __device__ bool more() const { return i < i1; }
+  __device__ int rows(const QueryTiles& q, const Shape& s) const { return q.rows_at(s, i); }
+  __device__ void step(const Shape&, int n) { i += n; }
+  template <bool EXACT, class R>
+  __device__ void load(const QueryTiles& q, const Shape& s, R& raw, float& nl, float& dl) const {
+    q.load<EXACT>(s, i, raw, nl, dl);
+  }
+};
+template <int T>
+struct Tiles<Spans, T> {
+  Walk walk;
+  __device__ Tiles(const Spans& v, const Shape& s, int b, int i0, int i1, int j0, int j1)
+      : walk(v, s, b, i0, i1, j0, j1, T) {}
+  __device__ bool more() const { return walk.i < walk.i1; }
+  __device__ int rows(const QueryTiles&, const Shape& s) const { return walk.rows(s); }
+  __device__ void step(const Shape& s, int) { walk.step(s); }
+  template <bool EXACT, class R>
+  __device__ void load(const QueryTiles& q, const Shape& s, R& raw, float& nl, float& dl) const {
+    q.load<EXACT>(s, walk, raw, nl, dl);
   }
 };
 
@@ -1345,10 +1441,10 @@ struct States {
 template <int W, int T, int B>
 struct States<W, T, Spans, B> {
   Cap cap;
-  int j, first;
+  int j, first, Tk;
   RowsOf<T>* rows;
   uint32_t* odd_bits;
-  __device__ States(const Spans& v, const Shape&, const Place&, int j) : cap(v), j(j) {
+  __device__ States(const Spans& v, const Shape& s, const Place&, int j) : cap(v), j(j), Tk(s.Tk) {
     __shared__ __attribute__((aligned(16))) RowsOf<T> seen[B];
     __shared__ uint32_t odd[4];
     rows = seen;
@@ -1362,9 +1458,9 @@ struct States<W, T, Spans, B> {
   __device__ bool live(int) const { return true; }
   __device__ void put(const RowSeen& r, int buf) const {
     rows[buf].lo[threadIdx.x] = r.lo;
-    rows[buf].len[threadIdx.x] = r.len;
-    rows[buf].at[threadIdx.x] = r.at;
-    rows[buf].slope[threadIdx.x] = r.slope;
+    rows[buf].len[threadIdx.x] = r.lo < r.hi && r.lo >= 0 && r.hi <= Tk ? r.hi - r.lo : 0;
+    rows[buf].at[threadIdx.x] = (float)r.at;
+    rows[buf].slope[threadIdx.x] = r.slope * kLog2e;
   }
   __device__ RowsSeen<T> at(int buf) const { return {rows + buf, j, first}; }
   __device__ uint32_t* odd_rows(int turn) const { return odd_bits + 2 * turn; }
@@ -1385,7 +1481,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dq_kernel(
   __shared__ __attribute__((aligned(16))) char ks[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) char vs[Rw::kBytes];
   __shared__ floatx2 tops[W];
-  const Place at = place<V::kSpan>(s, tiles);
+  const Place at = place<V, true, (DH <= 64)>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int col = (at.tile * W + w) * 32 + (lane & 31), here = min(col, s.R - 1);
@@ -1496,7 +1592,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
   __shared__ __attribute__((aligned(16))) char gs[Rw::kBytes];
   __shared__ __attribute__((aligned(16))) float nl[T], dl[T];
   __shared__ floatx2 tops[W];
-  const Place at = place<false>(s, tiles);
+  const Place at = place<V, false, (DH <= 64)>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int j = (at.tile * W + w) * 32 + (lane & 31);
@@ -1527,30 +1623,29 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
   Raw<DH, W, T> raw;
   float ll = 0.f, dd = 0.f;
   [[maybe_unused]] RowSeen rs{};
-  int i = i0;
+  Tiles<V, T> tiles_of(view, s, at.b, i0, i1, jt, jt + 32 * W);
   const auto load = [&] {
     if constexpr (V::kSpan) {
-      i = rows.next(s, view, i, jt, jt + 32 * W);
-      if ((int)threadIdx.x < T) rs = rows.seen(s, view, i);
+      if (tiles_of.more() && (int)threadIdx.x < T) rs = tiles_of.walk.seen(s, at.hk);
     }
-    if (i < i1) rows.load<EXACT>(s, i, raw, ll, dd);
+    if (tiles_of.more()) tiles_of.template load<EXACT>(rows, s, raw, ll, dd);
   };
   load();
-  for (; i < i1; turn ^= 1) {
+  for (; tiles_of.more(); turn ^= 1) {
     if constexpr (V::kSpan) raw.publish(tops, states.odd_rows(turn));
     else raw.publish(tops);
     __syncthreads();
     const int2 e = raw.exponents(tops);
     raw.store(qs, gs, e);
     if ((int)threadIdx.x < T) {
-      nl[threadIdx.x] = ll;
+      nl[threadIdx.x] = V::kSpan ? -ll * kLog2e : ll;
       dl[threadIdx.x] = dd;
       states.put(rs, 0);
     }
     if constexpr (V::kSpan) states.clear(turn ^ 1);
     __syncthreads();
-    const int there = rows.rows_at(s, i);
-    i += there;
+    const int there = tiles_of.rows(rows, s);
+    tiles_of.step(s, there);
     load();
     const float qf = exp2_of(e.x - 14), gf = exp2_of(e.y - 14), c = kc * qf, cv = vf * gf;
 #pragma unroll 1
@@ -1654,7 +1749,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   __shared__ __attribute__((aligned(16))) char mats[NB][2][Rw::kBytes];   // tiles of k and v
   __shared__ float4 meet[kPairs][2][2][64];
   __shared__ floatx2 tops[W];
-  const Place at = place<V::kSpan>(s, tiles);
+  const Place at = place<V, true, (DH <= 64)>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
@@ -1812,7 +1907,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   __shared__ __attribute__((aligned(16))) float nl[NB][T], dl[NB][T];
   __shared__ float4 meet[kPairs][4][64];
   __shared__ floatx2 tops[W];
-  const Place at = place<false>(s, tiles);
+  const Place at = place<V, false, (DH <= 64)>(s, tiles);
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
@@ -1850,32 +1945,30 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
     const int2 e = raw.exponents(tops);
     raw.store(mats[buf][0], mats[buf][1], e);
     if ((int)threadIdx.x < T) {
-      nl[buf][threadIdx.x] = ll;
+      nl[buf][threadIdx.x] = V::kSpan ? -ll * kLog2e : ll;
       dl[buf][threadIdx.x] = dd;
       states.put(rs, buf);
     }
     return e;
   };
-  int i = i0;
-  // the tile from row i on, or from the first one behind it that sees the columns
+  Tiles<V, T> tiles_of(view, s, at.b, i0, i1, at.tile * kPairs * 32, (at.tile + 1) * kPairs * 32);
   const auto load = [&] {
     if constexpr (V::kSpan) {
-      i = rows.next(s, view, i, at.tile * kPairs * 32, (at.tile + 1) * kPairs * 32);
-      if ((int)threadIdx.x < T) rs = rows.seen(s, view, i);
+      if ((int)threadIdx.x < T) rs = tiles_of.walk.seen(s, at.hk);
     }
-    rows.load<EXACT>(s, i, raw, ll, dd);
+    tiles_of.template load<EXACT>(rows, s, raw, ll, dd);
   };
   load();
-  if (i < i1) {
+  if (tiles_of.more()) {
     publish(raw, tops, 0);
     __syncthreads();
     int2 e = stage(0);
     int buf = 0;
-    i += rows.rows_at(s, i);
+    tiles_of.step(s, tiles_of.rows(rows, s));
     load();
     __syncthreads();
     for (;; turn ^= 1) {
-      const bool more = i < i1;
+      const bool more = tiles_of.more();
       floatx16 a = {};
       const char* z = mats[buf][role];
 #pragma unroll
@@ -1941,7 +2034,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
       const Pieces pp[2] = {split8(v, both(f, other)), split8(v + 8, both(f, other))};
       const auto advance = [&] {
         e = stage(NB - 1 - buf);
-        i += rows.rows_at(s, i);
+        tiles_of.step(s, tiles_of.rows(rows, s));
         load();
       };
       if (NB == 2 && role && more) advance();
@@ -1982,8 +2075,7 @@ __global__ void sum_kernel(const float* __restrict__ part, float* __restrict__ o
 }
 
 // ---------------------------------------------------------------- launches
-constexpr int64_t kFlatPairs = 32;
-Shape shape_of(const AttendShape& a, bool spans) {
+Shape shape_of(const AttendShape& a) {
   Shape s;
   s.B = (int)a.B; s.Tq = (int)a.Tq; s.Tk = (int)a.Tk; s.H = (int)a.H; s.Hkv = (int)a.Hkv;
   s.G = (int)(a.H / a.Hkv);
@@ -1992,7 +2084,6 @@ Shape shape_of(const AttendShape& a, bool spans) {
   s.ldq = a.H * a.dh;
   s.ldk = 2 * a.Hkv * a.dh;
   s.scale = 1.f / sqrtf((float)a.dh);
-  s.flat = spans && a.B * a.Hkv < kFlatPairs;
   return s;
 }
 
@@ -2002,9 +2093,10 @@ int back_columns(int64_t dh) {
 }
 int back_rows(int64_t dh) { return dh <= 64 ? Width<64>::kBackRows : Width<128>::kBackRows; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+template <class V>
 dim3 grid_of(const Shape& s, int tiles, int64_t slices) {
   const int64_t pairs = (int64_t)s.B * s.Hkv;
-  return dim3((unsigned)((s.flat ? pairs : ceil_div(pairs, kXcds) * kXcds) * tiles), (unsigned)slices);
+  return dim3((unsigned)((V::kSpan ? pairs : ceil_div(pairs, kXcds) * kXcds) * tiles), (unsigned)slices);
 }
 // Whether the forward's workgroups have 256 columns, not 128: where that leaves less than a tenth
 // more columns idle, which is what the wide ones gain (4096 x 4096: 0.86 against 0.96 ms at 2 x 16
@@ -2060,12 +2152,12 @@ bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows &&
     FROM_65_TO_128(CALL);                  \
   }
 #define LAUNCH(KERNEL, WAVES, TILES, SLICES, ...) \
-  hipLaunchKernelGGL(KERNEL, grid_of(s, TILES, SLICES), dim3(64 * WAVES), 0, st, __VA_ARGS__)
+  hipLaunchKernelGGL(KERNEL, grid_of<V>(s, TILES, SLICES), dim3(64 * WAVES), 0, st, __VA_ARGS__)
 
 template <class V>
 hipError_t attend_fwd(const float* q, const float* kv, const V& view, float* y, float* lse, float* part,
                       const AttendShape& a, int64_t slices, hipStream_t st) {
-  const Shape s = shape_of(a, V::kSpan);
+  const Shape s = shape_of(a);
   const bool few = few_rows(a);
   const int tiles = few ? 1 : (int)ceil_div(s.R, fwd_columns(a, V::kSpan));
   const int len = (int)slice_of(s.Tk, slices, few ? 32 : tile_rows(s.dh));
@@ -2100,7 +2192,7 @@ template <class V>
 hipError_t attend_bwd(const float* q, const float* kv, const V& view, const float* y, const float* lse,
                       const float* dy, float* dq, float* dkv, float* delta, float* part,
                       const AttendShape& a, int64_t q_slices, int64_t kv_slices, hipStream_t st) {
-  const Shape s = shape_of(a, V::kSpan);
+  const Shape s = shape_of(a);
   const int64_t q_size = a.B * a.Tq * s.ldq, kv_size = a.B * a.Tk * s.ldk;
   {
     const int tiles = (int)ceil_div(s.R, back_columns(s.dh));
