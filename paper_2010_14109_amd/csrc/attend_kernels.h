@@ -206,17 +206,22 @@ __device__ inline void trim(float* v, int d, int dh) {
 // ---------------------------------------------------------------- what a query sees
 // The first klen[b] states of its sequence, all of them as they are.
 struct FirstStates {
-  static constexpr bool kSpan = false;
+  static constexpr bool kSpan = false, kCap = false;
   const int32_t* klen;
 };
 // The states lo <= j < hi of the query's entry (lo, hi, at), whose scores are first capped, then lose
 // slope |at - j|.  A query whose span reaches outside the states sees none, and its results are NaN.
-struct Spans {
-  static constexpr bool kSpan = true;
+// The cap is a kernel's own matter: its code takes registers that the kernels without have no room for
+// (24 x 512 in documents, 245 us, with the code of both 331).
+struct AllSpans {
   const int32_t* span;
-  const float* mod;        // the cap iff `cap`, then a slope a head iff `bias`
+  const float* mod;        // the cap, where there is one, then a slope a head iff `bias`
   int32_t* bounds;         // backward: smallest lo and largest hi of every 32 queries of a sequence
-  bool cap, bias;
+  bool bias;
+};
+template <bool CAP>
+struct Spans : AllSpans {
+  static constexpr bool kSpan = true, kCap = CAP;
 };
 constexpr int kBoundRows = 32;
 
@@ -227,14 +232,15 @@ struct Seen {
   bool bad = false;
   __device__ Seen() {}
   // query row r of a key head; `head` its head
-  __device__ Seen(const Spans& v, int64_t query, int head, int Tk) {
+  template <class V>
+  __device__ Seen(const V& v, int64_t query, int head, int Tk) {
     lo = v.span[3 * query];
     const int hi = v.span[3 * query + 1];
     at = v.span[3 * query + 2];
     bad = lo < hi && (lo < 0 || hi > Tk);
     len = lo < hi && !bad ? hi - lo : 0;
     if (len == 0) lo = 0;
-    if (v.bias) slope = v.mod[(v.cap ? 1 : 0) + head] * kLog2e;
+    if (v.bias) slope = v.mod[V::kCap + head] * kLog2e;
   }
   __device__ int low() const { return len ? lo : 0x7fffffff; }
   __device__ int high() const { return lo + len; }
@@ -266,22 +272,36 @@ __device__ inline int wave_least(int x) {
 }
 __device__ inline int wave_most(int x) { return -wave_least(-x); }
 
-// A score S c (in powers of two) under the cap, C tanh(S c / C), and what the cap multiplies its
-// gradient by, 1 - tanh^2.  With r = 1 / (1 + exp(2 x)), tanh x = 1 - 2 r and 1 - tanh^2 = 4 r (1 - r);
-// below 1/4, where the difference loses bits, the Taylor series (the first term left out is 2^-26 of
-// the value).  The score is off by up to 2^-21 of itself, the factor by 2^-21.
+// A score z (in powers of two) under the cap, C tanh(z / C), and what the cap multiplies its gradient by,
+// 1 - tanh^2.  With r = 1 / (1 + exp(2 x)), tanh x = 1 - 2 r and 1 - tanh^2 = 4 r (1 - r); below 1/4,
+// where the difference loses bits, the Taylor series (the first term left out is 2^-26 of the value).
+// Scores mostly stay far below the cap: where a wave's are all within kNear of it, an odd polynomial
+// does (fitted at Chebyshev nodes of x^2, 2^-26 off), at half the instructions (2 x 4096 in a window
+// of 1024, 16 heads of 128 on 4, with gradients: 1230 us without, 1169).  The score is off by up to 2^-21
+// of itself, the factor
+// by 2^-21.
 struct Cap {
+  static constexpr float kNear = 0.6f;
   float c = 1.f, inv = 1.f;
   __device__ Cap() {}
-  __device__ Cap(const Spans& v) {
-    if (v.cap) {
+  template <class V>
+  __device__ Cap(const V& v) {
+    if constexpr (V::kCap) {
       c = v.mod[0] * kLog2e;
       inv = 1.f / c;
     }
   }
-  template <bool TURN>
-  __device__ float apply(float s, float& turn) const {
-    const float x = s * inv, x2 = x * x;
+  __device__ bool near(float most) const { return __all(most * inv < kNear); }
+  template <bool NEAR, bool TURN>
+  __device__ float apply(float z, float& turn) const {
+    const float x = z * inv, x2 = x * x;
+    if constexpr (NEAR) {
+      const float p = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, -0.006276390f, 0.021116216f), -0.053875137f),
+                                    0.133329242f), -0.333333313f);
+      const float t = fmaf(z * x2, p, z);
+      if (TURN) turn = fmaf(-t * inv, t * inv, 1.f);
+      return t;
+    }
     const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
     if (TURN) turn = 4.f * fmaf(-r, r, r);
     const float t = fmaf(-2.f, r, 1.f);
@@ -452,23 +472,56 @@ __device__ inline void mask_rows(floatx16& a, int r0, int left) {
   for (int i = 0; i < 16; ++i) a[i] = r0 + 8 * (i / 4) + 4 * half + i % 4 < left ? a[i] : -INFINITY;
 }
 
+// the largest |value|, a NaN if there is one
+__device__ inline float most_of(const floatx16& a) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = __builtin_elementwise_maximum(m, fabsf(a[i]));
+  return m;
+}
 // The scores of rows j .. j + 31, a column's, with what its span changes: a c in powers of two under
-// the cap and without slope |at - j|, -inf where it sees nothing (a masked row needs all of them masked
-// or cut).  turn: what the cap multiplies gradients by.
-template <bool TURN>
-__device__ inline void shape_rows(floatx16& a, float c, const Cap& cap, const Spans& v, const Seen& s, int j,
-                                  float (&turn)[TURN ? 16 : 1]) {
+// the cap and without slope |at - j|.
+template <class V>
+__device__ inline void shape_rows(floatx16& a, float c, const Cap& cap, const V& v, const Seen& s, int j) {
   const int half = (threadIdx.x >> 5) & 1;
-  if (v.cap)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) a[i] = cap.apply<TURN>(a[i] * c, turn[TURN ? i : 0]);
-  else
+  for (int i = 0; i < 16; ++i) a[i] *= c;
+  if constexpr (V::kCap) {
+    float none;
+    if (cap.near(most_of(a)))
 #pragma unroll
-    for (int i = 0; i < 16; ++i) a[i] *= c;
+      for (int i = 0; i < 16; ++i) a[i] = cap.apply<true, false>(a[i], none);
+    else
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a[i] = cap.apply<false, false>(a[i], none);
+  }
   if (v.bias) {
     const float from = (float)(s.at - j - 4 * half);
 #pragma unroll
     for (int i = 0; i < 16; ++i) a[i] = fmaf(-s.slope, fabsf(from - (float)(8 * (i / 4) + i % 4)), a[i]);
+  }
+}
+// Under the cap, the probabilities of these scores, exp2(score + nl), times what the cap multiplies
+// gradients by, 0 where nothing is seen; four values at a time, as more at once take registers that spill.
+__device__ inline void capped_rows(floatx16& a, float c, const Cap& cap, const Seen& s, int j, float nl) {
+  const int half4 = 4 * ((threadIdx.x >> 5) & 1);
+  const float at = (float)(s.at - j - half4);
+  const uint32_t from = (uint32_t)(j - s.lo) + half4;
+  const bool near = cap.near(most_of(a) * c);
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    float curve[4];
+    if (near)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[4 * g + k] = cap.apply<true, true>(a[4 * g + k] * c, curve[k]);
+    else
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[4 * g + k] = cap.apply<false, true>(a[4 * g + k] * c, curve[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float z = fmaf(-s.slope, fabsf(at - (float)(8 * g + k)), a[4 * g + k]);
+      a[4 * g + k] = from + (uint32_t)(8 * g + k) < (uint32_t)s.len ? __builtin_amdgcn_exp2f(z + nl) * curve[k] : 0.f;
+    }
   }
 }
 __device__ inline void mask_span(floatx16& a, const Seen& s, int j) {
@@ -619,15 +672,15 @@ struct Columns {
   __device__ bool bad(int) const { return wrong; }
   __device__ bool empty(int) const { return false; }
 };
-template <int C, int W>
-struct Columns<C, W, Spans> {
+template <int C, int W, bool CAP>
+struct Columns<C, W, Spans<CAP>> {
   int k0, k1;
   Seen seen[C];
   Cap cap;
   int low, high, last_low, first_high;   // of the wave: what any column sees, what all do
   uint32_t* odd_bits;                    // [2][2]: rows of the present and the next tile
   // col0: the lane's first column
-  __device__ Columns(const Spans& v, const Shape& s, const Place& at, int col0, int slice_len) : cap(v) {
+  __device__ Columns(const Spans<CAP>& v, const Shape& s, const Place& at, int col0, int slice_len) : cap(v) {
     __shared__ int2 limits[W];
     __shared__ uint32_t odd[4];
     odd_bits = odd;
@@ -746,7 +799,7 @@ struct Forward {
   static constexpr int kCols = 32 * kWaves * kSets / Width<DH>::kParts;
 };
 template <int DH, bool EXACT, bool WIDE, class V>
-__global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), V::kSpan && DH <= 64 ? 3 : DH <= 128 ? 2 : 1) void fwd_kernel(
+__global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), V::kSpan && !V::kCap && DH <= 64 ? 3 : DH <= 128 ? 2 : 1) void fwd_kernel(
     const float* __restrict__ q, const float* __restrict__ kv, V view, float* __restrict__ y, float* __restrict__ lse, Shape s, int tiles, int slice_len,
     int64_t y_slice, int64_t lse_slice) {
   using Wd = Width<DH>;
@@ -803,6 +856,10 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), V::kSpan && DH <=
       if (r0 && j0 + r0 >= k1) break;
       if constexpr (V::kSpan) {
         if (cols.none(j0 + r0)) continue;
+        // (here and in the other passes before the products: behind them, a branch that is rarely taken
+        // has had the compiler read their results some cycles early)
+#pragma unroll
+        for (int x = 0; x < C; ++x) cols.look(turn, r0, j0 + r0, x, odd[x]);
       }
       floatx16 a[C];
 #pragma unroll
@@ -825,10 +882,8 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), V::kSpan && DH <=
         // (no smaller than the normal numbers: a masked score stays -inf)
         c[x] = fmaxf(qc[x] * exp2_of(e.x - 14), 0x1p-126f);
         if constexpr (V::kSpan) {
-          cols.look(turn, r0, j0 + r0, x, odd[x]);
-          if (view.cap || view.bias) {
-            float none[1];
-            shape_rows<false>(a[x], c[x], cols.cap, view, cols.seen[x], j0 + r0, none);
+          if (V::kCap || view.bias) {
+            shape_rows(a[x], c[x], cols.cap, view, cols.seen[x], j0 + r0);
             c[x] = 1.f;
           }
           if (!cols.all(j0 + r0)) mask_span(a[x], cols.seen[x], j0 + r0);
@@ -1073,9 +1128,9 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
       const int row = 16 * (i / 4) + 4 * quarter + i % 4;
       if constexpr (V::kSpan) {
         p[i] = a[i / 4][i % 4];
-        if (view.cap || view.bias) {
+        if (V::kCap || view.bias) {
           float none;
-          p[i] = view.cap ? cap.apply<false>(p[i] * c, none) : p[i] * c;
+          p[i] = V::kCap ? cap.apply<false, false>(p[i] * c, none) : p[i] * c;
           if (view.bias) p[i] = fmaf(-seen.slope, fabsf((float)(seen.at - j0 - row)), p[i]);
         }
         p[i] = seen.sees(j0 + row) ? p[i] : -INFINITY;
@@ -1085,7 +1140,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
       top = fmaxf(top, p[i]);
     }
     if constexpr (V::kSpan) {
-      if (view.cap || view.bias) c = 1.f;
+      if (V::kCap || view.bias) c = 1.f;
       if (__builtin_expect(odd_rows != 0, 0)) odd |= (seen.bits(j0) & odd_rows) != 0;
     }
     top = score(max_of_quarters(top), c);
@@ -1265,8 +1320,8 @@ struct Walk {
   uint64_t some = 0;        // of blocks first .. first + 63: seen
   int first = -64;
   int b, j0, j1, T;
-  const Spans& v;
-  __device__ Walk(const Spans& v, const Shape& s, int b, int i0, int i1, int j0, int j1, int T)
+  const AllSpans& v;
+  __device__ Walk(const AllSpans& v, const Shape& s, int b, int i0, int i1, int j0, int j1, int T)
       : i(i0), i1(i1), g(i0 / s.Tq), b(b), j0(j0), j1(j1), T(T), v(v) {
     pos = i0 - g * s.Tq;
     find(s);
@@ -1307,7 +1362,7 @@ struct Walk {
     find(s);
   }
   // what row threadIdx.x sees, as it is in memory
-  __device__ RowSeen seen(const Shape& s, int hk) const {
+  __device__ RowSeen seen(const Shape& s, int hk, bool cap) const {
     if (i >= i1 || (int)threadIdx.x >= rows(s)) return {0, 0, 0, 0.f};
     int head = g, q = pos + (int)threadIdx.x;
     if (packed(s)) {
@@ -1315,7 +1370,7 @@ struct Walk {
       q = i + (int)threadIdx.x - head * s.Tq;
     }
     const int32_t* p = v.span + 3 * ((int64_t)b * s.Tq + q);
-    return {p[0], p[1], p[2], v.bias ? v.mod[(v.cap ? 1 : 0) + hk * s.G + head] : 0.f};
+    return {p[0], p[1], p[2], v.bias ? v.mod[cap + hk * s.G + head] : 0.f};
   }
 };
 template <bool EXACT, class R>
@@ -1348,10 +1403,10 @@ struct Tiles {
     q.load<EXACT>(s, i, raw, nl, dl);
   }
 };
-template <int T>
-struct Tiles<Spans, T> {
+template <bool CAP, int T>
+struct Tiles<Spans<CAP>, T> {
   Walk walk;
-  __device__ Tiles(const Spans& v, const Shape& s, int b, int i0, int i1, int j0, int j1)
+  __device__ Tiles(const AllSpans& v, const Shape& s, int b, int i0, int i1, int j0, int j1)
       : walk(v, s, b, i0, i1, j0, j1, T) {}
   __device__ bool more() const { return walk.i < walk.i1; }
   __device__ int rows(const QueryTiles&, const Shape& s) const { return walk.rows(s); }
@@ -1363,7 +1418,8 @@ struct Tiles<Spans, T> {
 };
 
 // leaves what the 32 queries of a wave's columns see, for the pass over the queries
-__device__ inline void leave_bounds(const Spans& v, const Shape& s, const Place& at, int col) {
+template <class V>
+__device__ inline void leave_bounds(const V& v, const Shape& s, const Place& at, int col) {
   const int first = __builtin_amdgcn_readfirstlane(col - (int)(threadIdx.x & 31));
   if (at.hk || at.slice || first >= s.Tq) return;
   Seen x;
@@ -1409,14 +1465,19 @@ struct RowsSeen {
 
 // Scores of rows r .. r + 3, of group g of a's, with what spans change; curve: what the cap multiplies
 // gradients by.
-template <class Rows>
+template <class V, class Rows>
 __device__ inline void shape_states(float (&z)[4], float (&curve)[4], const floatx16& a, int g, float c,
-                                    const Cap& cap, const Spans& v, const Rows& rows, int r) {
+                                    const Cap& cap, bool near, const V& v, const Rows& rows, int r) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) z[k] = a[4 * g + k] * c;
-  if (v.cap)
+  if constexpr (V::kCap) {
+    if (near)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) z[k] = cap.apply<true>(z[k], curve[k]);
+      for (int k = 0; k < 4; ++k) z[k] = cap.apply<true, true>(z[k], curve[k]);
+    else
+#pragma unroll
+      for (int k = 0; k < 4; ++k) z[k] = cap.apply<false, true>(z[k], curve[k]);
+  }
   if (v.bias) rows.bias(r, z);
 }
 
@@ -1438,13 +1499,13 @@ struct States {
   __device__ bool live(int j) const { return j < n; }
   __device__ void put(const RowSeen&, int) const {}
 };
-template <int W, int T, int B>
-struct States<W, T, Spans, B> {
+template <int W, int T, bool CAP, int B>
+struct States<W, T, Spans<CAP>, B> {
   Cap cap;
   int j, first, Tk;
   RowsOf<T>* rows;
   uint32_t* odd_bits;
-  __device__ States(const Spans& v, const Shape& s, const Place&, int j) : cap(v), j(j), Tk(s.Tk) {
+  __device__ States(const Spans<CAP>& v, const Shape& s, const Place&, int j) : cap(v), j(j), Tk(s.Tk) {
     __shared__ __attribute__((aligned(16))) RowsOf<T> seen[B];
     __shared__ uint32_t odd[4];
     rows = seen;
@@ -1532,36 +1593,32 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dq_kernel(
     for (int r0 = 0; r0 < T && j0 + r0 < k1; r0 += 32) {
       if constexpr (V::kSpan) {
         if (cols.none(j0 + r0)) continue;
+        cols.look(turn, r0, j0 + r0, 0, odd);
       }
       float c = cs;
-      [[maybe_unused]] float curve[V::kSpan ? 16 : 1];
       floatx16 a = {}, b = {};
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(ks, r0, t), qp[t], a);
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) b = mma(Rw::by_row(vs, r0, t), gp[t], b);
       if constexpr (V::kSpan) {
-        cols.look(turn, r0, j0 + r0, 0, odd);
-        if (view.cap || view.bias) {
-          shape_rows<true>(a, c, cols.cap, view, cols.seen[0], j0 + r0, curve);
-          c = 1.f;
+        if constexpr (V::kCap) {
+          capped_rows(a, c, cols.cap, cols.seen[0], j0 + r0, nl);
+        } else {
+          if (view.bias) {
+            shape_rows(a, c, cols.cap, view, cols.seen[0], j0 + r0);
+            c = 1.f;
+          }
+          if (!cols.all(j0 + r0)) mask_span(a, cols.seen[0], j0 + r0);
         }
-        if (!cols.all(j0 + r0)) mask_span(a, cols.seen[0], j0 + r0);
       } else {
         if (j0 + r0 + 32 > k1) mask_rows(a, r0, k1 - j0);
       }
       float x[16], top = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, nl)) * fmaf(b[i], cv, -dl);
-        if constexpr (!V::kSpan) top = fmaxf(top, fabsf(x[i]));
-      }
-      if constexpr (V::kSpan) {
-        if (view.cap)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] *= curve[i];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+        x[i] = (V::kCap ? a[i] : __builtin_amdgcn_exp2f(fmaf(a[i], c, nl))) * fmaf(b[i], cv, -dl);
+        top = fmaxf(top, fabsf(x[i]));
       }
       // dS 2^(e.x - 14) is what meets the pieces of k
       top = max_of_halves(top) * kf;
@@ -1626,7 +1683,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
   Tiles<V, T> tiles_of(view, s, at.b, i0, i1, jt, jt + 32 * W);
   const auto load = [&] {
     if constexpr (V::kSpan) {
-      if (tiles_of.more() && (int)threadIdx.x < T) rs = tiles_of.walk.seen(s, at.hk);
+      if (tiles_of.more() && (int)threadIdx.x < T) rs = tiles_of.walk.seen(s, at.hk, V::kCap);
     }
     if (tiles_of.more()) tiles_of.template load<EXACT>(rows, s, raw, ll, dd);
   };
@@ -1662,13 +1719,15 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
       for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(qs, r0, t), kp[t], a);
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) b = mma(Rw::by_row(gs, r0, t), vp[t], b);
+      [[maybe_unused]] bool near = false;
+      if constexpr (V::kCap) near = states.cap.near(most_of(a) * c);
       float p[16], x[16], ptop = 0.f, xtop = 0.f;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int row = r0 + 8 * g + 4 * half;
         const float4 l4 = at4(nl, row), d4 = at4(dl, row);
         [[maybe_unused]] float z[4], curve[4];
-        if constexpr (V::kSpan) shape_states(z, curve, a, g, c, states.cap, view, states.at(0), row);
+        if constexpr (V::kSpan) shape_states(z, curve, a, g, c, states.cap, near, view, states.at(0), row);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           if constexpr (V::kSpan) p[4 * g + k] = __builtin_amdgcn_exp2f(z[k] + pick(l4, k));
@@ -1676,7 +1735,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
           x[4 * g + k] = p[4 * g + k] * fmaf(b[4 * g + k], cv, -pick(d4, k));
         }
         if constexpr (V::kSpan) {
-          if (view.cap)
+          if constexpr (V::kCap)
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[4 * g + k] *= curve[k];
           if (!(seen & 2)) {
@@ -1809,26 +1868,24 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
     __syncthreads();
     for (int j0 = k0;; j0 += T, turn ^= 1) {
       const bool more = j0 + T < k1;
+      if constexpr (V::kSpan) cols.look(turn, 0, j0, 0, odd);
       floatx16 a = {};
       const char* z = mats[buf][role];
 #pragma unroll
       for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(z, 0, t), own[t], a);
       float c = cf * exp2_of((role ? e.y : e.x) - 14);
-      if constexpr (V::kSpan) cols.look(turn, 0, j0, 0, odd);
       if (!role) {
         c = fmaxf(c, 0x1p-126f);   // a masked score stays -inf
-        if constexpr (V::kSpan) {
-          float curve[16];
-          if (view.cap || view.bias) {
-            shape_rows<true>(a, c, cols.cap, view, cols.seen[0], j0, curve);
+        if constexpr (V::kCap) {
+          capped_rows(a, c, cols.cap, cols.seen[0], j0, row);
+        } else if constexpr (V::kSpan) {
+          if (view.bias) {
+            shape_rows(a, c, cols.cap, view, cols.seen[0], j0);
             c = 1.f;
           }
           if (!cols.all(j0)) mask_span(a, cols.seen[0], j0);
 #pragma unroll
           for (int i = 0; i < 16; ++i) a[i] = __builtin_amdgcn_exp2f(fmaf(a[i], c, row));
-          if (view.cap)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) a[i] *= curve[i];
         } else {
           if (j0 + T > k1) mask_rows(a, 0, k1 - j0);
 #pragma unroll
@@ -1954,7 +2011,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   Tiles<V, T> tiles_of(view, s, at.b, i0, i1, at.tile * kPairs * 32, (at.tile + 1) * kPairs * 32);
   const auto load = [&] {
     if constexpr (V::kSpan) {
-      if ((int)threadIdx.x < T) rs = tiles_of.walk.seen(s, at.hk);
+      if ((int)threadIdx.x < T) rs = tiles_of.walk.seen(s, at.hk, V::kCap);
     }
     tiles_of.template load<EXACT>(rows, s, raw, ll, dd);
   };
@@ -1969,18 +2026,20 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
     __syncthreads();
     for (;; turn ^= 1) {
       const bool more = tiles_of.more();
-      floatx16 a = {};
-      const char* z = mats[buf][role];
-#pragma unroll
-      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(z, 0, t), own[t], a);
-      const float c = cf * exp2_of((role ? e.y : e.x) - 14);
-      float v[16], top = 0.f;
       [[maybe_unused]] int seen = 3;
       if constexpr (V::kSpan) {
         seen = states.at(buf).look(0);
         const uint32_t bits = states.odd_rows(turn)[0];
         if (__builtin_expect(bits != 0, 0)) odd |= states.at(buf).odd(bits, 0);
       }
+      floatx16 a = {};
+      const char* z = mats[buf][role];
+#pragma unroll
+      for (int t = 0; t < Wd::kSteps; ++t) a = mma(Rw::by_row(z, 0, t), own[t], a);
+      const float c = cf * exp2_of((role ? e.y : e.x) - 14);
+      float v[16], top = 0.f;
+      [[maybe_unused]] bool near = false;
+      if constexpr (V::kCap) near = !role && states.cap.near(most_of(a) * c);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float4 r4 = at4(role ? dl[buf] : nl[buf], 8 * g + 4 * half);
@@ -1988,7 +2047,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
           if constexpr (V::kSpan) {
             float z[4], curve[4];
             const int r = 8 * g + 4 * half;
-            shape_states(z, curve, a, g, c, states.cap, view, states.at(buf), r);
+            shape_states(z, curve, a, g, c, states.cap, near, view, states.at(buf), r);
 #pragma unroll
             for (int k = 0; k < 4; ++k) z[k] = __builtin_amdgcn_exp2f(z[k] + pick(r4, k));
             if (!(seen & 2)) {
@@ -1999,7 +2058,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[4 * g + k] = z[k];
-            if (view.cap)   // role 1 multiplies by it
+            if constexpr (V::kCap)   // role 1 multiplies by it
 #pragma unroll
               for (int k = 0; k < 4; ++k) z[k] *= curve[k];
             meet[pair][g][lane] = make_float4(z[0], z[1], z[2], z[3]);
@@ -2171,7 +2230,11 @@ hipError_t attend_fwd(const float* q, const float* kv, const V& view, float* y, 
   if (few) {
     TO_128(FEW);
   } else if (wide(a, V::kSpan)) {
-    TO_128(WIDE);
+    if constexpr (V::kSpan) {
+      FROM_65_TO_128(WIDE);
+    } else {
+      TO_128(WIDE);
+    }
   } else if (s.dh <= 128) {
     TO_128(FWD);
   } else {

@@ -13,7 +13,9 @@ namespace ooc {
 hipError_t span_attention_fwd(const float* q, const float* kv, const int32_t* span, const float* mod,
                               bool cap, bool bias, float* y, float* lse, float* part,
                               const AttendShape& a, int64_t slices, hipStream_t s) {
-  return attend_fwd(q, kv, Spans{span, mod, nullptr, cap, bias}, y, lse, part, a, slices, s);
+  const AllSpans v{span, mod, nullptr, bias};
+  return cap ? attend_fwd(q, kv, Spans<true>{v}, y, lse, part, a, slices, s)
+             : attend_fwd(q, kv, Spans<false>{v}, y, lse, part, a, slices, s);
 }
 
 hipError_t span_attention_bwd(const float* q, const float* kv, const int32_t* span, const float* mod,
@@ -21,8 +23,9 @@ hipError_t span_attention_bwd(const float* q, const float* kv, const int32_t* sp
                               float* dq, float* dkv, float* delta, int32_t* bounds, float* part,
                               const AttendShape& a, int64_t q_slices, int64_t kv_slices,
                               hipStream_t s) {
-  return attend_bwd(q, kv, Spans{span, mod, bounds, cap, bias}, y, lse, dy, dq, dkv, delta, part, a,
-                    q_slices, kv_slices, s);
+  const AllSpans v{span, mod, bounds, bias};
+  return cap ? attend_bwd(q, kv, Spans<true>{v}, y, lse, dy, dq, dkv, delta, part, a, q_slices, kv_slices, s)
+             : attend_bwd(q, kv, Spans<false>{v}, y, lse, dy, dq, dkv, delta, part, a, q_slices, kv_slices, s);
 }
 
 }  // namespace ooc
