@@ -27,12 +27,18 @@ namespace ooc {
 
 namespace {
 
-constexpr int kWaves = 8;   // of a workgroup, at most
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+template <int CL>
+constexpr int kWaves = CL == 64 ? 8 : 16;   // of a workgroup, at most
+
+constexpr uint32_t kXcds = 8;
+
 struct Scan {
   int B, T, C, slices, slice_len;
+  // Neighbours run on one die: where a row is no multiple of a cache line, they share lines.
+  bool together;
 };
 
 // a = sigmoid(f) and 1 - a, each to a few units in its last place
@@ -74,15 +80,21 @@ struct Lane {
 };
 
 // SUM: only reduce the slice to (A, B), into part.
-template <bool BACK, bool SUM, int S>
-__global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(
+template <bool BACK, bool SUM, int S, int CL>
+__global__ __launch_bounds__(64 * kWaves<CL>, 4) void scan_kernel(
     const float* __restrict__ fx, const float* __restrict__ h0, const int32_t* __restrict__ fr,
     const float* __restrict__ hin, const float* __restrict__ dh, float* __restrict__ out,
     float* __restrict__ dh0, float* __restrict__ part, Scan s) {
-  __shared__ float2 runs[2][kWaves][64];
-  const int nw = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int blocks = (s.C + 63) / 64, b = blockIdx.x / blocks, c = (int)(blockIdx.x % blocks) * 64 + lane;
-  const int slice = blockIdx.y, begin = min(s.T, slice * s.slice_len), end = min(s.T, begin + s.slice_len);
+  constexpr int R = 64 / CL;   // runs of a wave
+  __shared__ float2 runs[2][kWaves<CL>][CL];
+  const int nw = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, col = lane % CL, sub = lane / CL;
+  const uint32_t blocks = (s.C + CL - 1) / CL, slices = SUM ? s.slices - 1 : s.slices;
+  const uint32_t items = blocks * s.B * slices, id = blockIdx.x;
+  const uint32_t item = s.together ? id % kXcds * (gridDim.x / kXcds) + id / kXcds : id;
+  if (item >= items) return;
+  const int b = item / blocks % s.B, c = (int)(item % blocks) * CL + col, slice = item / (blocks * s.B);
+  const int begin = min(s.T, slice * s.slice_len), end = min(s.T, begin + s.slice_len);
   float state = 0.f, A_all = 1.f;
   if (!SUM) {
     if (!BACK && h0 && c < s.C) state = h0[(int64_t)b * s.C + c];
@@ -93,10 +105,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(
       }
   }
   Lane<BACK, S> next;
-  if (begin < end) next.load(fx, h0, fr, hin, dh, s, b, c, begin + w * S, end, SUM);
+  if (begin < end) next.load(fx, h0, fr, hin, dh, s, b, c, begin + (w * R + sub) * S, end, SUM);
   int buf = 0;
-  for (int r = begin; r < end; r += nw * S, buf ^= 1) {
-    const int t0 = r + w * S;
+  for (int r = begin; r < end; r += nw * R * S, buf ^= 1) {
+    const int t0 = r + (w * R + sub) * S;
     float a[S], rest[S], al[S], B = 0.f, A = 1.f;
     const Lane<BACK, S> now = next;
 #pragma unroll
@@ -108,16 +120,31 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(
         A *= al[k];
       }
     }
-    runs[buf][w][lane] = make_float2(A, B);
-    if (r + nw * S < end) next.load(fx, h0, fr, hin, dh, s, b, c, t0 + nw * S, end, SUM);
+    // the wave's runs up to a lane's own; the last one's are the wave's
+    float A0 = 1.f, B0 = 0.f;
+    if constexpr (R > 1) {
+#pragma unroll
+      for (int o = CL; o < 64; o *= 2) {
+        const float a1 = __shfl_up(A, o, 64), b1 = __shfl_up(B, o, 64);
+        if (lane >= o) {
+          B = after(A, B, b1);
+          A *= a1;
+        }
+      }
+      A0 = __shfl_up(A, CL, 64);
+      B0 = __shfl_up(B, CL, 64);
+    }
+    if (sub == R - 1) runs[buf][w][col] = make_float2(A, B);
+    if (r + nw * R * S < end) next.load(fx, h0, fr, hin, dh, s, b, c, t0 + nw * R * S, end, SUM);
     __syncthreads();
     float mine = state;
     for (int k = 0; k < nw; ++k) {
-      const float2 run = runs[buf][k][lane];
+      const float2 run = runs[buf][k][col];
       if (k == w) mine = state;
       state = after(run.x, run.y, state);
       A_all *= run.x;
     }
+    if (R > 1 && sub) mine = after(A0, B0, mine);
     if (SUM || c >= s.C) continue;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
@@ -135,7 +162,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(
       }
     }
   }
-  if (w || c >= s.C) return;
+  if (w || sub || c >= s.C) return;
   if (SUM) {
     float* q = part + ((int64_t)b * s.slices + slice) * 2 * s.C + c;
     q[0] = A_all;
@@ -145,48 +172,62 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scan_kernel(
   }
 }
 
-// Rows of a lane: few enough that two workgroups of eight waves fit a CU with the next ones on
-// their way; one where there is one.
+// Rows of a lane, as many as leave a SIMD four waves with the next ones on their way; one where there
+// is one.
 constexpr int kSteps = 16, kBackSteps = 8;
 
-template <bool BACK, int S>
+// Columns of a workgroup: 64, a row's 256 bytes together; or 16, a wave holding four runs, where a
+// sequence is over in two rounds of such workgroups and values are so few that launches count and not
+// traffic (with gradients, 4 x 512 x 512: 24 us, 34 in slices of 64 columns; 16 x 512 x 512: 49 and 45; 2 x
+// 2048 x 256: 51 and 34).
+bool few(const ScanShape& a) { return a.T > 1 && a.T <= 1024 && a.B * a.T * a.C <= (1 << 21); }
+// Rows of f and x that do not start with a cache line of 128 bytes.
+bool odd_rows(const ScanShape& a) { return a.C % 32 != 0; }
+
+template <bool BACK, int S, int CL>
 hipError_t scan(const float* fx, const float* h0, const int32_t* fresh, const float* h, const float* dh,
                 float* out, float* dh0, float* part, const ScanShape& a, int64_t slices,
                 hipStream_t st) {
-  const Scan s{(int)a.B, (int)a.T, (int)a.C, (int)slices, (int)ceil_div(a.T, slices)};
-  const unsigned blocks = (unsigned)(a.B * ceil_div(a.C, 64));
-  const unsigned threads = 64 * (unsigned)std::min<int64_t>(kWaves, ceil_div(s.slice_len, S));
+  const Scan s{(int)a.B, (int)a.T, (int)a.C, (int)slices, (int)ceil_div(a.T, slices), odd_rows(a)};
+  const auto grid = [&](int64_t n) { return dim3((unsigned)(ceil_div(a.B * ceil_div(a.C, CL) * n, kXcds) * kXcds)); };
+  const unsigned threads = 64 * (unsigned)std::min<int64_t>(kWaves<CL>, ceil_div(s.slice_len, S * 64 / CL));
   if (slices > 1) {
-    hipLaunchKernelGGL((scan_kernel<BACK, true, S>), dim3(blocks, (unsigned)slices - 1), dim3(threads), 0,
-                       st, fx, h0, fresh, h, dh, out, dh0, part, s);
+    hipLaunchKernelGGL((scan_kernel<BACK, true, S, CL>), grid(slices - 1), dim3(threads), 0, st,
+                       fx, h0, fresh, h, dh, out, dh0, part, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((scan_kernel<BACK, false, S>), dim3(blocks, (unsigned)slices), dim3(threads), 0, st,
+  hipLaunchKernelGGL((scan_kernel<BACK, false, S, CL>), grid(slices), dim3(threads), 0, st,
                      fx, h0, fresh, h, dh, out, dh0, part, s);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Slices to fill the chip where the columns do not: each has 128 rows or more.
+// Slices where the columns of all sequences are too few workgroups: some 512 of them, twice as many where
+// neighbours share lines, and 128 rows or more in each.
 int64_t scan_slices(const ScanShape& a) {
   const int64_t blocks = a.B * ceil_div(a.C, 64);
-  if (blocks >= 256) return 1;
-  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, blocks), a.T / 128, kMaxScanSlices}));
+  if (few(a) || blocks >= 256) return 1;
+  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(odd_rows(a) ? 1024 : 512, blocks), a.T / 128,
+                                                  kMaxScanSlices}));
 }
 
 hipError_t scan_fwd(const float* fx, const float* h0, const int32_t* fresh, float* h, float* part,
                     const ScanShape& a, int64_t slices, hipStream_t s) {
-  if (a.T == 1) return scan<false, 1>(fx, h0, fresh, nullptr, nullptr, h, nullptr, part, a, slices, s);
-  return scan<false, kSteps>(fx, h0, fresh, nullptr, nullptr, h, nullptr, part, a, slices, s);
+#define FWD(S, CL) scan<false, S, CL>(fx, h0, fresh, nullptr, nullptr, h, nullptr, part, a, slices, s)
+  if (a.T == 1) return FWD(1, 64);
+  return few(a) ? FWD(kSteps, 16) : FWD(kSteps, 64);
+#undef FWD
 }
 
 hipError_t scan_bwd(const float* fx, const float* h0, const int32_t* fresh, const float* h,
                     const float* dh, float* dfx, float* dh0, float* part, const ScanShape& a,
                     int64_t slices, hipStream_t s) {
-  if (a.T == 1) return scan<true, 1>(fx, h0, fresh, h, dh, dfx, dh0, part, a, slices, s);
-  return scan<true, kBackSteps>(fx, h0, fresh, h, dh, dfx, dh0, part, a, slices, s);
+#define BWD(S, CL) scan<true, S, CL>(fx, h0, fresh, h, dh, dfx, dh0, part, a, slices, s)
+  if (a.T == 1) return BWD(1, 64);
+  return few(a) ? BWD(kBackSteps, 16) : BWD(kBackSteps, 64);
+#undef BWD
 }
 
 }  // namespace ooc
