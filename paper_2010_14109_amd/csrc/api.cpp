@@ -486,7 +486,7 @@ ooc_status ooc_join_slices(int64_t rows, int64_t d, int64_t groups, int64_t* sli
     g_create_error = "ooc_join_slices: " + e;
     return OOC_E_INVALID;
   }
-  *slices = join_slices(rows, groups);
+  *slices = join_slices(rows, d, groups);
   *part_bytes = (uint64_t)join_part_bytes(d, groups, *slices);
   return OOC_OK;
 } catch (const std::bad_alloc&) {

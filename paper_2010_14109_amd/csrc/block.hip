@@ -116,11 +116,30 @@ __device__ inline void store4(float* p, int c, int d, const Four& x) {
   }
 }
 
+template <int CTRL>
+__device__ inline float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL,
+                                                               0xf, 0xf, true));
+}
+// the sum of a wave's values, in every lane
+__device__ inline float wave_sum(float x) {
+  x += dpp<0xb1>(x);    // quad_perm 1 0 3 2
+  x += dpp<0x4e>(x);    // quad_perm 2 3 0 1
+  x += dpp<0x141>(x);   // mirrored within 8
+  x += dpp<0x140>(x);   // mirrored within 16
+  uint32_t v = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const uint32_t a = r[0], b = r[1];
+  x = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+  v = __builtin_bit_cast(uint32_t, x);
+  const auto t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  const uint32_t c = t[0], d = t[1];
+  return __builtin_bit_cast(float, c) + __builtin_bit_cast(float, d);
+}
 // The row's sum of x; `room` is kRows W floats of LDS, used once.
 template <int W>
 __device__ inline float row_sum(float x, float* room) {
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) x += __shfl_xor(x, s, 64);
+  x = wave_sum(x);
   if constexpr (W > 1) {
     const int w = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) room[w] = x;
@@ -223,7 +242,7 @@ __global__ __launch_bounds__((Row<W, E>::kThreads)) void join_fwd_kernel(
 // A workgroup takes the rows of one slice of a gate's rows and keeps their sums of dpost, dgate and
 // dpre in registers; its rows' waves add theirs up at the end.
 template <int W, int E, int KIND>
-__global__ __launch_bounds__((Row<W, E>::kThreads)) void join_bwd_kernel(
+__global__ __launch_bounds__((Row<W, E>::kThreads), 2) void join_bwd_kernel(
     const float* __restrict__ f, const float* __restrict__ h, const float* __restrict__ stats,
     Join4 j, const float* __restrict__ dh, const float* __restrict__ dn, float* __restrict__ dx,
     float* __restrict__ df, float* __restrict__ part, int64_t slices, int64_t slice_rows) {
@@ -345,8 +364,16 @@ __global__ __launch_bounds__(64 * kSumRows) void join_sum_kernel(const float* __
   const int which = what == 0 ? 0 : what == 1 ? 2 : 1;
   const int64_t first = what < 2 ? 0 : (what - 2) * slices, last = what < 2 ? groups * slices : first + slices;
   float acc = 0.f;
-  if (c < d)
-    for (int64_t s = first + sub; s < last; s += kSumRows) acc += part[(s * 3 + which) * d + c];
+  for (int64_t s = first + sub; s < last; s += 8 * kSumRows) {   // eight loads in flight
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t u = s + k * kSumRows;
+      x[k] = u < last && c < d ? part[(u * 3 + which) * d + c] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc += x[k];
+  }
   sums[sub][lane] = acc;
   __syncthreads();
   if (sub || c >= d) return;
@@ -384,10 +411,13 @@ hipError_t dropout(const float* x, const uint32_t* seed, float* y, int64_t n, in
   return hipGetLastError();
 }
 
-// Some 512 workgroups of four rows at once fill the chip; a slice has eight rows or more, where there
-// are as many, so that its three rows of sums are little beside them.
-int64_t join_slices(int64_t rows, int64_t groups) {
-  return std::max<int64_t>(1, std::min(ceil_div(512, groups), ceil_div(rows / groups, 8)));
+// Workgroups to fill the chip: three a CU where a wave holds a row, two where a row takes more waves
+// (12288 x 1024 with gradients: 112 us with 512, 103 with 768, 109 with 1024; 9193 x 1365: 148 with 512, 169
+// with 768).  A slice has eight rows or more, where there are as many, so that its three rows of sums are
+// little beside them.
+int64_t join_slices(int64_t rows, int64_t d, int64_t groups) {
+  const int64_t want = d <= 1024 ? 768 : 512;
+  return std::max<int64_t>(1, std::min(ceil_div(want, groups), ceil_div(rows / groups, 8)));
 }
 
 hipError_t join_fwd(const float* x, const float* f, const float* post, const float* gate,

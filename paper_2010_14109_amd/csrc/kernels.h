@@ -163,7 +163,7 @@ hipError_t dropout(const float* x, const uint32_t* seed, float* y, int64_t n, in
 struct JoinShape {
   int64_t rows, d, groups, drop, salt;
 };
-int64_t join_slices(int64_t rows, int64_t groups);   // of the rows of a gate
+int64_t join_slices(int64_t rows, int64_t d, int64_t groups);   // of the rows of a gate
 hipError_t join_fwd(const float* x, const float* f, const float* post, const float* gate,
                     const float* pre, const float* scale, const uint32_t* seed, float* h, float* n,
                     float* stats, const JoinShape& a, hipStream_t s);

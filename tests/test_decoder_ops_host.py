@@ -171,7 +171,7 @@ def test_scan_refusals(lib, carry, fresh, slices):
 
 
 def test_slice_counts(lib):
-    assert ooc.join_slices(12288, 1024, 24) == (22, 24 * 22 * 3 * 1024 * 4)
+    assert ooc.join_slices(12288, 1024, 24) == (32, 24 * 32 * 3 * 1024 * 4)
     assert ooc.join_slices(1, 1, 1) == (1, 12) and ooc.join_slices(24, 5, 24)[0] == 1
     assert ooc.scan_slices("scan_fwd", [24, 512, 1024]) == (1, 0)
     assert ooc.scan_slices("scan_bwd", [1, 1, 1]) == (1, 0)

@@ -114,7 +114,7 @@ SCAN = [
     (1, 1, 1, False, False), (3, 1, 70, True, False), (2, 1, 64, True, True), (1, 2, 5, True, True),
     (2, 16, 64, False, False), (3, 17, 65, True, False), (2, 127, 63, False, True), (2, 128, 130, True, True),
     (1, 129, 3, False, False), (1, 1000, 200, True, True), (5, 300, 33, True, False), (1, 4099, 64, True, True),
-    (300, 9, 64, False, True), (1, 20011, 5, False, True),
+    (300, 9, 64, False, True), (1, 20011, 5, False, True), (258, 1030, 2, True, False),
 ]
 
 
