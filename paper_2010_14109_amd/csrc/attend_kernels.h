@@ -657,13 +657,26 @@ struct Raw {
   }
 };
 
+// The states k0 .. k1 that a workgroup's columns see become those of its slice: whole tiles, so that every
+// slice has work wherever the spans lie (one query of 8 x 16 heads in a window of 4096 of 65536 states, 64
+// slices: 31 us with slices of the states, 19 so).
+__device__ inline void slice_of_span(int& k0, int& k1, int slice, int tile) {
+  if (k0 >= k1) {
+    k0 = k1 = 0;
+    return;
+  }
+  const int slices = gridDim.y, tiles = (k1 - k0 + tile - 1) / tile, len = (tiles + slices - 1) / slices * tile;
+  k0 = min(k1, k0 + slice * len);   // (a span ends below 2^28, and a slice has at most two tiles' rows too many)
+  k1 = min(k1, k0 + len);
+}
+
 // What the columns of a wave and of its workgroup (W waves, C sets of 32 columns each) see: the states
 // k0 .. k1 of the slice that any column of the workgroup does.
 template <int C, int W, class V>
 struct Columns {
   int k0, k1;
   bool wrong;
-  __device__ Columns(const V& v, const Shape& s, const Place& at, int, int slice_len) {
+  __device__ Columns(const V& v, const Shape& s, const Place& at, int, int slice_len, int) {
     const int n = v.klen[at.b];
     wrong = n < 0 || n > s.Tk;
     k0 = wrong ? 0 : min(n, at.slice * slice_len);
@@ -680,14 +693,13 @@ struct Columns<C, W, Spans<CAP>> {
   int low, high, last_low, first_high;   // of the wave: what any column sees, what all do
   uint32_t* odd_bits;                    // [2][2]: rows of the present and the next tile
   // col0: the lane's first column
-  __device__ Columns(const Spans<CAP>& v, const Shape& s, const Place& at, int col0, int slice_len) : cap(v) {
+  __device__ Columns(const Spans<CAP>& v, const Shape& s, const Place& at, int col0, int, int tile) : cap(v) {
     __shared__ int2 limits[W];
     __shared__ uint32_t odd[4];
     odd_bits = odd;
     if (threadIdx.x < 4) odd[threadIdx.x] = 0;
     low = last_low = 0x7fffffff;
     high = first_high = 0;
-    const int to = at.slice * slice_len, end = min(s.Tk, to + slice_len);
 #pragma unroll
     for (int x = 0; x < C; ++x) {
       const int col = col0 + 32 * x;
@@ -698,8 +710,8 @@ struct Columns<C, W, Spans<CAP>> {
       low = min(low, seen[x].low());
       high = max(high, seen[x].high());
     }
-    low = max(wave_least(low), to);
-    high = min(wave_most(high), end);
+    low = wave_least(low);
+    high = wave_most(high);
     if ((threadIdx.x & 63) == 0) limits[threadIdx.x >> 6] = make_int2(low, high);
     __syncthreads();
     k0 = 0x7fffffff;
@@ -711,11 +723,14 @@ struct Columns<C, W, Spans<CAP>> {
     }
     k0 = __builtin_amdgcn_readfirstlane(k0);
     k1 = __builtin_amdgcn_readfirstlane(k1);
+    slice_of_span(k0, k1, at.slice, tile);
+    low = max(low, k0);
+    high = min(high, k1);
     last_low = 0;
     first_high = 0x7fffffff;
 #pragma unroll
     for (int x = 0; x < C; ++x) {
-      seen[x].cut(end);
+      seen[x].cut(k1);
       last_low = max(last_low, seen[x].low());
       first_high = min(first_high, seen[x].high());
     }
@@ -813,7 +828,7 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), V::kSpan && !V::k
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int col0 = at.tile * Forward<DH, WIDE>::kCols + w / Wd::kParts * 32 * C + (lane & 31);
   const int first = w % Wd::kParts * Wd::kSums;
-  const Columns<C, W, V> cols(view, s, at, col0, slice_len);
+  const Columns<C, W, V> cols(view, s, at, col0, slice_len, T);
   const int k0 = cols.k0, k1 = cols.k1;
   bool odd[C] = {};   // sees a state with an infinity or a NaN
   int turn = 0;
@@ -1013,17 +1028,16 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
   [[maybe_unused]] Seen seen;
   [[maybe_unused]] Cap cap;
   if constexpr (V::kSpan) {
-    const int end = min(s.Tk, (at.slice + 1) * slice_len);
     cap = Cap(view);
     if (l16 < s.R) {
       const int g = l16 / s.Tq, i = l16 - g * s.Tq;
       seen = Seen(view, (int64_t)at.b * s.Tq + i, at.hk * s.G + g, s.Tk);
     }
     bad = seen.bad;
-    k0 = max(wave_least(seen.low()), at.slice * slice_len);
-    k1 = min(wave_most(seen.high()), end);
-    if (k0 >= k1) k0 = k1 = 0;
-    seen.cut(end);
+    k0 = wave_least(seen.low());
+    k1 = wave_most(seen.high());
+    slice_of_span(k0, k1, at.slice, T);
+    seen.cut(k1);
   } else {
     const int n = view.klen[at.b];
     bad = n < 0 || n > s.Tk;
@@ -1546,7 +1560,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dq_kernel(
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int col = (at.tile * W + w) * 32 + (lane & 31), here = min(col, s.R - 1);
-  const Columns<1, W, V> cols(view, s, at, col, slice_len);
+  const Columns<1, W, V> cols(view, s, at, col, slice_len, T);
   const int k0 = cols.k0, k1 = cols.k1;
   bool odd = false;   // sees a state with an infinity or a NaN
   int turn = 0;
@@ -1813,7 +1827,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
   const int col = (at.tile * kPairs + pair) * 32 + (lane & 31), here = min(col, s.R - 1);
-  const Columns<1, W, V> cols(view, s, at, col, slice_len);
+  const Columns<1, W, V> cols(view, s, at, col, slice_len, T);
   const int k0 = cols.k0, k1 = cols.k1;
   bool odd = false;   // sees a state with an infinity or a NaN
   int turn = 0;
