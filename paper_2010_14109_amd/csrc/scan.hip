@@ -41,9 +41,17 @@ struct Scan {
   bool together;
 };
 
-// a = sigmoid(f) and 1 - a, each to a few units in its last place
+// a = sigmoid(f) and 1 - a, each to a few units in its last place: with e = exp(-|f|), 1 / (1 + e) and
+// e / (1 + e).  The exponent -|f| log2 e is split in a float and its remainder, whose part e takes in as 1 +
+// x; the reciprocal is corrected once.  (The library's exponential and quotient, with more instructions:
+// 24 x 512 x 1024 forward 33 us, 31 so.)
 __device__ inline void gate_of(float f, float& a, float& rest) {
-  const float e = expf(-fabsf(f)), r = 1.f / (1.f + e), er = e * r;
+  constexpr float kLog2e = 1.44269504088896340736f, kLow = 1.92596299e-8f, kLn2 = 0.69314718055994530942f;
+  const float x = -fabsf(f), t = x * kLog2e, low = fmaf(x, kLog2e, -t) + x * kLow;
+  const float e0 = __builtin_amdgcn_exp2f(t), e = t < -126.f ? e0 : fmaf(e0 * low, kLn2, e0), d = 1.f + e;
+  float r = __builtin_amdgcn_rcpf(d);
+  r = fmaf(fmaf(-d, r, 1.f), r, r);
+  const float er = e * r;
   a = f >= 0.f ? r : er;
   rest = f >= 0.f ? er : r;
 }
