@@ -986,7 +986,7 @@ __global__ __launch_bounds__((64 * Forward<DH, WIDE>::kWaves), V::kSpan && !V::k
 // One token of 8 sequences of up to 4096 states, 16 heads of 64 on 4 key heads: 33.9 us with the
 // kernel for many queries, 18 with this one (14, and 4 for the join; reading the 34 MB at the rate of
 // a large copy takes 7).
-constexpr int kFewWaves = 4, kFewRows = 16;
+constexpr int kFewWaves = 4, kFewColumns = 16;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 __device__ inline floatx4 mma16(const Pieces& a, const Pieces& b, floatx4 c) {
   c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.l, b.h, c, 0, 0, 0);
@@ -1013,10 +1013,10 @@ __global__ __launch_bounds__(64 * kFewWaves, DH <= 64 ? 3 : 2) void few_kernel(
     int64_t y_slice, int64_t lse_slice) {
   constexpr int T = 32, W = kFewWaves, kSteps = DH / 32, kBlocks = DH / 16;
   __shared__ __attribute__((aligned(16))) char mine[W][Rows<DH, T>::kBytes];
-  __shared__ float ls[W][kFewRows];
+  __shared__ float ls[W][kFewColumns];
   // a wave's results take its tile's place
   constexpr int kYs = DH + 4;
-  static_assert(kFewRows * kYs * 4 <= Rows<DH, T>::kBytes, "room for the results");
+  static_assert(kFewColumns * kYs * 4 <= Rows<DH, T>::kBytes, "room for the results");
   const auto ys = [&](int wave, int r, int d) -> float* {
     return reinterpret_cast<float*>(mine[wave]) + r * kYs + d;
   };
@@ -1653,7 +1653,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dq_kernel(
 
 // Over the queries: dk and dv.  Columns are states.
 template <int DH, bool EXACT, class V>
-__global__ __launch_bounds__(64 * Width<DH>::kBackWaves, 2) void dkv_kernel(
+__global__ __launch_bounds__(64 * Width<DH>::kBackWaves, DH == 32 && !V::kCap ? 3 : 2) void dkv_kernel(
     const float* __restrict__ q, const float* __restrict__ kv, V view, const float* __restrict__ lse, const float* __restrict__ dy, const float* __restrict__ delta,
     float* __restrict__ dkv, Shape s, int tiles, int slice_len, int64_t dkv_slice) {
   using Wd = Width<DH>;
@@ -1831,10 +1831,6 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   const int k0 = cols.k0, k1 = cols.k1;
   bool odd = false;   // sees a state with an infinity or a NaN
   int turn = 0;
-  const auto publish = [&](auto& raw, floatx2* tops, int turn) {
-    if constexpr (V::kSpan) raw.publish(tops, cols.odd_rows(turn));
-    else raw.publish(tops);
-  };
   if constexpr (V::kSpan) {
     if (!role) leave_bounds(view, s, at, col);
   }
@@ -1874,7 +1870,8 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   };
   if (k0 < k1) {
     fetch(k0);
-    publish(raw, tops, 0);
+    if constexpr (V::kSpan) raw.publish(tops, cols.odd_rows(0));
+    else raw.publish(tops);
     __syncthreads();
     int2 e = stage(0);
     int buf = 0;
@@ -1916,7 +1913,8 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
         meet[pair][role][g][lane] = role ? make_float4(a[i], a[i + 1], a[i + 2], a[i + 3])
                                          : make_float4(a[i + 8], a[i + 9], a[i + 10], a[i + 11]);
       }
-      publish(raw, tops, turn ^ 1);
+      if constexpr (V::kSpan) raw.publish(tops, cols.odd_rows(turn ^ 1));
+      else raw.publish(tops);
       __syncthreads();
       if constexpr (V::kSpan) cols.clear(turn);
       // dS 2^(e.x - 14) is what meets the pieces of k
@@ -1984,10 +1982,6 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
   const int j = (at.tile * kPairs + pair) * 32 + (lane & 31);
   const States<W, T, V, NB> states(view, s, at, j);
-  const auto publish = [&](auto& raw, floatx2* tops, int turn) {
-    if constexpr (V::kSpan) raw.publish(tops, states.odd_rows(turn));
-    else raw.publish(tops);
-  };
   bool odd = false;   // seen by a row with an infinity or a NaN
   int turn = 0;
   // rows of this slice; a workgroup without states has nothing to add
@@ -2031,7 +2025,8 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   };
   load();
   if (tiles_of.more()) {
-    publish(raw, tops, 0);
+    if constexpr (V::kSpan) raw.publish(tops, states.odd_rows(0));
+    else raw.publish(tops);
     __syncthreads();
     int2 e = stage(0);
     int buf = 0;
@@ -2087,7 +2082,8 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
           for (int k = 0; k < 4; ++k) v[4 * g + k] = fmaf(a[4 * g + k], c, -pick(r4, k));
         }
       }
-      publish(raw, tops, turn ^ 1);
+      if constexpr (V::kSpan) raw.publish(tops, states.odd_rows(turn ^ 1));
+      else raw.publish(tops);
       __syncthreads();
       if constexpr (V::kSpan) states.clear(turn);
       if (role)
@@ -2171,17 +2167,7 @@ dim3 grid_of(const Shape& s, int tiles, int64_t slices) {
   const int64_t pairs = (int64_t)s.B * s.Hkv;
   return dim3((unsigned)((V::kSpan ? pairs : ceil_div(pairs, kXcds) * kXcds) * tiles), (unsigned)slices);
 }
-// Whether the forward's workgroups have 256 columns, not 128: where that leaves less than a tenth
-// more columns idle, which is what the wide ones gain (4096 x 4096: 0.86 against 0.96 ms at 2 x 16
-// heads of 128, 0.89 against 0.98 at 4 x 16 heads of 64; 333 queries, 12 heads of 85: 81 us wide,
-// 60 narrow), and there are two of them for each CU (77 states, 2 x 4096 queries, 8 heads of 64:
-// 18.1 us wide, 16.8 narrow).
-bool wide(const AttendShape& a, bool spans) {
-  if (spans && a.dh <= 64) return false;
-  const int64_t halves = ceil_div(a.Tq * (a.H / a.Hkv), 128);
-  return a.dh <= 128 && (halves % 2 == 0 || halves >= 10) && a.B * a.Hkv * ceil_div(halves, 2) >= 512;
-}
-int fwd_columns(const AttendShape& a, bool spans) { return wide(a, spans) ? 256 : a.dh <= 128 ? 128 : 64; }
+int fwd_columns(const AttendShape& a, bool spans) { return attention_wide(a, spans) ? 256 : a.dh <= 128 ? 128 : 64; }
 unsigned flat_grid(int64_t n) { return (unsigned)std::min<int64_t>(ceil_div(n, 256), 4096); }
 int64_t slice_of(int64_t n, int64_t slices, int64_t tile) {
   return ceil_div(ceil_div(n, slices), tile) * tile;
@@ -2197,7 +2183,6 @@ int64_t slices_for(int64_t groups, int64_t tiles, int64_t want = kWant, int64_t 
   return std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, groups), tiles / least,
                                                   kMaxAttentionSlices}));
 }
-bool few_rows(const AttendShape& a) { return a.Tq * (a.H / a.Hkv) <= kFewRows && a.dh <= 128; }
 
 #define TO_64(CALL)                        \
   if (s.dh == 32) CALL(32, true);          \
@@ -2231,7 +2216,7 @@ template <class V>
 hipError_t attend_fwd(const float* q, const float* kv, const V& view, float* y, float* lse, float* part,
                       const AttendShape& a, int64_t slices, hipStream_t st) {
   const Shape s = shape_of(a);
-  const bool few = few_rows(a);
+  const bool few = attention_few(a);
   const int tiles = few ? 1 : (int)ceil_div(s.R, fwd_columns(a, V::kSpan));
   const int len = (int)slice_of(s.Tk, slices, few ? 32 : tile_rows(s.dh));
   const int64_t size = a.B * a.Tq * s.ldq, rows = a.B * a.H * a.Tq;
@@ -2243,7 +2228,7 @@ hipError_t attend_fwd(const float* q, const float* kv, const V& view, float* y, 
 #define FWD(D, X) LAUNCH((fwd_kernel<D, X, false, V>), (Forward<D, false>::kWaves), tiles, slices, ARGS)
   if (few) {
     TO_128(FEW);
-  } else if (wide(a, V::kSpan)) {
+  } else if (attention_wide(a, V::kSpan)) {
     if constexpr (V::kSpan) {
       FROM_65_TO_128(WIDE);
     } else {

@@ -151,6 +151,9 @@ hipError_t span_attention_bwd(const float* q, const float* kv, const int32_t* sp
                               float* dq, float* dkv, float* delta, int32_t* bounds, float* part,
                               const AttendShape& a, int64_t q_slices, int64_t kv_slices,
                               hipStream_t s);
+// The forward's kernels: for a few query rows of a key head, and with 256 columns a workgroup (attend.hip).
+bool attention_few(const AttendShape& a);
+bool attention_wide(const AttendShape& a, bool spans);
 // Slice counts the launchers run best with: of the keys for a pass over query rows (forward, dq),
 // of the query rows for the pass over keys (dkv).
 int64_t attention_key_slices(const AttendShape& a, bool fwd, bool spans);
