@@ -256,8 +256,9 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *                holds f, then x; a = sigmoid(f), H_t = a_t H_(t-1) + (1 - a_t) x_t.  The state before
  *                the first row is h0 [B][C] iff carry = 1, else 0; iff fresh = 1, it is 0 too before
  *                each row whose entry in fresh [B T] (int32) is not 0.  Where a gate, or a product of
- *                gates, is 0 in fp32, the state before does not count, be it a NaN.  part = partial
- *                results, present iff slices > 1 (ooc_scan_slices gives a count and its bytes)
+ *                gates, is 0 in fp32, the state before does not count, be it a NaN.  B ceil(C / 64)
+ *                below 2^17.  part = partial results, present iff slices > 1 (ooc_scan_slices gives a
+ *                count and its bytes)
  *                                     FX[R] [h0[R]] [fresh[R]] H[W] [part[W]]
  *                                                                  B T C carry fresh slices
  *  SCAN_BWD      dFX, and dh0 iff carry = 1, of the above
