@@ -4,7 +4,9 @@
 //
 // All of this is bound by memory traffic: dropout 8 bytes a value, the join 16 forward (two tensors
 // read, two written) and 24 backward (four read, two written).  A row's values stay in registers
-// between its sums, so nothing is read twice.
+// between its sums, so nothing is read twice.  50 M values dropped: 70 us, 5.8 TB/s, the ten rounds of
+// the generator taking a third of the vector instructions' time; 12288 x 1024 joined: 35 us forward (5.7
+// TB/s), 59 backward (5.1) and 6 for the sums of the gains.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
