@@ -255,10 +255,11 @@ enum { OOC_PRE = 0, OOC_POST = 1, OOC_END = 2 };
  *  SCAN_FWD      gated recurrence along the T rows of each of B sequences, by column: FX [B T][2 C]
  *                holds f, then x; a = sigmoid(f), H_t = a_t H_(t-1) + (1 - a_t) x_t.  The state before
  *                the first row is h0 [B][C] iff carry = 1, else 0; iff fresh = 1, it is 0 too before
- *                each row whose entry in fresh [B T] (int32) is not 0.  Where a gate, or a product of
- *                gates, is 0 in fp32, the state before does not count, be it a NaN.  B ceil(C / 64)
- *                below 2^17.  part = partial results, present iff slices > 1 (ooc_scan_slices gives a
- *                count and its bytes)
+ *                each row whose entry in fresh [B T] (int32) is not 0.  Where a gate is 0 in fp32
+ *                (below 2^-126 it may be), the state before does not count, be it a NaN; up to such a
+ *                row or a fresh one, a state that is not finite makes those behind it NaN or infinite.
+ *                B ceil(C / 64) below 2^17.  part = partial results, present iff slices > 1
+ *                (ooc_scan_slices gives a count and its bytes)
  *                                     FX[R] [h0[R]] [fresh[R]] H[W] [part[W]]
  *                                                                  B T C carry fresh slices
  *  SCAN_BWD      dFX, and dh0 iff carry = 1, of the above

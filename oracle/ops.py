@@ -485,11 +485,18 @@ def _gates(FX, fresh, a):
     return x, gate, rest, live
 
 
+def _passed(gate, live, state):
+    """What a row takes of the state before it: nothing where it starts afresh or its gate is 0 in fp32,
+    whatever the state holds."""
+    with np.errstate(invalid="ignore"):
+        return np.where((live == 0) | (gate.astype(np.float32) == 0), 0.0, gate * state)
+
+
 def scan_fwd(FX, a, h0=None, fresh=None):
     x, gate, rest, live = _gates(FX, fresh, a)
     H, state = np.zeros(x.shape), np.zeros(x[:, 0].shape) if h0 is None else h0
     for t in range(a["T"]):
-        state = gate[:, t] * live[:, t] * state + rest[:, t] * x[:, t]
+        state = _passed(gate[:, t], live[:, t], state) + rest[:, t] * x[:, t]
         H[:, t] = state
     return H.reshape(-1, a["C"])
 
@@ -503,7 +510,7 @@ def scan_bwd(FX, H, dH, a, h0=None, fresh=None):
     g, later = np.zeros(x.shape), np.zeros(x[:, 0].shape)
     for t in range(a["T"] - 1, -1, -1):
         g[:, t] = dH[:, t] + later
-        later = gate[:, t] * live[:, t] * g[:, t]
+        later = _passed(gate[:, t], live[:, t], g[:, t])
     dFX = np.stack([g * (before - x) * gate * rest, g * rest], 2)
     return dFX.reshape(FX.shape), later
 

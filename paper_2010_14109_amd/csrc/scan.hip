@@ -15,8 +15,10 @@
 // and each workgroup of the second takes in the slices before its own.  24 x 512 x 1024: 30 us forward, 60
 // backward, 5.0 TB/s; 1 x 32765 x 1365 in 47 slices: 137 and 265, behind first passes of 88 and 77.
 //
-// A gate of exactly zero (f far below, or a row that starts afresh) cuts the state off, whatever it
-// was, an infinity or a NaN too; that goes for a product of gates that is below fp32's range as well.
+// A gate of exactly zero (f far below) or a row that starts afresh cuts the state off, whatever it was, an
+// infinity or a NaN too.  Such a run has a negative A, so that it is told from one whose product of gates is
+// below fp32's range, which hands on what is not finite: which rows that reaches does not depend on
+// how they are divided into runs.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -56,8 +58,13 @@ __device__ inline void gate_of(float f, float& a, float& rest) {
   a = f >= 0.f ? r : er;
   rest = f >= 0.f ? er : r;
 }
+// Whether a run cuts off what is before it, by the sign of A: its magnitude may fall to -0, and where A is a
+// NaN, whatever its sign, B is one too.
+__device__ inline bool cuts(float A) { return __builtin_bit_cast(int, A) < 0; }
 // the state behind a run (A, B)
-__device__ inline float after(float A, float B, float h) { return A == 0.f ? B : fmaf(A, h, B); }
+__device__ inline float after(float A, float B, float h) { return cuts(A) ? B : fmaf(A, h, B); }
+// A of a run and what is before it
+__device__ inline float gates(float A, float before) { return cuts(A) ? -1.f : A * before; }
 
 // One lane's rows: column c, rows t0 .. of its sequence in the order of the pass (backward: from the
 // last on), those at and past `end` being no rows (they change nothing).
@@ -123,10 +130,10 @@ __global__ __launch_bounds__(64 * kWaves<CL>, 4) void scan_kernel(
 #pragma unroll
     for (int k = 0; k < S; ++k) {
       gate_of(now.f[k], a[k], rest[k]);
-      al[k] = now.fresh[k] ? 0.f : a[k];
+      al[k] = now.fresh[k] || a[k] == 0.f ? -1.f : a[k];
       if (t0 + k < end) {
-        B = BACK ? (al[k] == 0.f ? 0.f : al[k] * (now.d[k] + B)) : after(al[k], rest[k] * now.x[k], B);
-        A *= al[k];
+        B = BACK ? (al[k] < 0.f ? 0.f : al[k] * (now.d[k] + B)) : after(al[k], rest[k] * now.x[k], B);
+        A = gates(al[k], A);
       }
     }
     // the wave's runs up to a lane's own; the last one's are the wave's
@@ -137,7 +144,7 @@ __global__ __launch_bounds__(64 * kWaves<CL>, 4) void scan_kernel(
         const float a1 = __shfl_up(A, o, 64), b1 = __shfl_up(B, o, 64);
         if (lane >= o) {
           B = after(A, B, b1);
-          A *= a1;
+          A = gates(A, a1);
         }
       }
       A0 = __shfl_up(A, CL, 64);
@@ -151,7 +158,7 @@ __global__ __launch_bounds__(64 * kWaves<CL>, 4) void scan_kernel(
       const float2 run = runs[buf][k][col];
       if (k == w) mine = state;
       state = after(run.x, run.y, state);
-      A_all *= run.x;
+      A_all = gates(run.x, A_all);
     }
     if (R > 1 && sub) mine = after(A0, B0, mine);
     if (SUM || c >= s.C) continue;
@@ -165,7 +172,7 @@ __global__ __launch_bounds__(64 * kWaves<CL>, 4) void scan_kernel(
         out[row * s.C + c] = mine;
       } else {
         const float g = now.d[k] + mine, before = now.fresh[k] ? 0.f : now.p[k];
-        mine = al[k] == 0.f ? 0.f : al[k] * g;
+        mine = al[k] < 0.f ? 0.f : al[k] * g;
         out[row * 2 * s.C + c] = g * (before - now.x[k]) * (a[k] * rest[k]);
         out[row * 2 * s.C + s.C + c] = rest[k] * g;
       }
