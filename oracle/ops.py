@@ -485,11 +485,16 @@ def _gates(FX, fresh, a):
     return x, gate, rest, live
 
 
+def _cut(gate, live):
+    """Rows that start afresh, and gates that are 0 in fp32: the state before does not count, whatever it
+    holds."""
+    return (live == 0) | (gate.astype(np.float32) == 0)
+
+
 def _passed(gate, live, state):
-    """What a row takes of the state before it: nothing where it starts afresh or its gate is 0 in fp32,
-    whatever the state holds."""
+    """What a row takes of the state before it."""
     with np.errstate(invalid="ignore"):
-        return np.where((live == 0) | (gate.astype(np.float32) == 0), 0.0, gate * state)
+        return np.where(_cut(gate, live), 0.0, gate * state)
 
 
 def scan_fwd(FX, a, h0=None, fresh=None):
@@ -506,7 +511,7 @@ def scan_bwd(FX, H, dH, a, h0=None, fresh=None):
     x, gate, rest, live = _gates(FX, fresh, a)
     H, dH = H.reshape(x.shape), dH.reshape(x.shape)
     first = np.zeros(x[:, :1].shape) if h0 is None else h0[:, None]
-    before = np.concatenate([first, H[:, :-1]], 1) * live
+    before = np.where(_cut(gate, live), 0.0, np.concatenate([first, H[:, :-1]], 1))
     g, later = np.zeros(x.shape), np.zeros(x[:, 0].shape)
     for t in range(a["T"] - 1, -1, -1):
         g[:, t] = dH[:, t] + later

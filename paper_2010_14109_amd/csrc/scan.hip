@@ -171,7 +171,7 @@ __global__ __launch_bounds__(64 * kWaves<CL>, 4) void scan_kernel(
         mine = after(al[k], rest[k] * now.x[k], mine);
         out[row * s.C + c] = mine;
       } else {
-        const float g = now.d[k] + mine, before = now.fresh[k] ? 0.f : now.p[k];
+        const float g = now.d[k] + mine, before = al[k] < 0.f ? 0.f : now.p[k];
         mine = al[k] < 0.f ? 0.f : al[k] * g;
         out[row * 2 * s.C + c] = g * (before - now.x[k]) * (a[k] * rest[k]);
         out[row * 2 * s.C + s.C + c] = rest[k] * g;

@@ -74,3 +74,21 @@ def test_any_count_of_slices_gives_the_same(cut):
     one, other = ([scan_fwd(a, bad, h0, fr, n)] + scan_bwd(a, bad, h0, fr, h, dh, n) for n in (1, slices))
     for name, x, y, b in zip(("h", "dfx", "dh0"), one, other, bounds):
         au.within(name, y, x, 2 * b)
+
+
+@pytest.mark.parametrize("shape", [(2, 200, 66, 1), (2, 200, 66, 5), (1, 1500, 130, 1), (1, 1500, 130, 64)], ids=str)
+def test_gradients_at_a_gate_of_zero(shape):
+    """A state that is no number does not count there, for the gate's own gradient either."""
+    B, T, C, slices = shape
+    a, fx, h0, fr, dh = case(B, T, C, 56)
+    fx[[20, 61], :C], fx[60, :C] = -np.inf, -200.0
+    clean = scan_fwd(a, fx, h0, fr, slices)
+    want = scan_bwd(a, fx, h0, fr, clean, dh, slices)
+    bad, nan_state = fx.copy(), h0.copy()
+    bad[10, C::2], bad[59, C::3], nan_state[0] = np.nan, np.inf, np.nan
+    h = scan_fwd(a, bad, nan_state, fr, slices)
+    assert np.array_equal(h[20:59], clean[20:59]) and np.array_equal(h[60:], clean[60:])
+    got = scan_bwd(a, bad, nan_state, fr, h, dh, slices)
+    rows = np.r_[20:59, 60:B * T]
+    assert np.array_equal(got[0][rows], want[0][rows]) and not got[0][[20, 60], :C].any()
+    assert np.array_equal(got[0][:, C:], want[0][:, C:]) and np.array_equal(got[1], want[1])

@@ -28,3 +28,5 @@ def test_the_oracle_cuts_off_what_is_not_finite():
     fx[8, 0], fx[6, 3] = -np.inf, np.nan      # a gate of zero behind a NaN
     h = ops.scan_fwd(fx, a, h0, fr)
     assert np.isnan(h[6:8, 0]).all() and h[8, 0] == fx[8, 3] and np.isfinite(h[8:]).all()
+    dfx = ops.scan_bwd(fx, h, dh, a, h0, fr)[0]
+    assert abs(dfx[8, 0]) < 1e-200 and np.isfinite(dfx[8:]).all() and np.isnan(dfx[6:8, 0]).all()
