@@ -1292,7 +1292,7 @@ struct RowSeen {   // what a row of the tile sees, as given
 };
 struct Walk;
 template <int T>
-struct RowsOf {   // the same of all its rows
+struct RowsOf {   // the same of all its rows, `at` from the workgroup's first state on
   int lo[T], len[T];
   float at[T], slope[T];
 };
@@ -1449,7 +1449,7 @@ __device__ inline void leave_bounds(const V& v, const Shape& s, const Place& at,
 template <int T>
 struct RowsSeen {
   const RowsOf<T>* rows;   // in LDS
-  int j, first;            // the column; the wave's first
+  int j, first, base;      // the column; the wave's first, the workgroup's
   // bit 0: a row of r0 .. r0 + 31 sees a column of the wave, bit 1: all see all
   __device__ int look(int r0) const {
     const int r = r0 + (int)(threadIdx.x & 31), lo = rows->lo[r], hi = lo + rows->len[r];
@@ -1468,7 +1468,7 @@ struct RowsSeen {
   __device__ void bias(int r, float (&z)[4]) const {
     const float4 at = at4(rows->at, r), slope = at4(rows->slope, r);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) z[k] = fmaf(-pick(slope, k), fabsf(pick(at, k) - (float)j), z[k]);
+    for (int k = 0; k < 4; ++k) z[k] = fmaf(-pick(slope, k), fabsf(pick(at, k) - (float)(j - base)), z[k]);
   }
   // whether one of the rows of `bits` from r0 on, which are not finite, sees the column
   __device__ bool odd(uint32_t bits, int r0) const {
@@ -1505,7 +1505,7 @@ template <int W, int T, class V, int B = 1>
 struct States {
   int n;
   bool wrong;
-  __device__ States(const V& v, const Shape& s, const Place& at, int) {
+  __device__ States(const V& v, const Shape& s, const Place& at, int, int) {
     n = v.klen[at.b];
     wrong = n < 0 || n > s.Tk;
   }
@@ -1517,10 +1517,13 @@ struct States {
 template <int W, int T, bool CAP, int B>
 struct States<W, T, Spans<CAP>, B> {
   Cap cap;
-  int j, first, Tk;
+  int j, first, base, Tk;
   RowsOf<T>* rows;
   uint32_t* odd_bits;
-  __device__ States(const Spans<CAP>& v, const Shape& s, const Place&, int j) : cap(v), j(j), Tk(s.Tk) {
+  // j: the lane's column, base: the workgroup's first.  Distances are taken from there, as a float has no
+  // room for the place of a state past 2^24.
+  __device__ States(const Spans<CAP>& v, const Shape& s, const Place&, int j, int base)
+      : cap(v), j(j), base(base), Tk(s.Tk) {
     __shared__ __attribute__((aligned(16))) RowsOf<T> seen[B];
     __shared__ uint32_t odd[4];
     rows = seen;
@@ -1535,10 +1538,10 @@ struct States<W, T, Spans<CAP>, B> {
   __device__ void put(const RowSeen& r, int buf) const {
     rows[buf].lo[threadIdx.x] = r.lo;
     rows[buf].len[threadIdx.x] = r.lo < r.hi && r.lo >= 0 && r.hi <= Tk ? r.hi - r.lo : 0;
-    rows[buf].at[threadIdx.x] = (float)r.at;
+    rows[buf].at[threadIdx.x] = (float)(r.at - base);
     rows[buf].slope[threadIdx.x] = r.slope * kLog2e;
   }
-  __device__ RowsSeen<T> at(int buf) const { return {rows + buf, j, first}; }
+  __device__ RowsSeen<T> at(int buf) const { return {rows + buf, j, first, base}; }
   __device__ uint32_t* odd_rows(int turn) const { return odd_bits + 2 * turn; }
   __device__ void clear(int turn) const {
     if (threadIdx.x < 2) odd_bits[2 * turn + threadIdx.x] = 0;
@@ -1668,7 +1671,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kBackWaves, DH == 32 && !V::kCap ? 
   if (at.none) return;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int j = (at.tile * W + w) * 32 + (lane & 31);
-  const States<W, T, V> states(view, s, at, j);
+  const States<W, T, V> states(view, s, at, j, at.tile * W * 32);
   // rows of this slice; a workgroup without states has nothing to add
   const bool any = states.any(at.tile * W * 32);
   const int i0 = any ? min(s.R, at.slice * slice_len) : 0, i1 = any ? min(s.R, i0 + slice_len) : 0;
@@ -1982,7 +1985,7 @@ __global__ __launch_bounds__(64 * Width<DH>::kPairWaves, Width<DH>::kOccupancy) 
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
   const int pair = w % kPairs, role = __builtin_amdgcn_readfirstlane(w / kPairs);
   const int j = (at.tile * kPairs + pair) * 32 + (lane & 31);
-  const States<W, T, V, NB> states(view, s, at, j);
+  const States<W, T, V, NB> states(view, s, at, j, at.tile * kPairs * 32);
   bool odd = false;   // seen by a row with an infinity or a NaN
   int turn = 0;
   // rows of this slice; a workgroup without states has nothing to add

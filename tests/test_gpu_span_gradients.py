@@ -23,4 +23,3 @@ def test_one_sided_scores_under_the_cap(dh, low, high):
     bq, bk = one_sided_bounds(q, kv, span, mod, dy, a)
     au.within("dq", dq, wq, bq)
     au.within("dkv", dkv, wk, bk)
-
