@@ -31,7 +31,9 @@ a block join keeps two floats per row, a gated recurrence and dropout nothing.
 
 A join's output ``name`` is the next block's input; ``name + ".h"`` is the residual
 stream, for the next join.  Its gate is a parameter, or the tensor ``gate`` names, a
-row for each rows / groups rows.
+row for each rows / groups rows.  Dropout and joins that drop draw their words by the
+input ``seed`` names and by ``salt``, 0 where it is left out.  Layers of the same seed and
+salt drop by the same words; each of them has to name the salt, one left out is refused.
 
 ``spec["input"]`` is the shape of the input ``x``; ``spec["inputs"]`` lists
 further INPUT variables, ``{"name", "shape", "dtype"}``: the tokens and lengths
@@ -326,6 +328,16 @@ class Net:
         self._call("span_attention_fwd", pairs, a + slices)
         self.slices[L["name"]] = slices + ooc.attention_slices("span_attention_bwd", a)[0]
         return self.shape[X]
+
+    def _check_salts(self):
+        """No layer drops by the words of another because its salt was left out."""
+        first = {}
+        for L in self.spec["layers"]:
+            if L["op"] in ("dropout", "join") and L.get("p", 0):
+                other = first.setdefault((L.get("seed"), L.get("salt", 0)), L)
+                if other is not L and not ("salt" in L and "salt" in other):
+                    raise ValueError(f"{L['name']}: drops by the same words as {other['name']}; "
+                                     "each needs a salt")
 
     def _dropped(self, L):
         """drop of 2^32 and salt of a layer's dropout, and its seed where it drops."""
@@ -623,6 +635,7 @@ class Net:
                "qknorm": self._fwd_qknorm, "cross_attention": self._fwd_cross_attention,
                "span_attention": self._fwd_span_attention, "dropout": self._fwd_dropout,
                "join": self._fwd_join, "scan": self._fwd_scan}
+        self._check_salts()
         for L in spec["layers"]:
             self.shape[L["name"]] = fwd[L["op"]](L, L["in"][0])
         logits = spec["logits"]
