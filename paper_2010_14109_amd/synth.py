@@ -460,17 +460,24 @@ def make_inputs(spec, seed=0):
 
 
 def make_extra_inputs(spec, tables=None, seed=2):
-    """``{name: array}`` of ``spec["inputs"]``, by type and name: i32 of two axes are tokens, uniform
-    over the vocabulary; i32 ``<tokens>_len`` their lengths, uniform over 1 .. the sequence; i32
-    ``*pos`` positions counting up in each sequence; i32 ``*fresh`` the first rows of some four documents
-    a sequence, i32 ``*span`` of three columns what each row sees of its own; i32 ``*seed`` two words; f32
-    ``*mod`` the network's cap, where it has one, then falling slopes; f32 ``*scale`` 1; f64 tables of angles, ``tables[name]`` or
-    10000^(-2 i / rot) radians per position and magnitude 1; f32 standard normal.  Anything else is a
-    ValueError."""
+    """``{name: array}`` of ``spec["inputs"]``.  By the layers that name them: ``fresh`` of a recurrence, the
+    first rows of some four documents a sequence; ``span`` of an attention, what each row sees of its own
+    document, and its ``mod``, the network's cap, where the layer has one, then falling slopes; ``seed``, two
+    words; ``scale`` of a join, 1.  The others by type and name: i32 of two axes are tokens, uniform over the
+    vocabulary; i32 ``<tokens>_len`` their lengths, uniform over 1 .. the sequence; i32 ``*pos`` positions
+    counting up in each sequence; f64 tables of angles, ``tables[name]`` or 10000^(-2 i / rot) radians per
+    position and magnitude 1; f32 standard normal.  Anything else is a ValueError."""
     g = np.random.Generator(np.random.PCG64(seed))
     shapes = {v["name"]: tuple(v["shape"]) for v in spec.get("inputs", ())}
     batch = spec["input"][0]
     out = {}
+    use, capped = {}, set()     # what a layer takes an input for
+    for L in spec.get("layers", ()):
+        for key in {"span_attention": ("span", "mod"), "scan": ("fresh",), "dropout": ("seed",),
+                    "join": ("seed", "scale")}.get(L["op"], ()):
+            use.setdefault(L.get(key), key)
+        if L["op"] == "span_attention" and L.get("cap"):
+            capped.add(L.get("mod"))
 
     def first_rows(rows):
         """Each row's document's first row, by sequence; the same for every input."""
@@ -481,19 +488,20 @@ def make_extra_inputs(spec, tables=None, seed=2):
 
     for v in spec.get("inputs", ()):
         name, shape = v["name"], tuple(v["shape"])
-        if v["dtype"] == "i32" and name.endswith("span") and shape[1:] == (3,) and shape[0] % batch == 0:
+        kind = (v["dtype"], use.get(name))
+        if kind == ("i32", "span") and shape[1:] == (3,) and shape[0] % batch == 0:
             first, at = first_rows(shape[0])
             out[name] = np.stack([first, at + 1, at], -1).reshape(shape).astype(np.int32)
-        elif v["dtype"] == "i32" and name.endswith("fresh") and len(shape) == 1 and shape[0] % batch == 0:
+        elif kind == ("i32", "fresh") and len(shape) == 1 and shape[0] % batch == 0:
             first, at = first_rows(shape[0])
             out[name] = (first == at).astype(np.int32).reshape(shape)
-        elif v["dtype"] == "i32" and name.endswith("seed") and shape == (2,):
+        elif kind == ("i32", "seed") and shape == (2,):
             out[name] = g.integers(-2 ** 31, 2 ** 31, 2).astype(np.int32)
-        elif v["dtype"] == "f32" and name.endswith("mod") and len(shape) == 1:
-            cap = [spec["cap"]] if spec.get("cap") else []
+        elif kind == ("f32", "mod") and len(shape) == 1:
+            cap = [spec["cap"]] if name in capped and spec.get("cap") else []
             n = shape[0] - len(cap)
             out[name] = np.array(cap + [2.0 ** (-8.0 * (h + 1) / n) for h in range(n)], np.float32)
-        elif v["dtype"] == "f32" and name.endswith("scale") and shape == (1,):
+        elif kind == ("f32", "scale") and shape == (1,):
             out[name] = np.ones(1, np.float32)
         elif name in (tables or {}):
             out[name] = np.asarray(tables[name], np.float64).reshape(shape)
