@@ -12,8 +12,8 @@
 // stretch meet in LDS, each lane takes in the runs before its own and walks its rows with the state
 // that it then knows.  Rows of the next stretch are on their way meanwhile.  Where the columns of all
 // sequences do not fill the chip, time is cut into slices: a first pass reduces every slice to (A, B),
-// and each workgroup of the second takes in the slices before its own.  24 x 512 x 1024: 30 us forward, 60
-// backward, 5.0 TB/s; 1 x 32765 x 1365 in 47 slices: 137 and 265, behind first passes of 88 and 77.
+// and each workgroup of the second takes in the slices before its own.  24 x 512 x 1024: 30 us forward, 61
+// backward, 5.0 TB/s; 1 x 32765 x 1365 in 47 slices: 140 and 267, behind first passes of 88 and 78.
 //
 // A gate of exactly zero (f far below) or a row that starts afresh cuts the state off, whatever it was, an
 // infinity or a NaN too.  Such a run has a negative A, so that it is told from one whose product of gates is
